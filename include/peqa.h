@@ -5,8 +5,9 @@
  * and trains only the quantization scale s; the effective weight of a linear
  * layer is W_hat = s * (Q - z) (Eq. 2, Sec. 3.2).  This library is the layer's
  * hot path: quantize once (Eq. 1), forward, backward (dX and the scale
- * gradient dS, without ever materialising dW), small-batch decode, and AdamW
- * on the scales.
+ * gradient dS, without ever materialising dW), small-batch decode, AdamW
+ * on the scales, and for token generation the paged key-value cache with the
+ * attention that reads it.
  *
  * Conventions for every entry point
  *   - All tensor pointers are DEVICE pointers owned by the caller, dense and
@@ -53,7 +54,8 @@ typedef enum {
   PEQA_ERR_ARCH = -6,           /* current device is not compute capability 10.x */
   PEQA_ERR_CUDA = -7,           /* a CUDA runtime/driver call failed; see peqa_last_cuda_error() */
   PEQA_ERR_DEVICE_TIMEOUT = -8, /* a bounded device-side wait expired */
-  PEQA_ERR_TOO_LARGE = -9       /* size exceeds a documented fixed capacity */
+  PEQA_ERR_TOO_LARGE = -9,      /* size exceeds a documented fixed capacity */
+  PEQA_ERR_DEVICE_INDEX = -10   /* a length, page number or position read on the device is out of range */
 } peqa_status;
 
 /* Frozen part (Q, z) and trainable scale s of one PEQA linear layer. */
@@ -452,6 +454,100 @@ int peqa_qlinear_decode_prepared(const peqa_qweight_t* w, const uint32_t* prepar
                                  void* stream);
 
 /*
+ * Token generation around the quantized linears (Sec. 3.1): between the q, k and v
+ * projections of a decoder layer and its output projection stand the rotation of
+ * the new queries and keys by their positions, the cache of keys and values, and
+ * the attention of each new token to the cached tokens of its sequence.
+ *
+ * The cache is paged.  k and v are two tensors of one shape [n_pages, page_size,
+ * n_kv_heads, head_dim] and one set of strides (in elements; the channels of a head
+ * are dense), in any order of the first three dimensions: no two elements share
+ * a place, strides are multiples of 16 bytes, each tensor spans less than 64 GiB
+ * (else PEQA_ERR_TOO_LARGE).  Token t of sequence b is at place t % page_size of page
+ * page_table[b, t / page_size]; entries behind a sequence's last page are not read.
+ * PEQA_KV_INT8 keeps codes in [-127, 127] and a binary32 scale for each token and
+ * head; a key or value is scale * code.
+ */
+typedef enum { PEQA_KV_BF16 = 0, PEQA_KV_INT8 = 1 } peqa_kv_type;
+
+typedef struct {
+  int32_t type;              /* peqa_kv_type */
+  int32_t n_pages;
+  int32_t page_size;         /* tokens of a page, 1 or more */
+  int32_t n_kv_heads;
+  int32_t head_dim;          /* 64, 128 or 256 */
+  int32_t n_seqs;            /* sequences of the batch (rows of page_table) */
+  int32_t max_pages;         /* pages a sequence can have (columns of page_table) */
+  int64_t page_stride;       /* strides of k and v in elements */
+  int64_t token_stride;
+  int64_t head_stride;
+  void* k;                   /* bf16 or int8 */
+  void* v;
+  float* k_scales;           /* [n_pages, n_kv_heads, page_size], PEQA_KV_INT8 only, else NULL */
+  float* v_scales;
+  const int32_t* page_table; /* [n_seqs, max_pages] */
+} peqa_kv_cache_t;
+
+/* bf16 [rows, heads, head_dim] with dense channels, 16-byte aligned; strides in
+ * elements, multiples of 8. */
+typedef struct {
+  void* data;
+  int64_t row_stride;
+  int64_t head_stride;
+} peqa_rows_t;
+
+/*
+ * Appends new tokens to the cache, rotated by their positions.  seq_lens[b] is the
+ * number of tokens of sequence b WITH the new ones, so that the same array serves
+ * the attention that follows.  starts == NULL: one new token per sequence, row b
+ * for sequence b (n_tokens == n_seqs).  Else rows starts[b] .. starts[b+1]-1 are the
+ * last tokens of sequence b, in order (starts: n_seqs + 1 values that do not fall;
+ * rows before starts[0] or from starts[n_seqs] on belong to no sequence).  A row of no
+ * sequence, or of one whose seq_lens is 0 (a place of a padded batch), is left out:
+ * nothing is written for it, not to q_out either.
+ *
+ * Rotation of position p (rotary_dim R, a multiple of 16, at most head_dim; channels from R
+ * on are copied): with c_i = cos_sin[p, i] and s_i = cos_sin[p, R/2 + i], i < R/2,
+ *   y[a] = x[a] c_i - x[b] s_i,   y[b] = x[b] c_i + x[a] s_i
+ * where (a, b) = (i, i + R/2), or (2i, 2i + 1) if interleaved.  Products, sum and
+ * difference are rounded to binary32 one by one, then to bf16; an 8-bit cache takes
+ * the binary32 values: scale = max|y| / 127 over the head (1 where all are 0),
+ * code = rint(y / scale), in IEEE binary32.  v is not rotated.  Inputs of an 8-bit
+ * cache are finite; a head with a value that is not gets a scale that is not either.
+ *   q      in   [n_tokens, n_heads, head_dim]; NULL together with q_out: keys and values alone
+ *   k, v   in   [n_tokens, n_kv_heads, head_dim]
+ *   q_out  out  [n_tokens, n_heads, head_dim]; q itself (the same strides too) or memory apart from it
+ *   cos_sin  in  fp32 [n_positions, R]
+ * No two new tokens may have one place: no page number stands twice among those that
+ * the new tokens of a call are written through.  No workspace.  What the kernel finds
+ * out of range (PEQA_ERR_DEVICE_INDEX) is left out.
+ */
+int peqa_kv_append(const peqa_kv_cache_t* cache, const peqa_rows_t* q, int n_heads, const peqa_rows_t* k,
+                   const peqa_rows_t* v, int n_tokens, const float* cos_sin, int n_positions, int rotary_dim,
+                   int interleaved, const int32_t* seq_lens, const int32_t* starts, const peqa_rows_t* q_out,
+                   void* stream);
+
+/*
+ * Attention of one new token per sequence to its cached tokens:
+ *   out[b,h] = sum_t p_t v_t,  p = softmax over t of scale * <q[b,h], k_t>,
+ *   t from max(0, seq_lens[b] - window) (from 0 if window is 0) to seq_lens[b] - 1,
+ * k_t and v_t of head h / (n_heads / n_kv_heads); n_heads is a multiple of n_kv_heads.
+ * A sequence of length 0 gets zeros, and -inf as lse.  What lies behind a sequence's end in its
+ * last page, or before the window, is not read into the result.
+ *   q    in   bf16 [n_seqs, n_heads, head_dim]
+ *   out  out  bf16 [n_seqs, n_heads, head_dim], dense (binary32 sums, rounded to nearest even)
+ *   lse  out  fp32 [n_seqs, n_heads], log of the sum of exp(scale * <q, k_t>); may be NULL
+ * workspace: peqa_attn_workspace_bytes(cache, n_heads), 256-byte aligned, in use until the call's
+ * work has ended; its contents before do not matter.  The work is dealt out evenly whatever the lengths are;
+ * the same lengths on the same device give the same bits.  For a page number or a length out
+ * of range (PEQA_ERR_DEVICE_INDEX) the sequence's outputs are undefined, the others are not.
+ */
+int peqa_attn_decode(const peqa_kv_cache_t* cache, const peqa_rows_t* q, int n_heads, const int32_t* seq_lens,
+                     float scale, int window, void* out_bf16, float* lse, void* workspace, size_t workspace_bytes,
+                     void* stream);
+size_t peqa_attn_workspace_bytes(const peqa_kv_cache_t* cache, int n_heads);
+
+/*
  * Measurement aid (the paper has no counterpart): reads `bytes` bytes (a
  * multiple of 16, 16-byte aligned) with one CTA per SM, each CTA a contiguous
  * range, and does nothing else.  Its duration is the ceiling for any kernel that
@@ -464,8 +560,9 @@ int peqa_probe_read(const void* src, size_t bytes, uint32_t* sink, size_t sink_b
 /*
  * Synchronises `stream`, then reads and clears the status word of that stream.
  * Returns PEQA_OK, PEQA_ERR_DEVICE_TIMEOUT (a bounded wait of a kernel launched on
- * `stream` expired since the last check; its outputs are undefined) or
- * PEQA_ERR_CUDA.  Status words live in the library's device image, one per stream
+ * `stream` expired since the last check; its outputs are undefined),
+ * PEQA_ERR_DEVICE_INDEX (a kernel of the key-value cache met a length, page number
+ * or position out of range, and left out what it stands for) or PEQA_ERR_CUDA.  Status words live in the library's device image, one per stream
  * (the first 31 streams seen on a device get a word of their own, any further
  * streams share one); entry points without a workspace argument have nowhere
  * else to report to.  The table is initialised by the first call of any entry

@@ -6,7 +6,7 @@ stream; all arithmetic runs in the library's CUDA kernels.  There is no CPU
 fallback: a missing library or a non-zero status raises.
 
 The calls a program makes once per layer and step (forward, decode, layer step,
-AdamW) are marshalled by the extension module ``_native`` (csrc/pybinding.cpp), the
+AdamW, the cache and its attention) are marshalled by the extension module ``_native`` (csrc/pybinding.cpp), the
 others through ctypes.
 """
 from __future__ import annotations
@@ -31,6 +31,7 @@ STATUS_NAMES = {
     0: "PEQA_OK", -1: "PEQA_ERR_NULL", -2: "PEQA_ERR_BAD_BITS", -3: "PEQA_ERR_BAD_SHAPE",
     -4: "PEQA_ERR_ALIGNMENT", -5: "PEQA_ERR_WORKSPACE", -6: "PEQA_ERR_ARCH", -7: "PEQA_ERR_CUDA",
     -8: "PEQA_ERR_DEVICE_TIMEOUT", -9: "PEQA_ERR_TOO_LARGE",
+    -10: "PEQA_ERR_DEVICE_INDEX",
 }
 
 
@@ -62,6 +63,16 @@ class _LayerHostLinear(ctypes.Structure):
                 ("d_dY", ctypes.c_void_p), ("d_Y", ctypes.c_void_p), ("d_dX", ctypes.c_void_p),
                 ("d_dS", ctypes.c_void_p), ("d_m", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class _KVCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("type", "n_pages", "page_size", "n_kv_heads", "head_dim", "n_seqs", "max_pages")] + \
+        [(n, ctypes.c_int64) for n in ("page_stride", "token_stride", "head_stride")] + \
+        [(n, ctypes.c_void_p) for n in ("k", "v", "k_scales", "v_scales", "page_table")]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 def lib() -> ctypes.CDLL:
@@ -126,6 +137,13 @@ def lib() -> ctypes.CDLL:
         L.peqa_layer_train_step_host.restype = ctypes.c_int
         L.peqa_probe_read.argtypes = [vp, sz, vp, sz, vp]
         L.peqa_probe_read.restype = ctypes.c_int
+        cp, rp = ctypes.POINTER(_KVCache), ctypes.POINTER(_Rows)
+        L.peqa_kv_append.argtypes = [cp, rp, i32, rp, rp, i32, vp, i32, i32, i32, vp, vp, rp, vp]
+        L.peqa_kv_append.restype = ctypes.c_int
+        L.peqa_attn_decode.argtypes = [cp, rp, i32, vp, f32, i32, vp, vp, vp, sz, vp]
+        L.peqa_attn_decode.restype = ctypes.c_int
+        L.peqa_attn_workspace_bytes.argtypes = [cp, i32]
+        L.peqa_attn_workspace_bytes.restype = sz
         for name in ("peqa_quantize_rtn", "peqa_pack", "peqa_unpack", "peqa_qlinear_fwd",
                      "peqa_qlinear_bwd", "peqa_qlinear_decode", "peqa_scale_adamw",
                      "peqa_train_step_host", "peqa_check_status"):
@@ -505,6 +523,57 @@ def qlinear_decode_prepared(w: QWeight, prepared: torch.Tensor, X: torch.Tensor,
     """Decode from the prepared weights; with scale_table [n_tasks, N, G] and task_ids [M] every
     token uses the scales of its own task."""
     return (_native or _load_native()).qlinear_decode_prepared(w, prepared, X, Y, scale_table, task_ids)
+
+
+@dataclass
+class KVCache:
+    """Device tensors of one layer's paged key-value cache.  Token t of sequence b is at place t % page_size of page
+    page_table[b, t // page_size].  k and v have one shape and one set of strides, in any order of the first three dimensions
+    (``torch.empty(n_pages, n_kv_heads, page_size, head_dim).transpose(1, 2)`` keeps the tokens of a head together).  In int8 they
+    hold codes, and a key or value is its code times the scale of its token and head."""
+    k: torch.Tensor                        # bfloat16 or int8 [n_pages, page_size, n_kv_heads, head_dim]
+    v: torch.Tensor
+    page_table: torch.Tensor               # int32 [n_seqs, max_pages]
+    k_scales: torch.Tensor | None = None   # float32 [n_pages, n_kv_heads, page_size], int8 only
+    v_scales: torch.Tensor | None = None
+
+
+def alloc_kv_cache(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, page_table: torch.Tensor,
+                   dtype=torch.bfloat16) -> KVCache:
+    """A cache of zeros on the page table's device, the tokens of a head together."""
+    new = lambda *shape, dtype: torch.zeros(shape, dtype=dtype, device=page_table.device)
+    pages = lambda: new(n_pages, n_kv_heads, page_size, head_dim, dtype=dtype).transpose(1, 2)
+    scales = (lambda: new(n_pages, n_kv_heads, page_size, dtype=torch.float32)) if dtype == torch.int8 else lambda: None
+    return KVCache(pages(), pages(), page_table, scales(), scales())
+
+
+def alloc_attn_workspace(cache: KVCache, n_heads: int) -> torch.Tensor:
+    """Scratch of attn_decode for n_heads query heads."""
+    c = _KVCache(n_kv_heads=cache.k.shape[2], head_dim=cache.k.shape[3])
+    n = int(lib().peqa_attn_workspace_bytes(ctypes.byref(c), n_heads))
+    if n == 0:
+        raise PeqaError(-3, "peqa_attn_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=cache.k.device)
+
+
+def kv_append(cache: KVCache, q, k: torch.Tensor, v: torch.Tensor, cos_sin: torch.Tensor, seq_lens: torch.Tensor, starts=None,
+              q_out=None, interleaved: bool = False):
+    """Appends new tokens to the cache, q and k rotated by the angles of their positions; returns the rotated q.
+
+    k, v bf16 [tokens, n_kv_heads, head_dim] and q bf16 [tokens, n_heads, head_dim] (or None) may be views with strides;
+    cos_sin fp32 [n_positions, rotary_dim], cosines before sines; seq_lens int32 [n_seqs], WITH the new tokens.
+    Without ``starts`` row b is the one new token of sequence b; with it (int32 [n_seqs + 1]) rows starts[b] to
+    starts[b + 1] - 1 are the last tokens of sequence b.  Rows of no sequence, or of one of length 0, are left out: q_out
+    (q itself, or memory apart from it) keeps what it has there, and a new one has zeros."""
+    return (_native or _load_native()).kv_append(cache, q, k, v, cos_sin, seq_lens, starts, q_out, interleaved)
+
+
+def attn_decode(cache: KVCache, q: torch.Tensor, seq_lens: torch.Tensor, scale: float | None = None, window: int = 0, out=None,
+                workspace=None, return_lse: bool = False):
+    """Attention of one new token per sequence to its cached tokens, or to the last ``window`` of them; q bf16
+    [n_seqs, n_heads, head_dim], scale 1/sqrt(head_dim) unless given.  Sequences of length 0 get zeros (and -inf as lse).
+    Returns out bf16 [n_seqs, n_heads, head_dim], with return_lse also log(sum(exp(scores))) fp32 [n_seqs, n_heads]."""
+    return (_native or _load_native()).attn_decode(cache, q, seq_lens, scale, window, out, workspace, return_lse)
 
 
 def probe_read(buf: torch.Tensor, sink: torch.Tensor) -> None:

@@ -4,6 +4,7 @@
 #include <mutex>
 
 #include "common.cuh"
+#include "kv_cache.cuh"
 #include "tensor_map.cuh"
 
 namespace peqa {
@@ -639,13 +640,14 @@ extern "C" int peqa_check_status(void* stream) {
   cudaStream_t st = as_stream(stream);
   int* dev = nullptr;
   PEQA_TRY(status_word(st, &dev));
-  int host[4] = {0, 0, 0, 0};
+  int host[kStatusInts] = {};
   PEQA_CUDA(cudaMemcpyAsync(host, dev, sizeof(host), cudaMemcpyDeviceToHost, st));
   PEQA_CUDA(cudaStreamSynchronize(st));
-  if (host[0] != 0) {
-    PEQA_CUDA(cudaMemsetAsync(dev, 0, sizeof(host), st));
+  if (host[0] != 0 || host[kStatusIndexWord] != 0) {
+    PEQA_CUDA(cudaMemsetAsync(dev, 0, 4 * sizeof(int), st));
+    PEQA_CUDA(cudaMemsetAsync(dev + kStatusIndexWord, 0, sizeof(int), st));
     PEQA_CUDA(cudaStreamSynchronize(st));
-    return PEQA_ERR_DEVICE_TIMEOUT;
+    return host[0] != 0 ? PEQA_ERR_DEVICE_TIMEOUT : PEQA_ERR_DEVICE_INDEX;
   }
   return PEQA_OK;
 }

@@ -1,0 +1,857 @@
+// Attention of one new token per sequence to its paged cache (Sec. 3.1: generation is bound by what it reads).
+//
+//   out[b,h] = sum_t p_t v_t,   p_t = exp(s_t - lse),   s_t = scale <q[b,h], k_t>,   lse = log sum_t exp(s_t)
+//
+// Every cached key and value is read once, by one warp, for all query heads that share it (a row of work: a sequence, a
+// key-value head and up to NH = 8 or 16 of its query heads).  4 NH flops per cached element are too few to bind anything
+// but memory, and the rest is laid out to keep copies in flight:
+//   * A tile is 16 tokens of a row.  Tiles are numbered through all sequences, heads and lengths, and dealt evenly: every CTA
+//     takes an equal run of them, every warp an equal run of its CTA's.  Nothing depends on how uneven the lengths are.
+//   * A warp copies its own tiles into its own ring of shared memory (cp.async, several tiles ahead).  Which lane copies what is chosen
+//     so that each lane reads back exactly the 16 bytes it has copied itself: as operands of the tensor cores' m16n8k16 product, with
+//     the channels of the contraction taken in whatever order this gives, q in the same one.  So there is no barrier, no bank conflict and no
+//     transposition in the loop.
+//       S = Q K^T      Q [16 heads x 16 channels] in registers, K the other operand: a lane holds 4 adjacent channels of a token
+//       O^T = V^T P^T  V^T [16 channels x 16 tokens]: a lane holds the same channels of four tokens and pairs them byte by byte (prmt);
+//                      S leaves the first product laid out as the operand P^T of the second
+//   * Running maximum and sum per row, as the softmax allows: the sums are rescaled only when the maximum has risen by more than
+//     kSlack (a factor of 2^8 that the binary32 sums carry easily).
+//   * p goes into the second product as the sum of two 16-bit numbers: with one, its rounding (2^-9 of p) would double the
+//     error variance that the rounding of the output has.  v and q are 16-bit numbers already, and 8-bit codes are exact ones.
+//   * A row that a warp has from its first tile to its last is written out.  Parts of rows are joined within the CTA in shared
+//     memory, and what crosses CTAs by a second kernel, which stands ready when the first ends (launch_after).
+#include "common.cuh"
+#include "kv_cache.cuh"
+#include "sm100_ptx.cuh"
+
+#include <type_traits>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+namespace peqa {
+namespace {
+
+constexpr int kTile = 16;            // tokens
+constexpr float kSlack = 8.f;        // of the running maximum, in powers of two
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kNegInf = -__builtin_huge_valf();
+
+struct AttnParams {
+  CacheView cache;
+  const uint16_t* q;                 // bf16 [n_seqs, n_heads, D]
+  long long q_row, q_head;
+  const int32_t* seq_lens;
+  int n_heads, group;                // query heads in all, and of one key-value head
+  int chunks, rows_of_seq;           // of NH query heads per key-value head; n_kv_heads * chunks
+  float scale_log2;
+  int window;
+  uint16_t* out;
+  float* lse;
+  int4* headers;                     // [2 * CTAs]: row, whether its last tile is in the part
+  float* parts;                      // [2 * CTAs][Shape::kPart]
+  int* status;
+};
+
+// Everything that follows from the channels D, the query heads NH of a row and the type of the cache.
+template <int D_, int NH_, bool I8_>
+struct Shape {
+  static constexpr int D = D_, NH = NH_;
+  static constexpr bool I8 = I8_;
+  static constexpr int kBytes = D * (I8 ? 1 : 2);               // of a token
+  static constexpr int kKC = kBytes / 64;                       // 16-byte pieces per lane of a token's key, 4 lanes side by side
+  static constexpr int kVB = kBytes >= 128 ? 16 : 8;            // bytes per lane of a token's value, 8 lanes side by side
+  static constexpr int kVC = kBytes / (8 * kVB);
+  static constexpr int kEV = kVB / (I8 ? 1 : 2);                // channels in them
+  static constexpr int kVOffset = kTile * kBytes;
+  static constexpr int kScaleOffset = 2 * kTile * kBytes;
+  static constexpr int kTileBytes = kScaleOffset + (I8 ? 128 : 0);
+  static constexpr int kWarps = D > 128 ? 4 : NH > 8 && kTileBytes > 8000 ? 6 : 8;   // as many as have three tiles in shared memory
+  static constexpr int kPart = NH * (D + 2);                    // floats of a part: sums, maxima, sums of p
+  static constexpr int kPartBytes = (kPart * 4 + 127) / 128 * 128;
+  static constexpr int kMost = 227 * 1024 - 2048;               // what a CTA may have, less what is declared statically
+  static constexpr int kSpare = kMost - kWarps * kPartBytes;
+  static constexpr int kStagesFit = kSpare / (kWarps * kTileBytes);
+  static constexpr int kStages = kStagesFit > 8 ? 8 : kStagesFit;
+  static constexpr int kRing = kStages * kTileBytes;
+  static constexpr int kSmem = kWarps * (kRing + kPartBytes);
+  static_assert(kStages >= 3 && kRing >= kPartBytes && kSmem <= kMost, "shared memory");
+};
+
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, uint32_t bytes, std::integral_constant<int, 16>) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, uint32_t bytes, std::integral_constant<int, 8>) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, uint32_t bytes, std::integral_constant<int, 4>) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+  return v;
+}
+__device__ __forceinline__ uint2 lds8(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+  return v;
+}
+__device__ __forceinline__ float lds_float(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at));
+  return v;
+}
+
+template <bool F16>
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (F16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Codes of 8 bits as binary16: with its sign bit turned a code c is the byte c + 128, and 0x6400 | byte is 1024 + 128 + c.
+__device__ __forceinline__ uint32_t less_bias(uint32_t h) {
+  const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&h), __half2half2(__ushort_as_half(0x6480)));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// two bytes of x, the lower pair or the higher
+__device__ __forceinline__ uint32_t low_codes(uint32_t x) { return less_bias(__byte_perm(x, 0x64646464u, 0x4140)); }
+__device__ __forceinline__ uint32_t high_codes(uint32_t x) { return less_bias(__byte_perm(x, 0x64646464u, 0x4342)); }
+
+// p as hi + lo, each of 16 bits; lower half: p0
+template <bool F16>
+__device__ __forceinline__ void split(float p0, float p1, uint32_t& hi, uint32_t& lo) {
+  if constexpr (F16) {
+    const __half2 h = __floats2half2_rn(p0, p1);
+    const float2 f = __half22float2(h);
+    const __half2 l = __floats2half2_rn(p0 - f.x, p1 - f.y);
+    hi = *reinterpret_cast<const uint32_t*>(&h);
+    lo = *reinterpret_cast<const uint32_t*>(&l);
+  } else {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
+    const float2 f = __bfloat1622float2(h);
+    const __nv_bfloat162 l = __floats2bfloat162_rn(p0 - f.x, p1 - f.y);
+    hi = *reinterpret_cast<const uint32_t*>(&h);
+    lo = *reinterpret_cast<const uint32_t*>(&l);
+  }
+}
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// The tokens of a sequence that are seen, and their tiles.
+struct Span {
+  int first, end;                    // tokens
+  __device__ __forceinline__ int tile0() const { return first / kTile; }
+  __device__ __forceinline__ int tiles() const { return end > first ? (end - 1) / kTile + 1 - first / kTile : 0; }
+};
+__device__ __forceinline__ Span span_of(const AttnParams& p, int b) {
+  Span s;
+  s.end = checked_length(ptx::ld_global(p.seq_lens + b), p.cache.capacity, p.status);
+  s.first = p.window > 0 && s.end > p.window ? s.end - p.window : 0;
+  return s;
+}
+
+// Where a warp is: tile `tile` (counted within the row) of row (b, r).
+struct Cursor {
+  int b, r, tile, tiles;
+  Span span;
+
+  __device__ __forceinline__ void next(const AttnParams& p) {
+    if (++tile < tiles) return;
+    tile = 0;
+    if (++r < p.rows_of_seq) return;
+    r = 0;
+    do {
+      if (++b >= p.cache.n_seqs) {   // behind the last tile there is none
+        span.first = span.end = 0;
+        tiles = 0x7fffffff;
+        return;
+      }
+      span = span_of(p, b);
+      tiles = span.tiles();
+    } while (tiles == 0);
+  }
+};
+
+// Sums of a row, or of a part of one, in a part's memory: O [NH][D], then the maxima and the sums of p.
+template <typename S>
+struct Part {
+  float* at;
+  __device__ __forceinline__ float& sum(int head, int d) const { return at[head * S::D + d]; }
+  __device__ __forceinline__ float& most(int head) const { return at[S::NH * S::D + head]; }
+  __device__ __forceinline__ float& total(int head) const { return at[S::NH * (S::D + 1) + head]; }
+};
+
+__device__ __forceinline__ float weight(float m, float most) { return m == kNegInf ? 0.f : exp2f(m - most); }
+
+// First query head of a row, and how many there are.
+template <typename S>
+__device__ __forceinline__ int first_head(const AttnParams& p, int r, int& heads) {
+  const int kv = r / p.chunks, chunk = r - kv * p.chunks;
+  heads = min(S::NH, p.group - chunk * S::NH);
+  return kv * p.group + chunk * S::NH;
+}
+
+template <typename S>
+__global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const AttnParams p) {
+  constexpr int D = S::D, NH = S::NH, kThreads = S::kWarps * 32;
+  constexpr bool I8 = S::I8;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int s_scan[kThreads];
+  __shared__ int s_warp[S::kWarps];
+  __shared__ int4 s_head[2 * S::kWarps];   // of a warp's parts: row (-1: none), begins its row, ends it
+
+  const int tid = threadIdx.x, lane = tid & 31, warp = ptx::warp_index();
+  const int lr = lane >> 2, lc = lane & 3;
+  const uint32_t ring = ptx::smem_u32(smem) + warp * S::kRing;
+  float* const first_part = reinterpret_cast<float*>(smem + S::kWarps * S::kRing + warp * S::kPartBytes);
+  float* const last_part = reinterpret_cast<float*>(smem + warp * S::kRing);
+
+  if (tid < 2 * S::kWarps) s_head[tid] = make_int4(-1, 0, 0, 0);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // ---- the tiles of all sequences, and this warp's share of them
+  const int B = p.cache.n_seqs;
+  int total = 0;
+  for (int b = tid; b < B; b += kThreads) total += span_of(p, b).tiles() * p.rows_of_seq;
+  const int mine = total;                   // of sequence tid, when one round takes them all
+  total = __reduce_add_sync(0xffffffffu, total);
+  if (lane == 0) s_warp[warp] = total;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < S::kWarps; ++w) total += s_warp[w];
+  // sequences that are not there have outputs all the same
+  for (int b = blockIdx.x; b < B; b += gridDim.x)
+    if (span_of(p, b).tiles() == 0) {
+      for (int i = tid; i < p.n_heads * (D / 8); i += kThreads)
+        reinterpret_cast<uint4*>(p.out)[(long long)b * p.n_heads * (D / 8) + i] = make_uint4(0, 0, 0, 0);
+      if (p.lse)
+        for (int i = tid; i < p.n_heads; i += kThreads) p.lse[(long long)b * p.n_heads + i] = kNegInf;
+    }
+  // no CTA without a tile for each of its warps, while there are enough
+  const int busy = min((int)gridDim.x, max(1, total / S::kWarps));
+  const bool works = (int)blockIdx.x < busy;
+  const int cta0 = works ? (int)((long long)total * blockIdx.x / busy) : 0;
+  const int cta1 = works ? (int)((long long)total * (blockIdx.x + 1) / busy) : 0;
+  const int begin = cta0 + (int)((long long)(cta1 - cta0) * warp / S::kWarps);
+  const int end = cta0 + (int)((long long)(cta1 - cta0) * (warp + 1) / S::kWarps);
+
+  Cursor in;                                // of the copies; the sums follow with `at`
+  in.b = in.r = in.tile = in.tiles = 0;
+  in.span.first = in.span.end = 0;
+  {
+    int before = 0;                         // tiles of the sequences before this round's
+    for (int base = 0; base < B; base += kThreads) {
+      const int b = base + tid;
+      const int n = B <= kThreads ? mine : (b < B ? span_of(p, b).tiles() * p.rows_of_seq : 0);
+      int sum = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += up;
+      }
+      __syncthreads();                      // s_scan and s_warp of the round before have been read
+      s_scan[tid] = sum;                    // up to and with this one, within the warp
+      if (lane == 31) s_warp[warp] = sum;
+      __syncthreads();
+      int left = begin - before;            // the sequence in which `left` tiles lie before this warp's first
+#pragma unroll
+      for (int w = 0; w < S::kWarps; ++w) {
+        const int of_warp = s_warp[w];
+        if (begin < end && left >= 0 && left < of_warp) {
+          const int upto = s_scan[w * 32 + lane];
+          const int l = __popc(__ballot_sync(0xffffffffu, upto <= left));   // sequences that end before it
+          in.b = base + w * 32 + l;
+          left -= l > 0 ? s_scan[w * 32 + l - 1] : 0;
+          in.span = span_of(p, in.b);
+          in.tiles = in.span.tiles();
+          in.r = left / in.tiles;
+          in.tile = left - in.r * in.tiles;
+          left = -1;
+        } else if (left >= 0) {
+          left -= of_warp;                  // (negative: found, or in a round before)
+        }
+        before += of_warp;
+      }
+    }
+  }
+
+  if (begin < end) {
+    Cursor at = in;
+    const int count = end - begin;
+
+    // Page of token (lane & 15) of the copies' tile, asked for a tile ahead of its use.
+    auto look_up = [&](const Cursor& c, bool there) -> int {
+      const int t = (c.span.tile0() + c.tile) * kTile + (lane & 15);
+      if (!there || t < c.span.first || t >= c.span.end) return 0;
+      return ptx::ld_global(p.cache.table + (long long)c.b * p.cache.max_pages + divide(t, p.cache.by_page));
+    };
+    auto copy_tile = [&](const Cursor& c, int page, int stage) {
+      const int t0 = (c.span.tile0() + c.tile) * kTile;
+      const int kv = c.r / p.chunks;
+      auto seen = [&](int token) { return t0 + token >= c.span.first && t0 + token < c.span.end; };
+      const int t = t0 + (lane & 15);
+      const uint32_t place = t - divide(t, p.cache.by_page) * p.cache.page_size;
+      if ((uint32_t)page >= (uint32_t)p.cache.n_pages) {
+        note_bad_index(p.status);
+        page = 0;
+      }
+      const uint32_t unit = page * p.cache.page16 + place * p.cache.token16 + kv * p.cache.head16;
+      const uint32_t slot = ring + stage * S::kTileBytes;
+      const char* const k = static_cast<const char*>(p.cache.k) + lc * 16;
+      const char* const v = static_cast<const char*>(p.cache.v) + lr * S::kVB;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const char* src = k + (uint64_t)__shfl_sync(0xffffffffu, unit, lr + 8 * i) * 16;
+        const uint32_t bytes = seen(lr + 8 * i) ? 16 : 0;
+#pragma unroll
+        for (int j = 0; j < S::kKC; ++j)
+          cp_async(slot + ((i * S::kKC + j) * 32 + lane) * 16, src + j * 64, bytes, std::integral_constant<int, 16>());
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int token = 2 * lc + (i & 1) + 8 * (i >> 1);
+        const char* src = v + (uint64_t)__shfl_sync(0xffffffffu, unit, token) * 16;
+        const uint32_t bytes = seen(token) ? S::kVB : 0;
+#pragma unroll
+        for (int j = 0; j < S::kVC; ++j)
+          cp_async(slot + S::kVOffset + ((i * S::kVC + j) * 32 + lane) * S::kVB, src + j * 8 * S::kVB, bytes,
+                   std::integral_constant<int, S::kVB>());
+      }
+      if constexpr (I8) {
+        const float* scales = lane < 16 ? p.cache.k_scales : p.cache.v_scales;
+        const long long i = ((long long)page * p.cache.n_kv_heads + kv) * p.cache.page_size + place;
+        cp_async(slot + S::kScaleOffset + lane * 4, scales + i, seen(lane & 15) ? 4 : 0, std::integral_constant<int, 4>());
+      }
+    };
+    auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
+
+    int page = look_up(in, true), issued = 0;
+    auto issue = [&]() {
+      if (issued < count) {
+        copy_tile(in, page, issued % S::kStages);
+        in.next(p);
+        page = look_up(in, issued + 1 < count);
+      }
+      commit();
+      ++issued;
+    };
+#pragma unroll 1
+    for (int i = 0; i < S::kStages - 1; ++i) issue();
+
+    uint32_t qa[D / 16][2], qb[NH > 8 ? D / 16 : 1][2];     // heads lr and lr + 8: words of adjacent channels
+    float to_log2[2] = {p.scale_log2, p.scale_log2};         // of a product of the tensor cores, per head
+    float most[2], sum[2];                                   // of heads lr and lr + 8; sum: of this lane's tokens
+    float acc[D / 16][NH / 8][4];                            // rows: channels, columns: heads 2 lc, 2 lc + 1 (+ 8)
+    float v_ref = 1.f, inv_ref = 1.f;                        // I8: acc is in units of it
+    bool from_start;
+
+    auto begin_row = [&]() {
+      int heads;
+      const int h0 = first_head<S>(p, at.r, heads);
+#pragma unroll
+      for (int i = 0; i < NH / 8; ++i) {
+        uint32_t(*to)[2] = i == 0 ? qa : qb;
+        const int h = lr + 8 * i;
+        const uint16_t* q = p.q + at.b * p.q_row + (long long)(h0 + h) * p.q_head;
+        constexpr int kAdjacent = I8 ? 16 : 8;               // channels of a 16-byte piece of a key
+#pragma unroll
+        for (int j = 0; j < S::kKC; ++j)
+#pragma unroll
+          for (int e = 0; e < kAdjacent / 8; ++e) {
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (h < heads) x = ptx::ld_global(reinterpret_cast<const uint4*>(q + (j * 4 + lc) * kAdjacent + e * 8));
+            const int s = (j * kAdjacent + e * 8) / 4;
+            to[s][0] = x.x, to[s][1] = x.y, to[s + 1][0] = x.z, to[s + 1][1] = x.w;
+          }
+        if constexpr (I8) {
+          // bf16 as binary16: times a power of two that brings the head's largest below 4.  What becomes subnormal there is
+          // 2^-14 of the largest or less, and off by 2^-25 of it at most.
+          float big = 0.f;
+#pragma unroll
+          for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&to[s][e]));
+              big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
+            }
+          big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+          big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+          const int e = min(max((int)(__float_as_uint(big) >> 23) - 127, -126), 126);
+          const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+          to_log2[i] = p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+          for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+              const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&to[s][w]));
+              const __half2 x = __floats2half2_rn(f.x * down, f.y * down);
+              to[s][w] = *reinterpret_cast<const uint32_t*>(&x);
+            }
+        }
+        most[i] = kNegInf;
+        sum[i] = 0.f;
+      }
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+        for (int n = 0; n < NH / 8; ++n) acc[d][n][0] = acc[d][n][1] = acc[d][n][2] = acc[d][n][3] = 0.f;
+      if constexpr (I8) v_ref = 0.f;
+      from_start = at.tile == 0;
+    };
+
+    // acc times a factor per head; lanes have those of heads lr (+ 8)
+    auto rescale = [&](const float (&f)[2]) {
+#pragma unroll
+      for (int n = 0; n < NH / 8; ++n) {
+        const float f0 = __shfl_sync(0xffffffffu, f[n], lc * 8), f1 = __shfl_sync(0xffffffffu, f[n], lc * 8 + 4);
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) {
+          acc[d][n][0] *= f0, acc[d][n][1] *= f1, acc[d][n][2] *= f0, acc[d][n][3] *= f1;
+        }
+      }
+    };
+
+    auto add_tile = [&](int stage) {
+      const uint32_t slot = ring + stage * S::kTileBytes;
+      const int t0 = (at.span.tile0() + at.tile) * kTile;
+      // ---- S = Q K^T, tokens 0..7 and 8..15; two sums each, so that a product waits for the one before the last
+      float s[2][2][4] = {};
+#pragma unroll
+      for (int j = 0; j < S::kKC; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint4 x = lds16(slot + ((i * S::kKC + j) * 32 + lane) * 16);
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          if constexpr (I8) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t u = w[e] ^ 0x80808080u;
+              const int k = 4 * j + e;
+              mma<true>(s[i][e & 1], qa[k][0], NH > 8 ? qb[k % (NH > 8 ? D / 16 : 1)][0] : 0u, qa[k][1],
+                        NH > 8 ? qb[k % (NH > 8 ? D / 16 : 1)][1] : 0u, low_codes(u), high_codes(u));
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int k = 2 * j + e;
+              mma<false>(s[i][e & 1], qa[k][0], NH > 8 ? qb[k % (NH > 8 ? D / 16 : 1)][0] : 0u, qa[k][1],
+                         NH > 8 ? qb[k % (NH > 8 ? D / 16 : 1)][1] : 0u, w[2 * e], w[2 * e + 1]);
+            }
+          }
+        }
+      // ---- scores in powers of two: x[n][i] of heads lr + 8 n and tokens 2 lc + {0, 1} + 8 {0, 1}
+      float x[NH / 8][4], k_scale[4] = {1.f, 1.f, 1.f, 1.f}, v_scale[4] = {1.f, 1.f, 1.f, 1.f};
+      if constexpr (I8) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t token = slot + S::kScaleOffset + (2 * lc + (i & 1) + 8 * (i >> 1)) * 4;
+          k_scale[i] = lds_float(token);
+          v_scale[i] = lds_float(token + 64);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NH / 8; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float y = s[i >> 1][0][2 * n + (i & 1)] + s[i >> 1][1][2 * n + (i & 1)];
+          x[n][i] = (I8 ? y * k_scale[i] : y) * to_log2[n];
+        }
+      if (t0 < at.span.first || at.span.end - t0 < kTile) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int t = t0 + 2 * lc + (i & 1) + 8 * (i >> 1);
+          if (t < at.span.first || t >= at.span.end)
+#pragma unroll
+            for (int n = 0; n < NH / 8; ++n) x[n][i] = kNegInf;
+        }
+      }
+      // ---- running maximum
+      float top[2] = {kNegInf, kNegInf};
+      bool higher = false;
+#pragma unroll
+      for (int n = 0; n < NH / 8; ++n) {
+        top[n] = fmaxf(fmaxf(x[n][0], x[n][1]), fmaxf(x[n][2], x[n][3]));
+        top[n] = fmaxf(top[n], __shfl_xor_sync(0xffffffffu, top[n], 1));
+        top[n] = fmaxf(top[n], __shfl_xor_sync(0xffffffffu, top[n], 2));
+        higher |= top[n] > most[n] + kSlack;
+      }
+      if (__any_sync(0xffffffffu, higher)) {
+        float f[2] = {1.f, 1.f};
+#pragma unroll
+        for (int n = 0; n < NH / 8; ++n) {
+          const float next = fmaxf(most[n], top[n]);
+          f[n] = weight(most[n], next);
+          sum[n] *= f[n];
+          most[n] = next;
+        }
+        rescale(f);
+      }
+      if constexpr (I8) {
+        // Values in units of 2^-6 of the largest scale so far, cut to a power of two: p (at most 2^kSlack) times what is left of its
+        // token's scale (below 2^7) is a binary16, and as two of them off by 2^-25 of a unit at most, 2^-31 of the largest.
+        float big = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) big = fmaxf(big, fabsf(v_scale[i]));
+        const uint32_t exponent = __reduce_max_sync(0xffffffffu, __float_as_uint(big)) & 0x7f800000u;
+        const float unit = __uint_as_float(exponent > (7u << 23) ? exponent - (6u << 23) : 1u << 23);
+        if (unit > v_ref) {
+          if (v_ref > 0.f) {
+            const float both[2] = {v_ref / unit, v_ref / unit};
+            rescale(both);
+          }
+          v_ref = unit;
+          inv_ref = 1.f / unit;
+        }
+      }
+      // ---- p, its sum, and O^T += V^T P^T
+      uint32_t hi[NH / 8][2], lo[NH / 8][2];
+#pragma unroll
+      for (int n = 0; n < NH / 8; ++n) {
+        const float base = most[n] == kNegInf ? 0.f : most[n];
+        float e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          e[i] = exp2f(x[n][i] - base);
+          sum[n] += e[i];
+          if constexpr (I8) e[i] *= v_scale[i] * inv_ref;
+        }
+        split<I8>(e[0], e[1], hi[n][0], lo[n][0]);
+        split<I8>(e[2], e[3], hi[n][1], lo[n][1]);
+      }
+#pragma unroll
+      for (int j = 0; j < S::kVC; ++j) {
+        constexpr int kWords = S::kVB / 4;
+        uint32_t w[4][kWords];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t from = slot + S::kVOffset + ((i * S::kVC + j) * 32 + lane) * S::kVB;
+          if constexpr (S::kVB == 16) {
+            const uint4 v = lds16(from);
+            w[i][0] = v.x, w[i][1] = v.y, w[i][kWords - 2] = v.z, w[i][kWords - 1] = v.w;
+          } else {
+            const uint2 v = lds8(from);
+            w[i][0] = v.x, w[i][1] = v.y;
+          }
+        }
+        auto product = [&](int d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+#pragma unroll
+          for (int n = 0; n < NH / 8; ++n) {
+            mma<I8>(acc[d][n], a0, a1, a2, a3, hi[n][0], hi[n][1]);
+            mma<I8>(acc[d][n], a0, a1, a2, a3, lo[n][0], lo[n][1]);
+          }
+        };
+#pragma unroll
+        for (int e = 0; e < kWords; ++e) {
+          if constexpr (I8) {
+            // bytes of two tokens side by side: channels 0, 0, 1, 1 and 2, 2, 3, 3 of the word
+            const uint32_t a = __byte_perm(w[0][e], w[1][e], 0x5140) ^ 0x80808080u, b = __byte_perm(w[2][e], w[3][e], 0x5140) ^ 0x80808080u;
+            const uint32_t c = __byte_perm(w[0][e], w[1][e], 0x7362) ^ 0x80808080u, f = __byte_perm(w[2][e], w[3][e], 0x7362) ^ 0x80808080u;
+            product(2 * (j * kWords + e), low_codes(a), high_codes(a), low_codes(b), high_codes(b));
+            product(2 * (j * kWords + e) + 1, low_codes(c), high_codes(c), low_codes(f), high_codes(f));
+          } else {
+            product(j * kWords + e, __byte_perm(w[0][e], w[1][e], 0x5410), __byte_perm(w[0][e], w[1][e], 0x7632),
+                    __byte_perm(w[2][e], w[3][e], 0x5410), __byte_perm(w[2][e], w[3][e], 0x7632));
+          }
+        }
+      }
+    };
+
+    // The row's sums, or what this warp has of them, are complete.  acc[d] holds channels base + 2 e and base + 2 e + 1 in its
+    // rows lr and lr + 8, where d = j * kEV / 2 + e and base = (j * 8 + lr) * kEV.
+    auto end_row = [&](bool to_end, bool more) {
+#pragma unroll
+      for (int n = 0; n < NH / 8; ++n) {
+        sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 1);
+        sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 2);
+      }
+      int heads;
+      const int h0 = first_head<S>(p, at.r, heads);
+      if (from_start && to_end) {
+#pragma unroll
+        for (int n = 0; n < NH / 8; ++n) {
+          const float inv = 1.f / sum[n];
+          const long long out0 = (long long)at.b * p.n_heads + h0 + 8 * n;
+          if (p.lse && lc == 0 && lr + 8 * n < heads) p.lse[out0 + lr] = kLn2 * (most[n] + log2f(sum[n]));
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const int h = 2 * lc + c;
+            const float f = __shfl_sync(0xffffffffu, inv, lc * 8 + c * 4) * v_ref;
+            if (h + 8 * n < heads) {
+              uint16_t* out = p.out + (out0 + h) * D + lr * S::kEV;
+#pragma unroll
+              for (int j = 0; j < S::kVC; ++j)
+#pragma unroll
+                for (int e = 0; e < S::kEV / 2; e += 4) {
+                  uint32_t o[4];
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) {
+                    const float* a = acc[j * (S::kEV / 2) + e + i][n];
+                    o[i] = bf16_pair(a[c] * f, a[c + 2] * f);
+                  }
+                  *reinterpret_cast<uint4*>(out + j * 8 * S::kEV + e * 2) = make_uint4(o[0], o[1], o[2], o[3]);
+                }
+            }
+          }
+        }
+        return;
+      }
+      // a warp's last part lies in its ring, which no copy of its own fills any more
+      if (!more) asm volatile("cp.async.wait_group 0;" ::: "memory");
+      __syncwarp();
+      const int which = more ? 0 : 1;
+      const Part<S> part{more ? first_part : last_part};
+#pragma unroll
+      for (int n = 0; n < NH / 8; ++n) {
+        if (lc == 0) {
+          part.most(lr + 8 * n) = most[n];
+          part.total(lr + 8 * n) = sum[n];
+        }
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) {
+          const int j = d / (S::kEV / 2), e = d % (S::kEV / 2);
+          const int ch = (j * 8 + lr) * S::kEV + 2 * e;
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+            *reinterpret_cast<float2*>(&part.sum(2 * lc + c + 8 * n, ch)) = make_float2(acc[d][n][c] * v_ref, acc[d][n][c + 2] * v_ref);
+        }
+      }
+      if (lane == 0) s_head[2 * warp + which] = make_int4(at.b * p.rows_of_seq + at.r, from_start, to_end, 0);
+    };
+
+    bool fresh = true;
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {
+      if (fresh) begin_row();
+      asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
+      if constexpr (I8) __syncwarp();       // the scales are read by other lanes than copied them
+      issue();
+      add_tile(i % S::kStages);
+      fresh = at.tile + 1 == at.tiles;
+      if (fresh || i + 1 == count) end_row(fresh, i + 1 < count);
+      at.next(p);
+    }
+  }
+  __syncthreads();
+
+  // ---- rows that no warp has alone: parts of one row follow one another
+  constexpr int kItems = NH * D / 4;
+  int4* const headers = p.headers + 2 * blockIdx.x;
+  int crossing[2] = {-1, -1}, ends_here[2] = {0, 0};
+  for (int item = tid; item < kItems; item += kThreads) {
+    const int head = item / (D / 4), d = item % (D / 4) * 4;
+    float most = kNegInf, total_p = 0.f;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    int row = -1, starts = 0, ends = 0;
+    auto finish = [&]() {
+      if (row < 0) return;
+      if (starts && ends) {
+        const int b = row / p.rows_of_seq;
+        int heads;
+        const int h0 = first_head<S>(p, row - b * p.rows_of_seq, heads);
+        if (head < heads) {
+          const float inv = 1.f / total_p;
+          const long long o = (long long)b * p.n_heads + h0 + head;
+          *reinterpret_cast<uint2*>(p.out + o * D + d) = make_uint2(bf16_pair(sum.x * inv, sum.y * inv), bf16_pair(sum.z * inv, sum.w * inv));
+          if (p.lse && d == 0) p.lse[o] = kLn2 * (most + log2f(total_p));
+        }
+        return;
+      }
+      const int which = starts ? 1 : 0;
+      const Part<S> part{p.parts + (2ll * blockIdx.x + which) * S::kPart};
+      *reinterpret_cast<float4*>(&part.sum(head, d)) = sum;
+      if (d == 0) {
+        part.most(head) = most;
+        part.total(head) = total_p;
+      }
+      crossing[which] = row;
+      ends_here[which] = ends;
+    };
+    for (int i = 0; i < 2 * S::kWarps; ++i) {
+      const int4 h = s_head[i];
+      if (h.x < 0) continue;
+      if (h.x != row) {
+        finish();
+        row = h.x, starts = h.y, most = kNegInf, total_p = 0.f, sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      ends = h.z;
+      const Part<S> part{reinterpret_cast<float*>(i & 1 ? smem + (i >> 1) * S::kRing
+                                                        : smem + S::kWarps * S::kRing + (i >> 1) * S::kPartBytes)};
+      const float m = part.most(head), next = fmaxf(most, m);
+      const float a = weight(most, next), b = weight(m, next);
+      const float4 v = *reinterpret_cast<const float4*>(&part.sum(head, d));
+      total_p = total_p * a + part.total(head) * b;
+      sum.x = sum.x * a + v.x * b, sum.y = sum.y * a + v.y * b, sum.z = sum.z * a + v.z * b, sum.w = sum.w * a + v.w * b;
+      most = next;
+    }
+    finish();
+  }
+  if (tid == 0) {
+    headers[0] = make_int4(crossing[0], ends_here[0], 0, 0);
+    headers[1] = make_int4(crossing[1], ends_here[1], 0, 0);
+  }
+}
+
+// Joins the rows that cross CTAs.  CTA i takes the row that begins in CTA i of the kernel before and goes on in the next ones.
+constexpr int kMaxCtas = 256;
+template <typename S>
+__global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, const int ctas) {
+  constexpr int D = S::D, NH = S::NH;
+  __shared__ float s_weight[NH][kMaxCtas];
+  __shared__ float s_inv[NH];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int4 own = ptx::behind_wait(p.headers)[2 * blockIdx.x + 1];
+  const int row = own.x;
+  if (row < 0) return;
+  // parts of the row: the own one, then the first ones of the CTAs behind, up to the one that has the row's end
+  int n = 1;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  for (int base = blockIdx.x + 1; base < ctas; base += 32) {
+    const int c = base + lane;
+    const int4 h = c < ctas ? ptx::behind_wait(p.headers)[2 * c] : make_int4(-1, 1, 0, 0);
+    const uint32_t stop = __ballot_sync(0xffffffffu, h.x != row || h.y);
+    if (stop) {
+      const int l = __ffs(stop) - 1;
+      n += l + (__shfl_sync(0xffffffffu, h.x, l) == row ? 1 : 0);
+      break;
+    }
+    n += 32;
+  }
+  auto part_of = [&](int i) { return Part<S>{p.parts + (i == 0 ? 2ll * blockIdx.x + 1 : 2ll * (blockIdx.x + i)) * S::kPart}; };
+  const int b = row / p.rows_of_seq;
+  int heads;
+  const int h0 = first_head<S>(p, row - b * p.rows_of_seq, heads);
+  for (int head = warp; head < heads; head += 8) {
+    float most = kNegInf;
+    for (int i = lane; i < n; i += 32) most = fmaxf(most, part_of(i).most(head));
+#pragma unroll
+    for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    float total = 0.f;
+    for (int i = lane; i < n; i += 32) {
+      const float w = weight(part_of(i).most(head), most);
+      s_weight[head][i] = w;
+      total += w * part_of(i).total(head);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    if (lane == 0) {
+      s_inv[head] = 1.f / total;
+      if (p.lse) p.lse[(long long)b * p.n_heads + h0 + head] = kLn2 * (most + log2f(total));
+    }
+  }
+  __syncthreads();
+  for (int item = tid; item < heads * (D / 4); item += 256) {
+    const int head = item / (D / 4), d = item % (D / 4) * 4;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const float w = s_weight[head][i];
+      const float4 v = *reinterpret_cast<const float4*>(&part_of(i).sum(head, d));
+      sum.x += w * v.x, sum.y += w * v.y, sum.z += w * v.z, sum.w += w * v.w;
+    }
+    const float inv = s_inv[head];
+    const long long o = (long long)b * p.n_heads + h0 + head;
+    *reinterpret_cast<uint2*>(p.out + o * D + d) = make_uint2(bf16_pair(sum.x * inv, sum.y * inv), bf16_pair(sum.z * inv, sum.w * inv));
+  }
+}
+
+int attn_ctas() { return min(sm_count_or(148), kMaxCtas); }
+
+// Query heads of a row of work.
+int heads_of_row(int group, int dim) { return group <= 8 || dim > 128 ? 8 : 16; }
+
+template <int D, int NH, bool I8>
+int launch(const AttnParams& p, cudaStream_t st) {
+  using S = Shape<D, NH, I8>;
+  static std::atomic<uint64_t> allowed{0};
+  PEQA_TRY(allow_smem(attn_decode_kernel<S>, S::kSmem, allowed));
+  const int ctas = attn_ctas();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas, 1, 1);
+  cfg.blockDim = dim3(S::kWarps * 32, 1, 1);
+  cfg.dynamicSmemBytes = S::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  PEQA_CUDA(cudaLaunchKernelEx(&cfg, attn_decode_kernel<S>, p));
+  return launch_after(attn_join_kernel<S>, ctas, 256, st, p, ctas);
+}
+
+template <int D, bool I8>
+int launch_heads(const AttnParams& p, int nh, cudaStream_t st) {
+  if constexpr (D <= 128)
+    if (nh == 16) return launch<D, 16, I8>(p, st);
+  return launch<D, 8, I8>(p, st);
+}
+
+template <bool I8>
+int launch_dim(const AttnParams& p, int dim, int nh, cudaStream_t st) {
+  switch (dim) {
+    case 64: return launch_heads<64, I8>(p, nh, st);
+    case 128: return launch_heads<128, I8>(p, nh, st);
+    default: return launch_heads<256, I8>(p, nh, st);
+  }
+}
+
+size_t workspace_bytes(int dim, int nh) {
+  return (size_t)attn_ctas() * 2 * (sizeof(int4) + (size_t)nh * (dim + 2) * sizeof(float));
+}
+
+}  // namespace
+}  // namespace peqa
+
+using namespace peqa;
+
+extern "C" size_t peqa_attn_workspace_bytes(const peqa_kv_cache_t* c, int n_heads) {
+  if (!c || c->n_kv_heads < 1 || n_heads < 1 || n_heads % c->n_kv_heads != 0) return 0;
+  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return 0;
+  return workspace_bytes(c->head_dim, heads_of_row(n_heads / c->n_kv_heads, c->head_dim));
+}
+
+extern "C" int peqa_attn_decode(const peqa_kv_cache_t* c, const peqa_rows_t* q, int n_heads, const int32_t* seq_lens,
+                                float scale, int window, void* out, float* lse, void* workspace, size_t bytes,
+                                void* stream) {
+  AttnParams p = {};
+  PEQA_TRY(check_kv_cache(c, &p.cache));
+  if (!q || !seq_lens || !out) return PEQA_ERR_NULL;
+  if (n_heads < 1 || n_heads % c->n_kv_heads != 0 || window < 0) return PEQA_ERR_BAD_SHAPE;
+  PEQA_TRY(check_rows(q, c->n_seqs, n_heads, c->head_dim, false));
+  if (!aligned16(out)) return PEQA_ERR_ALIGNMENT;
+  if ((reinterpret_cast<uintptr_t>(seq_lens) | reinterpret_cast<uintptr_t>(lse)) & 3u) return PEQA_ERR_ALIGNMENT;
+  p.group = n_heads / c->n_kv_heads;
+  const int nh = heads_of_row(p.group, c->head_dim);
+  p.chunks = (p.group + nh - 1) / nh;
+  // tiles and rows are numbered in 31 bits
+  const long long rows_of_seq = (long long)c->n_kv_heads * p.chunks, rows = c->n_seqs * rows_of_seq;
+  if (rows > 0x7fffffffll || rows > 0x7fffffffll / (p.cache.capacity / kTile + 2)) return PEQA_ERR_TOO_LARGE;
+  p.rows_of_seq = (int)rows_of_seq;
+  PEQA_TRY(check_arch());
+  if (!workspace || bytes < workspace_bytes(c->head_dim, nh)) return PEQA_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return PEQA_ERR_ALIGNMENT;
+  p.q = static_cast<const uint16_t*>(q->data);
+  p.q_row = c->n_seqs > 1 ? q->row_stride : 0;
+  p.q_head = n_heads > 1 ? q->head_stride : 0;
+  p.seq_lens = seq_lens;
+  p.n_heads = n_heads;
+  p.scale_log2 = scale * kLog2e;
+  p.window = window;
+  p.out = static_cast<uint16_t*>(out);
+  p.lse = lse;
+  p.headers = static_cast<int4*>(workspace);
+  p.parts = reinterpret_cast<float*>(p.headers + 2 * attn_ctas());
+  cudaStream_t st = as_stream(stream);
+  PEQA_TRY(status_word(st, &p.status));
+  return c->type == PEQA_KV_INT8 ? launch_dim<true>(p, c->head_dim, nh, st) : launch_dim<false>(p, c->head_dim, nh, st);
+}

@@ -88,7 +88,8 @@ int check_arch();
 
 // Device address of the status slot kernels launched on `st` report to, on the current
 // device.  A slot is int[8]: [0] status code, [1..3] where, [4] bound of a single device-side
-// wait in microseconds, [5] self-test knob (see peqa_selftest_configure), [6..7] unused.
+// wait in microseconds, [5] self-test knob (see peqa_selftest_configure), [6] set by the kernels of the key-value
+// cache (kv_cache.cuh), [7] unused.
 // Streams get slots of their own (first come, first served; the last slot is shared by any
 // further streams).  The first call on a device initialises the table with a blocking copy.
 constexpr int kStatusSlots = 32;

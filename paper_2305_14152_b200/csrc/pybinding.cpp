@@ -6,9 +6,12 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <cmath>
+#include <cstdint>
 #include <vector>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -19,6 +22,7 @@ namespace {
 
 PyObject* g_error = nullptr;                       // binding.PeqaError
 PyObject *s_bits, *s_N, *s_K, *s_group, *s_qweight, *s_zeros, *s_scales;
+PyObject *s_k, *s_v_cache, *s_page_table, *s_k_scales, *s_v_scales;
 PyObject *s_w, *s_X, *s_dY, *s_Y, *s_dX, *s_dS, *s_m, *s_v, *s_workspace;
 
 // A Python error is set; unwinds to the function's END_HANDLE_TH_ERRORS.
@@ -327,9 +331,205 @@ PyObject* layer_train_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- the paged key-value cache
+
+[[noreturn]] void refuse(const char* what, const char* wanted) {
+  PyErr_Format(PyExc_ValueError, "%s: expected %s", what, wanted);
+  fail();
+}
+
+// Memory of the current device, in use by the current stream.
+void here(const at::Tensor& t, const char* name) {
+  if (!t.is_cuda() || t.get_device() != c10::cuda::current_device()) refuse(name, "a tensor on the current CUDA device");
+}
+
+// A contiguous tensor of this type and of n values in all, on the current device.
+const at::Tensor& values(PyObject* o, at::ScalarType dtype, int64_t n, const char* name) {
+  const at::Tensor& t = dev(o, dtype, name);
+  here(t, name);
+  if (t.numel() != n) {
+    PyErr_Format(PyExc_ValueError, "%s: expected %lld values, got %lld", name, (long long)n, (long long)t.numel());
+    fail();
+  }
+  return t;
+}
+
+int whole(PyObject* o, const char* name) {
+  const long long v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) fail();
+  if (v < INT32_MIN || v > INT32_MAX) refuse(name, "a whole number of 32 bits");
+  return (int)v;
+}
+int size32(const at::Tensor& t, int dim, const char* name) {
+  const int64_t n = t.size(dim);
+  if (n > INT32_MAX) refuse(name, "sizes of 31 bits");
+  return (int)n;
+}
+
+// bf16 [rows, heads, head_dim], channels dense.
+struct HeadRows {
+  peqa_rows_t r;
+  int rows, heads;
+  HeadRows(PyObject* o, int head_dim, const char* name) {
+    const at::Tensor& t = tensor(o, name);
+    here(t, name);
+    if (t.scalar_type() != at::kBFloat16 || t.dim() != 3 || t.size(2) != head_dim || t.stride(2) != 1)
+      refuse(name, "a torch.bfloat16 tensor [rows, heads, head_dim] with dense channels");
+    r.data = t.data_ptr();
+    r.row_stride = t.stride(0);
+    r.head_stride = t.stride(1);
+    rows = size32(t, 0, name);
+    heads = size32(t, 1, name);
+  }
+};
+
+struct Cache {
+  peqa_kv_cache_t c = {};
+  explicit Cache(PyObject* o) {
+    const Ref pk(PyObject_GetAttr(o, s_k)), pv(PyObject_GetAttr(o, s_v_cache)), pt(PyObject_GetAttr(o, s_page_table)),
+        pks(PyObject_GetAttr(o, s_k_scales)), pvs(PyObject_GetAttr(o, s_v_scales));
+    const at::Tensor &k = tensor(pk.p, "k"), &v = tensor(pv.p, "v");
+    here(k, "cache.k");
+    here(v, "cache.v");
+    const bool codes = k.scalar_type() == at::kChar;
+    if ((!codes && k.scalar_type() != at::kBFloat16) || k.dim() != 4 || k.stride(3) != 1)
+      refuse("cache.k", "a torch.bfloat16 or torch.int8 tensor [n_pages, page_size, n_kv_heads, head_dim] with dense channels");
+    if (v.scalar_type() != k.scalar_type() || v.sizes() != k.sizes()) refuse("cache.v", "a tensor of cache.k's type and shape");
+    for (int d = 0; d < 4; ++d)
+      if (k.size(d) != 1 && k.stride(d) != v.stride(d)) refuse("cache.v", "cache.k's strides");
+    c.type = codes ? PEQA_KV_INT8 : PEQA_KV_BF16;
+    c.n_pages = size32(k, 0, "cache.k");
+    c.page_size = size32(k, 1, "cache.k");
+    c.n_kv_heads = size32(k, 2, "cache.k");
+    c.head_dim = size32(k, 3, "cache.k");
+    c.page_stride = k.stride(0);
+    c.token_stride = k.stride(1);
+    c.head_stride = k.stride(2);
+    c.k = k.data_ptr();
+    c.v = v.data_ptr();
+    if (codes) {
+      const int64_t n = k.size(0) * k.size(1) * k.size(2);
+      c.k_scales = static_cast<float*>(values(pks.p, at::kFloat, n, "cache.k_scales").data_ptr());
+      c.v_scales = static_cast<float*>(values(pvs.p, at::kFloat, n, "cache.v_scales").data_ptr());
+    }
+    const at::Tensor& t = dev(pt.p, at::kInt, "cache.page_table");
+    here(t, "cache.page_table");
+    if (t.dim() != 2) refuse("cache.page_table", "[n_seqs, max_pages]");
+    c.n_seqs = size32(t, 0, "cache.page_table");
+    c.max_pages = size32(t, 1, "cache.page_table");
+    c.page_table = static_cast<const int32_t*>(t.data_ptr());
+  }
+};
+
+// (cache, q, k, v, cos_sin, seq_lens, starts, q_out, interleaved) -> q_out
+PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  arity(n, 9);
+  const Cache cache(a[0]);
+  const HeadRows k(a[2], cache.c.head_dim, "k"), v(a[3], cache.c.head_dim, "v");
+  if (k.heads != cache.c.n_kv_heads) refuse("k", "the cache's heads");
+  if (v.heads != k.heads || v.rows != k.rows) refuse("v", "k's shape");
+  const at::Tensor& table = dev(a[4], at::kFloat, "cos_sin");
+  here(table, "cos_sin");
+  if (table.dim() != 2) refuse("cos_sin", "[n_positions, rotary_dim]");
+  const int positions = size32(table, 0, "cos_sin"), rotary = size32(table, 1, "cos_sin");
+  const int32_t* lens = static_cast<const int32_t*>(values(a[5], at::kInt, cache.c.n_seqs, "seq_lens").data_ptr());
+  const int32_t* starts = nullptr;
+  if (a[6] != Py_None)
+    starts = static_cast<const int32_t*>(values(a[6], at::kInt, (int64_t)cache.c.n_seqs + 1, "starts").data_ptr());
+  else if (k.rows != cache.c.n_seqs)
+    refuse("k", "one row per sequence, or starts");
+  const int interleaved = PyObject_IsTrue(a[8]);
+  if (interleaved < 0) fail();
+  void* st = stream();
+  const float* angles = static_cast<const float*>(table.data_ptr());
+  if (a[1] == Py_None) {
+    if (a[7] != Py_None) refuse("q_out", "q beside it");
+    check(unlocked([&] {
+            return peqa_kv_append(&cache.c, nullptr, 0, &k.r, &v.r, k.rows, angles, positions, rotary, interleaved, lens, starts,
+                                  nullptr, st);
+          }),
+          "peqa_kv_append");
+    Py_RETURN_NONE;
+  }
+  const HeadRows q(a[1], cache.c.head_dim, "q");
+  if (q.rows != k.rows) refuse("q", "k's rows");
+  PyObject* made = a[7];
+  if (made == Py_None) {
+    // rows that are left out keep what their memory had: a new tensor has zeros there
+    made = THPVariable_Wrap(at::zeros({q.rows, q.heads, cache.c.head_dim}, tensor(a[1], "q").options()));
+    if (!made) fail();
+  } else {
+    Py_INCREF(made);
+  }
+  Ref out(made);
+  const HeadRows to(out.p, cache.c.head_dim, "q_out");
+  if (to.rows != q.rows || to.heads != q.heads) refuse("q_out", "q's shape");
+  check(unlocked([&] {
+          return peqa_kv_append(&cache.c, &q.r, q.heads, &k.r, &v.r, k.rows, angles, positions, rotary, interleaved, lens, starts,
+                                &to.r, st);
+        }),
+        "peqa_kv_append");
+  Py_INCREF(out.p);
+  return out.p;
+  END_HANDLE_TH_ERRORS
+}
+
+// (cache, q, seq_lens, scale, window, out, workspace, return_lse) -> out, or (out, lse)
+PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  arity(n, 8);
+  const Cache cache(a[0]);
+  const HeadRows q(a[1], cache.c.head_dim, "q");
+  if (q.rows != cache.c.n_seqs) refuse("q", "one row per sequence");
+  const int32_t* lens = static_cast<const int32_t*>(values(a[2], at::kInt, cache.c.n_seqs, "seq_lens").data_ptr());
+  const float scale = a[3] == Py_None ? (float)(1.0 / std::sqrt((double)cache.c.head_dim)) : as_float(a[3]);
+  const int window = whole(a[4], "window");
+  const at::Tensor& like = tensor(a[1], "q");
+  at::Tensor out, lse, own;
+  if (a[5] == Py_None) {
+    out = at::empty({q.rows, q.heads, cache.c.head_dim}, like.options());
+  } else {
+    out = values(a[5], at::kBFloat16, (int64_t)q.rows * q.heads * cache.c.head_dim, "out");
+    if (out.dim() != 3 || out.size(0) != q.rows || out.size(1) != q.heads) refuse("out", "q's shape");
+  }
+  const int with_lse = PyObject_IsTrue(a[7]);
+  if (with_lse < 0) fail();
+  if (with_lse) lse = at::empty({q.rows, q.heads}, like.options().dtype(at::kFloat));
+  void* wp = nullptr;
+  size_t wb = 0;
+  if (a[6] == Py_None) {
+    wb = peqa_attn_workspace_bytes(&cache.c, q.heads);
+    if (wb > 0) {
+      own = at::empty({(int64_t)wb}, like.options().dtype(at::kByte));
+      wp = own.data_ptr();
+    }
+  } else {
+    const at::Tensor& t = tensor(a[6], "workspace");
+    here(t, "workspace");
+    if (!t.is_contiguous()) refuse("workspace", "a contiguous tensor");
+    const Workspace given(a[6]);
+    wp = given.p;
+    wb = given.bytes;
+  }
+  void *o = out.data_ptr(), *st = stream();
+  float* l = with_lse ? static_cast<float*>(lse.data_ptr()) : nullptr;
+  check(unlocked([&] { return peqa_attn_decode(&cache.c, &q.r, q.heads, lens, scale, window, o, l, wp, wb, st); }),
+        "peqa_attn_decode");
+  Ref first(a[5] == Py_None ? THPVariable_Wrap(std::move(out)) : (Py_INCREF(a[5]), a[5]));
+  if (!with_lse) {
+    Py_INCREF(first.p);
+    return first.p;
+  }
+  Ref second(THPVariable_Wrap(std::move(lse)));
+  return PyTuple_Pack(2, first.p, second.p);
+  END_HANDLE_TH_ERRORS
+}
+
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {FAST(qlinear_fwd),       FAST(qlinear_fwd_zf), FAST(qlinear_decode), FAST(qlinear_decode_prepared),
                           FAST(scale_adamw),       FAST(zero_adamw),     FAST(layer_train_step),
+                          FAST(kv_append),         FAST(attn_decode),
                           {"bind_error", bind_error, METH_O, nullptr},   {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
@@ -341,7 +541,9 @@ PyMODINIT_FUNC PyInit__native() {
     const char* text;
   } names[] = {{&s_bits, "bits"}, {&s_N, "N"}, {&s_K, "K"}, {&s_group, "group_size"}, {&s_qweight, "qweight"},
                {&s_zeros, "zeros"}, {&s_scales, "scales"}, {&s_w, "w"}, {&s_X, "X"}, {&s_dY, "dY"}, {&s_Y, "Y"},
-               {&s_dX, "dX"}, {&s_dS, "dS"}, {&s_m, "m"}, {&s_v, "v"}, {&s_workspace, "workspace"}};
+               {&s_dX, "dX"}, {&s_dS, "dS"}, {&s_m, "m"}, {&s_v, "v"}, {&s_workspace, "workspace"},
+               {&s_k, "k"}, {&s_v_cache, "v"}, {&s_page_table, "page_table"}, {&s_k_scales, "k_scales"},
+               {&s_v_scales, "v_scales"}};
   for (const auto& e : names)
     if (!(*e.to = PyUnicode_InternFromString(e.text))) return nullptr;
   return PyModule_Create(&kModule);
