@@ -7,12 +7,12 @@
 // but memory, and the rest is laid out to keep copies in flight:
 //   * A tile is 16 tokens of a row.  Tiles are numbered through all sequences, heads and lengths, and dealt evenly: every CTA
 //     takes an equal run of them, every warp an equal run of its CTA's.  Nothing depends on how uneven the lengths are.
-//   * A warp copies its own tiles into its own ring of shared memory (cp.async, several tiles ahead).  Which lane copies what is chosen
-//     so that each lane reads back exactly the 16 bytes it has copied itself: as operands of the tensor cores' m16n8k16 product, with
-//     the channels of the contraction taken in whatever order this gives, q in the same one.  So there is no barrier, no bank conflict and no
-//     transposition in the loop.
+//   * A warp copies its own tiles into its own ring of shared memory (cp.async, several units of 16 keys or values ahead), whole
+//     tokens at a time, and reads them as operands of the tensor cores' m16n8k16 product: the channels of the contraction and
+//     the tokens of a tile are taken in whatever order makes one 16-byte load serve several products without bank conflicts.  So there
+//     is no barrier between warps and no transposition in the loop.
 //       S = Q K^T      Q [16 heads x 16 channels] in registers, K the other operand: a lane holds 4 adjacent channels of a token
-//       O^T = V^T P^T  V^T [16 channels x 16 tokens]: a lane holds the same channels of four tokens and pairs them byte by byte (prmt);
+//       O^T = V^T P^T  V^T [16 channels x 16 tokens]: a lane loads the same channels of four tokens and pairs them byte by byte (prmt);
 //                      S leaves the first product laid out as the operand P^T of the second
 //   * Running maximum and sum per row, as the softmax allows: the sums are rescaled only when the maximum has risen by more than
 //     kSlack (a factor of 2^8 that the binary32 sums carry easily).
@@ -51,34 +51,38 @@ struct AttnParams {
   float* lse;
   int4* headers;                     // [2 * CTAs]: row, whether its last tile is in the part
   float* parts;                      // [2 * CTAs][Shape::kPart]
+  float* first_parts;                // [CTAs][warps][Shape::kPart]
   int* status;
 };
 
-// Everything that follows from the channels D, the query heads NH of a row and the type of the cache.
-template <int D_, int NH_, bool I8_>
+// Everything that follows from the channels D, the query heads NH of a row, the type of the cache and whether a tile lies in
+// one page (WHOLE: the page size is a multiple of 16).
+template <int D_, int NH_, bool I8_, bool WHOLE_>
 struct Shape {
   static constexpr int D = D_, NH = NH_;
-  static constexpr bool I8 = I8_;
+  static constexpr bool I8 = I8_, WHOLE = WHOLE_;
+  static constexpr bool kHalves = NH == 4;                      // the two numbers that p is are columns of one product
+  static constexpr int kCols = NH > 8 ? 2 : 1;                  // of eight heads (kHalves: of four, twice)
   static constexpr int kBytes = D * (I8 ? 1 : 2);               // of a token
   static constexpr int kKC = kBytes / 64;                       // 16-byte pieces per lane of a token's key, 4 lanes side by side
   static constexpr int kVB = kBytes >= 128 ? 16 : 8;            // bytes per lane of a token's value, 8 lanes side by side
   static constexpr int kVC = kBytes / (8 * kVB);
   static constexpr int kEV = kVB / (I8 ? 1 : 2);                // channels in them
-  static constexpr int kVOffset = kTile * kBytes;
-  static constexpr int kScaleOffset = 2 * kTile * kBytes;
-  static constexpr int kTileBytes = kScaleOffset + (I8 ? 128 : 0);
-  static constexpr int kWarps = D > 128 ? 4 : NH > 8 && kTileBytes > 8000 ? 6 : 8;   // as many as have three tiles in shared memory
+  static constexpr int kPieces = kBytes / 16;                   // 16-byte pieces of a token
+  static constexpr int kRows = 32 / kPieces;                    // tokens that a warp copies with one instruction
+  static constexpr int kUnit = kTile * kBytes;                  // keys or values of a tile
+  static constexpr int kWarps = D > 128 || NH > 8 ? 8 : 16;     // by the registers that a thread needs
+  static constexpr int kFit = 192 * 1024 / (kWarps * (kUnit + (I8 ? 64 : 0)));
+  static constexpr int kUnits = kFit >= 9 ? 9 : kFit >= 7 ? 7 : kFit >= 5 ? 5 : 3;   // odd: keys follow keys, values values
+  static constexpr int kRing = kUnits * kUnit;
+  static constexpr int kSmem = kWarps * (kRing + (I8 ? kUnits * 64 : 0));            // and the scales of a unit's 16 tokens
   static constexpr int kPart = NH * (D + 2);                    // floats of a part: sums, maxima, sums of p
-  static constexpr int kPartBytes = (kPart * 4 + 127) / 128 * 128;
-  static constexpr int kMost = 227 * 1024 - 2048;               // what a CTA may have, less what is declared statically
-  static constexpr int kSpare = kMost - kWarps * kPartBytes;
-  static constexpr int kStagesFit = kSpare / (kWarps * kTileBytes);
-  static constexpr int kStages = kStagesFit > 8 ? 8 : kStagesFit;
-  static constexpr int kRing = kStages * kTileBytes;
-  static constexpr int kSmem = kWarps * (kRing + kPartBytes);
-  static_assert(kStages >= 3 && kRing >= kPartBytes && kSmem <= kMost, "shared memory");
+  static_assert(kFit >= 3 && kRing >= kPart * 4 && kRing % 1024 == 0 && kPart % 4 == 0, "shared memory");
 };
 
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, std::integral_constant<int, 16>) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, uint32_t bytes, std::integral_constant<int, 16>) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
@@ -114,6 +118,22 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+template <bool F16>
+__device__ __forceinline__ void mma0(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (F16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// 2^x, 0 below 2^-126
+__device__ __forceinline__ float power_of_two(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Codes of 8 bits as binary16: with its sign bit turned a code c is the byte c + 128, and 0x6400 | byte is 1024 + 128 + c.
 __device__ __forceinline__ uint32_t less_bias(uint32_t h) {
   const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&h), __half2half2(__ushort_as_half(0x6480)));
@@ -123,22 +143,21 @@ __device__ __forceinline__ uint32_t less_bias(uint32_t h) {
 __device__ __forceinline__ uint32_t low_codes(uint32_t x) { return less_bias(__byte_perm(x, 0x64646464u, 0x4140)); }
 __device__ __forceinline__ uint32_t high_codes(uint32_t x) { return less_bias(__byte_perm(x, 0x64646464u, 0x4342)); }
 
-// p as hi + lo, each of 16 bits; lower half: p0
+// Two numbers rounded to 16 bits, and what that leaves of them; lower half: p0.
 template <bool F16>
-__device__ __forceinline__ void split(float p0, float p1, uint32_t& hi, uint32_t& lo) {
+__device__ __forceinline__ uint32_t round16(float& p0, float& p1) {
+  uint32_t w;
   if constexpr (F16) {
     const __half2 h = __floats2half2_rn(p0, p1);
     const float2 f = __half22float2(h);
-    const __half2 l = __floats2half2_rn(p0 - f.x, p1 - f.y);
-    hi = *reinterpret_cast<const uint32_t*>(&h);
-    lo = *reinterpret_cast<const uint32_t*>(&l);
+    p0 -= f.x, p1 -= f.y;
+    w = *reinterpret_cast<const uint32_t*>(&h);
   } else {
     const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
-    const float2 f = __bfloat1622float2(h);
-    const __nv_bfloat162 l = __floats2bfloat162_rn(p0 - f.x, p1 - f.y);
-    hi = *reinterpret_cast<const uint32_t*>(&h);
-    lo = *reinterpret_cast<const uint32_t*>(&l);
+    w = *reinterpret_cast<const uint32_t*>(&h);
+    p0 -= __uint_as_float(w << 16), p1 -= __uint_as_float(w & 0xffff0000u);
   }
+  return w;
 }
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
@@ -201,9 +220,9 @@ __device__ __forceinline__ int first_head(const AttnParams& p, int r, int& heads
 
 template <typename S>
 __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const AttnParams p) {
-  constexpr int D = S::D, NH = S::NH, kThreads = S::kWarps * 32;
+  constexpr int D = S::D, NH = S::NH, kCols = S::kCols, kThreads = S::kWarps * 32;
   constexpr bool I8 = S::I8;
-  extern __shared__ __align__(128) uint8_t smem[];
+  extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ int s_scan[kThreads];
   __shared__ int s_warp[S::kWarps];
   __shared__ int4 s_head[2 * S::kWarps];   // of a warp's parts: row (-1: none), begins its row, ends it
@@ -211,8 +230,9 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   const int tid = threadIdx.x, lane = tid & 31, warp = ptx::warp_index();
   const int lr = lane >> 2, lc = lane & 3;
   const uint32_t ring = ptx::smem_u32(smem) + warp * S::kRing;
-  float* const first_part = reinterpret_cast<float*>(smem + S::kWarps * S::kRing + warp * S::kPartBytes);
-  float* const last_part = reinterpret_cast<float*>(smem + warp * S::kRing);
+  // a warp's parts of rows: one that it goes on from lies in the workspace, its last in its ring
+  const auto first_part = [&](int w) { return Part<S>{p.first_parts + ((long long)blockIdx.x * S::kWarps + w) * S::kPart}; };
+  const auto last_part = [&](int w) { return Part<S>{reinterpret_cast<float*>(smem + w * S::kRing)}; };
 
   if (tid < 2 * S::kWarps) s_head[tid] = make_int4(-1, 0, 0, 0);
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -264,7 +284,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       if (lane == 31) s_warp[warp] = sum;
       __syncthreads();
       int left = begin - before;            // the sequence in which `left` tiles lie before this warp's first
-#pragma unroll
+#pragma unroll 4
       for (int w = 0; w < S::kWarps; ++w) {
         const int of_warp = s_warp[w];
         if (begin < end && left >= 0 && left < of_warp) {
@@ -289,69 +309,106 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     Cursor at = in;
     const int count = end - begin;
 
-    // Page of token (lane & 15) of the copies' tile, asked for a tile ahead of its use.
-    auto look_up = [&](const Cursor& c, bool there) -> int {
-      const int t = (c.span.tile0() + c.tile) * kTile + (lane & 15);
-      if (!there || t < c.span.first || t >= c.span.end) return 0;
-      return ptx::ld_global(p.cache.table + (long long)c.b * p.cache.max_pages + divide(t, p.cache.by_page));
+    // ---- copies.  Units of keys and of values follow one another through the ring, kUnits - 1 of them under way.
+    int page = 0, issued = 0;
+    uint32_t put = ring, get = ring;         // next unit to fill, and to read
+    const uint32_t scales_of = ptx::smem_u32(smem) + S::kWarps * S::kRing + warp * S::kUnits * 64;
+    uint32_t put_scales = scales_of, get_scales = scales_of;
+    const int copy_row = lane / S::kPieces, copy_piece = lane % S::kPieces;
+    // Piece c of token t lies in place c ^ (t & 7): the eight lanes that a load serves at a time read eight different places of 128 bytes,
+    // of two tokens four apart (keys) or of two times four tokens (values).  (64-byte tokens lie as they come.)
+    auto place_of = [](int t, int c) { return (uint32_t)(t * S::kPieces + (S::kPieces >= 8 ? c ^ (t & 7) : c)) * 16; };
+    const int key_token = (lr >> 1) + 4 * (lr & 1);         // of column lr of the first product, and 8 more
+    const uint32_t key_at = place_of(key_token, lc), key_at2 = key_at ^ 64;
+    const uint32_t value_at = S::kVB == 16 ? place_of(lc + 4 * (lr & 1), lr) : place_of(lc + 4 * (lr & 1), 0) + lr * 8;
+    const uint32_t value_at2 = S::kVB == 16 ? place_of(lc + 4 * (1 - (lr & 1)), lr) : place_of(lc + 4 * (1 - (lr & 1)), 0) + lr * 8;
+    const uint32_t pick_low = I8 ? (lr & 1 ? 0x1504u : 0x5140u) : (lr & 1 ? 0x1054u : 0x5410u);
+    const uint32_t pick_high = I8 ? (lr & 1 ? 0x3726u : 0x7362u) : (lr & 1 ? 0x3276u : 0x7632u);
+    uint32_t unit = 0;                       // place of the copies' tile (WHOLE) or of its token (lane & 15)
+    // Page of the copies' tile or of its token (lane & 15), asked for a tile ahead of its use.
+    auto look_up = [&](bool there) {
+      const int t = (in.span.tile0() + in.tile) * kTile + (S::WHOLE ? 0 : lane & 15);
+      page = 0;
+      if (there && (S::WHOLE || (t >= in.span.first && t < in.span.end)))
+        page = ptx::ld_global(p.cache.table + (long long)in.b * p.cache.max_pages + divide(t, p.cache.by_page));
     };
-    auto copy_tile = [&](const Cursor& c, int page, int stage) {
-      const int t0 = (c.span.tile0() + c.tile) * kTile;
-      const int kv = c.r / p.chunks;
-      auto seen = [&](int token) { return t0 + token >= c.span.first && t0 + token < c.span.end; };
-      const int t = t0 + (lane & 15);
+    auto in_span = [&](int t) { return t >= in.span.first && t < in.span.end; };
+    // A warp copies whole tokens, 512 bytes an instruction: in pieces of 64 bytes, as the products take keys, the same copies reach 4.9
+    // TB/s of 6.6 (blocks of 4 KB in no order).
+    auto copy_tokens = [&](const void* from, int t0, bool all) {
+      const char* const base = static_cast<const char*>(from) + copy_piece * 16;
+#pragma unroll
+      for (int j = 0; j < kTile / S::kRows; ++j) {
+        const int row = copy_row + j * S::kRows;
+        const uint32_t u = S::WHOLE ? unit + row * p.cache.token16 : __shfl_sync(0xffffffffu, unit, row);
+        const char* src = base + (uint64_t)u * 16;
+        if (all) cp_async(put + place_of(row, copy_piece), src, std::integral_constant<int, 16>());
+        else cp_async(put + place_of(row, copy_piece), src, in_span(t0 + row) ? 16 : 0, std::integral_constant<int, 16>());
+      }
+    };
+    auto copy_keys = [&]() {
+      const int t0 = (in.span.tile0() + in.tile) * kTile, kv = in.r / p.chunks;
+      const int t = t0 + (S::WHOLE ? 0 : lane & 15);
       const uint32_t place = t - divide(t, p.cache.by_page) * p.cache.page_size;
       if ((uint32_t)page >= (uint32_t)p.cache.n_pages) {
         note_bad_index(p.status);
         page = 0;
       }
-      const uint32_t unit = page * p.cache.page16 + place * p.cache.token16 + kv * p.cache.head16;
-      const uint32_t slot = ring + stage * S::kTileBytes;
-      const char* const k = static_cast<const char*>(p.cache.k) + lc * 16;
-      const char* const v = static_cast<const char*>(p.cache.v) + lr * S::kVB;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const char* src = k + (uint64_t)__shfl_sync(0xffffffffu, unit, lr + 8 * i) * 16;
-        const uint32_t bytes = seen(lr + 8 * i) ? 16 : 0;
-#pragma unroll
-        for (int j = 0; j < S::kKC; ++j)
-          cp_async(slot + ((i * S::kKC + j) * 32 + lane) * 16, src + j * 64, bytes, std::integral_constant<int, 16>());
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int token = 2 * lc + (i & 1) + 8 * (i >> 1);
-        const char* src = v + (uint64_t)__shfl_sync(0xffffffffu, unit, token) * 16;
-        const uint32_t bytes = seen(token) ? S::kVB : 0;
-#pragma unroll
-        for (int j = 0; j < S::kVC; ++j)
-          cp_async(slot + S::kVOffset + ((i * S::kVC + j) * 32 + lane) * S::kVB, src + j * 8 * S::kVB, bytes,
-                   std::integral_constant<int, S::kVB>());
-      }
+      unit = page * p.cache.page16 + place * p.cache.token16 + kv * p.cache.head16;
+      copy_tokens(p.cache.k, t0, S::WHOLE);   // keys behind a sequence's end have no score, whatever they are, but may be in no page
+    };
+    auto copy_values = [&]() {
+      const int t0 = (in.span.tile0() + in.tile) * kTile;
+      copy_tokens(p.cache.v, t0, t0 >= in.span.first && in.span.end - t0 >= kTile);   // 0 for what is not seen: its p is 0, and must stay so
+    };
+    auto copy_scales = [&](const float* scales) {
       if constexpr (I8) {
-        const float* scales = lane < 16 ? p.cache.k_scales : p.cache.v_scales;
-        const long long i = ((long long)page * p.cache.n_kv_heads + kv) * p.cache.page_size + place;
-        cp_async(slot + S::kScaleOffset + lane * 4, scales + i, seen(lane & 15) ? 4 : 0, std::integral_constant<int, 4>());
+        if (lane < 16) {
+          const int t = (in.span.tile0() + in.tile) * kTile + lane;
+          const uint32_t place = t - divide(t, p.cache.by_page) * p.cache.page_size;
+          const long long i = ((long long)page * p.cache.n_kv_heads + in.r / p.chunks) * p.cache.page_size + place;
+          cp_async(put_scales + lane * 4, scales + i, in_span(t) ? 4 : 0, std::integral_constant<int, 4>());
+        }
       }
     };
-    auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
-
-    int page = look_up(in, true), issued = 0;
-    auto issue = [&]() {
+    auto filled = [&]() {
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      put += S::kUnit, put_scales += 64;
+      if (put == ring + S::kRing) put = ring, put_scales = scales_of;
+    };
+    auto issue_keys = [&]() {
       if (issued < count) {
-        copy_tile(in, page, issued % S::kStages);
-        in.next(p);
-        page = look_up(in, issued + 1 < count);
+        copy_keys();
+        copy_scales(p.cache.k_scales);
       }
-      commit();
-      ++issued;
+      filled();
     };
+    auto issue_values = [&]() {
+      if (issued < count) {
+        copy_values();
+        copy_scales(p.cache.v_scales);
+        in.next(p);
+        look_up(issued + 1 < count);
+      }
+      ++issued;
+      filled();
+    };
+    auto landed = [&]() { asm volatile("cp.async.wait_group %0;" ::"n"(S::kUnits - 2) : "memory"); };
+    auto read = [&]() {
+      get += S::kUnit, get_scales += 64;
+      if (get == ring + S::kRing) get = ring, get_scales = scales_of;
+    };
+    look_up(true);
 #pragma unroll 1
-    for (int i = 0; i < S::kStages - 1; ++i) issue();
+    for (int i = 0; i < S::kUnits / 2; ++i) {
+      issue_keys();
+      issue_values();
+    }
 
-    uint32_t qa[D / 16][2], qb[NH > 8 ? D / 16 : 1][2];     // heads lr and lr + 8: words of adjacent channels
+    uint32_t q[kCols][D / 16][2];                            // heads lr (+ 8): words of adjacent channels
     float to_log2[2] = {p.scale_log2, p.scale_log2};         // of a product of the tensor cores, per head
-    float most[2], sum[2];                                   // of heads lr and lr + 8; sum: of this lane's tokens
-    float acc[D / 16][NH / 8][4];                            // rows: channels, columns: heads 2 lc, 2 lc + 1 (+ 8)
+    float most[2], sum[2];                                   // of heads lr (+ 8); sum: of this lane's tokens
+    float acc[D / 16][kCols][4];                             // rows: channels, columns: heads 2 lc, 2 lc + 1 (+ 8)
     float v_ref = 1.f, inv_ref = 1.f;                        // I8: acc is in units of it
     bool from_start;
 
@@ -359,19 +416,18 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       int heads;
       const int h0 = first_head<S>(p, at.r, heads);
 #pragma unroll
-      for (int i = 0; i < NH / 8; ++i) {
-        uint32_t(*to)[2] = i == 0 ? qa : qb;
-        const int h = lr + 8 * i;
-        const uint16_t* q = p.q + at.b * p.q_row + (long long)(h0 + h) * p.q_head;
+      for (int n = 0; n < kCols; ++n) {
+        const int h = (S::kHalves ? lr & 3 : lr) + 8 * n;
+        const uint16_t* from = p.q + at.b * p.q_row + (long long)(h0 + h) * p.q_head;
         constexpr int kAdjacent = I8 ? 16 : 8;               // channels of a 16-byte piece of a key
 #pragma unroll
         for (int j = 0; j < S::kKC; ++j)
 #pragma unroll
           for (int e = 0; e < kAdjacent / 8; ++e) {
             uint4 x = make_uint4(0, 0, 0, 0);
-            if (h < heads) x = ptx::ld_global(reinterpret_cast<const uint4*>(q + (j * 4 + lc) * kAdjacent + e * 8));
+            if (h < heads) x = ptx::ld_global(reinterpret_cast<const uint4*>(from + (j * 4 + lc) * kAdjacent + e * 8));
             const int s = (j * kAdjacent + e * 8) / 4;
-            to[s][0] = x.x, to[s][1] = x.y, to[s + 1][0] = x.z, to[s + 1][1] = x.w;
+            q[n][s][0] = x.x, q[n][s][1] = x.y, q[n][s + 1][0] = x.z, q[n][s + 1][1] = x.w;
           }
         if constexpr (I8) {
           // bf16 as binary16: times a power of two that brings the head's largest below 4.  What becomes subnormal there is
@@ -381,30 +437,30 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
           for (int s = 0; s < D / 16; ++s)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&to[s][e]));
+              const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&q[n][s][e]));
               big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
             }
           big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
           big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
           const int e = min(max((int)(__float_as_uint(big) >> 23) - 127, -126), 126);
           const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-          to_log2[i] = p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23);
+          to_log2[n] = p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
           for (int s = 0; s < D / 16; ++s)
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
-              const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&to[s][w]));
+              const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&q[n][s][w]));
               const __half2 x = __floats2half2_rn(f.x * down, f.y * down);
-              to[s][w] = *reinterpret_cast<const uint32_t*>(&x);
+              q[n][s][w] = *reinterpret_cast<const uint32_t*>(&x);
             }
         }
-        most[i] = kNegInf;
-        sum[i] = 0.f;
+        most[n] = kNegInf;
+        sum[n] = 0.f;
       }
 #pragma unroll
       for (int d = 0; d < D / 16; ++d)
 #pragma unroll
-        for (int n = 0; n < NH / 8; ++n) acc[d][n][0] = acc[d][n][1] = acc[d][n][2] = acc[d][n][3] = 0.f;
+        for (int n = 0; n < kCols; ++n) acc[d][n][0] = acc[d][n][1] = acc[d][n][2] = acc[d][n][3] = 0.f;
       if constexpr (I8) v_ref = 0.f;
       from_start = at.tile == 0;
     };
@@ -412,7 +468,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     // acc times a factor per head; lanes have those of heads lr (+ 8)
     auto rescale = [&](const float (&f)[2]) {
 #pragma unroll
-      for (int n = 0; n < NH / 8; ++n) {
+      for (int n = 0; n < kCols; ++n) {
         const float f0 = __shfl_sync(0xffffffffu, f[n], lc * 8), f1 = __shfl_sync(0xffffffffu, f[n], lc * 8 + 4);
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) {
@@ -421,65 +477,59 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       }
     };
 
-    auto add_tile = [&](int stage) {
-      const uint32_t slot = ring + stage * S::kTileBytes;
+    auto add_tile = [&]() {
       const int t0 = (at.span.tile0() + at.tile) * kTile;
+      landed();
+      __syncwarp();                          // for all lanes, and all have read what is filled next
+      issue_keys();
       // ---- S = Q K^T, tokens 0..7 and 8..15; two sums each, so that a product waits for the one before the last
-      float s[2][2][4] = {};
+      float s[2][2][4];
 #pragma unroll
       for (int j = 0; j < S::kKC; ++j)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const uint4 x = lds16(slot + ((i * S::kKC + j) * 32 + lane) * 16);
+          const uint4 x = lds16(get + (j & 1 ? key_at2 : key_at) + i * 8 * S::kBytes + (j >> 1) * 128);
           const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-          if constexpr (I8) {
+          constexpr int kSteps = I8 ? 4 : 2;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+          for (int e = 0; e < kSteps; ++e) {
+            const int k = kSteps * j + e;
+            uint32_t b0, b1;
+            if constexpr (I8) {
               const uint32_t u = w[e] ^ 0x80808080u;
-              const int k = 4 * j + e;
-              mma<true>(s[i][e & 1], qa[k][0], NH > 8 ? qb[k % (NH > 8 ? D / 16 : 1)][0] : 0u, qa[k][1],
-                        NH > 8 ? qb[k % (NH > 8 ? D / 16 : 1)][1] : 0u, low_codes(u), high_codes(u));
+              b0 = low_codes(u), b1 = high_codes(u);
+            } else {
+              b0 = w[2 * e], b1 = w[2 * e + 1];
             }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int k = 2 * j + e;
-              mma<false>(s[i][e & 1], qa[k][0], NH > 8 ? qb[k % (NH > 8 ? D / 16 : 1)][0] : 0u, qa[k][1],
-                         NH > 8 ? qb[k % (NH > 8 ? D / 16 : 1)][1] : 0u, w[2 * e], w[2 * e + 1]);
-            }
+            const uint32_t a1 = kCols > 1 ? q[kCols - 1][k][0] : 0u, a3 = kCols > 1 ? q[kCols - 1][k][1] : 0u;
+            if (k < 2) mma0<I8>(s[i][e & 1], q[0][k][0], a1, q[0][k][1], a3, b0, b1);
+            else mma<I8>(s[i][e & 1], q[0][k][0], a1, q[0][k][1], a3, b0, b1);
           }
         }
-      // ---- scores in powers of two: x[n][i] of heads lr + 8 n and tokens 2 lc + {0, 1} + 8 {0, 1}
-      float x[NH / 8][4], k_scale[4] = {1.f, 1.f, 1.f, 1.f}, v_scale[4] = {1.f, 1.f, 1.f, 1.f};
-      if constexpr (I8) {
+      // ---- scores in powers of two: x[n][i] of heads lr + 8 n and tokens lc + 4 {0, 1} + 8 {0, 1}
+      float x[kCols][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t token = slot + S::kScaleOffset + (2 * lc + (i & 1) + 8 * (i >> 1)) * 4;
-          k_scale[i] = lds_float(token);
-          v_scale[i] = lds_float(token + 64);
+      for (int i = 0; i < 4; ++i) {
+        float k_scale = 1.f;
+        if constexpr (I8) k_scale = lds_float(get_scales + (lc + 4 * i) * 4);
+#pragma unroll
+        for (int n = 0; n < kCols; ++n) {
+          const float y = s[i >> 1][0][2 * n + (i & 1)] + s[i >> 1][1][2 * n + (i & 1)];
+          x[n][i] = (I8 ? y * k_scale : y) * to_log2[n];
         }
       }
-#pragma unroll
-      for (int n = 0; n < NH / 8; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float y = s[i >> 1][0][2 * n + (i & 1)] + s[i >> 1][1][2 * n + (i & 1)];
-          x[n][i] = (I8 ? y * k_scale[i] : y) * to_log2[n];
-        }
       if (t0 < at.span.first || at.span.end - t0 < kTile) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int t = t0 + 2 * lc + (i & 1) + 8 * (i >> 1);
-          if (t < at.span.first || t >= at.span.end)
+        for (int i = 0; i < 4; ++i)
+          if (t0 + lc + 4 * i < at.span.first || t0 + lc + 4 * i >= at.span.end)
 #pragma unroll
-            for (int n = 0; n < NH / 8; ++n) x[n][i] = kNegInf;
-        }
+            for (int n = 0; n < kCols; ++n) x[n][i] = kNegInf;
       }
       // ---- running maximum
-      float top[2] = {kNegInf, kNegInf};
+      float top[kCols];
       bool higher = false;
 #pragma unroll
-      for (int n = 0; n < NH / 8; ++n) {
+      for (int n = 0; n < kCols; ++n) {
         top[n] = fmaxf(fmaxf(x[n][0], x[n][1]), fmaxf(x[n][2], x[n][3]));
         top[n] = fmaxf(top[n], __shfl_xor_sync(0xffffffffu, top[n], 1));
         top[n] = fmaxf(top[n], __shfl_xor_sync(0xffffffffu, top[n], 2));
@@ -488,7 +538,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       if (__any_sync(0xffffffffu, higher)) {
         float f[2] = {1.f, 1.f};
 #pragma unroll
-        for (int n = 0; n < NH / 8; ++n) {
+        for (int n = 0; n < kCols; ++n) {
           const float next = fmaxf(most[n], top[n]);
           f[n] = weight(most[n], next);
           sum[n] *= f[n];
@@ -496,45 +546,61 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
         }
         rescale(f);
       }
-      if constexpr (I8) {
-        // Values in units of 2^-6 of the largest scale so far, cut to a power of two: p (at most 2^kSlack) times what is left of its
-        // token's scale (below 2^7) is a binary16, and as two of them off by 2^-25 of a unit at most, 2^-31 of the largest.
-        float big = 0.f;
+      // ---- p and its sum
 #pragma unroll
-        for (int i = 0; i < 4; ++i) big = fmaxf(big, fabsf(v_scale[i]));
-        const uint32_t exponent = __reduce_max_sync(0xffffffffu, __float_as_uint(big)) & 0x7f800000u;
-        const float unit = __uint_as_float(exponent > (7u << 23) ? exponent - (6u << 23) : 1u << 23);
-        if (unit > v_ref) {
-          if (v_ref > 0.f) {
-            const float both[2] = {v_ref / unit, v_ref / unit};
-            rescale(both);
-          }
-          v_ref = unit;
-          inv_ref = 1.f / unit;
-        }
-      }
-      // ---- p, its sum, and O^T += V^T P^T
-      uint32_t hi[NH / 8][2], lo[NH / 8][2];
-#pragma unroll
-      for (int n = 0; n < NH / 8; ++n) {
+      for (int n = 0; n < kCols; ++n) {
         const float base = most[n] == kNegInf ? 0.f : most[n];
-        float e[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          e[i] = exp2f(x[n][i] - base);
-          sum[n] += e[i];
-          if constexpr (I8) e[i] *= v_scale[i] * inv_ref;
+          x[n][i] = power_of_two(x[n][i] - base);
+          sum[n] += x[n][i];
         }
-        split<I8>(e[0], e[1], hi[n][0], lo[n][0]);
-        split<I8>(e[2], e[3], hi[n][1], lo[n][1]);
       }
+      read();
+      // ---- O^T += V^T P^T
+      landed();
+      __syncwarp();
+      issue_values();
+      if constexpr (I8) {
+        float v_scale[4], big = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v_scale[i] = lds_float(get_scales + (lc + 4 * i) * 4);
+          big = fmaxf(big, fabsf(v_scale[i]));
+        }
+        // Values in units of 2^-6 of the largest scale so far, cut to a power of two: p (at most 2^kSlack) times what is left of its
+        // token's scale (below 2^7) is a binary16, and as two of them off by 2^-25 of a unit at most, 2^-31 of the largest.
+        const uint32_t exponent = __reduce_max_sync(0xffffffffu, __float_as_uint(big)) & 0x7f800000u;
+        const float ref = __uint_as_float(exponent > (7u << 23) ? exponent - (6u << 23) : 1u << 23);
+        if (ref > v_ref) {
+          if (v_ref > 0.f) {
+            const float both[2] = {v_ref / ref, v_ref / ref};
+            rescale(both);
+          }
+          v_ref = ref;
+          inv_ref = 1.f / ref;
+        }
+#pragma unroll
+        for (int n = 0; n < kCols; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[n][i] *= v_scale[i] * inv_ref;
+      }
+      uint32_t hi[kCols][2], lo[kCols][2];
+#pragma unroll
+      for (int n = 0; n < kCols; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          hi[n][i] = round16<I8>(x[n][2 * i], x[n][2 * i + 1]);
+          lo[n][i] = round16<I8>(x[n][2 * i], x[n][2 * i + 1]);
+          if (S::kHalves && lr >= 4) hi[n][i] = lo[n][i];
+        }
 #pragma unroll
       for (int j = 0; j < S::kVC; ++j) {
         constexpr int kWords = S::kVB / 4;
         uint32_t w[4][kWords];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t from = slot + S::kVOffset + ((i * S::kVC + j) * 32 + lane) * S::kVB;
+          const uint32_t from = get + (i & 1 ? value_at2 : value_at) + (i >> 1) * 8 * S::kBytes + j * 128;
           if constexpr (S::kVB == 16) {
             const uint4 v = lds16(from);
             w[i][0] = v.x, w[i][1] = v.y, w[i][kWords - 2] = v.z, w[i][kWords - 1] = v.w;
@@ -545,40 +611,47 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
         }
         auto product = [&](int d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
-          for (int n = 0; n < NH / 8; ++n) {
+          for (int n = 0; n < kCols; ++n) {
             mma<I8>(acc[d][n], a0, a1, a2, a3, hi[n][0], hi[n][1]);
-            mma<I8>(acc[d][n], a0, a1, a2, a3, lo[n][0], lo[n][1]);
+            if constexpr (!S::kHalves) mma<I8>(acc[d][n], a0, a1, a2, a3, lo[n][0], lo[n][1]);
           }
         };
 #pragma unroll
         for (int e = 0; e < kWords; ++e) {
           if constexpr (I8) {
             // bytes of two tokens side by side: channels 0, 0, 1, 1 and 2, 2, 3, 3 of the word
-            const uint32_t a = __byte_perm(w[0][e], w[1][e], 0x5140) ^ 0x80808080u, b = __byte_perm(w[2][e], w[3][e], 0x5140) ^ 0x80808080u;
-            const uint32_t c = __byte_perm(w[0][e], w[1][e], 0x7362) ^ 0x80808080u, f = __byte_perm(w[2][e], w[3][e], 0x7362) ^ 0x80808080u;
+            const uint32_t a = __byte_perm(w[0][e], w[1][e], pick_low) ^ 0x80808080u, b = __byte_perm(w[2][e], w[3][e], pick_low) ^ 0x80808080u;
+            const uint32_t c = __byte_perm(w[0][e], w[1][e], pick_high) ^ 0x80808080u, f = __byte_perm(w[2][e], w[3][e], pick_high) ^ 0x80808080u;
             product(2 * (j * kWords + e), low_codes(a), high_codes(a), low_codes(b), high_codes(b));
             product(2 * (j * kWords + e) + 1, low_codes(c), high_codes(c), low_codes(f), high_codes(f));
           } else {
-            product(j * kWords + e, __byte_perm(w[0][e], w[1][e], 0x5410), __byte_perm(w[0][e], w[1][e], 0x7632),
-                    __byte_perm(w[2][e], w[3][e], 0x5410), __byte_perm(w[2][e], w[3][e], 0x7632));
+            product(j * kWords + e, __byte_perm(w[0][e], w[1][e], pick_low), __byte_perm(w[0][e], w[1][e], pick_high),
+                    __byte_perm(w[2][e], w[3][e], pick_low), __byte_perm(w[2][e], w[3][e], pick_high));
           }
         }
       }
+      read();
     };
 
     // The row's sums, or what this warp has of them, are complete.  acc[d] holds channels base + 2 e and base + 2 e + 1 in its
     // rows lr and lr + 8, where d = j * kEV / 2 + e and base = (j * 8 + lr) * kEV.
     auto end_row = [&](bool to_end, bool more) {
 #pragma unroll
-      for (int n = 0; n < NH / 8; ++n) {
+      for (int n = 0; n < kCols; ++n) {
         sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 1);
         sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 2);
+      }
+      if constexpr (S::kHalves) {
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[d][0][i] += __shfl_xor_sync(0xffffffffu, acc[d][0][i], 2);
       }
       int heads;
       const int h0 = first_head<S>(p, at.r, heads);
       if (from_start && to_end) {
 #pragma unroll
-        for (int n = 0; n < NH / 8; ++n) {
+        for (int n = 0; n < kCols; ++n) {
           const float inv = 1.f / sum[n];
           const long long out0 = (long long)at.b * p.n_heads + h0 + 8 * n;
           if (p.lse && lc == 0 && lr + 8 * n < heads) p.lse[out0 + lr] = kLn2 * (most[n] + log2f(sum[n]));
@@ -605,14 +678,12 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
         }
         return;
       }
-      // a warp's last part lies in its ring, which no copy of its own fills any more
-      if (!more) asm volatile("cp.async.wait_group 0;" ::: "memory");
+      if (!more) asm volatile("cp.async.wait_group 0;" ::: "memory");   // the ring is no longer filled
       __syncwarp();
-      const int which = more ? 0 : 1;
-      const Part<S> part{more ? first_part : last_part};
+      const Part<S> part = more ? first_part(warp) : last_part(warp);
 #pragma unroll
-      for (int n = 0; n < NH / 8; ++n) {
-        if (lc == 0) {
+      for (int n = 0; n < kCols; ++n) {
+        if (lc == 0 && lr + 8 * n < NH) {
           part.most(lr + 8 * n) = most[n];
           part.total(lr + 8 * n) = sum[n];
         }
@@ -622,20 +693,18 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
           const int ch = (j * 8 + lr) * S::kEV + 2 * e;
 #pragma unroll
           for (int c = 0; c < 2; ++c)
-            *reinterpret_cast<float2*>(&part.sum(2 * lc + c + 8 * n, ch)) = make_float2(acc[d][n][c] * v_ref, acc[d][n][c + 2] * v_ref);
+            if (!S::kHalves || lc < 2)
+              *reinterpret_cast<float2*>(&part.sum(2 * lc + c + 8 * n, ch)) = make_float2(acc[d][n][c] * v_ref, acc[d][n][c + 2] * v_ref);
         }
       }
-      if (lane == 0) s_head[2 * warp + which] = make_int4(at.b * p.rows_of_seq + at.r, from_start, to_end, 0);
+      if (lane == 0) s_head[2 * warp + (more ? 0 : 1)] = make_int4(at.b * p.rows_of_seq + at.r, from_start, to_end, 0);
     };
 
     bool fresh = true;
 #pragma unroll 1
     for (int i = 0; i < count; ++i) {
       if (fresh) begin_row();
-      asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
-      if constexpr (I8) __syncwarp();       // the scales are read by other lanes than copied them
-      issue();
-      add_tile(i % S::kStages);
+      add_tile();
       fresh = at.tile + 1 == at.tiles;
       if (fresh || i + 1 == count) end_row(fresh, i + 1 < count);
       at.next(p);
@@ -684,8 +753,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
         row = h.x, starts = h.y, most = kNegInf, total_p = 0.f, sum = make_float4(0.f, 0.f, 0.f, 0.f);
       }
       ends = h.z;
-      const Part<S> part{reinterpret_cast<float*>(i & 1 ? smem + (i >> 1) * S::kRing
-                                                        : smem + S::kWarps * S::kRing + (i >> 1) * S::kPartBytes)};
+      const Part<S> part = i & 1 ? last_part(i >> 1) : first_part(i >> 1);
       const float m = part.most(head), next = fmaxf(most, m);
       const float a = weight(most, next), b = weight(m, next);
       const float4 v = *reinterpret_cast<const float4*>(&part.sum(head, d));
@@ -703,9 +771,9 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
 
 // Joins the rows that cross CTAs.  CTA i takes the row that begins in CTA i of the kernel before and goes on in the next ones.
 constexpr int kMaxCtas = 256;
-template <typename S>
+template <int D, int NH>
 __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, const int ctas) {
-  constexpr int D = S::D, NH = S::NH;
+  using S = Shape<D, NH, false, true>;
   __shared__ float s_weight[NH][kMaxCtas];
   __shared__ float s_inv[NH];
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -767,11 +835,11 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, cons
 int attn_ctas() { return min(sm_count_or(148), kMaxCtas); }
 
 // Query heads of a row of work.
-int heads_of_row(int group, int dim) { return group <= 8 || dim > 128 ? 8 : 16; }
+int heads_of_row(int group, int dim) { return group <= 4 ? 4 : group <= 8 || dim > 128 ? 8 : 16; }
 
-template <int D, int NH, bool I8>
+template <int D, int NH, bool I8, bool WHOLE>
 int launch(const AttnParams& p, cudaStream_t st) {
-  using S = Shape<D, NH, I8>;
+  using S = Shape<D, NH, I8, WHOLE>;
   static std::atomic<uint64_t> allowed{0};
   PEQA_TRY(allow_smem(attn_decode_kernel<S>, S::kSmem, allowed));
   const int ctas = attn_ctas();
@@ -786,27 +854,29 @@ int launch(const AttnParams& p, cudaStream_t st) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   PEQA_CUDA(cudaLaunchKernelEx(&cfg, attn_decode_kernel<S>, p));
-  return launch_after(attn_join_kernel<S>, ctas, 256, st, p, ctas);
+  return launch_after(attn_join_kernel<D, NH>, ctas, 256, st, p, ctas);
 }
 
-template <int D, bool I8>
-int launch_heads(const AttnParams& p, int nh, cudaStream_t st) {
+template <int D, int NH>
+int launch_type(const AttnParams& p, bool codes, cudaStream_t st) {
+  const bool whole = p.cache.page_size % kTile == 0;
+  if (codes) return whole ? launch<D, NH, true, true>(p, st) : launch<D, NH, true, false>(p, st);
+  return whole ? launch<D, NH, false, true>(p, st) : launch<D, NH, false, false>(p, st);
+}
+
+template <int D>
+int launch_heads(const AttnParams& p, int nh, bool codes, cudaStream_t st) {
+  if (nh == 4) return launch_type<D, 4>(p, codes, st);
   if constexpr (D <= 128)
-    if (nh == 16) return launch<D, 16, I8>(p, st);
-  return launch<D, 8, I8>(p, st);
+    if (nh == 16) return launch_type<D, 16>(p, codes, st);
+  return launch_type<D, 8>(p, codes, st);
 }
 
-template <bool I8>
-int launch_dim(const AttnParams& p, int dim, int nh, cudaStream_t st) {
-  switch (dim) {
-    case 64: return launch_heads<64, I8>(p, nh, st);
-    case 128: return launch_heads<128, I8>(p, nh, st);
-    default: return launch_heads<256, I8>(p, nh, st);
-  }
-}
-
+// headers, parts of CTAs, parts of warps
 size_t workspace_bytes(int dim, int nh) {
-  return (size_t)attn_ctas() * 2 * (sizeof(int4) + (size_t)nh * (dim + 2) * sizeof(float));
+  const int warps = dim > 128 || nh > 8 ? 8 : 16;
+  static_assert(Shape<128, 8, false, true>::kWarps == 16 && Shape<64, 16, false, true>::kWarps == 8 && Shape<256, 4, true, true>::kWarps == 8, "");
+  return (size_t)attn_ctas() * (2 * sizeof(int4) + (2 + warps) * (size_t)nh * (dim + 2) * sizeof(float));
 }
 
 }  // namespace
@@ -851,7 +921,13 @@ extern "C" int peqa_attn_decode(const peqa_kv_cache_t* c, const peqa_rows_t* q, 
   p.lse = lse;
   p.headers = static_cast<int4*>(workspace);
   p.parts = reinterpret_cast<float*>(p.headers + 2 * attn_ctas());
+  p.first_parts = p.parts + (size_t)attn_ctas() * 2 * nh * (c->head_dim + 2);
   cudaStream_t st = as_stream(stream);
   PEQA_TRY(status_word(st, &p.status));
-  return c->type == PEQA_KV_INT8 ? launch_dim<true>(p, c->head_dim, nh, st) : launch_dim<false>(p, c->head_dim, nh, st);
+  const bool codes = c->type == PEQA_KV_INT8;
+  switch (c->head_dim) {
+    case 64: return launch_heads<64>(p, nh, codes, st);
+    case 128: return launch_heads<128>(p, nh, codes, st);
+    default: return launch_heads<256>(p, nh, codes, st);
+  }
 }
