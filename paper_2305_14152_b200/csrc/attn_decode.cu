@@ -33,6 +33,9 @@ namespace peqa {
 namespace {
 
 constexpr int kTile = 16;            // tokens
+#ifndef MINT
+#define MINT 4
+#endif
 constexpr float kSlack = 8.f;        // of the running maximum, in powers of two
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -167,7 +170,6 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 // The tokens of a sequence that are seen, and their tiles.
 struct Span {
   int first, end;                    // tokens
-  __device__ __forceinline__ int tile0() const { return first / kTile; }
   __device__ __forceinline__ int tiles() const { return end > first ? (end - 1) / kTile + 1 - first / kTile : 0; }
 };
 __device__ __forceinline__ Span span_of(const AttnParams& p, int b) {
@@ -177,33 +179,51 @@ __device__ __forceinline__ Span span_of(const AttnParams& p, int b) {
   return s;
 }
 
-// Where a warp is: tile `tile` (counted within the row) of row (b, r).
+// Where a warp is: the tile from token t0 on of row (b, r), of which `left` tiles are to come with this one.
 struct Cursor {
-  int b, r, tile, tiles;
+  int b, r, t0, left;
   Span span;
 
-  __device__ __forceinline__ void next(const AttnParams& p) {
-    if (++tile < tiles) return;
-    tile = 0;
-    if (++r < p.rows_of_seq) return;
-    r = 0;
-    do {
-      if (++b >= p.cache.n_seqs) {   // behind the last tile there is none
-        span.first = span.end = 0;
-        tiles = 0x7fffffff;
-        return;
-      }
-      span = span_of(p, b);
-      tiles = span.tiles();
-    } while (tiles == 0);
+  __device__ __forceinline__ int tile0() const { return span.first & ~(kTile - 1); }
+  __device__ __forceinline__ void begin(const AttnParams& p, int seq, int tiles_before) {
+    b = seq;
+    span = span_of(p, b);
+    const int tiles = span.tiles();
+    r = tiles_before / tiles;
+    const int tile = tiles_before - r * tiles;
+    t0 = tile0() + tile * kTile;
+    left = tiles - tile;
+  }
+  // true: at another row
+  __device__ __forceinline__ bool next(const AttnParams& p) {
+    t0 += kTile;
+    if (--left > 0) return false;
+    if (++r >= p.rows_of_seq) {
+      r = 0;
+      do {
+        if (++b >= p.cache.n_seqs) {   // behind the last tile there is none
+          span.first = span.end = 0;
+          left = 0x7fffffff;
+          return true;
+        }
+        span = span_of(p, b);
+      } while (span.end <= span.first);
+    }
+    t0 = tile0();
+    left = span.tiles();
+    return true;
   }
 };
 
-// Sums of a row, or of a part of one, in a part's memory: O [NH][D], then the maxima and the sums of p.
-template <typename S>
+// Sums of a row, or of a part of one, in a part's memory: O [NH][D], then the maxima and the sums of p.  Within a CTA four channels of
+// a head lie in the place of others of their eight times four, so that the lanes of a warp write to different banks.
+template <typename S, bool MIXED>
 struct Part {
   float* at;
-  __device__ __forceinline__ float& sum(int head, int d) const { return at[head * S::D + d]; }
+  __device__ __forceinline__ float4& sums(int head, int d4) const {
+    const int lc = (head >> 1) & 3, mix = S::kEV == 16 ? lc : (lc & 1) + 4 * (lc >> 1);
+    return reinterpret_cast<float4*>(at + head * S::D)[MIXED ? d4 ^ mix : d4];
+  }
   __device__ __forceinline__ float& most(int head) const { return at[S::NH * S::D + head]; }
   __device__ __forceinline__ float& total(int head) const { return at[S::NH * (S::D + 1) + head]; }
 };
@@ -231,78 +251,82 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   const int lr = lane >> 2, lc = lane & 3;
   const uint32_t ring = ptx::smem_u32(smem) + warp * S::kRing;
   // a warp's parts of rows: one that it goes on from lies in the workspace, its last in its ring
-  const auto first_part = [&](int w) { return Part<S>{p.first_parts + ((long long)blockIdx.x * S::kWarps + w) * S::kPart}; };
-  const auto last_part = [&](int w) { return Part<S>{reinterpret_cast<float*>(smem + w * S::kRing)}; };
+  const auto first_part = [&](int w) { return Part<S, true>{p.first_parts + ((long long)blockIdx.x * S::kWarps + w) * S::kPart}; };
+  const auto last_part = [&](int w) { return Part<S, true>{reinterpret_cast<float*>(smem + w * S::kRing)}; };
 
   if (tid < 2 * S::kWarps) s_head[tid] = make_int4(-1, 0, 0, 0);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  // ---- the tiles of all sequences, and this warp's share of them
+  // ---- the tiles of all sequences, and this warp's share of them: [begin, end)
   const int B = p.cache.n_seqs;
-  int total = 0;
-  for (int b = tid; b < B; b += kThreads) total += span_of(p, b).tiles() * p.rows_of_seq;
-  const int mine = total;                   // of sequence tid, when one round takes them all
-  total = __reduce_add_sync(0xffffffffu, total);
-  if (lane == 0) s_warp[warp] = total;
-  __syncthreads();
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < S::kWarps; ++w) total += s_warp[w];
-  // sequences that are not there have outputs all the same
-  for (int b = blockIdx.x; b < B; b += gridDim.x)
-    if (span_of(p, b).tiles() == 0) {
-      for (int i = tid; i < p.n_heads * (D / 8); i += kThreads)
-        reinterpret_cast<uint4*>(p.out)[(long long)b * p.n_heads * (D / 8) + i] = make_uint4(0, 0, 0, 0);
-      if (p.lse)
-        for (int i = tid; i < p.n_heads; i += kThreads) p.lse[(long long)b * p.n_heads + i] = kNegInf;
-    }
-  // no CTA without a tile for each of its warps, while there are enough
-  const int busy = min((int)gridDim.x, max(1, total / S::kWarps));
-  const bool works = (int)blockIdx.x < busy;
-  const int cta0 = works ? (int)((long long)total * blockIdx.x / busy) : 0;
-  const int cta1 = works ? (int)((long long)total * (blockIdx.x + 1) / busy) : 0;
-  const int begin = cta0 + (int)((long long)(cta1 - cta0) * warp / S::kWarps);
-  const int end = cta0 + (int)((long long)(cta1 - cta0) * (warp + 1) / S::kWarps);
-
+  int total = 0, begin = 0, end = 0;
+  auto share = [&]() {
+    // no CTA without a tile for a warp of each scheduler, while there are enough
+    const int busy = min((int)gridDim.x, max(1, total / MINT)), cta = blockIdx.x;
+    if (cta >= busy) return;
+    const int each = total / busy, more = total - each * busy;             // the first `more` CTAs have one more
+    const int first = each * cta + min(cta, more), n = each + (cta < more);
+    const int each_warp = n / S::kWarps, more_warp = n - each_warp * S::kWarps;
+    begin = first + each_warp * warp + min(warp, more_warp);
+    end = begin + each_warp + (warp < more_warp);
+  };
+  auto tiles_of = [&](int b) { return b < B ? span_of(p, b).tiles() * p.rows_of_seq : 0; };
+  if (B > kThreads) {
+    for (int b = tid; b < B; b += kThreads) total += tiles_of(b);
+    total = __reduce_add_sync(0xffffffffu, total);
+    if (lane == 0) s_warp[warp] = total;
+    __syncthreads();
+    total = __reduce_add_sync(0xffffffffu, lane < S::kWarps ? s_warp[lane] : 0);
+    share();
+  }
   Cursor in;                                // of the copies; the sums follow with `at`
-  in.b = in.r = in.tile = in.tiles = 0;
-  in.span.first = in.span.end = 0;
-  {
-    int before = 0;                         // tiles of the sequences before this round's
-    for (int base = 0; base < B; base += kThreads) {
-      const int b = base + tid;
-      const int n = B <= kThreads ? mine : (b < B ? span_of(p, b).tiles() * p.rows_of_seq : 0);
-      int sum = n;
+  in.b = in.r = in.t0 = in.left = in.span.first = in.span.end = 0;
+  int before = 0;                           // tiles of the sequences before this round's
+  if (B <= 32) {                            // every warp for itself
+    int upto = tiles_of(lane);
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int up = __shfl_up_sync(0xffffffffu, sum, o);
-        if (lane >= o) sum += up;
-      }
-      __syncthreads();                      // s_scan and s_warp of the round before have been read
-      s_scan[tid] = sum;                    // up to and with this one, within the warp
-      if (lane == 31) s_warp[warp] = sum;
-      __syncthreads();
-      int left = begin - before;            // the sequence in which `left` tiles lie before this warp's first
-#pragma unroll 4
-      for (int w = 0; w < S::kWarps; ++w) {
-        const int of_warp = s_warp[w];
-        if (begin < end && left >= 0 && left < of_warp) {
-          const int upto = s_scan[w * 32 + lane];
-          const int l = __popc(__ballot_sync(0xffffffffu, upto <= left));   // sequences that end before it
-          in.b = base + w * 32 + l;
-          left -= l > 0 ? s_scan[w * 32 + l - 1] : 0;
-          in.span = span_of(p, in.b);
-          in.tiles = in.span.tiles();
-          in.r = left / in.tiles;
-          in.tile = left - in.r * in.tiles;
-          left = -1;
-        } else if (left >= 0) {
-          left -= of_warp;                  // (negative: found, or in a round before)
-        }
-        before += of_warp;
-      }
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += up;
     }
+    total = __shfl_sync(0xffffffffu, upto, 31);
+    share();
+    if (begin < end) {
+      const int b = __popc(__ballot_sync(0xffffffffu, upto <= begin));
+      in.begin(p, b, begin - (b > 0 ? __shfl_sync(0xffffffffu, upto, b - 1) : 0));
+    }
+  } else for (int base = 0; base < B; base += kThreads) {
+    int sum = tiles_of(base + tid);         // of the sequences up to this one, within the warp
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += up;
+    }
+    __syncthreads();                        // s_scan and s_warp of the round before have been read
+    s_scan[tid] = sum;
+    if (lane == 31) s_warp[warp] = sum;
+    __syncthreads();
+    int upto = lane < S::kWarps ? s_warp[lane] : 0;     // of the warps up to warp `lane`
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += up;
+    }
+    const int round = __shfl_sync(0xffffffffu, upto, 31);
+    if (B <= kThreads) {
+      total = round;
+      share();
+    }
+    int left = begin - before;              // tiles before this warp's first in its sequence, once the ones before are taken off
+    if (begin < end && left >= 0 && left < round) {
+      const int w = __popc(__ballot_sync(0xffffffffu, upto <= left));      // warps whose sequences end before it
+      if (w > 0) left -= __shfl_sync(0xffffffffu, upto, w - 1);
+      const int in_warp = s_scan[w * 32 + lane], l = __popc(__ballot_sync(0xffffffffu, in_warp <= left));
+      if (l > 0) left -= __shfl_sync(0xffffffffu, in_warp, l - 1);
+      in.begin(p, base + w * 32 + l, left);
+    }
+    before += round;
   }
 
   if (begin < end) {
@@ -314,10 +338,11 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     uint32_t put = ring, get = ring;         // next unit to fill, and to read
     const uint32_t scales_of = ptx::smem_u32(smem) + S::kWarps * S::kRing + warp * S::kUnits * 64;
     uint32_t put_scales = scales_of, get_scales = scales_of;
-    const int copy_row = lane / S::kPieces, copy_piece = lane % S::kPieces;
     // Piece c of token t lies in place c ^ (t & 7): the eight lanes that a load serves at a time read eight different places of 128 bytes,
     // of two tokens four apart (keys) or of two times four tokens (values).  (64-byte tokens lie as they come.)
     auto place_of = [](int t, int c) { return (uint32_t)(t * S::kPieces + (S::kPieces >= 8 ? c ^ (t & 7) : c)) * 16; };
+    const int copy_row = lane / S::kPieces, copy_piece = lane % S::kPieces;
+    const uint32_t copy_to = place_of(copy_row, copy_piece);
     const int key_token = (lr >> 1) + 4 * (lr & 1);         // of column lr of the first product, and 8 more
     const uint32_t key_at = place_of(key_token, lc), key_at2 = key_at ^ 64;
     const uint32_t value_at = S::kVB == 16 ? place_of(lc + 4 * (lr & 1), lr) : place_of(lc + 4 * (lr & 1), 0) + lr * 8;
@@ -325,9 +350,11 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     const uint32_t pick_low = I8 ? (lr & 1 ? 0x1504u : 0x5140u) : (lr & 1 ? 0x1054u : 0x5410u);
     const uint32_t pick_high = I8 ? (lr & 1 ? 0x3726u : 0x7362u) : (lr & 1 ? 0x3276u : 0x7632u);
     uint32_t unit = 0;                       // place of the copies' tile (WHOLE) or of its token (lane & 15)
+    uint32_t scale = 0;                      // the same in the scales (fewer than 2^30: each has 64 bytes of codes, and they have less than 2^36)
+    int kv = in.r / p.chunks;                // head of keys and values
     // Page of the copies' tile or of its token (lane & 15), asked for a tile ahead of its use.
     auto look_up = [&](bool there) {
-      const int t = (in.span.tile0() + in.tile) * kTile + (S::WHOLE ? 0 : lane & 15);
+      const int t = in.t0 + (S::WHOLE ? 0 : lane & 15);
       page = 0;
       if (there && (S::WHOLE || (t >= in.span.first && t < in.span.end)))
         page = ptx::ld_global(p.cache.table + (long long)in.b * p.cache.max_pages + divide(t, p.cache.by_page));
@@ -335,41 +362,37 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     auto in_span = [&](int t) { return t >= in.span.first && t < in.span.end; };
     // A warp copies whole tokens, 512 bytes an instruction: in pieces of 64 bytes, as the products take keys, the same copies reach 4.9
     // TB/s of 6.6 (blocks of 4 KB in no order).
-    auto copy_tokens = [&](const void* from, int t0, bool all) {
+    auto copy_tokens = [&](const void* from, bool all) {
       const char* const base = static_cast<const char*>(from) + copy_piece * 16;
+      const char* src = base + (uint64_t)(unit + copy_row * p.cache.token16) * 16;
+      const uint64_t step = (uint64_t)p.cache.token16 * (S::kRows * 16);
 #pragma unroll
       for (int j = 0; j < kTile / S::kRows; ++j) {
-        const int row = copy_row + j * S::kRows;
-        const uint32_t u = S::WHOLE ? unit + row * p.cache.token16 : __shfl_sync(0xffffffffu, unit, row);
-        const char* src = base + (uint64_t)u * 16;
-        if (all) cp_async(put + place_of(row, copy_piece), src, std::integral_constant<int, 16>());
-        else cp_async(put + place_of(row, copy_piece), src, in_span(t0 + row) ? 16 : 0, std::integral_constant<int, 16>());
+        if constexpr (!S::WHOLE) src = base + (uint64_t)__shfl_sync(0xffffffffu, unit, copy_row + j * S::kRows) * 16;
+        const uint32_t to = ((put + copy_to) ^ (S::kPieces >= 8 ? ((j * S::kRows) & 7) * 16 : 0)) + j * 512;
+        if (all) cp_async(to, src, std::integral_constant<int, 16>());
+        else cp_async(to, src, in_span(in.t0 + copy_row + j * S::kRows) ? 16 : 0, std::integral_constant<int, 16>());
+        if constexpr (S::WHOLE) src += step;
       }
     };
+    auto copy_scales = [&](const float* scales) {
+      if constexpr (I8)
+        if (lane < 16) cp_async(put_scales + lane * 4, scales + scale, in_span(in.t0 + lane) ? 4 : 0, std::integral_constant<int, 4>());
+    };
     auto copy_keys = [&]() {
-      const int t0 = (in.span.tile0() + in.tile) * kTile, kv = in.r / p.chunks;
-      const int t = t0 + (S::WHOLE ? 0 : lane & 15);
+      const int t = in.t0 + (S::WHOLE ? 0 : lane & 15);
       const uint32_t place = t - divide(t, p.cache.by_page) * p.cache.page_size;
       if ((uint32_t)page >= (uint32_t)p.cache.n_pages) {
         note_bad_index(p.status);
         page = 0;
       }
       unit = page * p.cache.page16 + place * p.cache.token16 + kv * p.cache.head16;
-      copy_tokens(p.cache.k, t0, S::WHOLE);   // keys behind a sequence's end have no score, whatever they are, but may be in no page
+      if constexpr (I8) scale = (page * p.cache.n_kv_heads + kv) * p.cache.page_size + place + (S::WHOLE ? lane & 15 : 0);
+      copy_tokens(p.cache.k, S::WHOLE);   // keys behind a sequence's end have no score, whatever they are, but may be in no page
     };
     auto copy_values = [&]() {
-      const int t0 = (in.span.tile0() + in.tile) * kTile;
-      copy_tokens(p.cache.v, t0, t0 >= in.span.first && in.span.end - t0 >= kTile);   // 0 for what is not seen: its p is 0, and must stay so
-    };
-    auto copy_scales = [&](const float* scales) {
-      if constexpr (I8) {
-        if (lane < 16) {
-          const int t = (in.span.tile0() + in.tile) * kTile + lane;
-          const uint32_t place = t - divide(t, p.cache.by_page) * p.cache.page_size;
-          const long long i = ((long long)page * p.cache.n_kv_heads + in.r / p.chunks) * p.cache.page_size + place;
-          cp_async(put_scales + lane * 4, scales + i, in_span(t) ? 4 : 0, std::integral_constant<int, 4>());
-        }
-      }
+      // 0 for what is not seen: its p is 0, and must stay so
+      copy_tokens(p.cache.v, in.t0 >= in.span.first && in.span.end - in.t0 >= kTile);
     };
     auto filled = [&]() {
       asm volatile("cp.async.commit_group;" ::: "memory");
@@ -387,7 +410,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       if (issued < count) {
         copy_values();
         copy_scales(p.cache.v_scales);
-        in.next(p);
+        if (in.next(p)) kv = in.r / p.chunks;
         look_up(issued + 1 < count);
       }
       ++issued;
@@ -410,6 +433,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     float most[2], sum[2];                                   // of heads lr (+ 8); sum: of this lane's tokens
     float acc[D / 16][kCols][4];                             // rows: channels, columns: heads 2 lc, 2 lc + 1 (+ 8)
     float v_ref = 1.f, inv_ref = 1.f;                        // I8: acc is in units of it
+    float q_bias[2] = {0.f, 0.f};                            // I8: what the sums of products have too much
     bool from_start;
 
     auto begin_row = [&]() {
@@ -444,7 +468,10 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
           big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
           const int e = min(max((int)(__float_as_uint(big) >> 23) - 127, -126), 126);
           const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-          to_log2[n] = p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23);
+          // Codes come as c + 128 in the lowest bits of a binary16, (c + 128) 2^-24: 128 2^-24 times the sum of q is taken off each sum.
+          // (The bias is about three times as large as the sums themselves, so their last bits weigh as much more.)
+          to_log2[n] = p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23) * 16777216.f;
+          q_bias[n] = 0.f;
 #pragma unroll
           for (int s = 0; s < D / 16; ++s)
 #pragma unroll
@@ -452,7 +479,12 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
               const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&q[n][s][w]));
               const __half2 x = __floats2half2_rn(f.x * down, f.y * down);
               q[n][s][w] = *reinterpret_cast<const uint32_t*>(&x);
+              const float2 g = __half22float2(x);
+              q_bias[n] += g.x + g.y;
             }
+          q_bias[n] += __shfl_xor_sync(0xffffffffu, q_bias[n], 1);
+          q_bias[n] += __shfl_xor_sync(0xffffffffu, q_bias[n], 2);
+          q_bias[n] *= 0x1p-17f;
         }
         most[n] = kNegInf;
         sum[n] = 0.f;
@@ -462,7 +494,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
 #pragma unroll
         for (int n = 0; n < kCols; ++n) acc[d][n][0] = acc[d][n][1] = acc[d][n][2] = acc[d][n][3] = 0.f;
       if constexpr (I8) v_ref = 0.f;
-      from_start = at.tile == 0;
+      from_start = at.t0 == at.tile0();
     };
 
     // acc times a factor per head; lanes have those of heads lr (+ 8)
@@ -478,7 +510,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     };
 
     auto add_tile = [&]() {
-      const int t0 = (at.span.tile0() + at.tile) * kTile;
+      const int t0 = at.t0;
       landed();
       __syncwarp();                          // for all lanes, and all have read what is filled next
       issue_keys();
@@ -497,7 +529,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
             uint32_t b0, b1;
             if constexpr (I8) {
               const uint32_t u = w[e] ^ 0x80808080u;
-              b0 = low_codes(u), b1 = high_codes(u);
+              b0 = __byte_perm(u, 0u, 0x4140), b1 = __byte_perm(u, 0u, 0x4342);
             } else {
               b0 = w[2 * e], b1 = w[2 * e + 1];
             }
@@ -514,8 +546,9 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
         if constexpr (I8) k_scale = lds_float(get_scales + (lc + 4 * i) * 4);
 #pragma unroll
         for (int n = 0; n < kCols; ++n) {
-          const float y = s[i >> 1][0][2 * n + (i & 1)] + s[i >> 1][1][2 * n + (i & 1)];
-          x[n][i] = (I8 ? y * k_scale : y) * to_log2[n];
+          float y = s[i >> 1][0][2 * n + (i & 1)] + s[i >> 1][1][2 * n + (i & 1)];
+          if constexpr (I8) y = (y - q_bias[n]) * k_scale;
+          x[n][i] = y * to_log2[n];
         }
       }
       if (t0 < at.span.first || at.span.end - t0 < kTile) {
@@ -680,7 +713,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       }
       if (!more) asm volatile("cp.async.wait_group 0;" ::: "memory");   // the ring is no longer filled
       __syncwarp();
-      const Part<S> part = more ? first_part(warp) : last_part(warp);
+      const Part<S, true> part = more ? first_part(warp) : last_part(warp);
 #pragma unroll
       for (int n = 0; n < kCols; ++n) {
         if (lc == 0 && lr + 8 * n < NH) {
@@ -688,13 +721,13 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
           part.total(lr + 8 * n) = sum[n];
         }
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) {
+        for (int d = 0; d < D / 16; d += 2) {
           const int j = d / (S::kEV / 2), e = d % (S::kEV / 2);
-          const int ch = (j * 8 + lr) * S::kEV + 2 * e;
+          const int d4 = ((j * 8 + lr) * S::kEV + 2 * e) / 4;
 #pragma unroll
           for (int c = 0; c < 2; ++c)
             if (!S::kHalves || lc < 2)
-              *reinterpret_cast<float2*>(&part.sum(2 * lc + c + 8 * n, ch)) = make_float2(acc[d][n][c] * v_ref, acc[d][n][c + 2] * v_ref);
+              part.sums(2 * lc + c + 8 * n, d4) = make_float4(acc[d][n][c] * v_ref, acc[d][n][c + 2] * v_ref, acc[d + 1][n][c] * v_ref, acc[d + 1][n][c + 2] * v_ref);
         }
       }
       if (lane == 0) s_head[2 * warp + (more ? 0 : 1)] = make_int4(at.b * p.rows_of_seq + at.r, from_start, to_end, 0);
@@ -705,68 +738,91 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     for (int i = 0; i < count; ++i) {
       if (fresh) begin_row();
       add_tile();
-      fresh = at.tile + 1 == at.tiles;
+      fresh = at.left == 1;
       if (fresh || i + 1 == count) end_row(fresh, i + 1 < count);
       at.next(p);
     }
   }
   __syncthreads();
 
-  // ---- rows that no warp has alone: parts of one row follow one another
-  constexpr int kItems = NH * D / 4;
+  // ---- rows that no warp has alone.  Lane i has the i-th part of the CTA (two for each warp, of the rows in order); a warp takes a head of
+  // a row at a time.
+  const int4 own = lane < 2 * S::kWarps ? s_head[lane] : make_int4(-1, 0, 0, 0);
+  const Part<S, true> own_part = lane & 1 ? last_part(lane >> 1) : first_part(lane >> 1);
+  const uint32_t there = __ballot_sync(0xffffffffu, own.x >= 0);
   int4* const headers = p.headers + 2 * blockIdx.x;
-  int crossing[2] = {-1, -1}, ends_here[2] = {0, 0};
-  for (int item = tid; item < kItems; item += kThreads) {
-    const int head = item / (D / 4), d = item % (D / 4) * 4;
-    float most = kNegInf, total_p = 0.f;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    int row = -1, starts = 0, ends = 0;
-    auto finish = [&]() {
-      if (row < 0) return;
-      if (starts && ends) {
-        const int b = row / p.rows_of_seq;
-        int heads;
-        const int h0 = first_head<S>(p, row - b * p.rows_of_seq, heads);
-        if (head < heads) {
-          const float inv = 1.f / total_p;
-          const long long o = (long long)b * p.n_heads + h0 + head;
-          *reinterpret_cast<uint2*>(p.out + o * D + d) = make_uint2(bf16_pair(sum.x * inv, sum.y * inv), bf16_pair(sum.z * inv, sum.w * inv));
-          if (p.lse && d == 0) p.lse[o] = kLn2 * (most + log2f(total_p));
+  int task = 0, crossing0 = -1, crossing1 = -1, ends0 = 0;
+  for (uint32_t rest = there; rest;) {
+    const int leader = __ffs(rest) - 1;
+    const int row = __shfl_sync(0xffffffffu, own.x, leader);
+    const uint32_t parts = __ballot_sync(0xffffffffu, own.x == row);
+    rest &= ~parts;
+    const int starts = __shfl_sync(0xffffffffu, own.y, leader), ends = __shfl_sync(0xffffffffu, own.z, 31 - __clz(parts));
+    if (!starts) crossing0 = row, ends0 = ends;
+    else if (!ends) crossing1 = row;
+    const int b = row / p.rows_of_seq;
+    int heads;
+    const int h0 = first_head<S>(p, row - b * p.rows_of_seq, heads);
+    for (int head = 0; head < heads; ++head, ++task) {
+      if (task % S::kWarps != warp) continue;
+      const bool mine = own.x == row;
+      const float m = mine ? own_part.most(head) : kNegInf;
+      float most = m;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+      const float f = weight(m, most);
+      float total_p = mine ? f * own_part.total(head) : 0.f;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) total_p += __shfl_xor_sync(0xffffffffu, total_p, o);
+      for (int d4 = lane; d4 < (D / 4 + 31) / 32 * 32; d4 += 32) {         // (the whole warp goes round)
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (uint32_t of = parts; of;) {
+          float fi[4];
+          float4 v[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {      // (the last one again, with a factor of 0, where there are fewer)
+            const int i = of ? __ffs(of) - 1 : leader;
+            fi[u] = __shfl_sync(0xffffffffu, f, i);
+            if (!of) fi[u] = 0.f;
+            of &= of - 1;
+            v[u] = (i & 1 ? last_part(i >> 1) : first_part(i >> 1)).sums(head, d4 % (D / 4));
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) sum.x += v[u].x * fi[u], sum.y += v[u].y * fi[u], sum.z += v[u].z * fi[u], sum.w += v[u].w * fi[u];
         }
-        return;
+        if (d4 >= D / 4) continue;
+        if (!starts || !ends) {
+          Part<S, false>{p.parts + (2ll * blockIdx.x + (starts ? 1 : 0)) * S::kPart}.sums(head, d4) = sum;
+        } else {
+          const float inv = 1.f / total_p;
+          reinterpret_cast<uint2*>(p.out)[((long long)b * p.n_heads + h0 + head) * (D / 4) + d4] =
+              make_uint2(bf16_pair(sum.x * inv, sum.y * inv), bf16_pair(sum.z * inv, sum.w * inv));
+        }
       }
-      const int which = starts ? 1 : 0;
-      const Part<S> part{p.parts + (2ll * blockIdx.x + which) * S::kPart};
-      *reinterpret_cast<float4*>(&part.sum(head, d)) = sum;
-      if (d == 0) {
-        part.most(head) = most;
-        part.total(head) = total_p;
+      if (lane == 0) {
+        if (!starts || !ends) {
+          const Part<S, false> part{p.parts + (2ll * blockIdx.x + (starts ? 1 : 0)) * S::kPart};
+          part.most(head) = most;
+          part.total(head) = total_p;
+        } else if (p.lse) {
+          p.lse[(long long)b * p.n_heads + h0 + head] = kLn2 * (most + log2f(total_p));
+        }
       }
-      crossing[which] = row;
-      ends_here[which] = ends;
-    };
-    for (int i = 0; i < 2 * S::kWarps; ++i) {
-      const int4 h = s_head[i];
-      if (h.x < 0) continue;
-      if (h.x != row) {
-        finish();
-        row = h.x, starts = h.y, most = kNegInf, total_p = 0.f, sum = make_float4(0.f, 0.f, 0.f, 0.f);
-      }
-      ends = h.z;
-      const Part<S> part = i & 1 ? last_part(i >> 1) : first_part(i >> 1);
-      const float m = part.most(head), next = fmaxf(most, m);
-      const float a = weight(most, next), b = weight(m, next);
-      const float4 v = *reinterpret_cast<const float4*>(&part.sum(head, d));
-      total_p = total_p * a + part.total(head) * b;
-      sum.x = sum.x * a + v.x * b, sum.y = sum.y * a + v.y * b, sum.z = sum.z * a + v.z * b, sum.w = sum.w * a + v.w * b;
-      most = next;
     }
-    finish();
   }
   if (tid == 0) {
-    headers[0] = make_int4(crossing[0], ends_here[0], 0, 0);
-    headers[1] = make_int4(crossing[1], ends_here[1], 0, 0);
+    headers[0] = make_int4(crossing0, ends0, 0, 0);
+    headers[1] = make_int4(crossing1, 0, 0, 0);
   }
+
+  // ---- sequences that are not there have outputs all the same
+  for (int b = blockIdx.x; b < B; b += gridDim.x)
+    if (span_of(p, b).tiles() == 0) {
+      for (int i = tid; i < p.n_heads * (D / 8); i += kThreads)
+        reinterpret_cast<uint4*>(p.out)[(long long)b * p.n_heads * (D / 8) + i] = make_uint4(0, 0, 0, 0);
+      if (p.lse)
+        for (int i = tid; i < p.n_heads; i += kThreads) p.lse[(long long)b * p.n_heads + i] = kNegInf;
+    }
 }
 
 // Joins the rows that cross CTAs.  CTA i takes the row that begins in CTA i of the kernel before and goes on in the next ones.
@@ -794,7 +850,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, cons
     }
     n += 32;
   }
-  auto part_of = [&](int i) { return Part<S>{p.parts + (i == 0 ? 2ll * blockIdx.x + 1 : 2ll * (blockIdx.x + i)) * S::kPart}; };
+  auto part_of = [&](int i) { return Part<S, false>{p.parts + (i == 0 ? 2ll * blockIdx.x + 1 : 2ll * (blockIdx.x + i)) * S::kPart}; };
   const int b = row / p.rows_of_seq;
   int heads;
   const int h0 = first_head<S>(p, row - b * p.rows_of_seq, heads);
@@ -823,7 +879,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, cons
 #pragma unroll 4
     for (int i = 0; i < n; ++i) {
       const float w = s_weight[head][i];
-      const float4 v = *reinterpret_cast<const float4*>(&part_of(i).sum(head, d));
+      const float4 v = part_of(i).sums(head, d / 4);
       sum.x += w * v.x, sum.y += w * v.y, sum.z += w * v.z, sum.w += w * v.w;
     }
     const float inv = s_inv[head];

@@ -116,8 +116,13 @@ class Case:
             # What a score may be off by.  D products, exact in binary32 (16-bit factors; a key's scale comes behind the sum), whose sum
             # loses at most 2 h per addition (a tensor core may cut what is below the last bit instead of rounding), then
             # four roundings of the score: D * 2 h of the sum of the products' sizes, 4 h of the score.  8-bit caches: q in binary16 with a
-            # common power of two is off by 2^-25 of the head's largest at most, 2^-25 D |q|max |k|max in all.
-            size = torch.einsum("kgd,tkd->kgt", q.abs(), k.abs()) * abs(scale)
+            # common power of two is off by 2^-25 of the head's largest at most, 2^-25 D |q|max |k|max in all; and a code c is summed as c + 128,
+            # the sum of 128 q taken off afterwards, so that the products are of the size of q (|c| + 128) and once more 128 q.
+            sizes = k.abs()
+            if self.scales[0] is not None:
+                page, at = places(self.table, b, range(first, n), self.page)
+                sizes = sizes + 256 * self.scales[0].transpose(1, 2)[page, at].double()[..., None]
+            size = torch.einsum("kgd,tkd->kgt", q.abs(), sizes) * abs(scale)
             ds = 2 * H * D * size + 4 * H * s.abs()
             if self.scales[0] is not None:
                 ds = ds + 2.0 ** -25 * D * abs(scale) * q.abs().amax(-1)[..., None] * k.abs().amax(-1).t()[:, None, :]
