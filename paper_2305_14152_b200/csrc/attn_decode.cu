@@ -8,12 +8,11 @@
 //   * A tile is 16 tokens of a row.  Tiles are numbered through all sequences, heads and lengths, and dealt evenly: every CTA
 //     takes an equal run of them, every warp an equal run of its CTA's.  Nothing depends on how uneven the lengths are.
 //   * A warp copies its own tiles into its own ring of shared memory (cp.async, several units of 16 keys or values ahead), whole
-//     tokens at a time, and reads them as operands of the tensor cores' m16n8k16 product: the channels of the contraction and
-//     the tokens of a tile are taken in whatever order makes one 16-byte load serve several products without bank conflicts.  So there
-//     is no barrier between warps and no transposition in the loop.
-//       S = Q K^T      Q [16 heads x 16 channels] in registers, K the other operand: a lane holds 4 adjacent channels of a token
-//       O^T = V^T P^T  V^T [16 channels x 16 tokens]: a lane loads the same channels of four tokens and pairs them byte by byte (prmt);
-//                      S leaves the first product laid out as the operand P^T of the second
+//     tokens at a time, and reads them with ldmatrix as the 16-row operand of the tensor cores' m16n8k16 product, the heads as its 8 columns:
+//       S^T = K Q^T     K [16 tokens x 16 channels] as it lies, Q in registers
+//       O^T = V^T P^T   V^T [16 channels x 16 tokens] by the transposing ldmatrix; P^T from S^T by movmatrix
+//     So there is no barrier between warps in the loop, and a lane has the factors of the sums that it holds.
+//   * Up to four query heads stand in the columns twice, and p's two numbers (below) in the two places.
 //   * Running maximum and sum per row, as the softmax allows: the sums are rescaled only when the maximum has risen by more than
 //     kSlack (a factor of 2^8 that the binary32 sums carry easily).
 //   * p goes into the second product as the sum of two 16-bit numbers: with one, its rounding (2^-9 of p) would double the
@@ -67,10 +66,6 @@ struct Shape {
   static constexpr bool kHalves = NH == 4;                      // the two numbers that p is are columns of one product
   static constexpr int kCols = NH > 8 ? 2 : 1;                  // of eight heads (kHalves: of four, twice)
   static constexpr int kBytes = D * (I8 ? 1 : 2);               // of a token
-  static constexpr int kKC = kBytes / 64;                       // 16-byte pieces per lane of a token's key, 4 lanes side by side
-  static constexpr int kVB = kBytes >= 128 ? 16 : 8;            // bytes per lane of a token's value, 8 lanes side by side
-  static constexpr int kVC = kBytes / (8 * kVB);
-  static constexpr int kEV = kVB / (I8 ? 1 : 2);                // channels in them
   static constexpr int kPieces = kBytes / 16;                   // 16-byte pieces of a token
   static constexpr int kRows = 32 / kPieces;                    // tokens that a warp copies with one instruction
   static constexpr int kUnit = kTile * kBytes;                  // keys or values of a tile
@@ -89,21 +84,22 @@ __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, std::int
 __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, uint32_t bytes, std::integral_constant<int, 16>) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, uint32_t bytes, std::integral_constant<int, 8>) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, uint32_t bytes, std::integral_constant<int, 4>) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ uint4 lds16(uint32_t at) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
-  return v;
+// Four 8 x 8 matrices of 16-bit elements, their rows at the addresses that the lanes give (lanes 8 i .. 8 i + 7: matrix i).  Lane (r, c) gets
+// elements 2 c and 2 c + 1 of row r, or (transposed) of column r.
+__device__ __forceinline__ void ldmatrix(uint32_t (&x)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at) : "memory");
 }
-__device__ __forceinline__ uint2 lds8(uint32_t at) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
-  return v;
+__device__ __forceinline__ void ldmatrix_transposed(uint32_t (&x)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 __device__ __forceinline__ float lds_float(uint32_t at) {
   float v;
@@ -137,14 +133,12 @@ __device__ __forceinline__ float power_of_two(float x) {
   return y;
 }
 
-// Codes of 8 bits as binary16: with its sign bit turned a code c is the byte c + 128, and 0x6400 | byte is 1024 + 128 + c.
-__device__ __forceinline__ uint32_t less_bias(uint32_t h) {
+// Codes of 8 bits, with their sign bits turned: c + 128 as a byte.  Two of them as binary16: 0x6400 | byte is 1024 + 128 + c.
+__device__ __forceinline__ uint32_t codes(uint32_t x, uint32_t which) {
+  const uint32_t h = __byte_perm(x, 0x64646464u, which);
   const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&h), __half2half2(__ushort_as_half(0x6480)));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
-// two bytes of x, the lower pair or the higher
-__device__ __forceinline__ uint32_t low_codes(uint32_t x) { return less_bias(__byte_perm(x, 0x64646464u, 0x4140)); }
-__device__ __forceinline__ uint32_t high_codes(uint32_t x) { return less_bias(__byte_perm(x, 0x64646464u, 0x4342)); }
 
 // Two numbers rounded to 16 bits, and what that leaves of them; lower half: p0.
 template <bool F16>
@@ -215,20 +209,41 @@ struct Cursor {
   }
 };
 
-// Sums of a row, or of a part of one, in a part's memory: O [NH][D], then the maxima and the sums of p.  Within a CTA four channels of
-// a head lie in the place of others of their eight times four, so that the lanes of a warp write to different banks.
-template <typename S, bool MIXED>
+// Sums of a row, or of a part of one, in a part's memory: O^T [D][NH], then the maxima and the sums of p.
+template <int D, int NH>
 struct Part {
   float* at;
-  __device__ __forceinline__ float4& sums(int head, int d4) const {
-    const int lc = (head >> 1) & 3, mix = S::kEV == 16 ? lc : (lc & 1) + 4 * (lc >> 1);
-    return reinterpret_cast<float4*>(at + head * S::D)[MIXED ? d4 ^ mix : d4];
-  }
-  __device__ __forceinline__ float& most(int head) const { return at[S::NH * S::D + head]; }
-  __device__ __forceinline__ float& total(int head) const { return at[S::NH * (S::D + 1) + head]; }
+  __device__ __forceinline__ float2& two(int d, int head) const { return *reinterpret_cast<float2*>(at + d * NH + head); }
+  // four heads of a channel, by their place
+  __device__ __forceinline__ float4& four(int i) const { return reinterpret_cast<float4*>(at)[i]; }
+  __device__ __forceinline__ float2& most(int head) const { return *reinterpret_cast<float2*>(at + D * NH + head); }
+  __device__ __forceinline__ float2& total(int head) const { return *reinterpret_cast<float2*>(at + (D + 1) * NH + head); }
+  __device__ __forceinline__ float4& most4(int head) const { return *reinterpret_cast<float4*>(at + D * NH + head); }
+  __device__ __forceinline__ float4& total4(int head) const { return *reinterpret_cast<float4*>(at + (D + 1) * NH + head); }
 };
+__device__ __forceinline__ float4 operator*(float4 a, float4 b) { return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w); }
+__device__ __forceinline__ float4 operator+(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
+__device__ __forceinline__ float4 larger(float4 a, float4 b) {
+  return make_float4(fmaxf(a.x, b.x), fmaxf(a.y, b.y), fmaxf(a.z, b.z), fmaxf(a.w, b.w));
+}
 
 __device__ __forceinline__ float weight(float m, float most) { return m == kNegInf ? 0.f : exp2f(m - most); }
+__device__ __forceinline__ float4 weight(float4 m, float4 most) {
+  return make_float4(weight(m.x, most.x), weight(m.y, most.y), weight(m.z, most.z), weight(m.w, most.w));
+}
+
+// Channel d of heads h0 + head .. + 3, as far as there are heads, and their log-sums where d is 0.
+template <int D>
+__device__ __forceinline__ void put_out(const AttnParams& p, long long row0, int heads, int head, int d, float4 sum, float4 most, float4 total) {
+  const float o[4] = {sum.x, sum.y, sum.z, sum.w}, m[4] = {most.x, most.y, most.z, most.w}, t[4] = {total.x, total.y, total.z, total.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (head + i < heads) {
+      const __nv_bfloat16 x = __float2bfloat16_rn(o[i] * (1.f / t[i]));
+      p.out[(row0 + head + i) * D + d] = *reinterpret_cast<const uint16_t*>(&x);
+      if (p.lse && d == 0) p.lse[row0 + head + i] = kLn2 * (m[i] + log2f(t[i]));
+    }
+}
 
 // First query head of a row, and how many there are.
 template <typename S>
@@ -251,8 +266,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   const int lr = lane >> 2, lc = lane & 3;
   const uint32_t ring = ptx::smem_u32(smem) + warp * S::kRing;
   // a warp's parts of rows: one that it goes on from lies in the workspace, its last in its ring
-  const auto first_part = [&](int w) { return Part<S, true>{p.first_parts + ((long long)blockIdx.x * S::kWarps + w) * S::kPart}; };
-  const auto last_part = [&](int w) { return Part<S, true>{reinterpret_cast<float*>(smem + w * S::kRing)}; };
+  const auto first_part = [&](int w) { return Part<D, NH>{p.first_parts + ((long long)blockIdx.x * S::kWarps + w) * S::kPart}; };
+  const auto last_part = [&](int w) { return Part<D, NH>{reinterpret_cast<float*>(smem + w * S::kRing)}; };
 
   if (tid < 2 * S::kWarps) s_head[tid] = make_int4(-1, 0, 0, 0);
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -338,17 +353,16 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     uint32_t put = ring, get = ring;         // next unit to fill, and to read
     const uint32_t scales_of = ptx::smem_u32(smem) + S::kWarps * S::kRing + warp * S::kUnits * 64;
     uint32_t put_scales = scales_of, get_scales = scales_of;
-    // Piece c of token t lies in place c ^ (t & 7): the eight lanes that a load serves at a time read eight different places of 128 bytes,
-    // of two tokens four apart (keys) or of two times four tokens (values).  (64-byte tokens lie as they come.)
-    auto place_of = [](int t, int c) { return (uint32_t)(t * S::kPieces + (S::kPieces >= 8 ? c ^ (t & 7) : c)) * 16; };
+    // Piece c of token t lies in place c ^ (t & 7) (of 64-byte tokens: c ^ (t / 2 & 3)): the eight rows of a matrix, and what eight lanes copy,
+    // are in different banks.
+    auto turn_of = [](int t) { return S::kPieces >= 8 ? t & 7 : t >> 1 & 3; };
+    auto place_of = [&](int t, int c) { return (uint32_t)(t * S::kPieces + (c ^ turn_of(t))) * 16; };
     const int copy_row = lane / S::kPieces, copy_piece = lane % S::kPieces;
     const uint32_t copy_to = place_of(copy_row, copy_piece);
-    const int key_token = (lr >> 1) + 4 * (lr & 1);         // of column lr of the first product, and 8 more
-    const uint32_t key_at = place_of(key_token, lc), key_at2 = key_at ^ 64;
-    const uint32_t value_at = S::kVB == 16 ? place_of(lc + 4 * (lr & 1), lr) : place_of(lc + 4 * (lr & 1), 0) + lr * 8;
-    const uint32_t value_at2 = S::kVB == 16 ? place_of(lc + 4 * (1 - (lr & 1)), lr) : place_of(lc + 4 * (1 - (lr & 1)), 0) + lr * 8;
-    const uint32_t pick_low = I8 ? (lr & 1 ? 0x1504u : 0x5140u) : (lr & 1 ? 0x1054u : 0x5410u);
-    const uint32_t pick_high = I8 ? (lr & 1 ? 0x3726u : 0x7362u) : (lr & 1 ? 0x3276u : 0x7632u);
+    // matrices of keys, and of 8-bit values: tokens 0..7 and 8..15 of a piece, then of the next; of values: two pieces of tokens 0..7, then of 8..15
+    const uint32_t key_at = place_of((lane & 7) + (lane & 8), lane >> 4);
+    const uint32_t value_at = I8 ? key_at : place_of((lane & 7) + (lane >> 4) * 8, lane >> 3 & 1);
+    auto pair_at = [](uint32_t at, int j) { return (at ^ (S::kPieces >= 8 ? (2 * j & 7) * 16 : 2 * j * 16)) + (S::kPieces > 8 ? j / 4 * 128 : 0); };   // pieces 2 j and 2 j + 1
     uint32_t unit = 0;                       // place of the copies' tile (WHOLE) or of its token (lane & 15)
     uint32_t scale = 0;                      // the same in the scales (fewer than 2^30: each has 64 bytes of codes, and they have less than 2^36)
     int kv = in.r / p.chunks;                // head of keys and values
@@ -369,7 +383,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
 #pragma unroll
       for (int j = 0; j < kTile / S::kRows; ++j) {
         if constexpr (!S::WHOLE) src = base + (uint64_t)__shfl_sync(0xffffffffu, unit, copy_row + j * S::kRows) * 16;
-        const uint32_t to = ((put + copy_to) ^ (S::kPieces >= 8 ? ((j * S::kRows) & 7) * 16 : 0)) + j * 512;
+        const uint32_t to = ((put + copy_to) ^ (turn_of(j * S::kRows) * 16)) + j * 512;
         if (all) cp_async(to, src, std::integral_constant<int, 16>());
         else cp_async(to, src, in_span(in.t0 + copy_row + j * S::kRows) ? 16 : 0, std::integral_constant<int, 16>());
         if constexpr (S::WHOLE) src += step;
@@ -428,12 +442,12 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       issue_values();
     }
 
-    uint32_t q[kCols][D / 16][2];                            // heads lr (+ 8): words of adjacent channels
-    float to_log2[2] = {p.scale_log2, p.scale_log2};         // of a product of the tensor cores, per head
-    float most[2], sum[2];                                   // of heads lr (+ 8); sum: of this lane's tokens
-    float acc[D / 16][kCols][4];                             // rows: channels, columns: heads 2 lc, 2 lc + 1 (+ 8)
+    uint32_t q[kCols][D / 16][2];                            // head lr (+ 8): two and two channels for each product
+    float to_log2[kCols][2];                                 // of a product of the tensor cores; here and below: heads 2 lc, 2 lc + 1 (+ 8)
+    float q_bias[kCols][2];                                  // I8: what the sums of products have too much
+    float most[kCols][2], sum[kCols][2];                     // sum: of this lane's tokens
+    float acc[D / 16][kCols][4];                             // two channels of each of the two heads
     float v_ref = 1.f, inv_ref = 1.f;                        // I8: acc is in units of it
-    float q_bias[2] = {0.f, 0.f};                            // I8: what the sums of products have too much
     bool from_start;
 
     auto begin_row = [&]() {
@@ -443,16 +457,18 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       for (int n = 0; n < kCols; ++n) {
         const int h = (S::kHalves ? lr & 3 : lr) + 8 * n;
         const uint16_t* from = p.q + at.b * p.q_row + (long long)(h0 + h) * p.q_head;
-        constexpr int kAdjacent = I8 ? 16 : 8;               // channels of a 16-byte piece of a key
 #pragma unroll
-        for (int j = 0; j < S::kKC; ++j)
-#pragma unroll
-          for (int e = 0; e < kAdjacent / 8; ++e) {
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (h < heads) x = ptx::ld_global(reinterpret_cast<const uint4*>(from + (j * 4 + lc) * kAdjacent + e * 8));
-            const int s = (j * kAdjacent + e * 8) / 4;
-            q[n][s][0] = x.x, q[n][s][1] = x.y, q[n][s + 1][0] = x.z, q[n][s + 1][1] = x.w;
+        for (int s = 0; s < D / 16; ++s) {
+          uint2 x = make_uint2(0u, 0u);
+          if (h < heads) {
+            // as the matrices have the channels: 2 lc and 8 + 2 lc of a product's sixteen, of 8-bit keys 4 lc .. 4 lc + 3
+            if constexpr (I8) x = ptx::ld_global(reinterpret_cast<const uint2*>(from + 16 * s + 4 * lc));
+            else x = make_uint2(ptx::ld_global(reinterpret_cast<const uint32_t*>(from + 16 * s + 2 * lc)),
+                                ptx::ld_global(reinterpret_cast<const uint32_t*>(from + 16 * s + 8 + 2 * lc)));
           }
+          q[n][s][0] = x.x, q[n][s][1] = x.y;
+        }
+        float scale = p.scale_log2, bias = 0.f;
         if constexpr (I8) {
           // bf16 as binary16: times a power of two that brings the head's largest below 4.  What becomes subnormal there is
           // 2^-14 of the largest or less, and off by 2^-25 of it at most.
@@ -470,8 +486,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
           const float down = __uint_as_float((uint32_t)(127 - e) << 23);
           // Codes come as c + 128 in the lowest bits of a binary16, (c + 128) 2^-24: 128 2^-24 times the sum of q is taken off each sum.
           // (The bias is about three times as large as the sums themselves, so their last bits weigh as much more.)
-          to_log2[n] = p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23) * 16777216.f;
-          q_bias[n] = 0.f;
+          scale = p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23) * 16777216.f;
 #pragma unroll
           for (int s = 0; s < D / 16; ++s)
 #pragma unroll
@@ -480,14 +495,19 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
               const __half2 x = __floats2half2_rn(f.x * down, f.y * down);
               q[n][s][w] = *reinterpret_cast<const uint32_t*>(&x);
               const float2 g = __half22float2(x);
-              q_bias[n] += g.x + g.y;
+              bias += g.x + g.y;
             }
-          q_bias[n] += __shfl_xor_sync(0xffffffffu, q_bias[n], 1);
-          q_bias[n] += __shfl_xor_sync(0xffffffffu, q_bias[n], 2);
-          q_bias[n] *= 0x1p-17f;
+          bias += __shfl_xor_sync(0xffffffffu, bias, 1);
+          bias += __shfl_xor_sync(0xffffffffu, bias, 2);
+          bias *= 0x1p-17f;
         }
-        most[n] = kNegInf;
-        sum[n] = 0.f;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {                        // from the lanes of head lr to those of its column
+          to_log2[n][c] = I8 ? __shfl_sync(0xffffffffu, scale, lc * 8 + c * 4) : scale;
+          q_bias[n][c] = I8 ? __shfl_sync(0xffffffffu, bias, lc * 8 + c * 4) : 0.f;
+          most[n][c] = kNegInf;
+          sum[n][c] = 0.f;
+        }
       }
 #pragma unroll
       for (int d = 0; d < D / 16; ++d)
@@ -497,16 +517,11 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       from_start = at.t0 == at.tile0();
     };
 
-    // acc times a factor per head; lanes have those of heads lr (+ 8)
-    auto rescale = [&](const float (&f)[2]) {
+    auto rescale = [&](const float (&f)[kCols][2]) {
 #pragma unroll
-      for (int n = 0; n < kCols; ++n) {
-        const float f0 = __shfl_sync(0xffffffffu, f[n], lc * 8), f1 = __shfl_sync(0xffffffffu, f[n], lc * 8 + 4);
+      for (int d = 0; d < D / 16; ++d)
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) {
-          acc[d][n][0] *= f0, acc[d][n][1] *= f1, acc[d][n][2] *= f0, acc[d][n][3] *= f1;
-        }
-      }
+        for (int n = 0; n < kCols; ++n) acc[d][n][0] *= f[n][0], acc[d][n][1] *= f[n][1], acc[d][n][2] *= f[n][0], acc[d][n][3] *= f[n][1];
     };
 
     auto add_tile = [&]() {
@@ -514,101 +529,98 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       landed();
       __syncwarp();                          // for all lanes, and all have read what is filled next
       issue_keys();
-      // ---- S = Q K^T, tokens 0..7 and 8..15; two sums each, so that a product waits for the one before the last
-      float s[2][2][4];
+      // ---- S^T = K Q^T, in two sums, so that a product waits for the one before the last
+      float s[2][kCols][4];
 #pragma unroll
-      for (int j = 0; j < S::kKC; ++j)
+      for (int j = 0; j < S::kPieces / 2; ++j) {
+        uint32_t k[4];
+        ldmatrix(k, pair_at(get + key_at, j));
+        if constexpr (I8) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint4 x = lds16(get + (j & 1 ? key_at2 : key_at) + i * 8 * S::kBytes + (j >> 1) * 128);
-          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-          constexpr int kSteps = I8 ? 4 : 2;
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t u = k[2 * e] ^ 0x80808080u, w = k[2 * e + 1] ^ 0x80808080u;
+            const uint32_t a0 = __byte_perm(u, 0u, 0x4140), a1 = __byte_perm(w, 0u, 0x4140), a2 = __byte_perm(u, 0u, 0x4342), a3 = __byte_perm(w, 0u, 0x4342);
 #pragma unroll
-          for (int e = 0; e < kSteps; ++e) {
-            const int k = kSteps * j + e;
-            uint32_t b0, b1;
-            if constexpr (I8) {
-              const uint32_t u = w[e] ^ 0x80808080u;
-              b0 = __byte_perm(u, 0u, 0x4140), b1 = __byte_perm(u, 0u, 0x4342);
-            } else {
-              b0 = w[2 * e], b1 = w[2 * e + 1];
+            for (int n = 0; n < kCols; ++n) {
+              if (j == 0) mma0<true>(s[e][n], a0, a1, a2, a3, q[n][2 * j + e][0], q[n][2 * j + e][1]);
+              else mma<true>(s[e][n], a0, a1, a2, a3, q[n][2 * j + e][0], q[n][2 * j + e][1]);
             }
-            const uint32_t a1 = kCols > 1 ? q[kCols - 1][k][0] : 0u, a3 = kCols > 1 ? q[kCols - 1][k][1] : 0u;
-            if (k < 2) mma0<I8>(s[i][e & 1], q[0][k][0], a1, q[0][k][1], a3, b0, b1);
-            else mma<I8>(s[i][e & 1], q[0][k][0], a1, q[0][k][1], a3, b0, b1);
+          }
+        } else {
+#pragma unroll
+          for (int n = 0; n < kCols; ++n) {
+            if (j < 2) mma0<false>(s[j & 1][n], k[0], k[1], k[2], k[3], q[n][j][0], q[n][j][1]);
+            else mma<false>(s[j & 1][n], k[0], k[1], k[2], k[3], q[n][j][0], q[n][j][1]);
           }
         }
-      // ---- scores in powers of two: x[n][i] of heads lr + 8 n and tokens lc + 4 {0, 1} + 8 {0, 1}
+      }
+      // ---- scores in powers of two: x[n][i] of head 2 lc + (i & 1) + 8 n and token lr + 8 (i >> 1)
       float x[kCols][4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float k_scale = 1.f;
-        if constexpr (I8) k_scale = lds_float(get_scales + (lc + 4 * i) * 4);
+        if constexpr (I8) k_scale = lds_float(get_scales + (lr + 8 * (i >> 1)) * 4);
 #pragma unroll
         for (int n = 0; n < kCols; ++n) {
-          float y = s[i >> 1][0][2 * n + (i & 1)] + s[i >> 1][1][2 * n + (i & 1)];
-          if constexpr (I8) y = (y - q_bias[n]) * k_scale;
-          x[n][i] = y * to_log2[n];
+          float y = s[0][n][i] + s[1][n][i];
+          if constexpr (I8) y = (y - q_bias[n][i & 1]) * k_scale;
+          x[n][i] = y * to_log2[n][i & 1];
         }
       }
       if (t0 < at.span.first || at.span.end - t0 < kTile) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (t0 + lc + 4 * i < at.span.first || t0 + lc + 4 * i >= at.span.end)
+          if (t0 + lr + 8 * (i >> 1) < at.span.first || t0 + lr + 8 * (i >> 1) >= at.span.end)
 #pragma unroll
             for (int n = 0; n < kCols; ++n) x[n][i] = kNegInf;
       }
-      // ---- running maximum
-      float top[kCols];
+      // ---- running maximum, brought up to date where one is passed by more than kSlack
       bool higher = false;
 #pragma unroll
-      for (int n = 0; n < kCols; ++n) {
-        top[n] = fmaxf(fmaxf(x[n][0], x[n][1]), fmaxf(x[n][2], x[n][3]));
-        top[n] = fmaxf(top[n], __shfl_xor_sync(0xffffffffu, top[n], 1));
-        top[n] = fmaxf(top[n], __shfl_xor_sync(0xffffffffu, top[n], 2));
-        higher |= top[n] > most[n] + kSlack;
-      }
-      if (__any_sync(0xffffffffu, higher)) {
-        float f[2] = {1.f, 1.f};
+      for (int n = 0; n < kCols; ++n)
 #pragma unroll
-        for (int n = 0; n < kCols; ++n) {
-          const float next = fmaxf(most[n], top[n]);
-          f[n] = weight(most[n], next);
-          sum[n] *= f[n];
-          most[n] = next;
-        }
+        for (int c = 0; c < 2; ++c) higher |= fmaxf(x[n][c], x[n][c + 2]) > most[n][c] + kSlack;
+      if (__any_sync(0xffffffffu, higher)) {
+        float f[kCols][2];
+#pragma unroll
+        for (int n = 0; n < kCols; ++n)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float next = fmaxf(x[n][c], x[n][c + 2]);
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) next = fmaxf(next, __shfl_xor_sync(0xffffffffu, next, o));
+            next = fmaxf(next, most[n][c]);
+            f[n][c] = weight(most[n][c], next);
+            sum[n][c] *= f[n][c];
+            most[n][c] = next;
+          }
         rescale(f);
       }
       // ---- p and its sum
 #pragma unroll
-      for (int n = 0; n < kCols; ++n) {
-        const float base = most[n] == kNegInf ? 0.f : most[n];
+      for (int n = 0; n < kCols; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          x[n][i] = power_of_two(x[n][i] - base);
-          sum[n] += x[n][i];
+          x[n][i] = power_of_two(x[n][i] - (most[n][i & 1] == kNegInf ? 0.f : most[n][i & 1]));
+          sum[n][i & 1] += x[n][i];
         }
-      }
-      read();
       // ---- O^T += V^T P^T
+      read();
       landed();
       __syncwarp();
       issue_values();
       if constexpr (I8) {
-        float v_scale[4], big = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v_scale[i] = lds_float(get_scales + (lc + 4 * i) * 4);
-          big = fmaxf(big, fabsf(v_scale[i]));
-        }
+        const float v_scale[2] = {lds_float(get_scales + lr * 4), lds_float(get_scales + lr * 4 + 32)};
         // Values in units of 2^-6 of the largest scale so far, cut to a power of two: p (at most 2^kSlack) times what is left of its
         // token's scale (below 2^7) is a binary16, and as two of them off by 2^-25 of a unit at most, 2^-31 of the largest.
-        const uint32_t exponent = __reduce_max_sync(0xffffffffu, __float_as_uint(big)) & 0x7f800000u;
+        const uint32_t exponent = __reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(fabsf(v_scale[0]), fabsf(v_scale[1])))) & 0x7f800000u;
         const float ref = __uint_as_float(exponent > (7u << 23) ? exponent - (6u << 23) : 1u << 23);
         if (ref > v_ref) {
           if (v_ref > 0.f) {
-            const float both[2] = {v_ref / ref, v_ref / ref};
-            rescale(both);
+            float f[kCols][2];
+#pragma unroll
+            for (int n = 0; n < kCols; ++n) f[n][0] = f[n][1] = v_ref / ref;
+            rescale(f);
           }
           v_ref = ref;
           inv_ref = 1.f / ref;
@@ -616,64 +628,51 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
 #pragma unroll
         for (int n = 0; n < kCols; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[n][i] *= v_scale[i] * inv_ref;
+          for (int i = 0; i < 4; ++i) x[n][i] *= v_scale[i >> 1] * inv_ref;
       }
-      uint32_t hi[kCols][2], lo[kCols][2];
+      uint32_t hi[kCols][2], lo[kCols][2];                   // tokens 0..7, 8..15
 #pragma unroll
       for (int n = 0; n < kCols; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           hi[n][i] = round16<I8>(x[n][2 * i], x[n][2 * i + 1]);
           lo[n][i] = round16<I8>(x[n][2 * i], x[n][2 * i + 1]);
-          if (S::kHalves && lr >= 4) hi[n][i] = lo[n][i];
+          if constexpr (S::kHalves) hi[n][i] = transposed(lc >= 2 ? lo[n][i] : hi[n][i]);
+          else hi[n][i] = transposed(hi[n][i]), lo[n][i] = transposed(lo[n][i]);
         }
+      auto product = [&](int d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
-      for (int j = 0; j < S::kVC; ++j) {
-        constexpr int kWords = S::kVB / 4;
-        uint32_t w[4][kWords];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t from = get + (i & 1 ? value_at2 : value_at) + (i >> 1) * 8 * S::kBytes + j * 128;
-          if constexpr (S::kVB == 16) {
-            const uint4 v = lds16(from);
-            w[i][0] = v.x, w[i][1] = v.y, w[i][kWords - 2] = v.z, w[i][kWords - 1] = v.w;
-          } else {
-            const uint2 v = lds8(from);
-            w[i][0] = v.x, w[i][1] = v.y;
-          }
+        for (int n = 0; n < kCols; ++n) {
+          mma<I8>(acc[d][n], a0, a1, a2, a3, hi[n][0], hi[n][1]);
+          if constexpr (!S::kHalves) mma<I8>(acc[d][n], a0, a1, a2, a3, lo[n][0], lo[n][1]);
         }
-        auto product = [&](int d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+      };
 #pragma unroll
-          for (int n = 0; n < kCols; ++n) {
-            mma<I8>(acc[d][n], a0, a1, a2, a3, hi[n][0], hi[n][1]);
-            if constexpr (!S::kHalves) mma<I8>(acc[d][n], a0, a1, a2, a3, lo[n][0], lo[n][1]);
-          }
-        };
+      for (int j = 0; j < S::kPieces / 2; ++j) {
+        uint32_t v[4];
+        ldmatrix_transposed(v, pair_at(get + value_at, j));
+        if constexpr (I8) {
+          // a lane has channels 2 lr and 2 lr + 1 of two tokens, byte by byte
 #pragma unroll
-        for (int e = 0; e < kWords; ++e) {
-          if constexpr (I8) {
-            // bytes of two tokens side by side: channels 0, 0, 1, 1 and 2, 2, 3, 3 of the word
-            const uint32_t a = __byte_perm(w[0][e], w[1][e], pick_low) ^ 0x80808080u, b = __byte_perm(w[2][e], w[3][e], pick_low) ^ 0x80808080u;
-            const uint32_t c = __byte_perm(w[0][e], w[1][e], pick_high) ^ 0x80808080u, f = __byte_perm(w[2][e], w[3][e], pick_high) ^ 0x80808080u;
-            product(2 * (j * kWords + e), low_codes(a), high_codes(a), low_codes(b), high_codes(b));
-            product(2 * (j * kWords + e) + 1, low_codes(c), high_codes(c), low_codes(f), high_codes(f));
-          } else {
-            product(j * kWords + e, __byte_perm(w[0][e], w[1][e], pick_low), __byte_perm(w[0][e], w[1][e], pick_high),
-                    __byte_perm(w[2][e], w[3][e], pick_low), __byte_perm(w[2][e], w[3][e], pick_high));
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t u = v[2 * e] ^ 0x80808080u, w = v[2 * e + 1] ^ 0x80808080u;
+            product(2 * j + e, codes(u, 0x4240), codes(u, 0x4341), codes(w, 0x4240), codes(w, 0x4341));
           }
+        } else {
+          product(j, v[0], v[1], v[2], v[3]);
         }
       }
       read();
     };
 
-    // The row's sums, or what this warp has of them, are complete.  acc[d] holds channels base + 2 e and base + 2 e + 1 in its
-    // rows lr and lr + 8, where d = j * kEV / 2 + e and base = (j * 8 + lr) * kEV.
+    // The row's sums, or what this warp has of them, are complete.  acc[d][n]: channels 16 d + lr and 16 d + lr + 8 (I8: 16 d + 2 lr and + 1).
     auto end_row = [&](bool to_end, bool more) {
 #pragma unroll
-      for (int n = 0; n < kCols; ++n) {
-        sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 1);
-        sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 2);
-      }
+      for (int n = 0; n < kCols; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) sum[n][c] += __shfl_xor_sync(0xffffffffu, sum[n][c], o);
       if constexpr (S::kHalves) {
 #pragma unroll
         for (int d = 0; d < D / 16; ++d)
@@ -685,27 +684,24 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       if (from_start && to_end) {
 #pragma unroll
         for (int n = 0; n < kCols; ++n) {
-          const float inv = 1.f / sum[n];
-          const long long out0 = (long long)at.b * p.n_heads + h0 + 8 * n;
-          if (p.lse && lc == 0 && lr + 8 * n < heads) p.lse[out0 + lr] = kLn2 * (most[n] + log2f(sum[n]));
+          const float f[2] = {1.f / sum[n][0] * v_ref, 1.f / sum[n][1] * v_ref};
+          const long long row0 = (long long)at.b * p.n_heads + h0 + 8 * n;
+          if (p.lse && lr == 0)
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const int h = 2 * lc + c;
-            const float f = __shfl_sync(0xffffffffu, inv, lc * 8 + c * 4) * v_ref;
-            if (h + 8 * n < heads) {
-              uint16_t* out = p.out + (out0 + h) * D + lr * S::kEV;
+            for (int c = 0; c < 2; ++c)
+              if (2 * lc + c + 8 * n < heads) p.lse[row0 + 2 * lc + c] = kLn2 * (most[n][c] + log2f(sum[n][c]));
+          uint16_t* const out = p.out + (row0 + lr) * D;     // head lr, once transposed
 #pragma unroll
-              for (int j = 0; j < S::kVC; ++j)
-#pragma unroll
-                for (int e = 0; e < S::kEV / 2; e += 4) {
-                  uint32_t o[4];
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) {
-                    const float* a = acc[j * (S::kEV / 2) + e + i][n];
-                    o[i] = bf16_pair(a[c] * f, a[c + 2] * f);
-                  }
-                  *reinterpret_cast<uint4*>(out + j * 8 * S::kEV + e * 2) = make_uint4(o[0], o[1], o[2], o[3]);
-                }
+          for (int d = 0; d < D / 16; ++d) {
+            const uint32_t a = transposed(bf16_pair(acc[d][n][0] * f[0], acc[d][n][1] * f[1]));
+            const uint32_t b = transposed(bf16_pair(acc[d][n][2] * f[0], acc[d][n][3] * f[1]));
+            if (lr + 8 * n < heads) {
+              if constexpr (I8) {                            // a: channels 4 lc and 4 lc + 2, b: the ones behind them
+                *reinterpret_cast<uint2*>(out + 16 * d + 4 * lc) = make_uint2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+              } else {
+                *reinterpret_cast<uint32_t*>(out + 16 * d + 2 * lc) = a;
+                *reinterpret_cast<uint32_t*>(out + 16 * d + 8 + 2 * lc) = b;
+              }
             }
           }
         }
@@ -713,23 +709,21 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       }
       if (!more) asm volatile("cp.async.wait_group 0;" ::: "memory");   // the ring is no longer filled
       __syncwarp();
-      const Part<S, true> part = more ? first_part(warp) : last_part(warp);
+      const Part<D, NH> part = more ? first_part(warp) : last_part(warp);
+      if (!S::kHalves || lc < 2)
 #pragma unroll
-      for (int n = 0; n < kCols; ++n) {
-        if (lc == 0 && lr + 8 * n < NH) {
-          part.most(lr + 8 * n) = most[n];
-          part.total(lr + 8 * n) = sum[n];
+        for (int n = 0; n < kCols; ++n) {
+          const int head = 2 * lc + 8 * n;
+          if (lr == 0) {
+            part.most(head) = make_float2(most[n][0], most[n][1]);
+            part.total(head) = make_float2(sum[n][0], sum[n][1]);
+          }
+#pragma unroll
+          for (int d = 0; d < D / 16; ++d) {
+            part.two(16 * d + (I8 ? 2 * lr : lr), head) = make_float2(acc[d][n][0] * v_ref, acc[d][n][1] * v_ref);
+            part.two(16 * d + (I8 ? 2 * lr + 1 : lr + 8), head) = make_float2(acc[d][n][2] * v_ref, acc[d][n][3] * v_ref);
+          }
         }
-#pragma unroll
-        for (int d = 0; d < D / 16; d += 2) {
-          const int j = d / (S::kEV / 2), e = d % (S::kEV / 2);
-          const int d4 = ((j * 8 + lr) * S::kEV + 2 * e) / 4;
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-            if (!S::kHalves || lc < 2)
-              part.sums(2 * lc + c + 8 * n, d4) = make_float4(acc[d][n][c] * v_ref, acc[d][n][c + 2] * v_ref, acc[d + 1][n][c] * v_ref, acc[d + 1][n][c + 2] * v_ref);
-        }
-      }
       if (lane == 0) s_head[2 * warp + (more ? 0 : 1)] = make_int4(at.b * p.rows_of_seq + at.r, from_start, to_end, 0);
     };
 
@@ -745,14 +739,13 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   }
   __syncthreads();
 
-  // ---- rows that no warp has alone.  Lane i has the i-th part of the CTA (two for each warp, of the rows in order); a warp takes a head of
-  // a row at a time.
+  // ---- rows that no warp has alone.  Lane i has the i-th part of the CTA (two for each warp, of the rows in order); a warp takes 128 sums of
+  // a row at a time, a lane four heads of a channel.
+  constexpr int kSlices = NH * D / 128;
   const int4 own = lane < 2 * S::kWarps ? s_head[lane] : make_int4(-1, 0, 0, 0);
-  const Part<S, true> own_part = lane & 1 ? last_part(lane >> 1) : first_part(lane >> 1);
-  const uint32_t there = __ballot_sync(0xffffffffu, own.x >= 0);
-  int4* const headers = p.headers + 2 * blockIdx.x;
+  auto part_of = [&](int i) { return i & 1 ? last_part(i >> 1) : first_part(i >> 1); };
   int task = 0, crossing0 = -1, crossing1 = -1, ends0 = 0;
-  for (uint32_t rest = there; rest;) {
+  for (uint32_t rest = __ballot_sync(0xffffffffu, own.x >= 0); rest;) {
     const int leader = __ffs(rest) - 1;
     const int row = __shfl_sync(0xffffffffu, own.x, leader);
     const uint32_t parts = __ballot_sync(0xffffffffu, own.x == row);
@@ -760,59 +753,33 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     const int starts = __shfl_sync(0xffffffffu, own.y, leader), ends = __shfl_sync(0xffffffffu, own.z, 31 - __clz(parts));
     if (!starts) crossing0 = row, ends0 = ends;
     else if (!ends) crossing1 = row;
-    const int b = row / p.rows_of_seq;
-    int heads;
-    const int h0 = first_head<S>(p, row - b * p.rows_of_seq, heads);
-    for (int head = 0; head < heads; ++head, ++task) {
+    for (int slice = 0; slice < kSlices; ++slice, ++task) {
       if (task % S::kWarps != warp) continue;
-      const bool mine = own.x == row;
-      const float m = mine ? own_part.most(head) : kNegInf;
-      float most = m;
-#pragma unroll
-      for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-      const float f = weight(m, most);
-      float total_p = mine ? f * own_part.total(head) : 0.f;
-#pragma unroll
-      for (int o = 16; o; o >>= 1) total_p += __shfl_xor_sync(0xffffffffu, total_p, o);
-      for (int d4 = lane; d4 < (D / 4 + 31) / 32 * 32; d4 += 32) {         // (the whole warp goes round)
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (uint32_t of = parts; of;) {
-          float fi[4];
-          float4 v[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {      // (the last one again, with a factor of 0, where there are fewer)
-            const int i = of ? __ffs(of) - 1 : leader;
-            fi[u] = __shfl_sync(0xffffffffu, f, i);
-            if (!of) fi[u] = 0.f;
-            of &= of - 1;
-            v[u] = (i & 1 ? last_part(i >> 1) : first_part(i >> 1)).sums(head, d4 % (D / 4));
-          }
-#pragma unroll
-          for (int u = 0; u < 4; ++u) sum.x += v[u].x * fi[u], sum.y += v[u].y * fi[u], sum.z += v[u].z * fi[u], sum.w += v[u].w * fi[u];
-        }
-        if (d4 >= D / 4) continue;
-        if (!starts || !ends) {
-          Part<S, false>{p.parts + (2ll * blockIdx.x + (starts ? 1 : 0)) * S::kPart}.sums(head, d4) = sum;
-        } else {
-          const float inv = 1.f / total_p;
-          reinterpret_cast<uint2*>(p.out)[((long long)b * p.n_heads + h0 + head) * (D / 4) + d4] =
-              make_uint2(bf16_pair(sum.x * inv, sum.y * inv), bf16_pair(sum.z * inv, sum.w * inv));
-        }
+      const int place = slice * 32 + lane, head = place * 4 % NH, d = place * 4 / NH;
+      float4 top = make_float4(kNegInf, kNegInf, kNegInf, kNegInf), total_p = make_float4(0.f, 0.f, 0.f, 0.f), sums = total_p;
+      for (uint32_t of = parts; of; of &= of - 1) top = larger(top, part_of(__ffs(of) - 1).most4(head));
+#pragma unroll 2
+      for (uint32_t of = parts; of; of &= of - 1) {
+        const Part<D, NH> part = part_of(__ffs(of) - 1);
+        const float4 f = weight(part.most4(head), top);
+        total_p = total_p + f * part.total4(head);
+        sums = sums + f * part.four(place);
       }
-      if (lane == 0) {
-        if (!starts || !ends) {
-          const Part<S, false> part{p.parts + (2ll * blockIdx.x + (starts ? 1 : 0)) * S::kPart};
-          part.most(head) = most;
-          part.total(head) = total_p;
-        } else if (p.lse) {
-          p.lse[(long long)b * p.n_heads + h0 + head] = kLn2 * (most + log2f(total_p));
-        }
+      if (starts && ends) {
+        const int b = row / p.rows_of_seq;
+        int heads;
+        const int h0 = first_head<S>(p, row - b * p.rows_of_seq, heads);
+        put_out<D>(p, (long long)b * p.n_heads + h0, heads, head, d, sums, top, total_p);
+      } else {
+        const Part<D, NH> part{p.parts + (2ll * blockIdx.x + (starts ? 1 : 0)) * S::kPart};
+        part.four(place) = sums;
+        if (d == 0) part.most4(head) = top, part.total4(head) = total_p;
       }
     }
   }
   if (tid == 0) {
-    headers[0] = make_int4(crossing0, ends0, 0, 0);
-    headers[1] = make_int4(crossing1, 0, 0, 0);
+    p.headers[2 * blockIdx.x] = make_int4(crossing0, ends0, 0, 0);
+    p.headers[2 * blockIdx.x + 1] = make_int4(crossing1, 0, 0, 0);
   }
 
   // ---- sequences that are not there have outputs all the same
@@ -830,11 +797,10 @@ constexpr int kMaxCtas = 256;
 template <int D, int NH>
 __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, const int ctas) {
   using S = Shape<D, NH, false, true>;
-  __shared__ float s_weight[NH][kMaxCtas];
-  __shared__ float s_inv[NH];
+  __shared__ __align__(16) float s_weight[kMaxCtas][NH];
+  __shared__ __align__(16) float s_most[NH], s_total[NH];
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int4 own = ptx::behind_wait(p.headers)[2 * blockIdx.x + 1];
-  const int row = own.x;
+  const int row = ptx::behind_wait(p.headers)[2 * blockIdx.x + 1].x;
   if (row < 0) return;
   // parts of the row: the own one, then the first ones of the CTAs behind, up to the one that has the row's end
   int n = 1;
@@ -850,41 +816,38 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, cons
     }
     n += 32;
   }
-  auto part_of = [&](int i) { return Part<S, false>{p.parts + (i == 0 ? 2ll * blockIdx.x + 1 : 2ll * (blockIdx.x + i)) * S::kPart}; };
-  const int b = row / p.rows_of_seq;
-  int heads;
-  const int h0 = first_head<S>(p, row - b * p.rows_of_seq, heads);
-  for (int head = warp; head < heads; head += 8) {
+  auto part_of = [&](int i) { return Part<D, NH>{p.parts + (i == 0 ? 2ll * blockIdx.x + 1 : 2ll * (blockIdx.x + i)) * S::kPart}; };
+  for (int head = warp; head < NH; head += 8) {
+    const int even = head & ~1, odd = head & 1;
     float most = kNegInf;
-    for (int i = lane; i < n; i += 32) most = fmaxf(most, part_of(i).most(head));
+    for (int i = lane; i < n; i += 32) {
+      const float2 m = part_of(i).most(even);
+      most = fmaxf(most, odd ? m.y : m.x);
+    }
 #pragma unroll
     for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
     float total = 0.f;
     for (int i = lane; i < n; i += 32) {
-      const float w = weight(part_of(i).most(head), most);
-      s_weight[head][i] = w;
-      total += w * part_of(i).total(head);
+      const float2 m = part_of(i).most(even), t = part_of(i).total(even);
+      const float w = weight(odd ? m.y : m.x, most);
+      s_weight[i][head] = w;
+      total += w * (odd ? t.y : t.x);
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    if (lane == 0) {
-      s_inv[head] = 1.f / total;
-      if (p.lse) p.lse[(long long)b * p.n_heads + h0 + head] = kLn2 * (most + log2f(total));
-    }
+    if (lane == 0) s_most[head] = most, s_total[head] = total;
   }
   __syncthreads();
-  for (int item = tid; item < heads * (D / 4); item += 256) {
-    const int head = item / (D / 4), d = item % (D / 4) * 4;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int b = row / p.rows_of_seq;
+  int heads;
+  const int h0 = first_head<S>(p, row - b * p.rows_of_seq, heads);
+  for (int place = tid; place < NH * D / 4; place += 256) {
+    const int head = place * 4 % NH, d = place * 4 / NH;
+    float4 sums = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-      const float w = s_weight[head][i];
-      const float4 v = part_of(i).sums(head, d / 4);
-      sum.x += w * v.x, sum.y += w * v.y, sum.z += w * v.z, sum.w += w * v.w;
-    }
-    const float inv = s_inv[head];
-    const long long o = (long long)b * p.n_heads + h0 + head;
-    *reinterpret_cast<uint2*>(p.out + o * D + d) = make_uint2(bf16_pair(sum.x * inv, sum.y * inv), bf16_pair(sum.z * inv, sum.w * inv));
+    for (int i = 0; i < n; ++i) sums = sums + *reinterpret_cast<const float4*>(&s_weight[i][head]) * part_of(i).four(place);
+    put_out<D>(p, (long long)b * p.n_heads + h0, heads, head, d, sums, *reinterpret_cast<const float4*>(&s_most[head]),
+               *reinterpret_cast<const float4*>(&s_total[head]));
   }
 }
 
