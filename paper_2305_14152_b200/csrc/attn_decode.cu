@@ -7,8 +7,9 @@
 // but memory, and the rest is laid out to keep copies in flight:
 //   * A tile is 16 tokens of a row.  Tiles are numbered through all sequences, heads and lengths, and dealt evenly: every CTA
 //     takes an equal run of them, every warp an equal run of its CTA's.  Nothing depends on how uneven the lengths are.
-//   * A warp copies its own tiles into its own ring of shared memory (cp.async, several units of 16 keys or values ahead), whole
-//     tokens at a time, and reads them with ldmatrix as the 16-row operand of the tensor cores' m16n8k16 product, the heads as its 8 columns:
+//   * A warp copies its own tiles into its own ring of shared memory, several units of 16 keys or values ahead (tensor copies, or
+//     cp.async where pages end within tiles), and reads them with ldmatrix as the 16-row operand of the tensor cores' m16n8k16 product, the
+//     heads as its 8 columns:
 //       S^T = K Q^T     K [16 tokens x 16 channels] as it lies, Q in registers
 //       O^T = V^T P^T   V^T [16 channels x 16 tokens] by the transposing ldmatrix; P^T from S^T by movmatrix
 //     So there is no barrier between warps in the loop, and a lane has the factors of the sums that it holds.
@@ -18,10 +19,11 @@
 //   * p goes into the second product as the sum of two 16-bit numbers: with one, its rounding (2^-9 of p) would double the
 //     error variance that the rounding of the output has.  v and q are 16-bit numbers already, and 8-bit codes are exact ones.
 //   * A row that a warp has from its first tile to its last is written out.  Parts of rows are joined within the CTA in shared
-//     memory, and what crosses CTAs by a second kernel, which stands ready when the first ends (launch_after).
+//     memory, and what crosses CTAs by a second kernel, which stands ready when the first ends.
 #include "common.cuh"
 #include "kv_cache.cuh"
 #include "sm100_ptx.cuh"
+#include "tensor_map.cuh"
 
 #include <type_traits>
 
@@ -57,8 +59,8 @@ struct AttnParams {
   int* status;
 };
 
-// Everything that follows from the channels D, the query heads NH of a row, the type of the cache and whether a tile lies in
-// one page (WHOLE: the page size is a multiple of 16).
+// Everything that follows from the channels D, the query heads NH of a row, the type of the cache and whether a tile comes by
+// tensor copies (WHOLE: it lies in one page).
 template <int D_, int NH_, bool I8_, bool WHOLE_>
 struct Shape {
   static constexpr int D = D_, NH = NH_;
@@ -67,6 +69,7 @@ struct Shape {
   static constexpr int kCols = NH > 8 ? 2 : 1;                  // of eight heads (kHalves: of four, twice)
   static constexpr int kBytes = D * (I8 ? 1 : 2);               // of a token
   static constexpr int kPieces = kBytes / 16;                   // 16-byte pieces of a token
+  static constexpr int kLine = kBytes < 128 ? kBytes : 128;     // bytes of a token that lie together in shared memory
   static constexpr int kRows = 32 / kPieces;                    // tokens that a warp copies with one instruction
   static constexpr int kUnit = kTile * kBytes;                  // keys or values of a tile
   static constexpr int kWarps = D > 128 || NH > 8 ? 8 : 16;     // by the registers that a thread needs
@@ -78,8 +81,15 @@ struct Shape {
   static_assert(kFit >= 3 && kRing >= kPart * 4 && kRing % 1024 == 0 && kPart % 4 == 0, "shared memory");
 };
 
-__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, std::integral_constant<int, 16>) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+// A box of 16 tokens from token y on: channels from x on of head `head` in page `page`.
+__device__ __forceinline__ void tensor_copy(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int head, int y, int page) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(head), "r"(y), "r"(page)
+      : "memory");
+}
+__device__ __forceinline__ void bulk_copy_64(uint32_t dst, const void* src, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 64, [%2];" ::"r"(dst), "l"(src), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, uint32_t bytes, std::integral_constant<int, 16>) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -246,21 +256,24 @@ __device__ __forceinline__ void put_out(const AttnParams& p, long long row0, int
 }
 
 // First query head of a row, and how many there are.
-template <typename S>
+template <int NH>
 __device__ __forceinline__ int first_head(const AttnParams& p, int r, int& heads) {
   const int kv = r / p.chunks, chunk = r - kv * p.chunks;
-  heads = min(S::NH, p.group - chunk * S::NH);
-  return kv * p.group + chunk * S::NH;
+  heads = min(NH, p.group - chunk * NH);
+  return kv * p.group + chunk * NH;
 }
 
 template <typename S>
-__global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const AttnParams p) {
+__global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const AttnParams p, const __grid_constant__ CUtensorMap keys,
+                                                                        const __grid_constant__ CUtensorMap values) {
   constexpr int D = S::D, NH = S::NH, kCols = S::kCols, kThreads = S::kWarps * 32;
   constexpr bool I8 = S::I8;
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ int s_scan[kThreads];
   __shared__ int s_warp[S::kWarps];
   __shared__ int4 s_head[2 * S::kWarps];   // of a warp's parts: row (-1: none), begins its row, ends it
+  __shared__ __align__(8) uint64_t s_full[S::WHOLE ? S::kWarps * S::kUnits : 1];
+  __shared__ int s_abort[2];               // as the bounded waits of sm100_ptx.cuh have it
 
   const int tid = threadIdx.x, lane = tid & 31, warp = ptx::warp_index();
   const int lr = lane >> 2, lc = lane & 3;
@@ -269,7 +282,19 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   const auto first_part = [&](int w) { return Part<D, NH>{p.first_parts + ((long long)blockIdx.x * S::kWarps + w) * S::kPart}; };
   const auto last_part = [&](int w) { return Part<D, NH>{reinterpret_cast<float*>(smem + w * S::kRing)}; };
 
+  volatile int* const abort_flag = s_abort;
   if (tid < 2 * S::kWarps) s_head[tid] = make_int4(-1, 0, 0, 0);
+  if constexpr (S::WHOLE) {
+    if (lane < S::kUnits) ptx::mbar_init(ptx::smem_u32(&s_full[warp * S::kUnits + lane]), 1);
+    ptx::fence_mbar_init();
+    if (tid == 0) {
+      s_abort[0] = 0;
+      s_abort[1] = p.status[4];
+      ptx::prefetch_tmap(&keys);
+      ptx::prefetch_tmap(&values);
+    }
+    __syncthreads();
+  }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
@@ -353,89 +378,117 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     uint32_t put = ring, get = ring;         // next unit to fill, and to read
     const uint32_t scales_of = ptx::smem_u32(smem) + S::kWarps * S::kRing + warp * S::kUnits * 64;
     uint32_t put_scales = scales_of, get_scales = scales_of;
-    // Piece c of token t lies in place c ^ (t & 7) (of 64-byte tokens: c ^ (t / 2 & 3)): the eight rows of a matrix, and what eight lanes copy,
-    // are in different banks.
-    auto turn_of = [](int t) { return S::kPieces >= 8 ? t & 7 : t >> 1 & 3; };
-    auto place_of = [&](int t, int c) { return (uint32_t)(t * S::kPieces + (c ^ turn_of(t))) * 16; };
-    const int copy_row = lane / S::kPieces, copy_piece = lane % S::kPieces;
-    const uint32_t copy_to = place_of(copy_row, copy_piece);
+    const uint32_t full_of = ptx::smem_u32(&s_full[S::WHOLE ? warp * S::kUnits : 0]);
+    uint32_t put_full = full_of, get_full = full_of, get_phase = 0;
+    // A token's 16-byte pieces lie in lines of 128 bytes, the lines of the unit's tokens one behind another; piece c of token t in place
+    // c ^ (t & 7) of its line (lines of 64 bytes: c ^ (t / 2 & 3)), as tensor copies mix them: the eight rows of a matrix are in different banks.
+    auto turn_of = [](int t) { return S::kLine == 128 ? t & 7 : t >> 1 & 3; };
+    auto place_of = [&](int t, int c) { return (uint32_t)(c / 8 * kTile * S::kLine + t * S::kLine + ((c & 7) ^ turn_of(t)) * 16); };
     // matrices of keys, and of 8-bit values: tokens 0..7 and 8..15 of a piece, then of the next; of values: two pieces of tokens 0..7, then of 8..15
     const uint32_t key_at = place_of((lane & 7) + (lane & 8), lane >> 4);
     const uint32_t value_at = I8 ? key_at : place_of((lane & 7) + (lane >> 4) * 8, lane >> 3 & 1);
-    auto pair_at = [](uint32_t at, int j) { return (at ^ (S::kPieces >= 8 ? (2 * j & 7) * 16 : 2 * j * 16)) + (S::kPieces > 8 ? j / 4 * 128 : 0); };   // pieces 2 j and 2 j + 1
-    uint32_t unit = 0;                       // place of the copies' tile (WHOLE) or of its token (lane & 15)
-    uint32_t scale = 0;                      // the same in the scales (fewer than 2^30: each has 64 bytes of codes, and they have less than 2^36)
+    auto pair_at = [](uint32_t at, int j) { return (at ^ ((2 * j & 7) * 16)) + j / 4 * kTile * S::kLine; };   // pieces 2 j and 2 j + 1
+    int entry = 0, place = 0;                // of the copies' tile: of the page table, and in the page (WHOLE)
+    uint32_t unit = 0;                       // else place of token (lane & 15) of it in the cache
+    uint32_t scale = 0;                      // and in the scales (fewer than 2^30: each has 64 bytes of codes, and they have less than 2^36)
     int kv = in.r / p.chunks;                // head of keys and values
+    auto table_of = [&](int e) { return ptx::ld_global(p.cache.table + (long long)in.b * p.cache.max_pages + e); };
     // Page of the copies' tile or of its token (lane & 15), asked for a tile ahead of its use.
-    auto look_up = [&](bool there) {
-      const int t = in.t0 + (S::WHOLE ? 0 : lane & 15);
-      page = 0;
-      if (there && (S::WHOLE || (t >= in.span.first && t < in.span.end)))
-        page = ptx::ld_global(p.cache.table + (long long)in.b * p.cache.max_pages + divide(t, p.cache.by_page));
-    };
-    auto in_span = [&](int t) { return t >= in.span.first && t < in.span.end; };
-    // A warp copies whole tokens, 512 bytes an instruction: in pieces of 64 bytes, as the products take keys, the same copies reach 4.9
-    // TB/s of 6.6 (blocks of 4 KB in no order).
-    auto copy_tokens = [&](const void* from, bool all) {
-      const char* const base = static_cast<const char*>(from) + copy_piece * 16;
-      const char* src = base + (uint64_t)(unit + copy_row * p.cache.token16) * 16;
-      const uint64_t step = (uint64_t)p.cache.token16 * (S::kRows * 16);
-#pragma unroll
-      for (int j = 0; j < kTile / S::kRows; ++j) {
-        if constexpr (!S::WHOLE) src = base + (uint64_t)__shfl_sync(0xffffffffu, unit, copy_row + j * S::kRows) * 16;
-        const uint32_t to = ((put + copy_to) ^ (turn_of(j * S::kRows) * 16)) + j * 512;
-        if (all) cp_async(to, src, std::integral_constant<int, 16>());
-        else cp_async(to, src, in_span(in.t0 + copy_row + j * S::kRows) ? 16 : 0, std::integral_constant<int, 16>());
-        if constexpr (S::WHOLE) src += step;
+    auto look_up = [&](bool new_row, bool there) {
+      if constexpr (S::WHOLE) {
+        place += kTile;
+        if (new_row) {
+          entry = divide(in.t0, p.cache.by_page);
+          place = in.t0 - entry * p.cache.page_size;
+          kv = in.r / p.chunks;
+        } else if (place == p.cache.page_size) {
+          ++entry;
+          place = 0;
+        } else {
+          return;                            // the page it has
+        }
+        page = there ? table_of(entry) : 0;
+      } else {
+        if (new_row) kv = in.r / p.chunks;
+        const int t = in.t0 + (lane & 15);
+        page = there && t >= in.span.first && t < in.span.end ? table_of(divide(t, p.cache.by_page)) : 0;
       }
     };
-    auto copy_scales = [&](const float* scales) {
-      if constexpr (I8)
-        if (lane < 16) cp_async(put_scales + lane * 4, scales + scale, in_span(in.t0 + lane) ? 4 : 0, std::integral_constant<int, 4>());
-    };
-    auto copy_keys = [&]() {
-      const int t = in.t0 + (S::WHOLE ? 0 : lane & 15);
-      const uint32_t place = t - divide(t, p.cache.by_page) * p.cache.page_size;
+    auto in_span = [&](int t) { return t >= in.span.first && t < in.span.end; };
+    auto check_page = [&]() {
       if ((uint32_t)page >= (uint32_t)p.cache.n_pages) {
         note_bad_index(p.status);
         page = 0;
       }
-      unit = page * p.cache.page16 + place * p.cache.token16 + kv * p.cache.head16;
-      if constexpr (I8) scale = (page * p.cache.n_kv_heads + kv) * p.cache.page_size + place + (S::WHOLE ? lane & 15 : 0);
-      copy_tokens(p.cache.k, S::WHOLE);   // keys behind a sequence's end have no score, whatever they are, but may be in no page
     };
-    auto copy_values = [&]() {
-      // 0 for what is not seen: its p is 0, and must stay so
-      copy_tokens(p.cache.v, in.t0 >= in.span.first && in.span.end - in.t0 >= kTile);
+    // Keys or values of the tile, by tensor copies: a page has all of them, or places of its own for what is behind the sequence's end.
+    auto copy_whole = [&](const CUtensorMap* map, const float* scales) {
+      ptx::fence_proxy_async_smem();
+      __syncwarp();
+      if (ptx::elect_lane() == 0) {
+        ptx::mbar_arrive_expect_tx(put_full, S::kUnit + (I8 ? 64 : 0));
+#pragma unroll
+        for (int c = 0; c < S::kBytes / S::kLine; ++c)
+          tensor_copy(put + c * kTile * S::kLine, map, put_full, c * (S::kLine / (I8 ? 1 : 2)), kv, place, page);
+        if constexpr (I8) bulk_copy_64(put_scales, scales + (uint32_t)((page * p.cache.n_kv_heads + kv) * p.cache.page_size + place), put_full);
+      }
+      __syncwarp();
+    };
+    // The same where pages end within tiles, token by token: 512 bytes an instruction.  (In pieces of 64 bytes, as the products take keys,
+    // copies of blocks of 4 KB reach 4.9 TB/s of 6.6.)  0 for what is not seen.
+    auto copy_tokens = [&](const void* from, const float* scales) {
+      const int row = lane / S::kPieces, piece = lane % S::kPieces;
+      const char* const base = static_cast<const char*>(from) + piece * 16;
+      const uint32_t to = put + place_of(row, piece);
+#pragma unroll
+      for (int j = 0; j < kTile / S::kRows; ++j)
+        cp_async((to ^ (turn_of(j * S::kRows) * 16)) + j * S::kRows * S::kLine,
+                 base + (uint64_t)__shfl_sync(0xffffffffu, unit, row + j * S::kRows) * 16, in_span(in.t0 + row + j * S::kRows) ? 16 : 0,
+                 std::integral_constant<int, 16>());
+      if constexpr (I8)
+        if (lane < 16) cp_async(put_scales + lane * 4, scales + scale, in_span(in.t0 + lane) ? 4 : 0, std::integral_constant<int, 4>());
     };
     auto filled = [&]() {
-      asm volatile("cp.async.commit_group;" ::: "memory");
-      put += S::kUnit, put_scales += 64;
-      if (put == ring + S::kRing) put = ring, put_scales = scales_of;
+      if constexpr (!S::WHOLE) asm volatile("cp.async.commit_group;" ::: "memory");
+      put += S::kUnit, put_scales += 64, put_full += 8;
+      if (put == ring + S::kRing) put = ring, put_scales = scales_of, put_full = full_of;
     };
     auto issue_keys = [&]() {
       if (issued < count) {
-        copy_keys();
-        copy_scales(p.cache.k_scales);
+        check_page();
+        if constexpr (S::WHOLE) {
+          copy_whole(&keys, p.cache.k_scales);
+        } else {
+          const int t = in.t0 + (lane & 15);
+          const uint32_t at_place = t - divide(t, p.cache.by_page) * p.cache.page_size;
+          unit = page * p.cache.page16 + at_place * p.cache.token16 + kv * p.cache.head16;
+          scale = (page * p.cache.n_kv_heads + kv) * p.cache.page_size + at_place;
+          copy_tokens(p.cache.k, p.cache.k_scales);
+        }
       }
       filled();
     };
     auto issue_values = [&]() {
       if (issued < count) {
-        copy_values();
-        copy_scales(p.cache.v_scales);
-        if (in.next(p)) kv = in.r / p.chunks;
-        look_up(issued + 1 < count);
+        if constexpr (S::WHOLE) copy_whole(&values, p.cache.v_scales);
+        else copy_tokens(p.cache.v, p.cache.v_scales);
+        const bool new_row = in.next(p);
+        look_up(new_row, issued + 1 < count);
       }
       ++issued;
       filled();
     };
-    auto landed = [&]() { asm volatile("cp.async.wait_group %0;" ::"n"(S::kUnits - 2) : "memory"); };
-    auto read = [&]() {
-      get += S::kUnit, get_scales += 64;
-      if (get == ring + S::kRing) get = ring, get_scales = scales_of;
+    bool sound = true;                       // no wait has run out
+    auto landed = [&]() {
+      if constexpr (S::WHOLE) sound = ptx::warp_wait(get_full, get_phase, abort_flag) && sound;
+      else asm volatile("cp.async.wait_group %0;" ::"n"(S::kUnits - 2) : "memory");
+      __syncwarp();                          // for all lanes, and all have read what is filled next
     };
-    look_up(true);
+    auto read = [&]() {
+      get += S::kUnit, get_scales += 64, get_full += 8;
+      if (get == ring + S::kRing) get = ring, get_scales = scales_of, get_full = full_of, get_phase ^= 1;
+    };
+    look_up(true, true);
 #pragma unroll 1
     for (int i = 0; i < S::kUnits / 2; ++i) {
       issue_keys();
@@ -452,7 +505,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
 
     auto begin_row = [&]() {
       int heads;
-      const int h0 = first_head<S>(p, at.r, heads);
+      const int h0 = first_head<NH>(p, at.r, heads);
 #pragma unroll
       for (int n = 0; n < kCols; ++n) {
         const int h = (S::kHalves ? lr & 3 : lr) + 8 * n;
@@ -527,7 +580,6 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     auto add_tile = [&]() {
       const int t0 = at.t0;
       landed();
-      __syncwarp();                          // for all lanes, and all have read what is filled next
       issue_keys();
       // ---- S^T = K Q^T, in two sums, so that a product waits for the one before the last
       float s[2][kCols][4];
@@ -567,7 +619,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
           x[n][i] = y * to_log2[n][i & 1];
         }
       }
-      if (t0 < at.span.first || at.span.end - t0 < kTile) {
+      const bool cut = t0 < at.span.first || at.span.end - t0 < kTile;     // not all of the tile is seen
+      if (cut) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (t0 + lr + 8 * (i >> 1) < at.span.first || t0 + lr + 8 * (i >> 1) >= at.span.end)
@@ -607,10 +660,21 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       // ---- O^T += V^T P^T
       read();
       landed();
-      __syncwarp();
       issue_values();
+      if (S::WHOLE && !I8 && cut) {          // p is 0 there, and must stay so whatever the page has
+        for (int i = lane; i < kTile * S::kPieces; i += 32) {
+          const int t = i / S::kPieces;
+          if (t0 + t < at.span.first || t0 + t >= at.span.end)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(get + place_of(t, i % S::kPieces)), "r"(0u) : "memory");
+        }
+        __syncwarp();
+      }
       if constexpr (I8) {
-        const float v_scale[2] = {lds_float(get_scales + lr * 4), lds_float(get_scales + lr * 4 + 32)};
+        float v_scale[2] = {lds_float(get_scales + lr * 4), lds_float(get_scales + lr * 4 + 32)};
+        if (cut)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (t0 + lr + 8 * i < at.span.first || t0 + lr + 8 * i >= at.span.end) v_scale[i] = 0.f;
         // Values in units of 2^-6 of the largest scale so far, cut to a power of two: p (at most 2^kSlack) times what is left of its
         // token's scale (below 2^7) is a binary16, and as two of them off by 2^-25 of a unit at most, 2^-31 of the largest.
         const uint32_t exponent = __reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(fabsf(v_scale[0]), fabsf(v_scale[1])))) & 0x7f800000u;
@@ -680,7 +744,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
           for (int i = 0; i < 4; ++i) acc[d][0][i] += __shfl_xor_sync(0xffffffffu, acc[d][0][i], 2);
       }
       int heads;
-      const int h0 = first_head<S>(p, at.r, heads);
+      const int h0 = first_head<NH>(p, at.r, heads);
       if (from_start && to_end) {
 #pragma unroll
         for (int n = 0; n < kCols; ++n) {
@@ -729,7 +793,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
 
     bool fresh = true;
 #pragma unroll 1
-    for (int i = 0; i < count; ++i) {
+    for (int i = 0; i < count && sound; ++i) {
       if (fresh) begin_row();
       add_tile();
       fresh = at.left == 1;
@@ -738,6 +802,14 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     }
   }
   __syncthreads();
+  if (S::WHOLE && *abort_flag) {
+    // copies still in flight must land before the shared memory is given back
+    for (int i = 0; i < 64; ++i) __nanosleep(1000);
+    if (tid == 0) {
+      atomicExch(p.status, (int)PEQA_ERR_DEVICE_TIMEOUT);
+      p.status[1] = (int)blockIdx.x;
+    }
+  }
 
   // ---- rows that no warp has alone.  Lane i has the i-th part of the CTA (two for each warp, of the rows in order); a warp takes 128 sums of
   // a row at a time, a lane four heads of a channel.
@@ -768,7 +840,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       if (starts && ends) {
         const int b = row / p.rows_of_seq;
         int heads;
-        const int h0 = first_head<S>(p, row - b * p.rows_of_seq, heads);
+        const int h0 = first_head<NH>(p, row - b * p.rows_of_seq, heads);
         put_out<D>(p, (long long)b * p.n_heads + h0, heads, head, d, sums, top, total_p);
       } else {
         const Part<D, NH> part{p.parts + (2ll * blockIdx.x + (starts ? 1 : 0)) * S::kPart};
@@ -792,13 +864,15 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     }
 }
 
-// Joins the rows that cross CTAs.  CTA i takes the row that begins in CTA i of the kernel before and goes on in the next ones.
+// Joins the rows that cross CTAs.  CTAs (i, .) take the row that begins in CTA i of the kernel before and goes on in the next ones, CTA
+// (i, j) 128 of its sums: a lane four heads of a channel, the warps the parts in turn (one row of 16 heads over all CTAs: by one CTA 50 us).
 constexpr int kMaxCtas = 256;
 template <int D, int NH>
 __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, const int ctas) {
-  using S = Shape<D, NH, false, true>;
+  constexpr int kPart = NH * (D + 2), kWarps = 8;
   __shared__ __align__(16) float s_weight[kMaxCtas][NH];
   __shared__ __align__(16) float s_most[NH], s_total[NH];
+  __shared__ float4 s_sums[kWarps][32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int row = ptx::behind_wait(p.headers)[2 * blockIdx.x + 1].x;
   if (row < 0) return;
@@ -816,8 +890,8 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, cons
     }
     n += 32;
   }
-  auto part_of = [&](int i) { return Part<D, NH>{p.parts + (i == 0 ? 2ll * blockIdx.x + 1 : 2ll * (blockIdx.x + i)) * S::kPart}; };
-  for (int head = warp; head < NH; head += 8) {
+  auto part_of = [&](int i) { return Part<D, NH>{p.parts + (i == 0 ? 2ll * blockIdx.x + 1 : 2ll * (blockIdx.x + i)) * kPart}; };
+  for (int head = warp; head < NH; head += kWarps) {
     const int even = head & ~1, odd = head & 1;
     float most = kNegInf;
     for (int i = lane; i < n; i += 32) {
@@ -837,24 +911,46 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, cons
     for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
     if (lane == 0) s_most[head] = most, s_total[head] = total;
   }
+  const int place = blockIdx.y * 32 + lane, head = place * 4 % NH, d = place * 4 / NH;
   __syncthreads();
+  float4 sums = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int i = warp; i < n; i += kWarps) sums = sums + *reinterpret_cast<const float4*>(&s_weight[i][head]) * part_of(i).four(place);
+  s_sums[warp][lane] = sums;
+  __syncthreads();
+  if (warp > 0) return;
+  for (int w = 1; w < min(n, kWarps); ++w) sums = sums + s_sums[w][lane];
   const int b = row / p.rows_of_seq;
   int heads;
-  const int h0 = first_head<S>(p, row - b * p.rows_of_seq, heads);
-  for (int place = tid; place < NH * D / 4; place += 256) {
-    const int head = place * 4 % NH, d = place * 4 / NH;
-    float4 sums = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) sums = sums + *reinterpret_cast<const float4*>(&s_weight[i][head]) * part_of(i).four(place);
-    put_out<D>(p, (long long)b * p.n_heads + h0, heads, head, d, sums, *reinterpret_cast<const float4*>(&s_most[head]),
-               *reinterpret_cast<const float4*>(&s_total[head]));
-  }
+  const int h0 = first_head<NH>(p, row - b * p.rows_of_seq, heads);
+  put_out<D>(p, (long long)b * p.n_heads + h0, heads, head, d, sums, *reinterpret_cast<const float4*>(&s_most[head]),
+             *reinterpret_cast<const float4*>(&s_total[head]));
 }
 
 int attn_ctas() { return min(sm_count_or(148), kMaxCtas); }
 
 // Query heads of a row of work.
 int heads_of_row(int group, int dim) { return group <= 4 ? 4 : group <= 8 || dim > 128 ? 8 : 16; }
+
+// Keys or values [n_pages, page_size, n_kv_heads, D] in boxes of 16 tokens and a line of their channels.
+template <typename S>
+int tensor_map_of(const CacheView& c, const void* at, CUtensorMap* map) {
+  EncodeTiledFn encode = nullptr;
+  PEQA_TRY(tensor_map_encoder(&encode));
+  // (the stride of a dimension of one says nothing, and 0 is none)
+  auto bytes = [](uint32_t stride16) { return stride16 ? (cuuint64_t)stride16 * 16 : (cuuint64_t)16; };
+  const cuuint64_t dims[4] = {(cuuint64_t)S::D, (cuuint64_t)c.n_kv_heads, (cuuint64_t)c.page_size, (cuuint64_t)c.n_pages};
+  const cuuint64_t strides[3] = {bytes(c.head16), bytes(c.token16), bytes(c.page16)};
+  const cuuint32_t box[4] = {(cuuint32_t)(S::kLine / (S::I8 ? 1 : 2)), 1, kTile, 1}, steps[4] = {1, 1, 1, 1};
+  if (encode(map, S::I8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(at), dims, strides, box, steps,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, S::kLine == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+             // no more than a head has of a token: what lies beside it may be another head's
+             S::kBytes >= 256 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B
+                              : S::kBytes == 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_64B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return cuda_fail(cudaErrorInvalidValue);
+  return PEQA_OK;
+}
 
 template <int D, int NH, bool I8, bool WHOLE>
 int launch(const AttnParams& p, cudaStream_t st) {
@@ -872,13 +968,25 @@ int launch(const AttnParams& p, cudaStream_t st) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  PEQA_CUDA(cudaLaunchKernelEx(&cfg, attn_decode_kernel<S>, p));
-  return launch_after(attn_join_kernel<D, NH>, ctas, 256, st, p, ctas);
+  CUtensorMap keys = {}, values = {};
+  if constexpr (WHOLE) {
+    PEQA_TRY(tensor_map_of<S>(p.cache, p.cache.k, &keys));
+    PEQA_TRY(tensor_map_of<S>(p.cache, p.cache.v, &values));
+  }
+  PEQA_CUDA(cudaLaunchKernelEx(&cfg, attn_decode_kernel<S>, p, keys, values));
+  cfg.gridDim = dim3(ctas, NH * D / 128, 1);
+  cfg.blockDim = dim3(256, 1, 1);
+  cfg.dynamicSmemBytes = 0;
+  PEQA_CUDA(cudaLaunchKernelEx(&cfg, attn_join_kernel<D, NH>, p, ctas));
+  return PEQA_OK;
 }
 
 template <int D, int NH>
 int launch_type(const AttnParams& p, bool codes, cudaStream_t st) {
-  const bool whole = p.cache.page_size % kTile == 0;
+  // Tensor copies take fewer instructions than copies token by token, which the clock feels where the power limit holds it: 64 sequences of up to
+  // 8190 tokens in 8 bits 138 -> 123 us.  But lines of 128 bytes that lie apart come slower by them: 4 sequences of up to 32003, all
+  // heads of a token together, 286 -> 355 us; 16 of up to 8000, heads of 64 channels in bf16, 134 -> 192 us.
+  const bool whole = p.cache.page_size % kTile == 0 && (D * (codes ? 1 : 2) >= 256 || p.cache.token16 == D * (codes ? 1 : 2) / 16);
   if (codes) return whole ? launch<D, NH, true, true>(p, st) : launch<D, NH, true, false>(p, st);
   return whole ? launch<D, NH, false, true>(p, st) : launch<D, NH, false, false>(p, st);
 }

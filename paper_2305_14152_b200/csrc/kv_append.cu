@@ -22,9 +22,7 @@ int check_kv_cache(const peqa_kv_cache_t* c, CacheView* view) {
   if (c->n_pages < 1 || c->page_size < 1 || c->n_kv_heads < 1 || c->n_seqs < 1 || c->max_pages < 1) return PEQA_ERR_BAD_SHAPE;
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return PEQA_ERR_BAD_SHAPE;
   if (!aligned16(c->k) || !aligned16(c->v)) return PEQA_ERR_ALIGNMENT;
-  if ((reinterpret_cast<uintptr_t>(c->page_table) | reinterpret_cast<uintptr_t>(c->k_scales) |
-       reinterpret_cast<uintptr_t>(c->v_scales)) & 3u)
-    return PEQA_ERR_ALIGNMENT;
+  if (!aligned16(c->k_scales) || !aligned16(c->v_scales) || (reinterpret_cast<uintptr_t>(c->page_table) & 3u)) return PEQA_ERR_ALIGNMENT;
   if ((long long)c->max_pages * c->page_size > 0x7fffffffll) return PEQA_ERR_TOO_LARGE;
   // the three outer dimensions from the nearest to the furthest: each steps over all that lies within
   struct Dim {
