@@ -4,8 +4,7 @@
 //
 // Bound by memory: each row of a head is read once and written once.  head_dim / 16 adjacent lanes take a head of a token, 16 channels
 // each, in two pieces of 16 bytes that hold whole pairs: channels 8 i and R/2 + 8 i on (pairs a half apart), or
-// 16 i on (adjacent pairs, channels behind R, values).  What a row needs of its token, its place in the cache and its
-// angles, is found while the rows themselves are on their way.
+// 16 i on (adjacent pairs, channels behind R, values).
 #include "common.cuh"
 #include "kv_cache.cuh"
 #include "sm100_ptx.cuh"
@@ -85,6 +84,7 @@ int check_rows(const peqa_rows_t* r, int rows, int heads, int dim, bool written)
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kBatch = 8;              // tokens whose places are resolved together
 
 struct Rows {
   uint16_t* data;
@@ -94,7 +94,7 @@ struct Rows {
 struct AppendParams {
   CacheView cache;
   Rows q, k, v, q_out;
-  int n_heads, rotary;               // query heads (0: none); channels that turn
+  int n_tokens, n_heads, rotary;     // query heads (0: none); channels that turn
   bool interleaved;
   const float* cos_sin;
   int n_positions;
@@ -133,79 +133,136 @@ __device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
   a = y;
 }
 
+// Codes of a lane's 16 channels, rint(y / step) of the IEEE quotient.  Values of half the largest are frequent among 16-bit numbers, and
+// their quotient, 63.5, lies between two codes: it has to be the quotient to the last bit.  By Markstein's theorem (IBM J. Res. Dev. 34, 1990): with
+// inv the reciprocal rounded to nearest and q one of the two numbers next to y / step, the remainder r = y - q step is exact, and q + r inv
+// rounded once is the quotient rounded to nearest.  The product y inv is off by less than two units in the last place; once
+// corrected in the same way by less than one, as the theorem wants it, twice it is the quotient.  (Exponents far from the ends of their range;
+// quotients that are far below 1/2 may be off and round to 0 all the same.)
+__device__ __forceinline__ void encode(const float (&a)[8], const float (&z)[8], float step, uint32_t (&codes)[4]) {
+  constexpr float kMagic = 12582912.f;                         // 1.5 * 2^23: the sum's lowest bits are the rounded number
+  if (step > 0x1p-100f && step < 0x1p100f) {
+    const float inv = __frcp_rn(step);
+    auto rounded = [&](float y) {
+      float q = __fmul_rn(y, inv);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) q = __fmaf_rn(__fmaf_rn(-q, step, y), inv, q);
+      return __float_as_uint(__fadd_rn(q, kMagic));
+    };
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float* y = k < 2 ? a + 4 * k : z + 4 * (k - 2);
+      const uint32_t lo = __byte_perm(rounded(y[0]), rounded(y[1]), 0x0040), hi = __byte_perm(rounded(y[2]), rounded(y[3]), 0x0040);
+      codes[k] = __byte_perm(lo, hi, 0x5410);
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    codes[k] = 0;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const float q = __fdiv_rn(k < 2 ? a[4 * k + m] : z[4 * (k - 2) + m], step);
+      codes[k] |= (uint32_t)(min(max(__float2int_rn(q), -127), 127) & 0xff) << (8 * m);
+    }
+  }
+}
+
+// The CTAs take equal runs of items: the heads of a token that one takes at once, of the tokens in order.  Each resolves the places of its
+// next kBatch tokens at a time, and copies their angles to shared memory; the rows of the next item are asked for before those of the
+// item at hand are used.  One CTA for every item, its chain of dependent reads (bounds of the sequences, length, page) before it,
+// took 79 us for 4096 tokens of 192 rows of 128, and 44 us for 2048 of 96 rows into 8 bits.
 template <int D, bool I8>
-__global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(kThreads, 4) kv_append_kernel(const AppendParams p) {
   constexpr int kLanes = D / 16, kRows = kThreads / kLanes;    // of a head of a token; heads that a CTA takes at once
-  constexpr int kAtOnce = 2;                                   // heads of a thread whose loads are in flight together
-  __shared__ int s_seq;
+  __shared__ int s_seq[kBatch];
+  __shared__ int s_page[kBatch], s_place[kBatch];              // of a token's place; page -1: it has none; place -1: it is left out
+  __shared__ __align__(16) float s_angles[kBatch][D];
   const int tid = threadIdx.x, i = tid % kLanes;
-  const int t = blockIdx.x;
-  const int kv_heads = p.cache.n_kv_heads, rows = p.n_heads + 2 * kv_heads;
+  const int kv_heads = p.cache.n_kv_heads, rows = p.n_heads + 2 * kv_heads, passes = (rows + kRows - 1) / kRows;
   const bool turns = 16 * i < p.rotary;
   const bool apart = turns && !p.interleaved;
   const int d0 = apart ? 8 * i : 16 * i, d1 = apart ? p.rotary / 2 + 8 * i : 16 * i + 8;
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
-  uint4 x0[kAtOnce], x1[kAtOnce];
-  auto load = [&](int first) {
-#pragma unroll
-    for (int e = 0; e < kAtOnce; ++e) {
-      const int r = first + e * gridDim.y * kRows;
-      x0[e] = x1[e] = make_uint4(0, 0, 0, 0);
-      if (r >= rows) continue;
-      const bool is_q = r < p.n_heads, is_k = !is_q && r < p.n_heads + kv_heads;
-      const Rows& from = is_q ? p.q : is_k ? p.k : p.v;
-      const int h = is_q ? r : is_k ? r - p.n_heads : r - p.n_heads - kv_heads;
-      const uint16_t* x = from.data + t * from.row + h * from.head;
-      const bool value = !is_q && !is_k;                       // not turned: its 16 channels lie side by side
-      x0[e] = ptx::ld_global(reinterpret_cast<const uint4*>(x + (value ? 16 * i : d0)));
-      x1[e] = ptx::ld_global(reinterpret_cast<const uint4*>(x + (value ? 16 * i + 8 : d1)));
-    }
-  };
-  int r0 = blockIdx.y * kRows + tid / kLanes;
-  load(r0);
+  const long long items = (long long)p.n_tokens * passes;
+  const long long first = items * blockIdx.x / gridDim.x, end = items * (blockIdx.x + 1) / gridDim.x;
+  int left = (int)(end - first), t = (int)(first / passes), pass = (int)(first - (long long)t * passes);
+  if (left == 0) return;
+  const int last = (int)((end - 1) / passes);                  // token
 
-  // ---- the token's sequence and position
-  int b = t, position;
-  if (p.starts) {
-    if (tid == 0) s_seq = -1;
-    __syncthreads();
-    for (int k = tid; k < p.cache.n_seqs; k += kThreads)
-      if (ptx::ld_global(p.starts + k) <= t && t < ptx::ld_global(p.starts + k + 1)) s_seq = k;
-    __syncthreads();
-    b = s_seq;
-    if (b < 0) return;
-  }
-  const int len = ptx::ld_global(p.seq_lens + b);
-  if (len == 0) return;
-  position = p.starts ? len - ptx::ld_global(p.starts + b + 1) + t : len - 1;
-  if (len < 0 || len > p.cache.capacity || position < 0 || position >= p.n_positions) {
-    if (tid == 0) note_bad_index(p.status);
-    return;
-  }
-  const int entry = divide(position, p.cache.by_page);
-  const int page = ptx::ld_global(p.cache.table + (long long)b * p.cache.max_pages + entry);
-  const int place = position - entry * p.cache.page_size;
-  const bool there = (uint32_t)page < (uint32_t)p.cache.n_pages;
-  if (!there && tid == 0) note_bad_index(p.status);
-  float c[8], s[8];
-  if (turns) {
-    const float* at = p.cos_sin + (long long)position * p.rotary + 8 * i;
-    *reinterpret_cast<float4*>(c) = ptx::ld_global(reinterpret_cast<const float4*>(at));
-    *reinterpret_cast<float4*>(c + 4) = ptx::ld_global(reinterpret_cast<const float4*>(at + 4));
-    *reinterpret_cast<float4*>(s) = ptx::ld_global(reinterpret_cast<const float4*>(at + p.rotary / 2));
-    *reinterpret_cast<float4*>(s + 4) = ptx::ld_global(reinterpret_cast<const float4*>(at + p.rotary / 2 + 4));
-  }
+  uint4 x0, x1;
+  auto load = [&](int token, int of_pass) {
+    const int r = of_pass * kRows + tid / kLanes;
+    x0 = x1 = make_uint4(0, 0, 0, 0);
+    if (r >= rows) return;
+    const bool is_q = r < p.n_heads, is_k = !is_q && r < p.n_heads + kv_heads;
+    const Rows& from = is_q ? p.q : is_k ? p.k : p.v;
+    const uint16_t* x = from.data + token * from.row + (is_q ? r : is_k ? r - p.n_heads : r - p.n_heads - kv_heads) * from.head;
+    const bool value = !is_q && !is_k;                         // not turned: its 16 channels lie side by side
+    x0 = ptx::ld_global(reinterpret_cast<const uint4*>(x + (value ? 16 * i : d0)));
+    x1 = ptx::ld_global(reinterpret_cast<const uint4*>(x + (value ? 16 * i + 8 : d1)));
+  };
+  load(t, pass);
 
   while (true) {
-#pragma unroll
-    for (int e = 0; e < kAtOnce; ++e) {
-      const int r = r0 + e * gridDim.y * kRows;
+    // ---- the places of the next tokens
+    const int t0 = t, n = min(kBatch, last + 1 - t0);
+    if (p.starts) {
+      if (tid < kBatch) s_seq[tid] = -1;
+      __syncthreads();
+      for (int k = tid; k < p.cache.n_seqs; k += kThreads) {
+        const int from = max(ptx::ld_global(p.starts + k), t0), to = min(ptx::ld_global(p.starts + k + 1), t0 + n);
+        for (int e = from; e < to; ++e) s_seq[e - t0] = k;
+      }
+      __syncthreads();
+    }
+    if (tid < n) {
+      const int b = p.starts ? s_seq[tid] : t0 + tid;
+      int page = -1, place = -1, position = 0;
+      const int len = b < 0 ? 0 : ptx::ld_global(p.seq_lens + b);
+      if (len != 0) {
+        position = p.starts ? len - ptx::ld_global(p.starts + b + 1) + t0 + tid : len - 1;
+        if (len < 0 || len > p.cache.capacity || position < 0 || position >= p.n_positions) {
+          note_bad_index(p.status);
+          position = 0;
+        } else {
+          const int entry = divide(position, p.cache.by_page);
+          place = position - entry * p.cache.page_size;
+          page = ptx::ld_global(p.cache.table + (long long)b * p.cache.max_pages + entry);
+          if ((uint32_t)page >= (uint32_t)p.cache.n_pages) {
+            note_bad_index(p.status);
+            page = -1;
+          }
+        }
+      }
+      s_page[tid] = page, s_place[tid] = place;
+      s_seq[tid] = position;
+    }
+    __syncthreads();
+    for (int k = tid; k < n * (p.rotary / 4); k += kThreads) {
+      const int token = k / (p.rotary / 4), e = k % (p.rotary / 4);
+      reinterpret_cast<float4*>(s_angles[token])[e] =
+          ptx::ld_global(reinterpret_cast<const float4*>(p.cos_sin + (long long)s_seq[token] * p.rotary) + e);
+    }
+    __syncthreads();
+
+    while (true) {
+      const int r = pass * kRows + tid / kLanes, at = t - t0;
+      const int page = s_page[at], place = s_place[at];
       const bool is_q = r < p.n_heads, is_k = !is_q && r < p.n_heads + kv_heads;
+      const int h = is_q ? r : is_k ? r - p.n_heads : r - p.n_heads - kv_heads, token = t;
       float a[8], z[8];
-      widen(x0[e], a);
-      widen(x1[e], z);
-      if (turns && (is_q || is_k)) {
+      widen(x0, a);
+      widen(x1, z);
+      if (++pass == passes) pass = 0, ++t;
+      if (--left > 0) load(t, pass);
+      if (turns && r < p.n_heads + kv_heads) {
+        float c[8], s[8];
+        const float4* angles = reinterpret_cast<const float4*>(&s_angles[at][8 * i]);
+        *reinterpret_cast<float4*>(c) = angles[0], *reinterpret_cast<float4*>(c + 4) = angles[1];
+        angles = reinterpret_cast<const float4*>(&s_angles[at][p.rotary / 2 + 8 * i]);
+        *reinterpret_cast<float4*>(s) = angles[0], *reinterpret_cast<float4*>(s + 4) = angles[1];
         if (p.interleaved) {
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -218,60 +275,46 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams 
         }
       }
       const int e0 = is_q || is_k ? d0 : 16 * i, e1 = is_q || is_k ? d1 : 16 * i + 8;
-      if constexpr (I8) {
+      const uint64_t unit = (uint64_t)(uint32_t)page * p.cache.page16 + (uint64_t)(uint32_t)place * p.cache.token16 + (uint64_t)(uint32_t)h * p.cache.head16;
+      if (I8 && __any_sync(0xffffffffu, !is_q)) {
         // the largest of the head, over the lanes that have it (all lanes of the warp take part)
         float most = 0.f;
 #pragma unroll
         for (int k = 0; k < 8; ++k) most = larger(most, larger(fabsf(a[k]), fabsf(z[k])));
 #pragma unroll
         for (int o = 1; o < kLanes; o <<= 1) most = larger(most, __shfl_xor_sync(0xffffffffu, most, o));
-        if (r >= p.n_heads && r < rows && there) {
-          const int h = is_k ? r - p.n_heads : r - p.n_heads - kv_heads;
+        if (!is_q && r < rows && page >= 0) {
           const float step = most == 0.f ? 1.f : __fdiv_rn(most, 127.f);
           uint32_t codes[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            uint32_t word = 0;
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-              const float y = k < 2 ? a[4 * k + m] : z[4 * (k - 2) + m];
-              const int code = min(max(__float2int_rn(__fdiv_rn(y, step)), -127), 127);
-              word |= (uint32_t)(code & 0xff) << (8 * m);
-            }
-            codes[k] = word;
-          }
-          int8_t* to = static_cast<int8_t*>(const_cast<void*>(is_k ? p.cache.k : p.cache.v)) +
-                       ((uint64_t)page * p.cache.page16 + (uint64_t)place * p.cache.token16 + (uint64_t)h * p.cache.head16) * 16;
+          encode(a, z, step, codes);
+          int8_t* to = static_cast<int8_t*>(const_cast<void*>(is_k ? p.cache.k : p.cache.v)) + unit * 16;
           *reinterpret_cast<uint2*>(to + e0) = make_uint2(codes[0], codes[1]);
           *reinterpret_cast<uint2*>(to + e1) = make_uint2(codes[2], codes[3]);
           if (i == 0)
             const_cast<float*>(is_k ? p.cache.k_scales : p.cache.v_scales)[((long long)page * kv_heads + h) * p.cache.page_size + place] = step;
         }
       }
-      if (r < rows && (is_q || (!I8 && there))) {
-        const int h = is_q ? r : is_k ? r - p.n_heads : r - p.n_heads - kv_heads;
-        uint16_t* to = is_q ? p.q_out.data + t * p.q_out.row + h * p.q_out.head
-                            : static_cast<uint16_t*>(const_cast<void*>(is_k ? p.cache.k : p.cache.v)) +
-                                  ((uint64_t)page * p.cache.page16 + (uint64_t)place * p.cache.token16 + (uint64_t)h * p.cache.head16) * 8;
+      if (r < rows && (is_q ? place >= 0 : !I8 && page >= 0)) {
+        uint16_t* to = is_q ? p.q_out.data + token * p.q_out.row + h * p.q_out.head
+                            : static_cast<uint16_t*>(const_cast<void*>(is_k ? p.cache.k : p.cache.v)) + unit * 8;
         *reinterpret_cast<uint4*>(to + e0) = narrow(a);
         *reinterpret_cast<uint4*>(to + e1) = narrow(z);
       }
+      if (left == 0) return;
+      if (t == t0 + n) break;
     }
-    // (the whole CTA goes on together)
-    r0 += kAtOnce * gridDim.y * kRows;
-    if (r0 - tid / kLanes >= rows) return;
-    load(r0);
+    __syncthreads();                                           // the places and angles have been read
   }
 }
 
 template <int D, bool I8>
-int launch(const AppendParams& p, int n_tokens, cudaStream_t st) {
+int launch(const AppendParams& p, cudaStream_t st) {
   constexpr int kRows = kThreads / (D / 16);
   const int rows = p.n_heads + 2 * p.cache.n_kv_heads, passes = (rows + kRows - 1) / kRows;
-  // a CTA for every so many heads where there are few tokens, for every token where there are many
-  const int split = n_tokens * (long long)passes <= 4 * sm_count_or(148) ? passes : (passes + 1) / 2;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(n_tokens, min(split, 65535), 1);
+  // As many CTAs as can be at once; or one for each item, if that is not much more: 512 tokens of 96 rows 12.6 us and 10.3.
+  const long long items = (long long)p.n_tokens * passes, sms = sm_count_or(148);
+  cfg.gridDim = dim3((unsigned)(items <= 12 * sms ? items : 4 * sms), 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -284,11 +327,11 @@ int launch(const AppendParams& p, int n_tokens, cudaStream_t st) {
 }
 
 template <bool I8>
-int launch_dim(const AppendParams& p, int dim, int n_tokens, cudaStream_t st) {
+int launch_dim(const AppendParams& p, int dim, cudaStream_t st) {
   switch (dim) {
-    case 64: return launch<64, I8>(p, n_tokens, st);
-    case 128: return launch<128, I8>(p, n_tokens, st);
-    default: return launch<256, I8>(p, n_tokens, st);
+    case 64: return launch<64, I8>(p, st);
+    case 128: return launch<128, I8>(p, st);
+    default: return launch<256, I8>(p, st);
   }
 }
 
@@ -326,6 +369,7 @@ extern "C" int peqa_kv_append(const peqa_kv_cache_t* c, const peqa_rows_t* q, in
   PEQA_TRY(check_arch());
   p.k = rows_of(k, n_tokens, c->n_kv_heads);
   p.v = rows_of(v, n_tokens, c->n_kv_heads);
+  p.n_tokens = n_tokens;
   p.rotary = rotary_dim;
   p.interleaved = interleaved != 0;
   p.cos_sin = cos_sin;
@@ -334,5 +378,5 @@ extern "C" int peqa_kv_append(const peqa_kv_cache_t* c, const peqa_rows_t* q, in
   p.starts = starts;
   cudaStream_t st = as_stream(stream);
   PEQA_TRY(status_word(st, &p.status));
-  return c->type == PEQA_KV_INT8 ? launch_dim<true>(p, c->head_dim, n_tokens, st) : launch_dim<false>(p, c->head_dim, n_tokens, st);
+  return c->type == PEQA_KV_INT8 ? launch_dim<true>(p, c->head_dim, st) : launch_dim<false>(p, c->head_dim, st);
 }
