@@ -84,11 +84,11 @@ int check_rows(const peqa_rows_t* r, int rows, int heads, int dim, bool written)
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBatch = 8;              // tokens whose places are resolved together
+constexpr int kBatch = 16;             // tokens whose places are resolved together
 
 struct Rows {
   uint16_t* data;
-  long long row, head;
+  uint32_t row, head;                // strides in elements
 };
 
 struct AppendParams {
@@ -168,142 +168,140 @@ __device__ __forceinline__ void encode(const float (&a)[8], const float (&z)[8],
   }
 }
 
-// The CTAs take equal runs of items: the heads of a token that one takes at once, of the tokens in order.  Each resolves the places of its
-// next kBatch tokens at a time, and copies their angles to shared memory; the rows of the next item are asked for before those of the
-// item at hand are used.  One CTA for every item, its chain of dependent reads (bounds of the sequences, length, page) before it,
-// took 79 us for 4096 tokens of 192 rows of 128, and 44 us for 2048 of 96 rows into 8 bits.
+// An item is the heads of a token that a CTA takes at once (a pass over its heads has several); items are numbered through the tokens, then the
+// passes, and the CTAs take equal runs.  So a thread has the same head of one token after another: where it reads and writes moves by a
+// stride.  A CTA resolves the places of its next kBatch tokens together and copies their angles to shared memory; the row of the next token is
+// asked for before the one at hand is used.  With one CTA for every item, the chain of dependent reads (bounds of the sequences,
+// length, page) before each, 4096 tokens of 192 rows of 128 took 79 us, and 2048 of 96 into 8 bits 34 us.
 template <int D, bool I8>
 __global__ void __launch_bounds__(kThreads, 4) kv_append_kernel(const AppendParams p) {
   constexpr int kLanes = D / 16, kRows = kThreads / kLanes;    // of a head of a token; heads that a CTA takes at once
   __shared__ int s_seq[kBatch];
-  __shared__ int s_page[kBatch], s_place[kBatch];              // of a token's place; page -1: it has none; place -1: it is left out
+  __shared__ int s_state[kBatch];                              // of a token: 0 left out, 1 its place is in no page, 2 it has one
+  __shared__ uint32_t s_unit[kBatch], s_scale[kBatch];         // its place in the cache, in units of 16 bytes, and in the scales
   __shared__ __align__(16) float s_angles[kBatch][D];
   const int tid = threadIdx.x, i = tid % kLanes;
   const int kv_heads = p.cache.n_kv_heads, rows = p.n_heads + 2 * kv_heads, passes = (rows + kRows - 1) / kRows;
-  const bool turns = 16 * i < p.rotary;
-  const bool apart = turns && !p.interleaved;
-  const int d0 = apart ? 8 * i : 16 * i, d1 = apart ? p.rotary / 2 + 8 * i : 16 * i + 8;
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
   const long long items = (long long)p.n_tokens * passes;
   const long long first = items * blockIdx.x / gridDim.x, end = items * (blockIdx.x + 1) / gridDim.x;
-  int left = (int)(end - first), t = (int)(first / passes), pass = (int)(first - (long long)t * passes);
-  if (left == 0) return;
-  const int last = (int)((end - 1) / passes);                  // token
+  int left = (int)(end - first), pass = (int)(first / p.n_tokens), t = (int)(first - (long long)pass * p.n_tokens);
 
-  uint4 x0, x1;
-  auto load = [&](int token, int of_pass) {
-    const int r = of_pass * kRows + tid / kLanes;
-    x0 = x1 = make_uint4(0, 0, 0, 0);
-    if (r >= rows) return;
-    const bool is_q = r < p.n_heads, is_k = !is_q && r < p.n_heads + kv_heads;
-    const Rows& from = is_q ? p.q : is_k ? p.k : p.v;
-    const uint16_t* x = from.data + token * from.row + (is_q ? r : is_k ? r - p.n_heads : r - p.n_heads - kv_heads) * from.head;
-    const bool value = !is_q && !is_k;                         // not turned: its 16 channels lie side by side
-    x0 = ptx::ld_global(reinterpret_cast<const uint4*>(x + (value ? 16 * i : d0)));
-    x1 = ptx::ld_global(reinterpret_cast<const uint4*>(x + (value ? 16 * i + 8 : d1)));
-  };
-  load(t, pass);
+  for (; left > 0; ++pass, t = 0) {
+    // ---- this thread's head in this pass
+    const int r = pass * kRows + tid / kLanes;
+    const bool there = r < rows, is_q = r < p.n_heads, is_k = !is_q && r < p.n_heads + kv_heads;
+    const uint32_t h = is_q ? r : is_k ? r - p.n_heads : r - p.n_heads - kv_heads;
+    const Rows from = is_q ? p.q : is_k ? p.k : p.v;
+    const bool turns = (is_q || is_k) && 16 * i < p.rotary, apart = turns && !p.interleaved;
+    // its 16 channels, in bytes: two pieces of whole pairs
+    const uint32_t at0 = apart ? 16 * i : 32 * i, at1 = apart ? p.rotary + 16 * i : 32 * i + 16;
+    const char* src = reinterpret_cast<const char*>(from.data + (uint64_t)(uint32_t)t * from.row + (uint64_t)h * from.head);
+    const uint64_t step_in = (uint64_t)from.row * 2;
+    char* to_q = reinterpret_cast<char*>(p.q_out.data + (uint64_t)(uint32_t)t * p.q_out.row + (uint64_t)h * p.q_out.head);
+    char* const to_cache = static_cast<char*>(const_cast<void*>(is_k ? p.cache.k : p.cache.v)) + (uint64_t)(h * p.cache.head16) * 16;
+    uint4 x0 = make_uint4(0, 0, 0, 0), x1 = x0;
+    auto load = [&]() {
+      if (!there) return;
+      x0 = ptx::ld_global(reinterpret_cast<const uint4*>(src + at0));
+      x1 = ptx::ld_global(reinterpret_cast<const uint4*>(src + at1));
+      src += step_in;
+    };
+    load();
 
-  while (true) {
-    // ---- the places of the next tokens
-    const int t0 = t, n = min(kBatch, last + 1 - t0);
-    if (p.starts) {
-      if (tid < kBatch) s_seq[tid] = -1;
-      __syncthreads();
-      for (int k = tid; k < p.cache.n_seqs; k += kThreads) {
-        const int from = max(ptx::ld_global(p.starts + k), t0), to = min(ptx::ld_global(p.starts + k + 1), t0 + n);
-        for (int e = from; e < to; ++e) s_seq[e - t0] = k;
+    for (int tokens = min(left, p.n_tokens - t); tokens > 0;) {
+      // ---- the places of the next tokens
+      const int n = min(kBatch, tokens);
+      __syncthreads();                                         // those of the ones before have been read
+      if (p.starts) {
+        if (tid < kBatch) s_seq[tid] = -1;
+        __syncthreads();
+        for (int k = tid; k < p.cache.n_seqs; k += kThreads) {
+          const int lo = max(ptx::ld_global(p.starts + k), t), hi = min(ptx::ld_global(p.starts + k + 1), t + n);
+          for (int e = lo; e < hi; ++e) s_seq[e - t] = k;
+        }
+        __syncthreads();
       }
-      __syncthreads();
-    }
-    if (tid < n) {
-      const int b = p.starts ? s_seq[tid] : t0 + tid;
-      int page = -1, place = -1, position = 0;
-      const int len = b < 0 ? 0 : ptx::ld_global(p.seq_lens + b);
-      if (len != 0) {
-        position = p.starts ? len - ptx::ld_global(p.starts + b + 1) + t0 + tid : len - 1;
-        if (len < 0 || len > p.cache.capacity || position < 0 || position >= p.n_positions) {
-          note_bad_index(p.status);
-          position = 0;
-        } else {
-          const int entry = divide(position, p.cache.by_page);
-          place = position - entry * p.cache.page_size;
-          page = ptx::ld_global(p.cache.table + (long long)b * p.cache.max_pages + entry);
-          if ((uint32_t)page >= (uint32_t)p.cache.n_pages) {
+      if (tid < n) {
+        const int b = p.starts ? s_seq[tid] : t + tid;
+        int state = 0, position = 0;
+        const int len = b < 0 ? 0 : ptx::ld_global(p.seq_lens + b);
+        if (len != 0) {
+          position = p.starts ? len - ptx::ld_global(p.starts + b + 1) + t + tid : len - 1;
+          if (len < 0 || len > p.cache.capacity || position < 0 || position >= p.n_positions) {
             note_bad_index(p.status);
-            page = -1;
+            position = 0;
+          } else {
+            const uint32_t entry = divide(position, p.cache.by_page), place = position - entry * p.cache.page_size;
+            const uint32_t page = (uint32_t)ptx::ld_global(p.cache.table + (long long)b * p.cache.max_pages + entry);
+            state = page < (uint32_t)p.cache.n_pages ? 2 : 1;
+            if (state == 1) note_bad_index(p.status);
+            s_unit[tid] = page * p.cache.page16 + place * p.cache.token16;
+            s_scale[tid] = page * (uint32_t)kv_heads * p.cache.page_size + place;   // (fewer than 2^30: the codes have less than 2^36 bytes)
           }
         }
+        s_state[tid] = state;
+        s_seq[tid] = position;
       }
-      s_page[tid] = page, s_place[tid] = place;
-      s_seq[tid] = position;
-    }
-    __syncthreads();
-    for (int k = tid; k < n * (p.rotary / 4); k += kThreads) {
-      const int token = k / (p.rotary / 4), e = k % (p.rotary / 4);
-      reinterpret_cast<float4*>(s_angles[token])[e] =
-          ptx::ld_global(reinterpret_cast<const float4*>(p.cos_sin + (long long)s_seq[token] * p.rotary) + e);
-    }
-    __syncthreads();
+      __syncthreads();
+      for (int k = tid; k < n * (p.rotary / 4); k += kThreads) {
+        const int token = k / (p.rotary / 4), e = k % (p.rotary / 4);
+        reinterpret_cast<float4*>(s_angles[token])[e] =
+            ptx::ld_global(reinterpret_cast<const float4*>(p.cos_sin + (long long)s_seq[token] * p.rotary) + e);
+      }
+      __syncthreads();
 
-    while (true) {
-      const int r = pass * kRows + tid / kLanes, at = t - t0;
-      const int page = s_page[at], place = s_place[at];
-      const bool is_q = r < p.n_heads, is_k = !is_q && r < p.n_heads + kv_heads;
-      const int h = is_q ? r : is_k ? r - p.n_heads : r - p.n_heads - kv_heads, token = t;
-      float a[8], z[8];
-      widen(x0, a);
-      widen(x1, z);
-      if (++pass == passes) pass = 0, ++t;
-      if (--left > 0) load(t, pass);
-      if (turns && r < p.n_heads + kv_heads) {
-        float c[8], s[8];
-        const float4* angles = reinterpret_cast<const float4*>(&s_angles[at][8 * i]);
-        *reinterpret_cast<float4*>(c) = angles[0], *reinterpret_cast<float4*>(c + 4) = angles[1];
-        angles = reinterpret_cast<const float4*>(&s_angles[at][p.rotary / 2 + 8 * i]);
-        *reinterpret_cast<float4*>(s) = angles[0], *reinterpret_cast<float4*>(s + 4) = angles[1];
-        if (p.interleaved) {
+      for (int e = 0; e < n; ++e) {
+        float a[8], z[8];
+        widen(x0, a);
+        widen(x1, z);
+        if (--tokens > 0) load();
+        if (turns) {
+          float c[8], s[8];
+          const float4* angles = reinterpret_cast<const float4*>(&s_angles[e][8 * i]);
+          *reinterpret_cast<float4*>(c) = angles[0], *reinterpret_cast<float4*>(c + 4) = angles[1];
+          angles = reinterpret_cast<const float4*>(&s_angles[e][p.rotary / 2 + 8 * i]);
+          *reinterpret_cast<float4*>(s) = angles[0], *reinterpret_cast<float4*>(s + 4) = angles[1];
+          if (apart) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            turn(a[2 * k], a[2 * k + 1], c[k], s[k]);
-            turn(z[2 * k], z[2 * k + 1], c[4 + k], s[4 + k]);
+            for (int k = 0; k < 8; ++k) turn(a[k], z[k], c[k], s[k]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              turn(a[2 * k], a[2 * k + 1], c[k], s[k]);
+              turn(z[2 * k], z[2 * k + 1], c[4 + k], s[4 + k]);
+            }
           }
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) turn(a[k], z[k], c[k], s[k]);
         }
-      }
-      const int e0 = is_q || is_k ? d0 : 16 * i, e1 = is_q || is_k ? d1 : 16 * i + 8;
-      const uint64_t unit = (uint64_t)(uint32_t)page * p.cache.page16 + (uint64_t)(uint32_t)place * p.cache.token16 + (uint64_t)(uint32_t)h * p.cache.head16;
-      if (I8 && __any_sync(0xffffffffu, !is_q)) {
-        // the largest of the head, over the lanes that have it (all lanes of the warp take part)
-        float most = 0.f;
+        const int state = s_state[e];
+        if (I8 && __any_sync(0xffffffffu, !is_q)) {
+          // the largest of the head, over the lanes that have it (all lanes of the warp take part)
+          float most = 0.f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) most = larger(most, larger(fabsf(a[k]), fabsf(z[k])));
+          for (int k = 0; k < 8; ++k) most = larger(most, larger(fabsf(a[k]), fabsf(z[k])));
 #pragma unroll
-        for (int o = 1; o < kLanes; o <<= 1) most = larger(most, __shfl_xor_sync(0xffffffffu, most, o));
-        if (!is_q && r < rows && page >= 0) {
-          const float step = most == 0.f ? 1.f : __fdiv_rn(most, 127.f);
-          uint32_t codes[4];
-          encode(a, z, step, codes);
-          int8_t* to = static_cast<int8_t*>(const_cast<void*>(is_k ? p.cache.k : p.cache.v)) + unit * 16;
-          *reinterpret_cast<uint2*>(to + e0) = make_uint2(codes[0], codes[1]);
-          *reinterpret_cast<uint2*>(to + e1) = make_uint2(codes[2], codes[3]);
-          if (i == 0)
-            const_cast<float*>(is_k ? p.cache.k_scales : p.cache.v_scales)[((long long)page * kv_heads + h) * p.cache.page_size + place] = step;
+          for (int o = 1; o < kLanes; o <<= 1) most = larger(most, __shfl_xor_sync(0xffffffffu, most, o));
+          if (!is_q && there && state == 2) {
+            const float step = most == 0.f ? 1.f : __fdiv_rn(most, 127.f);
+            uint32_t codes[4];
+            encode(a, z, step, codes);
+            char* const to = to_cache + (uint64_t)s_unit[e] * 16;
+            *reinterpret_cast<uint2*>(to + at0 / 2) = make_uint2(codes[0], codes[1]);
+            *reinterpret_cast<uint2*>(to + at1 / 2) = make_uint2(codes[2], codes[3]);
+            if (i == 0) const_cast<float*>(is_k ? p.cache.k_scales : p.cache.v_scales)[s_scale[e] + h * p.cache.page_size] = step;
+          }
         }
+        if (there && (is_q ? state > 0 : !I8 && state == 2)) {
+          char* const to = is_q ? to_q : to_cache + (uint64_t)s_unit[e] * 16;
+          *reinterpret_cast<uint4*>(to + at0) = narrow(a);
+          *reinterpret_cast<uint4*>(to + at1) = narrow(z);
+        }
+        to_q += (uint64_t)p.q_out.row * 2;
       }
-      if (r < rows && (is_q ? place >= 0 : !I8 && page >= 0)) {
-        uint16_t* to = is_q ? p.q_out.data + token * p.q_out.row + h * p.q_out.head
-                            : static_cast<uint16_t*>(const_cast<void*>(is_k ? p.cache.k : p.cache.v)) + unit * 8;
-        *reinterpret_cast<uint4*>(to + e0) = narrow(a);
-        *reinterpret_cast<uint4*>(to + e1) = narrow(z);
-      }
-      if (left == 0) return;
-      if (t == t0 + n) break;
+      t += n;
+      left -= n;
     }
-    __syncthreads();                                           // the places and angles have been read
   }
 }
 
@@ -336,7 +334,7 @@ int launch_dim(const AppendParams& p, int dim, cudaStream_t st) {
 }
 
 Rows rows_of(const peqa_rows_t* r, int rows, int heads) {
-  return Rows{static_cast<uint16_t*>(r->data), rows > 1 ? (long long)r->row_stride : 0, heads > 1 ? (long long)r->head_stride : 0};
+  return Rows{static_cast<uint16_t*>(r->data), rows > 1 ? (uint32_t)r->row_stride : 0u, heads > 1 ? (uint32_t)r->head_stride : 0u};
 }
 
 }  // namespace
