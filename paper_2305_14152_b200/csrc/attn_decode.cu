@@ -51,6 +51,7 @@ struct AttnParams {
   int chunks, rows_of_seq;           // of NH query heads per key-value head; n_kv_heads * chunks
   float scale_log2;
   int window;
+  bool row_each;                     // a CTA has a row to itself
   uint16_t* out;
   float* lse;
   int4* headers;                     // [2 * CTAs]: row, whether its last tile is in the part
@@ -233,14 +234,8 @@ struct Part {
 };
 __device__ __forceinline__ float4 operator*(float4 a, float4 b) { return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w); }
 __device__ __forceinline__ float4 operator+(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
-__device__ __forceinline__ float4 larger(float4 a, float4 b) {
-  return make_float4(fmaxf(a.x, b.x), fmaxf(a.y, b.y), fmaxf(a.z, b.z), fmaxf(a.w, b.w));
-}
 
 __device__ __forceinline__ float weight(float m, float most) { return m == kNegInf ? 0.f : exp2f(m - most); }
-__device__ __forceinline__ float4 weight(float4 m, float4 most) {
-  return make_float4(weight(m.x, most.x), weight(m.y, most.y), weight(m.z, most.z), weight(m.w, most.w));
-}
 
 // Channel d of heads h0 + head .. + 3, as far as there are heads, and their log-sums where d is 0.
 template <int D>
@@ -271,6 +266,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ int s_scan[kThreads];
   __shared__ int s_warp[S::kWarps];
+  __shared__ __align__(16) float s_weight[32][NH], s_most[32][NH];   // of a part and head
   __shared__ int4 s_head[2 * S::kWarps];   // of a warp's parts: row (-1: none), begins its row, ends it
   __shared__ __align__(8) uint64_t s_full[S::WHOLE ? S::kWarps * S::kUnits : 1];
   __shared__ int s_abort[2];               // as the bounded waits of sm100_ptx.cuh have it
@@ -301,18 +297,20 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   // ---- the tiles of all sequences, and this warp's share of them: [begin, end)
   const int B = p.cache.n_seqs;
   int total = 0, begin = 0, end = 0;
+  auto among_warps = [&](int first, int n) {
+    const int each = n / S::kWarps, more = n - each * S::kWarps;           // the first `more` warps have one more
+    begin = first + each * warp + min(warp, more);
+    end = begin + each + (warp < more);
+  };
   auto share = [&]() {
     // no CTA without a tile for a warp of each scheduler, while there are enough
     const int busy = min((int)gridDim.x, max(1, total / MINT)), cta = blockIdx.x;
     if (cta >= busy) return;
     const int each = total / busy, more = total - each * busy;             // the first `more` CTAs have one more
-    const int first = each * cta + min(cta, more), n = each + (cta < more);
-    const int each_warp = n / S::kWarps, more_warp = n - each_warp * S::kWarps;
-    begin = first + each_warp * warp + min(warp, more_warp);
-    end = begin + each_warp + (warp < more_warp);
+    among_warps(each * cta + min(cta, more), each + (cta < more));
   };
   auto tiles_of = [&](int b) { return b < B ? span_of(p, b).tiles() * p.rows_of_seq : 0; };
-  if (B > kThreads) {
+  if (B > kThreads && !p.row_each) {
     for (int b = tid; b < B; b += kThreads) total += tiles_of(b);
     total = __reduce_add_sync(0xffffffffu, total);
     if (lane == 0) s_warp[warp] = total;
@@ -323,7 +321,12 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   Cursor in;                                // of the copies; the sums follow with `at`
   in.b = in.r = in.t0 = in.left = in.span.first = in.span.end = 0;
   int before = 0;                           // tiles of the sequences before this round's
-  if (B <= 32) {                            // every warp for itself
+  if (p.row_each) {
+    const int b = blockIdx.x / p.rows_of_seq, r = blockIdx.x - b * p.rows_of_seq;
+    const int tiles = span_of(p, b).tiles();
+    among_warps(r * tiles, tiles);          // of the sequence's tiles
+    if (begin < end) in.begin(p, b, begin);
+  } else if (B <= 32) {                     // every warp for itself
     int upto = tiles_of(lane);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -811,16 +814,28 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     }
   }
 
-  // ---- rows that no warp has alone.  Lane i has the i-th part of the CTA (two for each warp, of the rows in order); a warp takes 128 sums of
-  // a row at a time, a lane four heads of a channel.
+  // ---- rows that no warp has alone.  Lane i has the i-th part of the CTA (two for each warp, of the rows in order).  A warp finds the weights
+  // of all parts for a head, then takes 128 sums of a row at a time, a lane four heads of a channel.
   constexpr int kSlices = NH * D / 128;
   const int4 own = lane < 2 * S::kWarps ? s_head[lane] : make_int4(-1, 0, 0, 0);
   auto part_of = [&](int i) { return i & 1 ? last_part(i >> 1) : first_part(i >> 1); };
+  const uint32_t parts_of_own = __match_any_sync(0xffffffffu, own.x);
+  for (int head = warp; head < NH; head += S::kWarps) {
+    float m = kNegInf;
+    if (own.x >= 0) m = part_of(lane).at[NH * D + head];
+    // the largest of the row's: as whole numbers that have the order of the floats
+    const int bits = __float_as_int(m), key = bits ^ (bits >> 31 & 0x7fffffff);
+    const int most_key = __reduce_max_sync(parts_of_own, key);
+    const float most = __int_as_float(most_key ^ (most_key >> 31 & 0x7fffffff));
+    s_weight[lane][head] = weight(m, most);
+    s_most[lane][head] = most;
+  }
+  __syncthreads();
   int task = 0, crossing0 = -1, crossing1 = -1, ends0 = 0;
   for (uint32_t rest = __ballot_sync(0xffffffffu, own.x >= 0); rest;) {
     const int leader = __ffs(rest) - 1;
     const int row = __shfl_sync(0xffffffffu, own.x, leader);
-    const uint32_t parts = __ballot_sync(0xffffffffu, own.x == row);
+    const uint32_t parts = __shfl_sync(0xffffffffu, parts_of_own, leader);
     rest &= ~parts;
     const int starts = __shfl_sync(0xffffffffu, own.y, leader), ends = __shfl_sync(0xffffffffu, own.z, 31 - __clz(parts));
     if (!starts) crossing0 = row, ends0 = ends;
@@ -828,15 +843,24 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     for (int slice = 0; slice < kSlices; ++slice, ++task) {
       if (task % S::kWarps != warp) continue;
       const int place = slice * 32 + lane, head = place * 4 % NH, d = place * 4 / NH;
-      float4 top = make_float4(kNegInf, kNegInf, kNegInf, kNegInf), total_p = make_float4(0.f, 0.f, 0.f, 0.f), sums = total_p;
-      for (uint32_t of = parts; of; of &= of - 1) top = larger(top, part_of(__ffs(of) - 1).most4(head));
-#pragma unroll 2
-      for (uint32_t of = parts; of; of &= of - 1) {
-        const Part<D, NH> part = part_of(__ffs(of) - 1);
-        const float4 f = weight(part.most4(head), top);
-        total_p = total_p + f * part.total4(head);
-        sums = sums + f * part.four(place);
+      float4 total_p = make_float4(0.f, 0.f, 0.f, 0.f), sums = total_p;
+      for (uint32_t of = parts; of;) {
+        constexpr int kAtOnce = 4;             // parts whose loads are under way together; one that is not there is the leader with no weight
+        float4 f[kAtOnce], t[kAtOnce], v[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int i = of ? __ffs(of) - 1 : leader;
+          const float on = of ? 1.f : 0.f;
+          of &= of - 1;
+          const Part<D, NH> part = part_of(i);
+          f[u] = *reinterpret_cast<const float4*>(&s_weight[i][head]) * make_float4(on, on, on, on);
+          t[u] = part.total4(head);
+          v[u] = part.four(place);
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) total_p = total_p + f[u] * t[u], sums = sums + f[u] * v[u];
       }
+      const float4 top = *reinterpret_cast<const float4*>(&s_most[leader][head]);
       if (starts && ends) {
         const int b = row / p.rows_of_seq;
         int heads;
@@ -849,7 +873,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       }
     }
   }
-  if (tid == 0) {
+  if (tid == 0 && !p.row_each) {
     p.headers[2 * blockIdx.x] = make_int4(crossing0, ends0, 0, 0);
     p.headers[2 * blockIdx.x + 1] = make_int4(crossing1, 0, 0, 0);
   }
@@ -959,7 +983,7 @@ int launch(const AttnParams& p, cudaStream_t st) {
   PEQA_TRY(allow_smem(attn_decode_kernel<S>, S::kSmem, allowed));
   const int ctas = attn_ctas();
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ctas, 1, 1);
+  cfg.gridDim = dim3(p.row_each ? p.cache.n_seqs * p.rows_of_seq : ctas, 1, 1);
   cfg.blockDim = dim3(S::kWarps * 32, 1, 1);
   cfg.dynamicSmemBytes = S::kSmem;
   cfg.stream = st;
@@ -974,6 +998,7 @@ int launch(const AttnParams& p, cudaStream_t st) {
     PEQA_TRY(tensor_map_of<S>(p.cache, p.cache.v, &values));
   }
   PEQA_CUDA(cudaLaunchKernelEx(&cfg, attn_decode_kernel<S>, p, keys, values));
+  if (p.row_each) return PEQA_OK;
   cfg.gridDim = dim3(ctas, NH * D / 128, 1);
   cfg.blockDim = dim3(256, 1, 1);
   cfg.dynamicSmemBytes = 0;
@@ -1042,6 +1067,11 @@ extern "C" int peqa_attn_decode(const peqa_kv_cache_t* c, const peqa_rows_t* q, 
   p.q_head = n_heads > 1 ? q->head_stride : 0;
   p.seq_lens = seq_lens;
   p.n_heads = n_heads;
+  // A CTA for every row needs no second kernel, but is as long as the longest row.  Rows of T tiles, rows x T: dealt out evenly / a CTA each, us:
+  // 8 x 9 9.5 / 8.0, 8 x 16 9.5 / 11.0, 8 x 64 10.4 / 13.9; 32 x 9 9.0 / 7.4, 32 x 64 12.7 / 12.5; 128 x 9 10.0 / 7.4, 128 x 64 19.9 / 15.9, 128 x
+  // 128 26.4 / 22.8 (four sequences of uneven lengths).  What is known here of the lengths is what they can be at most.
+  const long long ctas = attn_ctas(), most = (min(p.cache.capacity, window > 0 ? window + kTile - 1 : p.cache.capacity) + kTile - 1) / kTile;
+  p.row_each = rows <= ctas && (most <= 9 || (4 * rows >= ctas && most * (ctas - rows) <= 48 * ctas && most <= 129));
   p.scale_log2 = scale * kLog2e;
   p.window = window;
   p.out = static_cast<uint16_t*>(out);
