@@ -244,7 +244,7 @@ __device__ __forceinline__ void put_out(const AttnParams& p, long long row0, int
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (head + i < heads) {
-      const __nv_bfloat16 x = __float2bfloat16_rn(o[i] * (1.f / t[i]));
+      const __nv_bfloat16 x = __float2bfloat16_rn(o[i] * __fdividef(1.f, t[i]));
       p.out[(row0 + head + i) * D + d] = *reinterpret_cast<const uint16_t*>(&x);
       if (p.lse && d == 0) p.lse[row0 + head + i] = kLn2 * (m[i] + log2f(t[i]));
     }
@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   __shared__ int s_scan[kThreads];
   __shared__ int s_warp[S::kWarps];
   __shared__ __align__(16) float s_weight[32][NH], s_most[32][NH];   // of a part and head
-  __shared__ int4 s_head[2 * S::kWarps];   // of a warp's parts: row (-1: none), begins its row, ends it
+  __shared__ int4 s_head[2 * S::kWarps];   // of a warp's parts: row (-1: none), 1 if it begins its row + 2 if it ends it + 4 times its heads, its first head's place in out
   __shared__ __align__(8) uint64_t s_full[S::WHOLE ? S::kWarps * S::kUnits : 1];
   __shared__ int s_abort[2];               // as the bounded waits of sm100_ptx.cuh have it
 
@@ -751,7 +751,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       if (from_start && to_end) {
 #pragma unroll
         for (int n = 0; n < kCols; ++n) {
-          const float f[2] = {1.f / sum[n][0] * v_ref, 1.f / sum[n][1] * v_ref};
+          const float f[2] = {__fdividef(v_ref, sum[n][0]), __fdividef(v_ref, sum[n][1])};
           const long long row0 = (long long)at.b * p.n_heads + h0 + 8 * n;
           if (p.lse && lr == 0)
 #pragma unroll
@@ -791,7 +791,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
             part.two(16 * d + (I8 ? 2 * lr + 1 : lr + 8), head) = make_float2(acc[d][n][2] * v_ref, acc[d][n][3] * v_ref);
           }
         }
-      if (lane == 0) s_head[2 * warp + (more ? 0 : 1)] = make_int4(at.b * p.rows_of_seq + at.r, from_start, to_end, 0);
+      if (lane == 0) s_head[2 * warp + (more ? 0 : 1)] = 
+            make_int4(at.b * p.rows_of_seq + at.r, (from_start ? 1 : 0) + (to_end ? 2 : 0) + heads * 4, at.b * p.n_heads + h0, 0);
     };
 
     bool fresh = true;
@@ -830,52 +831,53 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     s_weight[lane][head] = weight(m, most);
     s_most[lane][head] = most;
   }
-  __syncthreads();
-  int task = 0, crossing0 = -1, crossing1 = -1, ends0 = 0;
-  for (uint32_t rest = __ballot_sync(0xffffffffu, own.x >= 0); rest;) {
-    const int leader = __ffs(rest) - 1;
-    const int row = __shfl_sync(0xffffffffu, own.x, leader);
-    const uint32_t parts = __shfl_sync(0xffffffffu, parts_of_own, leader);
-    rest &= ~parts;
-    const int starts = __shfl_sync(0xffffffffu, own.y, leader), ends = __shfl_sync(0xffffffffu, own.z, 31 - __clz(parts));
-    if (!starts) crossing0 = row, ends0 = ends;
-    else if (!ends) crossing1 = row;
-    for (int slice = 0; slice < kSlices; ++slice, ++task) {
-      if (task % S::kWarps != warp) continue;
-      const int place = slice * 32 + lane, head = place * 4 % NH, d = place * 4 / NH;
-      float4 total_p = make_float4(0.f, 0.f, 0.f, 0.f), sums = total_p;
-      for (uint32_t of = parts; of;) {
-        constexpr int kAtOnce = 4;             // parts whose loads are under way together; one that is not there is the leader with no weight
-        float4 f[kAtOnce], t[kAtOnce], v[kAtOnce];
-#pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-          const int i = of ? __ffs(of) - 1 : leader;
-          const float on = of ? 1.f : 0.f;
-          of &= of - 1;
-          const Part<D, NH> part = part_of(i);
-          f[u] = *reinterpret_cast<const float4*>(&s_weight[i][head]) * make_float4(on, on, on, on);
-          t[u] = part.total4(head);
-          v[u] = part.four(place);
-        }
-#pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) total_p = total_p + f[u] * t[u], sums = sums + f[u] * v[u];
-      }
-      const float4 top = *reinterpret_cast<const float4*>(&s_most[leader][head]);
-      if (starts && ends) {
-        const int b = row / p.rows_of_seq;
-        int heads;
-        const int h0 = first_head<NH>(p, row - b * p.rows_of_seq, heads);
-        put_out<D>(p, (long long)b * p.n_heads + h0, heads, head, d, sums, top, total_p);
-      } else {
-        const Part<D, NH> part{p.parts + (2ll * blockIdx.x + (starts ? 1 : 0)) * S::kPart};
-        part.four(place) = sums;
-        if (d == 0) part.most4(head) = top, part.total4(head) = total_p;
-      }
+  // of the row that a lane's part is of: whether the CTA has its first tile and its last
+  const int run_starts = __shfl_sync(0xffffffffu, own.y, __ffs(parts_of_own) - 1) & 1;
+  const int run_ends = __shfl_sync(0xffffffffu, own.y, 31 - __clz(parts_of_own)) & 2;
+  const uint32_t leaders = __ballot_sync(0xffffffffu, own.x >= 0 && lane == __ffs(parts_of_own) - 1);
+  if (warp == 0 && !p.row_each) {
+    const uint32_t behind = __ballot_sync(0xffffffffu, own.x >= 0 && !run_starts), before = __ballot_sync(0xffffffffu, own.x >= 0 && run_starts && !run_ends);
+    const int row0 = __shfl_sync(0xffffffffu, own.x, behind ? __ffs(behind) - 1 : 0), ends0 = __shfl_sync(0xffffffffu, run_ends, behind ? __ffs(behind) - 1 : 0);
+    const int row1 = __shfl_sync(0xffffffffu, own.x, before ? __ffs(before) - 1 : 0);
+    if (lane == 0) {
+      p.headers[2 * blockIdx.x] = make_int4(behind ? row0 : -1, ends0, 0, 0);
+      p.headers[2 * blockIdx.x + 1] = make_int4(before ? row1 : -1, 0, 0, 0);
     }
   }
-  if (tid == 0 && !p.row_each) {
-    p.headers[2 * blockIdx.x] = make_int4(crossing0, ends0, 0, 0);
-    p.headers[2 * blockIdx.x + 1] = make_int4(crossing1, 0, 0, 0);
+  __syncthreads();
+  for (int task = warp; task < __popc(leaders) * kSlices; task += S::kWarps) {
+    uint32_t from = leaders;
+    for (int i = task / kSlices; i > 0; --i) from &= from - 1;
+    const int leader = __ffs(from) - 1;
+    const uint32_t parts = __shfl_sync(0xffffffffu, parts_of_own, leader);
+    const int starts = __shfl_sync(0xffffffffu, run_starts, leader), ends = __shfl_sync(0xffffffffu, run_ends, leader);
+    const int out_row = __shfl_sync(0xffffffffu, own.z, leader), heads = __shfl_sync(0xffffffffu, own.y, leader) >> 2;
+    const int place = task % kSlices * 32 + lane, head = place * 4 % NH, d = place * 4 / NH;
+    float4 total_p = make_float4(0.f, 0.f, 0.f, 0.f), sums = total_p;
+    for (uint32_t of = parts; of;) {
+      constexpr int kAtOnce = 4;               // parts whose loads are under way together; one that is not there is the leader with no weight
+      float4 f[kAtOnce], t[kAtOnce], v[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int i = of ? __ffs(of) - 1 : leader;
+        const float on = of ? 1.f : 0.f;
+        of &= of - 1;
+        const Part<D, NH> part = part_of(i);
+        f[u] = *reinterpret_cast<const float4*>(&s_weight[i][head]) * make_float4(on, on, on, on);
+        t[u] = part.total4(head);
+        v[u] = part.four(place);
+      }
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) total_p = total_p + f[u] * t[u], sums = sums + f[u] * v[u];
+    }
+    const float4 top = *reinterpret_cast<const float4*>(&s_most[leader][head]);
+    if (starts && ends) {
+      put_out<D>(p, out_row, heads, head, d, sums, top, total_p);
+    } else {
+      const Part<D, NH> part{p.parts + (2ll * blockIdx.x + (starts ? 1 : 0)) * S::kPart};
+      part.four(place) = sums;
+      if (d == 0) part.most4(head) = top, part.total4(head) = total_p;
+    }
   }
 
   // ---- sequences that are not there have outputs all the same
@@ -1057,7 +1059,7 @@ extern "C" int peqa_attn_decode(const peqa_kv_cache_t* c, const peqa_rows_t* q, 
   p.chunks = (p.group + nh - 1) / nh;
   // tiles and rows are numbered in 31 bits
   const long long rows_of_seq = (long long)c->n_kv_heads * p.chunks, rows = c->n_seqs * rows_of_seq;
-  if (rows > 0x7fffffffll || rows > 0x7fffffffll / (p.cache.capacity / kTile + 2)) return PEQA_ERR_TOO_LARGE;
+  if (rows > 0x7fffffffll / (p.cache.capacity / kTile + 2) || (long long)c->n_seqs * n_heads > 0x7fffffffll) return PEQA_ERR_TOO_LARGE;
   p.rows_of_seq = (int)rows_of_seq;
   PEQA_TRY(check_arch());
   if (!workspace || bytes < workspace_bytes(c->head_dim, nh)) return PEQA_ERR_WORKSPACE;
