@@ -60,6 +60,9 @@ struct AttnParams {
   int* status;
 };
 
+// By the registers that a thread needs.
+constexpr int warps_of(int dim, int nh) { return dim > 128 ? 8 : nh <= 8 ? 16 : dim <= 64 ? 12 : 8; }
+
 // Everything that follows from the channels D, the query heads NH of a row, the type of the cache and whether a tile comes by
 // tensor copies (WHOLE: it lies in one page).
 template <int D_, int NH_, bool I8_, bool WHOLE_>
@@ -73,7 +76,7 @@ struct Shape {
   static constexpr int kLine = kBytes < 128 ? kBytes : 128;     // bytes of a token that lie together in shared memory
   static constexpr int kRows = 32 / kPieces;                    // tokens that a warp copies with one instruction
   static constexpr int kUnit = kTile * kBytes;                  // keys or values of a tile
-  static constexpr int kWarps = D > 128 || NH > 8 ? 8 : 16;     // by the registers that a thread needs
+  static constexpr int kWarps = warps_of(D, NH);
   static constexpr int kFit = 192 * 1024 / (kWarps * (kUnit + (I8 ? 64 : 0)));
   static constexpr int kUnits = kFit >= 9 ? 9 : kFit >= 7 ? 7 : kFit >= 5 ? 5 : 3;   // odd: keys follow keys, values values
   static constexpr int kRing = kUnits * kUnit;
@@ -235,6 +238,13 @@ struct Part {
 __device__ __forceinline__ float4 operator*(float4 a, float4 b) { return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w); }
 __device__ __forceinline__ float4 operator+(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 
+__device__ __forceinline__ float4 larger(float4 a, float4 b) {
+  return make_float4(fmaxf(a.x, b.x), fmaxf(a.y, b.y), fmaxf(a.z, b.z), fmaxf(a.w, b.w));
+}
+__device__ __forceinline__ float4 shuffled(float4 a, int o) {
+  return make_float4(__shfl_xor_sync(0xffffffffu, a.x, o), __shfl_xor_sync(0xffffffffu, a.y, o), __shfl_xor_sync(0xffffffffu, a.z, o),
+                     __shfl_xor_sync(0xffffffffu, a.w, o));
+}
 __device__ __forceinline__ float weight(float m, float most) { return m == kNegInf ? 0.f : exp2f(m - most); }
 
 // Channel d of heads h0 + head .. + 3, as far as there are heads, and their log-sums where d is 0.
@@ -891,66 +901,60 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
 }
 
 // Joins the rows that cross CTAs.  CTAs (i, .) take the row that begins in CTA i of the kernel before and goes on in the next ones, CTA
-// (i, j) 128 of its sums: a lane four heads of a channel, the warps the parts in turn (one row of 16 heads over all CTAs: by one CTA 50 us).
+// (i, j) 32 channels of four of its heads: a thread finds the weights of a part, then a lane sums a channel, the warps the parts in
+// turn.  (One row of 16 heads over all CTAs: by one CTA 50 us.)
 constexpr int kMaxCtas = 256;
 template <int D, int NH>
-__global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, const int ctas) {
-  constexpr int kPart = NH * (D + 2), kWarps = 8;
-  __shared__ __align__(16) float s_weight[kMaxCtas][NH];
-  __shared__ __align__(16) float s_most[NH], s_total[NH];
-  __shared__ float4 s_sums[kWarps][32];
+__global__ void __launch_bounds__(kMaxCtas) attn_join_kernel(const AttnParams p, const int ctas) {
+  constexpr int kPart = NH * (D + 2), kWarps = kMaxCtas / 32;
+  __shared__ float4 s_weight[kMaxCtas], s_top[kWarps], s_total[kWarps], s_sums[kWarps][32];
+  __shared__ int s_stop;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) s_stop = 0x7fffffff;
+  __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int row = ptx::behind_wait(p.headers)[2 * blockIdx.x + 1].x;
   if (row < 0) return;
   // parts of the row: the own one, then the first ones of the CTAs behind, up to the one that has the row's end
-  int n = 1;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  for (int base = blockIdx.x + 1; base < ctas; base += 32) {
-    const int c = base + lane;
-    const int4 h = c < ctas ? ptx::behind_wait(p.headers)[2 * c] : make_int4(-1, 1, 0, 0);
-    const uint32_t stop = __ballot_sync(0xffffffffu, h.x != row || h.y);
-    if (stop) {
-      const int l = __ffs(stop) - 1;
-      n += l + (__shfl_sync(0xffffffffu, h.x, l) == row ? 1 : 0);
-      break;
-    }
-    n += 32;
-  }
+  const int c = blockIdx.x + 1 + tid;
+  const int4 h = c < ctas ? ptx::behind_wait(p.headers)[2 * c] : make_int4(-1, 1, 0, 0);
+  const uint32_t stops = __ballot_sync(0xffffffffu, h.x != row || h.y);
+  if (stops && lane == __ffs(stops) - 1) atomicMin(&s_stop, 2 * tid + (h.x != row));
+  __syncthreads();
+  const int n = min(ctas, 1 + (s_stop >> 1) + (s_stop & 1 ? 0 : 1));
+  const int group = blockIdx.y % (NH / 4), d = blockIdx.y / (NH / 4) * 32 + lane, head = group * 4;
   auto part_of = [&](int i) { return Part<D, NH>{p.parts + (i == 0 ? 2ll * blockIdx.x + 1 : 2ll * (blockIdx.x + i)) * kPart}; };
-  for (int head = warp; head < NH; head += kWarps) {
-    const int even = head & ~1, odd = head & 1;
-    float most = kNegInf;
-    for (int i = lane; i < n; i += 32) {
-      const float2 m = part_of(i).most(even);
-      most = fmaxf(most, odd ? m.y : m.x);
-    }
+  float4 m = make_float4(kNegInf, kNegInf, kNegInf, kNegInf), total = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (tid < n) m = part_of(tid).most4(head), total = part_of(tid).total4(head);
+  float4 top = m;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-    float total = 0.f;
-    for (int i = lane; i < n; i += 32) {
-      const float2 m = part_of(i).most(even), t = part_of(i).total(even);
-      const float w = weight(odd ? m.y : m.x, most);
-      s_weight[i][head] = w;
-      total += w * (odd ? t.y : t.x);
-    }
+  for (int o = 16; o; o >>= 1) top = larger(top, shuffled(top, o));
+  if (lane == 0) s_top[warp] = top;
+  __syncthreads();
 #pragma unroll
-    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    if (lane == 0) s_most[head] = most, s_total[head] = total;
-  }
-  const int place = blockIdx.y * 32 + lane, head = place * 4 % NH, d = place * 4 / NH;
+  for (int w = 0; w < kWarps; ++w) top = larger(top, s_top[w]);
+  const float4 f = make_float4(weight(m.x, top.x), weight(m.y, top.y), weight(m.z, top.z), weight(m.w, top.w));
+  s_weight[tid] = f;
+  total = total * f;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) total = total + shuffled(total, o);
+  if (lane == 0) s_total[warp] = total;
   __syncthreads();
   float4 sums = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int i = warp; i < n; i += kWarps) sums = sums + *reinterpret_cast<const float4*>(&s_weight[i][head]) * part_of(i).four(place);
+  for (int i = warp; i < n; i += kWarps) sums = sums + s_weight[i] * part_of(i).four(d * (NH / 4) + group);
   s_sums[warp][lane] = sums;
   __syncthreads();
   if (warp > 0) return;
-  for (int w = 1; w < min(n, kWarps); ++w) sums = sums + s_sums[w][lane];
+#pragma unroll
+  for (int w = 1; w < kWarps; ++w) sums = sums + s_sums[w][lane];
+  total = s_total[0];
+#pragma unroll
+  for (int w = 1; w < kWarps; ++w) total = total + s_total[w];
   const int b = row / p.rows_of_seq;
   int heads;
   const int h0 = first_head<NH>(p, row - b * p.rows_of_seq, heads);
-  put_out<D>(p, (long long)b * p.n_heads + h0, heads, head, d, sums, *reinterpret_cast<const float4*>(&s_most[head]),
-             *reinterpret_cast<const float4*>(&s_total[head]));
+  put_out<D>(p, (long long)b * p.n_heads + h0, heads, head, d, sums, top, total);
 }
 
 int attn_ctas() { return min(sm_count_or(148), kMaxCtas); }
@@ -1002,7 +1006,7 @@ int launch(const AttnParams& p, cudaStream_t st) {
   PEQA_CUDA(cudaLaunchKernelEx(&cfg, attn_decode_kernel<S>, p, keys, values));
   if (p.row_each) return PEQA_OK;
   cfg.gridDim = dim3(ctas, NH * D / 128, 1);
-  cfg.blockDim = dim3(256, 1, 1);
+  cfg.blockDim = dim3(kMaxCtas, 1, 1);
   cfg.dynamicSmemBytes = 0;
   PEQA_CUDA(cudaLaunchKernelEx(&cfg, attn_join_kernel<D, NH>, p, ctas));
   return PEQA_OK;
@@ -1028,9 +1032,7 @@ int launch_heads(const AttnParams& p, int nh, bool codes, cudaStream_t st) {
 
 // headers, parts of CTAs, parts of warps
 size_t workspace_bytes(int dim, int nh) {
-  const int warps = dim > 128 || nh > 8 ? 8 : 16;
-  static_assert(Shape<128, 8, false, true>::kWarps == 16 && Shape<64, 16, false, true>::kWarps == 8 && Shape<256, 4, true, true>::kWarps == 8, "");
-  return (size_t)attn_ctas() * (2 * sizeof(int4) + (2 + warps) * (size_t)nh * (dim + 2) * sizeof(float));
+  return (size_t)attn_ctas() * (2 * sizeof(int4) + (2 + warps_of(dim, nh)) * (size_t)nh * (dim + 2) * sizeof(float));
 }
 
 }  // namespace
