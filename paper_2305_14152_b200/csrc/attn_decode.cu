@@ -13,11 +13,11 @@
 //       S^T = K Q^T     K [16 tokens x 16 channels] as it lies, Q in registers
 //       O^T = V^T P^T   V^T [16 channels x 16 tokens] by the transposing ldmatrix; P^T from S^T by movmatrix
 //     So there is no barrier between warps in the loop, and a lane has the factors of the sums that it holds.
-//   * Up to four query heads stand in the columns twice, and p's two numbers (below) in the two places.
+//   * With bf16 up to four query heads stand in the columns twice, and p's two numbers (below) in the two places.
 //   * Running maximum and sum per row, as the softmax allows: the sums are rescaled only when the maximum has risen by more than
 //     kSlack (a factor of 2^8 that the binary32 sums carry easily).
-//   * p goes into the second product as the sum of two 16-bit numbers: with one, its rounding (2^-9 of p) would double the
-//     error variance that the rounding of the output has.  v and q are 16-bit numbers already, and 8-bit codes are exact ones.
+//   * With bf16 values p goes into the second product as the sum of two of them: with one, its rounding (2^-9 of p) would double the
+//     error variance that the rounding of the output has.  8-bit codes are exact in binary16, and p in it is off by 2^-12 (3 % of that variance).
 //   * A row that a warp has from its first tile to its last is written out.  Parts of rows are joined within the CTA in shared
 //     memory, and what crosses CTAs by a second kernel, which stands ready when the first ends.
 #include "common.cuh"
@@ -34,9 +34,6 @@ namespace peqa {
 namespace {
 
 constexpr int kTile = 16;            // tokens
-#ifndef MINT
-#define MINT 4
-#endif
 constexpr float kSlack = 8.f;        // of the running maximum, in powers of two
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -69,7 +66,7 @@ template <int D_, int NH_, bool I8_, bool WHOLE_>
 struct Shape {
   static constexpr int D = D_, NH = NH_;
   static constexpr bool I8 = I8_, WHOLE = WHOLE_;
-  static constexpr bool kHalves = NH == 4;                      // the two numbers that p is are columns of one product
+  static constexpr bool kHalves = NH == 4 && !I8;               // the two numbers that p is are columns of one product
   static constexpr int kCols = NH > 8 ? 2 : 1;                  // of eight heads (kHalves: of four, twice)
   static constexpr int kBytes = D * (I8 ? 1 : 2);               // of a token
   static constexpr int kPieces = kBytes / 16;                   // 16-byte pieces of a token
@@ -139,6 +136,11 @@ __device__ __forceinline__ void mma0(float (&d)[4], uint32_t a0, uint32_t a1, ui
   else
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// the same from sums c0, c1 of the columns on
+__device__ __forceinline__ void mma_from(float (&d)[4], float c0, float c1, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%10,%11};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
 }
 // 2^x, 0 below 2^-126
 __device__ __forceinline__ float power_of_two(float x) {
@@ -314,7 +316,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   };
   auto share = [&]() {
     // no CTA without a tile for a warp of each scheduler, while there are enough
-    const int busy = min((int)gridDim.x, max(1, total / MINT)), cta = blockIdx.x;
+    const int busy = min((int)gridDim.x, max(1, total / 4)), cta = blockIdx.x;
     if (cta >= busy) return;
     const int each = total / busy, more = total - each * busy;             // the first `more` CTAs have one more
     among_warps(each * cta + min(cta, more), each + (cta < more));
@@ -510,8 +512,9 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
 
     uint32_t q[kCols][D / 16][2];                            // head lr (+ 8): two and two channels for each product
     float to_log2[kCols][2];                                 // of a product of the tensor cores; here and below: heads 2 lc, 2 lc + 1 (+ 8)
-    float q_bias[kCols][2];                                  // I8: what the sums of products have too much
+    float q_bias[kCols][2];                                  // I8: what the sums of products begin with
     float most[kCols][2], sum[kCols][2];                     // sum: of this lane's tokens
+    float base[kCols][2];                                    // most, or 0 where there is none
     float acc[D / 16][kCols][4];                             // two channels of each of the two heads
     float v_ref = 1.f, inv_ref = 1.f;                        // I8: acc is in units of it
     bool from_start;
@@ -550,7 +553,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
           big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
           const int e = min(max((int)(__float_as_uint(big) >> 23) - 127, -126), 126);
           const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-          // Codes come as c + 128 in the lowest bits of a binary16, (c + 128) 2^-24: 128 2^-24 times the sum of q is taken off each sum.
+          // Codes come as c + 128 in the lowest bits of a binary16, (c + 128) 2^-24: each sum begins with -128 2^-24 times the sum of q.
           // (The bias is about three times as large as the sums themselves, so their last bits weigh as much more.)
           scale = p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23) * 16777216.f;
 #pragma unroll
@@ -565,21 +568,21 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
             }
           bias += __shfl_xor_sync(0xffffffffu, bias, 1);
           bias += __shfl_xor_sync(0xffffffffu, bias, 2);
-          bias *= 0x1p-17f;
+          bias *= -0x1p-17f;
         }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {                        // from the lanes of head lr to those of its column
           to_log2[n][c] = I8 ? __shfl_sync(0xffffffffu, scale, lc * 8 + c * 4) : scale;
           q_bias[n][c] = I8 ? __shfl_sync(0xffffffffu, bias, lc * 8 + c * 4) : 0.f;
           most[n][c] = kNegInf;
-          sum[n][c] = 0.f;
+          sum[n][c] = base[n][c] = 0.f;
         }
       }
 #pragma unroll
       for (int d = 0; d < D / 16; ++d)
 #pragma unroll
         for (int n = 0; n < kCols; ++n) acc[d][n][0] = acc[d][n][1] = acc[d][n][2] = acc[d][n][3] = 0.f;
-      if constexpr (I8) v_ref = 0.f;
+      if constexpr (I8) v_ref = 0x1p-126f, inv_ref = 0x1p126f;
       from_start = at.t0 == at.tile0();
     };
 
@@ -607,7 +610,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
             const uint32_t a0 = __byte_perm(u, 0u, 0x4140), a1 = __byte_perm(w, 0u, 0x4140), a2 = __byte_perm(u, 0u, 0x4342), a3 = __byte_perm(w, 0u, 0x4342);
 #pragma unroll
             for (int n = 0; n < kCols; ++n) {
-              if (j == 0) mma0<true>(s[e][n], a0, a1, a2, a3, q[n][2 * j + e][0], q[n][2 * j + e][1]);
+              if (j == 0 && e == 0) mma_from(s[e][n], q_bias[n][0], q_bias[n][1], a0, a1, a2, a3, q[n][0][0], q[n][0][1]);
+              else if (j == 0) mma0<true>(s[e][n], a0, a1, a2, a3, q[n][e][0], q[n][e][1]);
               else mma<true>(s[e][n], a0, a1, a2, a3, q[n][2 * j + e][0], q[n][2 * j + e][1]);
             }
           }
@@ -628,7 +632,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
 #pragma unroll
         for (int n = 0; n < kCols; ++n) {
           float y = s[0][n][i] + s[1][n][i];
-          if constexpr (I8) y = (y - q_bias[n][i & 1]) * k_scale;
+          if constexpr (I8) y *= k_scale;
           x[n][i] = y * to_log2[n][i & 1];
         }
       }
@@ -659,6 +663,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
             f[n][c] = weight(most[n][c], next);
             sum[n][c] *= f[n][c];
             most[n][c] = next;
+            base[n][c] = next == kNegInf ? 0.f : next;
           }
         rescale(f);
       }
@@ -667,7 +672,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       for (int n = 0; n < kCols; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          x[n][i] = power_of_two(x[n][i] - (most[n][i & 1] == kNegInf ? 0.f : most[n][i & 1]));
+          x[n][i] = power_of_two(x[n][i] - base[n][i & 1]);
           sum[n][i & 1] += x[n][i];
         }
       // ---- O^T += V^T P^T
@@ -689,23 +694,23 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
           for (int i = 0; i < 2; ++i)
             if (t0 + lr + 8 * i < at.span.first || t0 + lr + 8 * i >= at.span.end) v_scale[i] = 0.f;
         // Values in units of 2^-6 of the largest scale so far, cut to a power of two: p (at most 2^kSlack) times what is left of its
-        // token's scale (below 2^7) is a binary16, and as two of them off by 2^-25 of a unit at most, 2^-31 of the largest.
-        const uint32_t exponent = __reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(fabsf(v_scale[0]), fabsf(v_scale[1])))) & 0x7f800000u;
-        const float ref = __uint_as_float(exponent > (7u << 23) ? exponent - (6u << 23) : 1u << 23);
-        if (ref > v_ref) {
-          if (v_ref > 0.f) {
-            float f[kCols][2];
+        // token's scale (below 2^7) is a binary16, off by 2^-11 of it, or by 2^-25 of a unit, 2^-31 of the largest.
+        float v_rest[2] = {v_scale[0] * inv_ref, v_scale[1] * inv_ref};
+        if (__any_sync(0xffffffffu, fmaxf(fabsf(v_rest[0]), fabsf(v_rest[1])) >= 128.f)) {
+          const uint32_t exponent = __reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(fabsf(v_scale[0]), fabsf(v_scale[1])))) & 0x7f800000u;
+          const float ref = __uint_as_float(exponent - (6u << 23));
+          float f[kCols][2];
 #pragma unroll
-            for (int n = 0; n < kCols; ++n) f[n][0] = f[n][1] = v_ref / ref;
-            rescale(f);
-          }
+          for (int n = 0; n < kCols; ++n) f[n][0] = f[n][1] = v_ref / ref;
+          rescale(f);
           v_ref = ref;
           inv_ref = 1.f / ref;
+          v_rest[0] = v_scale[0] * inv_ref, v_rest[1] = v_scale[1] * inv_ref;
         }
 #pragma unroll
         for (int n = 0; n < kCols; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[n][i] *= v_scale[i >> 1] * inv_ref;
+          for (int i = 0; i < 4; ++i) x[n][i] *= v_rest[i >> 1];
       }
       uint32_t hi[kCols][2], lo[kCols][2];                   // tokens 0..7, 8..15
 #pragma unroll
@@ -713,15 +718,16 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           hi[n][i] = round16<I8>(x[n][2 * i], x[n][2 * i + 1]);
-          lo[n][i] = round16<I8>(x[n][2 * i], x[n][2 * i + 1]);
-          if constexpr (S::kHalves) hi[n][i] = transposed(lc >= 2 ? lo[n][i] : hi[n][i]);
-          else hi[n][i] = transposed(hi[n][i]), lo[n][i] = transposed(lo[n][i]);
+          lo[n][i] = I8 ? 0u : round16<I8>(x[n][2 * i], x[n][2 * i + 1]);
+          if (S::kHalves && lc >= 2) hi[n][i] = lo[n][i];
+          hi[n][i] = transposed(hi[n][i]);
+          if constexpr (!I8 && !S::kHalves) lo[n][i] = transposed(lo[n][i]);
         }
       auto product = [&](int d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
         for (int n = 0; n < kCols; ++n) {
           mma<I8>(acc[d][n], a0, a1, a2, a3, hi[n][0], hi[n][1]);
-          if constexpr (!S::kHalves) mma<I8>(acc[d][n], a0, a1, a2, a3, lo[n][0], lo[n][1]);
+          if constexpr (!I8 && !S::kHalves) mma<I8>(acc[d][n], a0, a1, a2, a3, lo[n][0], lo[n][1]);
         }
       };
 #pragma unroll
@@ -787,7 +793,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       if (!more) asm volatile("cp.async.wait_group 0;" ::: "memory");   // the ring is no longer filled
       __syncwarp();
       const Part<D, NH> part = more ? first_part(warp) : last_part(warp);
-      if (!S::kHalves || lc < 2)
+      if (NH > 4 || lc < 2)
 #pragma unroll
         for (int n = 0; n < kCols; ++n) {
           const int head = 2 * lc + 8 * n;

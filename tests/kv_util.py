@@ -128,17 +128,17 @@ class Case:
                 ds = ds + 2.0 ** -25 * D * abs(scale) * q.abs().amax(-1)[..., None] * k.abs().amax(-1).t()[:, None, :]
             off = (p * torch.expm1(ds)).nan_to_num(nan=0.0)   # a token whose p is 0 has no part, however far off its score is
             # exp2 (2 ulp, and the rounding of its argument, whose size is below 2^7 where p matters: 2^7 h ln 2 of p), p as two numbers of 8
-            # and more bits (2^-17 of p; 8-bit caches: and twice a rounding of its scale), n additions of p and of p v, a few roundings
-            # where parts are joined; numerator and denominator both.
+            # and more bits (2^-17 of p), n additions of p and of p v, a few roundings where parts are joined; numerator and denominator both.
             rel = 2 * (100 * H + 2.0 ** -16 + 2 * H * (n + 64))
             spread = torch.einsum("kgt,tkd->kgd", p, v.abs())
             o = torch.einsum("kgt,tkd->kgd", p, v)
             out[b], lse[b] = o.reshape(-1, D), total.reshape(-1)
             inner = torch.einsum("kgt,tkd->kgd", off, v.abs()) + (off.sum(-1)[..., None] + rel) * spread
             if self.scales[1] is not None:
-                # p times the scale of its value is a pair of binary16 numbers in units of 2^-6 of the row's largest scale: the second is off by half
-                # of their smallest step, 2^-25, at most, whatever p is.  p is relative to the largest score or to one that was up to 2^8 smaller,
+                # p times the scale of its value is a binary16 number in units of 2^-6 of the row's largest scale: off by half a step, 2^-11 of it, or
+                # by half of the smallest, 2^-25, whatever p is.  p is relative to the largest score or to one that was up to 2^8 smaller,
                 # which only makes it larger.  So 2^-31 of the largest scale per code, over the sum of p relative to the largest.
+                inner = inner + 2.0 ** -11 * spread
                 page, at = places(self.table, b, range(first, n), self.page)
                 most = self.scales[1].transpose(1, 2)[page, at].double().abs().amax(0)             # [kv_heads]
                 codes = self.kv[1][page, at].double().abs().sum(0)                                 # [kv_heads, dim]
