@@ -95,6 +95,7 @@ struct AppendParams {
   CacheView cache;
   Rows q, k, v, q_out;
   int n_tokens, n_heads, rotary;     // query heads (0: none); channels that turn
+  int passes;                        // of kThreads over the heads of a token
   bool interleaved;
   const float* cos_sin;
   int n_positions;
@@ -168,48 +169,151 @@ __device__ __forceinline__ void encode(const float (&a)[8], const float (&z)[8],
   }
 }
 
-// An item is the heads of a token that a CTA takes at once (a pass over its heads has several); items are numbered through the tokens, then the
-// passes, and the CTAs take equal runs.  So a thread has the same head of one token after another: where it reads and writes moves by a
-// stride.  A CTA resolves the places of its next kBatch tokens together and copies their angles to shared memory; the row of the next token is
-// asked for before the one at hand is used.  With one CTA for every item, the chain of dependent reads (bounds of the sequences,
-// length, page) before each, 4096 tokens of 192 rows of 128 took 79 us, and 2048 of 96 into 8 bits 34 us.
+// An item is the heads of a token that a CTA takes at once: a pass over its rows (queries, keys, values) has several.
+// A thread's head in a pass, for token t.
+template <int D>
+struct Head {
+  static constexpr int kLanes = D / 16, kRows = kThreads / kLanes;   // of a head of a token; heads of an item
+  bool there, is_q, is_k, turns, apart;
+  uint32_t h, at0, at1;              // its 16 channels, in bytes: two pieces of whole pairs
+  const char* from;
+  uint64_t from_step;
+  char *to_q, *to_cache;
+
+  __device__ __forceinline__ Head(const AppendParams& p, int pass, int t) {
+    const int r = pass * kRows + threadIdx.x / kLanes, i = threadIdx.x % kLanes, kv_heads = p.cache.n_kv_heads;
+    there = r < p.n_heads + 2 * kv_heads, is_q = r < p.n_heads, is_k = !is_q && r < p.n_heads + kv_heads;
+    h = is_q ? r : is_k ? r - p.n_heads : r - p.n_heads - kv_heads;
+    const Rows rows = is_q ? p.q : is_k ? p.k : p.v;
+    turns = (is_q || is_k) && 16 * i < p.rotary, apart = turns && !p.interleaved;
+    at0 = apart ? 16 * i : 32 * i, at1 = apart ? p.rotary + 16 * i : 32 * i + 16;
+    from = reinterpret_cast<const char*>(rows.data + (uint64_t)(uint32_t)t * rows.row + (uint64_t)h * rows.head);
+    from_step = (uint64_t)rows.row * 2;
+    to_q = reinterpret_cast<char*>(p.q_out.data + (uint64_t)(uint32_t)t * p.q_out.row + (uint64_t)h * p.q_out.head);
+    to_cache = static_cast<char*>(const_cast<void*>(is_k ? p.cache.k : p.cache.v)) + (uint64_t)(h * p.cache.head16) * 16;
+  }
+  __device__ __forceinline__ void load(uint4& x0, uint4& x1) const {
+    if (!there) return;
+    x0 = ptx::ld_global(reinterpret_cast<const uint4*>(from + at0));
+    x1 = ptx::ld_global(reinterpret_cast<const uint4*>(from + at1));
+  }
+};
+
+// state of a token: 0 left out, 1 its place is in no page, 2 it has one: `unit` in the cache, in units of 16 bytes, and `scale` in the scales (fewer than
+// 2^30: the codes have less than 2^36 bytes).  All lanes of a warp take part.
+template <int D, bool I8>
+__device__ __forceinline__ void put_row(const AppendParams& p, const Head<D>& head, uint4 x0, uint4 x1, const float* angles, int state, uint32_t unit,
+                                        uint32_t scale) {
+  constexpr int kLanes = Head<D>::kLanes;
+  const int i = threadIdx.x % kLanes;
+  float a[8], z[8];
+  widen(x0, a);
+  widen(x1, z);
+  if (head.turns) {
+    float c[8], s[8];
+    const float4 *cos = reinterpret_cast<const float4*>(angles + 8 * i), *sin = reinterpret_cast<const float4*>(angles + p.rotary / 2 + 8 * i);
+    *reinterpret_cast<float4*>(c) = cos[0], *reinterpret_cast<float4*>(c + 4) = cos[1];
+    *reinterpret_cast<float4*>(s) = sin[0], *reinterpret_cast<float4*>(s + 4) = sin[1];
+    if (head.apart) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) turn(a[k], z[k], c[k], s[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        turn(a[2 * k], a[2 * k + 1], c[k], s[k]);
+        turn(z[2 * k], z[2 * k + 1], c[4 + k], s[4 + k]);
+      }
+    }
+  }
+  if (I8 && __any_sync(0xffffffffu, !head.is_q)) {
+    // the largest of the head, over the lanes that have it
+    float most = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) most = larger(most, larger(fabsf(a[k]), fabsf(z[k])));
+#pragma unroll
+    for (int o = 1; o < kLanes; o <<= 1) most = larger(most, __shfl_xor_sync(0xffffffffu, most, o));
+    if (!head.is_q && head.there && state == 2) {
+      const float step = most == 0.f ? 1.f : __fdiv_rn(most, 127.f);
+      uint32_t codes[4];
+      encode(a, z, step, codes);
+      char* const to = head.to_cache + (uint64_t)unit * 16;
+      *reinterpret_cast<uint2*>(to + head.at0 / 2) = make_uint2(codes[0], codes[1]);
+      *reinterpret_cast<uint2*>(to + head.at1 / 2) = make_uint2(codes[2], codes[3]);
+      if (i == 0) const_cast<float*>(head.is_k ? p.cache.k_scales : p.cache.v_scales)[scale + head.h * p.cache.page_size] = step;
+    }
+  }
+  if (head.there && (head.is_q ? state > 0 : !I8 && state == 2)) {
+    char* const to = head.is_q ? head.to_q : head.to_cache + (uint64_t)unit * 16;
+    *reinterpret_cast<uint4*>(to + head.at0) = narrow(a);
+    *reinterpret_cast<uint4*>(to + head.at1) = narrow(z);
+  }
+}
+
+// A token's position: -1 if it is left out.
+__device__ __forceinline__ int position_of(const AppendParams& p, int t, int b) {
+  const int len = b < 0 ? 0 : ptx::ld_global(p.seq_lens + b);
+  if (len == 0) return -1;
+  const int position = p.starts ? len - ptx::ld_global(p.starts + b + 1) + t : len - 1;
+  if (len > 0 && len <= p.cache.capacity && position >= 0 && position < p.n_positions) return position;
+  note_bad_index(p.status);
+  return -1;
+}
+// Its state, its place in the cache and in the scales.
+__device__ __forceinline__ int place_of(const AppendParams& p, int b, int position, uint32_t& unit, uint32_t& scale) {
+  const uint32_t entry = divide(position, p.cache.by_page), place = position - entry * p.cache.page_size;
+  const uint32_t page = (uint32_t)ptx::ld_global(p.cache.table + (long long)b * p.cache.max_pages + entry);
+  unit = page * p.cache.page16 + place * p.cache.token16;
+  scale = page * (uint32_t)p.cache.n_kv_heads * p.cache.page_size + place;
+  if (page < (uint32_t)p.cache.n_pages) return 2;
+  note_bad_index(p.status);
+  return 1;
+}
+
+// Few items: a CTA for each, which finds the token's place while its row is on its way.
+template <int D, bool I8>
+__global__ void __launch_bounds__(kThreads) kv_append_few_kernel(const AppendParams p) {
+  __shared__ int s_seq;
+  const int t = blockIdx.x;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const Head<D> head(p, blockIdx.y, t);
+  uint4 x0 = make_uint4(0, 0, 0, 0), x1 = x0;
+  head.load(x0, x1);
+  int b = t;
+  if (p.starts) {
+    if (threadIdx.x == 0) s_seq = -1;
+    __syncthreads();
+    for (int k = threadIdx.x; k < p.cache.n_seqs; k += kThreads)
+      if (ptx::ld_global(p.starts + k) <= t && t < ptx::ld_global(p.starts + k + 1)) s_seq = k;
+    __syncthreads();
+    b = s_seq;
+  }
+  const int position = position_of(p, t, b);
+  if (position < 0) return;
+  uint32_t unit, scale;
+  const int state = place_of(p, b, position, unit, scale);
+  put_row<D, I8>(p, head, x0, x1, p.cos_sin + (long long)position * p.rotary, state, unit, scale);
+}
+
+// Many: items are numbered through the tokens, then the passes, and the CTAs take equal runs.  So a thread has the same head of one token
+// after another: where it reads and writes moves by a stride.  A CTA resolves the places of its next kBatch tokens together and copies their
+// angles to shared memory; the row of the next token is asked for before the one at hand is used.  With one CTA for every item 4096 tokens of
+// 192 rows of 128 took 79 us, and 2048 of 96 into 8 bits 34 us.
 template <int D, bool I8>
 __global__ void __launch_bounds__(kThreads, 4) kv_append_kernel(const AppendParams p) {
-  constexpr int kLanes = D / 16, kRows = kThreads / kLanes;    // of a head of a token; heads that a CTA takes at once
-  __shared__ int s_seq[kBatch];
-  __shared__ int s_state[kBatch];                              // of a token: 0 left out, 1 its place is in no page, 2 it has one
-  __shared__ uint32_t s_unit[kBatch], s_scale[kBatch];         // its place in the cache, in units of 16 bytes, and in the scales
+  __shared__ int s_seq[kBatch], s_position[kBatch], s_state[kBatch];
+  __shared__ uint32_t s_unit[kBatch], s_scale[kBatch];
   __shared__ __align__(16) float s_angles[kBatch][D];
-  const int tid = threadIdx.x, i = tid % kLanes;
-  const int kv_heads = p.cache.n_kv_heads, rows = p.n_heads + 2 * kv_heads, passes = (rows + kRows - 1) / kRows;
+  const int tid = threadIdx.x;
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
-  const long long items = (long long)p.n_tokens * passes;
+  const long long items = (long long)p.n_tokens * p.passes;
   const long long first = items * blockIdx.x / gridDim.x, end = items * (blockIdx.x + 1) / gridDim.x;
   int left = (int)(end - first), pass = (int)(first / p.n_tokens), t = (int)(first - (long long)pass * p.n_tokens);
 
   for (; left > 0; ++pass, t = 0) {
-    // ---- this thread's head in this pass
-    const int r = pass * kRows + tid / kLanes;
-    const bool there = r < rows, is_q = r < p.n_heads, is_k = !is_q && r < p.n_heads + kv_heads;
-    const uint32_t h = is_q ? r : is_k ? r - p.n_heads : r - p.n_heads - kv_heads;
-    const Rows from = is_q ? p.q : is_k ? p.k : p.v;
-    const bool turns = (is_q || is_k) && 16 * i < p.rotary, apart = turns && !p.interleaved;
-    // its 16 channels, in bytes: two pieces of whole pairs
-    const uint32_t at0 = apart ? 16 * i : 32 * i, at1 = apart ? p.rotary + 16 * i : 32 * i + 16;
-    const char* src = reinterpret_cast<const char*>(from.data + (uint64_t)(uint32_t)t * from.row + (uint64_t)h * from.head);
-    const uint64_t step_in = (uint64_t)from.row * 2;
-    char* to_q = reinterpret_cast<char*>(p.q_out.data + (uint64_t)(uint32_t)t * p.q_out.row + (uint64_t)h * p.q_out.head);
-    char* const to_cache = static_cast<char*>(const_cast<void*>(is_k ? p.cache.k : p.cache.v)) + (uint64_t)(h * p.cache.head16) * 16;
+    Head<D> head(p, pass, t);
     uint4 x0 = make_uint4(0, 0, 0, 0), x1 = x0;
-    auto load = [&]() {
-      if (!there) return;
-      x0 = ptx::ld_global(reinterpret_cast<const uint4*>(src + at0));
-      x1 = ptx::ld_global(reinterpret_cast<const uint4*>(src + at1));
-      src += step_in;
-    };
-    load();
-
+    head.load(x0, x1);
     for (int tokens = min(left, p.n_tokens - t); tokens > 0;) {
       // ---- the places of the next tokens
       const int n = min(kBatch, tokens);
@@ -223,81 +327,26 @@ __global__ void __launch_bounds__(kThreads, 4) kv_append_kernel(const AppendPara
         }
         __syncthreads();
       }
+      int b = -1, position = -1;
       if (tid < n) {
-        const int b = p.starts ? s_seq[tid] : t + tid;
-        int state = 0, position = 0;
-        const int len = b < 0 ? 0 : ptx::ld_global(p.seq_lens + b);
-        if (len != 0) {
-          position = p.starts ? len - ptx::ld_global(p.starts + b + 1) + t + tid : len - 1;
-          if (len < 0 || len > p.cache.capacity || position < 0 || position >= p.n_positions) {
-            note_bad_index(p.status);
-            position = 0;
-          } else {
-            const uint32_t entry = divide(position, p.cache.by_page), place = position - entry * p.cache.page_size;
-            const uint32_t page = (uint32_t)ptx::ld_global(p.cache.table + (long long)b * p.cache.max_pages + entry);
-            state = page < (uint32_t)p.cache.n_pages ? 2 : 1;
-            if (state == 1) note_bad_index(p.status);
-            s_unit[tid] = page * p.cache.page16 + place * p.cache.token16;
-            s_scale[tid] = page * (uint32_t)kv_heads * p.cache.page_size + place;   // (fewer than 2^30: the codes have less than 2^36 bytes)
-          }
-        }
-        s_state[tid] = state;
-        s_seq[tid] = position;
+        b = p.starts ? s_seq[tid] : t + tid;
+        position = position_of(p, t + tid, b);
+        s_position[tid] = max(position, 0);
       }
       __syncthreads();
-      for (int k = tid; k < n * (p.rotary / 4); k += kThreads) {
-        const int token = k / (p.rotary / 4), e = k % (p.rotary / 4);
-        reinterpret_cast<float4*>(s_angles[token])[e] =
-            ptx::ld_global(reinterpret_cast<const float4*>(p.cos_sin + (long long)s_seq[token] * p.rotary) + e);
-      }
+      if (tid < n) s_state[tid] = position < 0 ? 0 : place_of(p, b, position, s_unit[tid], s_scale[tid]);
+      for (int token = tid / Head<D>::kLanes; token < n; token += Head<D>::kRows)
+        for (int e = tid % Head<D>::kLanes; e < p.rotary / 4; e += Head<D>::kLanes)
+          reinterpret_cast<float4*>(s_angles[token])[e] =
+              ptx::ld_global(reinterpret_cast<const float4*>(p.cos_sin + (long long)s_position[token] * p.rotary) + e);
       __syncthreads();
 
       for (int e = 0; e < n; ++e) {
-        float a[8], z[8];
-        widen(x0, a);
-        widen(x1, z);
-        if (--tokens > 0) load();
-        if (turns) {
-          float c[8], s[8];
-          const float4* angles = reinterpret_cast<const float4*>(&s_angles[e][8 * i]);
-          *reinterpret_cast<float4*>(c) = angles[0], *reinterpret_cast<float4*>(c + 4) = angles[1];
-          angles = reinterpret_cast<const float4*>(&s_angles[e][p.rotary / 2 + 8 * i]);
-          *reinterpret_cast<float4*>(s) = angles[0], *reinterpret_cast<float4*>(s + 4) = angles[1];
-          if (apart) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) turn(a[k], z[k], c[k], s[k]);
-          } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              turn(a[2 * k], a[2 * k + 1], c[k], s[k]);
-              turn(z[2 * k], z[2 * k + 1], c[4 + k], s[4 + k]);
-            }
-          }
-        }
-        const int state = s_state[e];
-        if (I8 && __any_sync(0xffffffffu, !is_q)) {
-          // the largest of the head, over the lanes that have it (all lanes of the warp take part)
-          float most = 0.f;
-#pragma unroll
-          for (int k = 0; k < 8; ++k) most = larger(most, larger(fabsf(a[k]), fabsf(z[k])));
-#pragma unroll
-          for (int o = 1; o < kLanes; o <<= 1) most = larger(most, __shfl_xor_sync(0xffffffffu, most, o));
-          if (!is_q && there && state == 2) {
-            const float step = most == 0.f ? 1.f : __fdiv_rn(most, 127.f);
-            uint32_t codes[4];
-            encode(a, z, step, codes);
-            char* const to = to_cache + (uint64_t)s_unit[e] * 16;
-            *reinterpret_cast<uint2*>(to + at0 / 2) = make_uint2(codes[0], codes[1]);
-            *reinterpret_cast<uint2*>(to + at1 / 2) = make_uint2(codes[2], codes[3]);
-            if (i == 0) const_cast<float*>(is_k ? p.cache.k_scales : p.cache.v_scales)[s_scale[e] + h * p.cache.page_size] = step;
-          }
-        }
-        if (there && (is_q ? state > 0 : !I8 && state == 2)) {
-          char* const to = is_q ? to_q : to_cache + (uint64_t)s_unit[e] * 16;
-          *reinterpret_cast<uint4*>(to + at0) = narrow(a);
-          *reinterpret_cast<uint4*>(to + at1) = narrow(z);
-        }
-        to_q += (uint64_t)p.q_out.row * 2;
+        const uint4 y0 = x0, y1 = x1;
+        head.from += head.from_step;
+        if (--tokens > 0) head.load(x0, x1);
+        put_row<D, I8>(p, head, y0, y1, s_angles[e], s_state[e], s_unit[e], s_scale[e]);
+        head.to_q += (uint64_t)p.q_out.row * 2;
       }
       t += n;
       left -= n;
@@ -306,13 +355,10 @@ __global__ void __launch_bounds__(kThreads, 4) kv_append_kernel(const AppendPara
 }
 
 template <int D, bool I8>
-int launch(const AppendParams& p, cudaStream_t st) {
-  constexpr int kRows = kThreads / (D / 16);
-  const int rows = p.n_heads + 2 * p.cache.n_kv_heads, passes = (rows + kRows - 1) / kRows;
+int launch(AppendParams& p, cudaStream_t st) {
+  p.passes = (p.n_heads + 2 * p.cache.n_kv_heads + Head<D>::kRows - 1) / Head<D>::kRows;
+  const long long items = (long long)p.n_tokens * p.passes, sms = sm_count_or(148);
   cudaLaunchConfig_t cfg = {};
-  // As many CTAs as can be at once; or one for each item, if that is not much more: 512 tokens of 96 rows 12.6 us and 10.3.
-  const long long items = (long long)p.n_tokens * passes, sms = sm_count_or(148);
-  cfg.gridDim = dim3((unsigned)(items <= 12 * sms ? items : 4 * sms), 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -320,12 +366,19 @@ int launch(const AppendParams& p, cudaStream_t st) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  PEQA_CUDA(cudaLaunchKernelEx(&cfg, kv_append_kernel<D, I8>, p));
+  // 256 tokens of 80 rows (768 items): a CTA for each 3.4 us, runs of items 5.4; 512 of 96 (1536): 6.7 and 7.8; 2048 of 96 into 8 bits 34 and 23.
+  if (items <= 12 * sms && p.passes <= 65535) {
+    cfg.gridDim = dim3(p.n_tokens, p.passes, 1);
+    PEQA_CUDA(cudaLaunchKernelEx(&cfg, kv_append_few_kernel<D, I8>, p));
+  } else {
+    cfg.gridDim = dim3((unsigned)min(items, 4 * sms), 1, 1);   // as many as can be at once
+    PEQA_CUDA(cudaLaunchKernelEx(&cfg, kv_append_kernel<D, I8>, p));
+  }
   return PEQA_OK;
 }
 
 template <bool I8>
-int launch_dim(const AppendParams& p, int dim, cudaStream_t st) {
+int launch_dim(AppendParams& p, int dim, cudaStream_t st) {
   switch (dim) {
     case 64: return launch<64, I8>(p, st);
     case 128: return launch<128, I8>(p, st);
