@@ -516,7 +516,7 @@ typedef struct {
  * cache are finite; a head with a value that is not gets a scale that is not either.
  *   q      in   [n_tokens, n_heads, head_dim]; NULL together with q_out: keys and values alone
  *   k, v   in   [n_tokens, n_kv_heads, head_dim]
- *   q_out  out  [n_tokens, n_heads, head_dim]; q itself (the same strides too) or memory apart from it
+ *   q_out  out  [n_tokens, n_heads, head_dim]; q itself (the same strides too) or memory apart from it, and apart from k and v
  *   cos_sin  in  fp32 [n_positions, R]
  * No two new tokens may have one place: no page number stands twice among those that
  * the new tokens of a call are written through.  No workspace.  What the kernel finds
@@ -535,12 +535,14 @@ int peqa_kv_append(const peqa_kv_cache_t* cache, const peqa_rows_t* q, int n_hea
  * A sequence of length 0 gets zeros, and -inf as lse.  What lies behind a sequence's end in its
  * last page, or before the window, is not read into the result.
  *   q    in   bf16 [n_seqs, n_heads, head_dim]
- *   out  out  bf16 [n_seqs, n_heads, head_dim], dense (binary32 sums, rounded to nearest even)
+ *   out  out  bf16 [n_seqs, n_heads, head_dim], dense (binary32 sums, rounded to nearest even); apart from q, whose
+ *             rows are read by several warps, the last perhaps when the first has written
  *   lse  out  fp32 [n_seqs, n_heads], log of the sum of exp(scale * <q, k_t>); may be NULL
  * workspace: peqa_attn_workspace_bytes(cache, n_heads), 256-byte aligned, in use until the call's
  * work has ended; its contents before do not matter.  The work is dealt out evenly whatever the lengths are;
  * the same lengths on the same device give the same bits.  For a page number or a length out
- * of range (PEQA_ERR_DEVICE_INDEX) the sequence's outputs are undefined, the others are not.
+ * of range (PEQA_ERR_DEVICE_INDEX) the sequence's outputs are undefined, the others are not.  With an 8-bit cache
+ * scale * |q| is to be below 2^100 (its sums are scaled back by that and 2^24 in binary32).
  */
 int peqa_attn_decode(const peqa_kv_cache_t* cache, const peqa_rows_t* q, int n_heads, const int32_t* seq_lens,
                      float scale, int window, void* out_bf16, float* lse, void* workspace, size_t workspace_bytes,

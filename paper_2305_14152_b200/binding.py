@@ -571,7 +571,7 @@ def kv_append(cache: KVCache, q, k: torch.Tensor, v: torch.Tensor, cos_sin: torc
 def attn_decode(cache: KVCache, q: torch.Tensor, seq_lens: torch.Tensor, scale: float | None = None, window: int = 0, out=None,
                 workspace=None, return_lse: bool = False):
     """Attention of one new token per sequence to its cached tokens, or to the last ``window`` of them; q bf16
-    [n_seqs, n_heads, head_dim], scale 1/sqrt(head_dim) unless given.  Sequences of length 0 get zeros (and -inf as lse).
+    [n_seqs, n_heads, head_dim], scale 1/sqrt(head_dim) unless given; out, if given, apart from q.  Sequences of length 0 get zeros (and -inf as lse).
     Returns out bf16 [n_seqs, n_heads, head_dim], with return_lse also log(sum(exp(scores))) fp32 [n_seqs, n_heads]."""
     return (_native or _load_native()).attn_decode(cache, q, seq_lens, scale, window, out, workspace, return_lse)
 

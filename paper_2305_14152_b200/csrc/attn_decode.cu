@@ -206,8 +206,10 @@ struct Cursor {
   }
   // true: at another row
   __device__ __forceinline__ bool next(const AttnParams& p) {
-    t0 += kTile;
-    if (--left > 0) return false;
+    if (--left > 0) {
+      t0 += kTile;
+      return false;
+    }
     if (++r >= p.rows_of_seq) {
       r = 0;
       do {
@@ -807,7 +809,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
             part.two(16 * d + (I8 ? 2 * lr + 1 : lr + 8), head) = make_float2(acc[d][n][2] * v_ref, acc[d][n][3] * v_ref);
           }
         }
-      if (lane == 0) s_head[2 * warp + (more ? 0 : 1)] = 
+      if (lane == 0)
+        s_head[2 * warp + (more ? 0 : 1)] =
             make_int4(at.b * p.rows_of_seq + at.r, (from_start ? 1 : 0) + (to_end ? 2 : 0) + heads * 4, at.b * p.n_heads + h0, 0);
     };
 
@@ -1080,7 +1083,8 @@ extern "C" int peqa_attn_decode(const peqa_kv_cache_t* c, const peqa_rows_t* q, 
   // A CTA for every row needs no second kernel, but is as long as the longest row.  Rows of T tiles, rows x T: dealt out evenly / a CTA each, us:
   // 8 x 9 9.5 / 8.0, 8 x 16 9.5 / 11.0, 8 x 64 10.4 / 13.9; 32 x 9 9.0 / 7.4, 32 x 64 12.7 / 12.5; 128 x 9 10.0 / 7.4, 128 x 64 19.9 / 15.9, 128 x
   // 128 26.4 / 22.8 (four sequences of uneven lengths).  What is known here of the lengths is what they can be at most.
-  const long long ctas = attn_ctas(), most = (min(p.cache.capacity, window > 0 ? window + kTile - 1 : p.cache.capacity) + kTile - 1) / kTile;
+  const long long ctas = attn_ctas(), capacity = p.cache.capacity;
+  const long long most = (min(capacity, window > 0 ? window + kTile - 1ll : capacity) + kTile - 1) / kTile;
   p.row_each = rows <= ctas && (most <= 9 || (4 * rows >= ctas && most * (ctas - rows) <= 48 * ctas && most <= 129));
   p.scale_log2 = scale * kLog2e;
   p.window = window;

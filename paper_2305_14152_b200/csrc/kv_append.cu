@@ -358,6 +358,7 @@ template <int D, bool I8>
 int launch(AppendParams& p, cudaStream_t st) {
   p.passes = (p.n_heads + 2 * p.cache.n_kv_heads + Head<D>::kRows - 1) / Head<D>::kRows;
   const long long items = (long long)p.n_tokens * p.passes, sms = sm_count_or(148);
+  if (items > 0x7fffffffll) return PEQA_ERR_TOO_LARGE;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.stream = st;

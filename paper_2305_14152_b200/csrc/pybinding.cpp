@@ -492,6 +492,9 @@ PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
   } else {
     out = values(a[5], at::kBFloat16, (int64_t)q.rows * q.heads * cache.c.head_dim, "out");
     if (out.dim() != 3 || out.size(0) != q.rows || out.size(1) != q.heads) refuse("out", "q's shape");
+    const char *o = static_cast<const char*>(out.data_ptr()), *first = static_cast<const char*>(q.r.data);
+    const int64_t last = q.rows > 0 && q.heads > 0 ? (q.rows - 1) * q.r.row_stride + (q.heads - 1) * q.r.head_stride + cache.c.head_dim : 0;
+    if (o < first + 2 * last && first < o + out.nbytes()) refuse("out", "memory apart from q");
   }
   const int with_lse = PyObject_IsTrue(a[7]);
   if (with_lse < 0) fail();

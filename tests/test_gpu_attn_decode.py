@@ -273,3 +273,35 @@ def test_refusals():
     assert status(binding.KVCache(same(cache.k), same(cache.v), cache.page_table), q, lens) == -3
     binding.check_status()
     attend(cache, q, lens)
+
+
+@pytest.mark.gpu
+def test_outputs_over_the_queries_are_refused():
+    """Several warps read a row of queries, the last perhaps when the first has written its outputs."""
+    case = Case(16, [100, 200], 8, 2, 128, 16)
+    cache, lens = case.on_gpu(), case.lens()
+    pool = torch.zeros((5, 8, 128), dtype=torch.bfloat16, device="cuda")
+    pool[1:3] = case.q.cuda()
+    q = pool[1:3]
+    for out in (q, pool[0:2], pool[2:4]):
+        with pytest.raises(ValueError, match="out: expected memory apart from q"):
+            binding.attn_decode(cache, q, lens, out=out)
+    assert torch.equal(binding.attn_decode(cache, q, lens, out=pool[3:5]), binding.attn_decode(cache, case.q.cuda(), lens))
+    assert torch.equal(q, case.q.cuda())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.int8])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("window", [5, 33, 1000, 2 ** 31 - 1])
+def test_windows_where_the_work_is_dealt_out(dtype, dim, window):
+    """More rows than CTAs; first and last tiles are cut by the window, the end or both."""
+    lengths = [1500, 0, 1, 999, 1001] + [16 * i + i % 17 for i in range(60)]
+    check(Case(dim + window % 64, lengths, 6, 3, dim, 16 if dim != 256 else 48, dtype, window=window))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads,kv_heads,n", [(8, 2, 74), (8, 2, 75), (4, 1, 37), (4, 1, 36)])
+def test_about_as_many_rows_as_ctas(heads, kv_heads, n):
+    lengths = [(37 * i) % 300 for i in range(n)]
+    check(Case(n, lengths, heads, kv_heads, 64, 16))

@@ -272,3 +272,60 @@ def test_refusals():
     assert err.value.status == -3
     assert torch.equal(cache.k.cpu(), batch.cache[0]) and torch.equal(cache.v.cpu(), batch.cache[1])
     binding.check_status()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.int8])
+@pytest.mark.parametrize("what", ["in place", "page too high", "page below 0", "length too high", "length below 0", "length below the new tokens"])
+def test_runs_of_many_tokens(dtype, what):
+    """In place, and with one sequence that is out of range (a page: some of its tokens)."""
+    batch = Batch(11, [2000, 300, 1500], [1900, 290, 1400], 4, 2, 128, 16, dtype, behind=3)
+    cache, (q, k, v, cos_sin, lens, starts) = batch.on_gpu(), batch.args()
+    good = batch.on_gpu()
+    want = binding.kv_append(good, q, k, v, cos_sin, lens, starts)
+    binding.check_status()
+    if what == "in place":
+        kept = q.clone()
+        binding.kv_append(cache, q, k, v, cos_sin, lens, starts, q_out=q)
+        assert torch.equal(q[:-3], want[:-3]) and torch.equal(q[-3:], kept[-3:])
+    else:
+        if what.startswith("page"):
+            cache.page_table[1, 5] = cache.k.shape[0] if what.endswith("high") else -1
+        else:
+            lens[1] = {"h": cache.page_table.shape[1] * 16 + 1, "0": -25, "s": 289}[what[-1]]
+        got = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+        binding.kv_append(cache, q, k, v, cos_sin, lens, starts, q_out=got)
+        with pytest.raises(binding.PeqaError) as err:
+            binding.check_status()
+        assert err.value.status == -10
+        for first, end in ((0, 1900), (2190, 3590)):
+            assert torch.equal(got[first:end], want[first:end])
+        if what.startswith("length") and what[-1] != "s":
+            assert (got[1900:2190] == 7).all()
+    for b in (0, 2) if what != "in place" else (0, 1, 2):
+        page, at = places(batch.table, b, range(batch.lengths[b]), 16)
+        assert torch.equal(cache.k[page, at], good.k[page, at]) and torch.equal(cache.v[page, at], good.v[page, at])
+    binding.check_status()
+
+
+@pytest.mark.gpu
+def test_captured_pieces_follow_their_starts():
+    """A captured call of a fixed number of rows, replayed with other pieces and lengths."""
+    batch = Batch(12, [90, 80, 100], [20, 10, 10], 6, 2, 64, 16, behind=8)
+    q, k, v, cos_sin, lens, starts = batch.args()
+    cache, q_out = batch.on_gpu(), torch.zeros(q.shape, dtype=torch.bfloat16, device="cuda")
+    binding.kv_append(cache, q, k, v, cos_sin, lens, starts, q_out=q_out)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        binding.kv_append(cache, q, k, v, cos_sin, lens, starts, q_out=q_out)
+    for lengths, bounds in (([33, 0, 48], [0, 33, 33, 48]), ([34, 80, 49], [5, 6, 40, 41]), ([90, 1, 100], [0, 20, 20, 20])):
+        lens.copy_(torch.tensor(lengths, dtype=torch.int32))
+        starts.copy_(torch.tensor(bounds, dtype=torch.int32))
+        q_out.zero_()
+        for x, y in zip((cache.k, cache.v), batch.cache):
+            x.copy_(y)
+        g.replay()
+        fresh = batch.on_gpu()
+        want = binding.kv_append(fresh, q, k, v, cos_sin, lens, starts)
+        assert torch.equal(q_out, want) and torch.equal(cache.k, fresh.k) and torch.equal(cache.v, fresh.v)
+    binding.check_status()
