@@ -234,8 +234,6 @@ struct Part {
   __device__ __forceinline__ float2& two(int d, int head) const { return *reinterpret_cast<float2*>(at + d * NH + head); }
   // four heads of a channel, by their place
   __device__ __forceinline__ float4& four(int i) const { return reinterpret_cast<float4*>(at)[i]; }
-  __device__ __forceinline__ float2& most(int head) const { return *reinterpret_cast<float2*>(at + D * NH + head); }
-  __device__ __forceinline__ float2& total(int head) const { return *reinterpret_cast<float2*>(at + (D + 1) * NH + head); }
   __device__ __forceinline__ float4& most4(int head) const { return *reinterpret_cast<float4*>(at + D * NH + head); }
   __device__ __forceinline__ float4& total4(int head) const { return *reinterpret_cast<float4*>(at + (D + 1) * NH + head); }
 };
@@ -280,7 +278,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ int s_scan[kThreads];
   __shared__ int s_warp[S::kWarps];
-  __shared__ __align__(16) float s_weight[32][NH], s_most[32][NH];   // of a part and head
+  __shared__ __align__(16) float s_weight[32][NH], s_most[32][NH], s_total[32][NH];   // of a part and head; s_most: at last of its row
   __shared__ int4 s_head[2 * S::kWarps];   // of a warp's parts: row (-1: none), 1 if it begins its row + 2 if it ends it + 4 times its heads, its first head's place in out
   __shared__ __align__(8) uint64_t s_full[S::WHOLE ? S::kWarps * S::kUnits : 1];
   __shared__ int s_abort[2];               // as the bounded waits of sm100_ptx.cuh have it
@@ -505,23 +503,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       get += S::kUnit, get_scales += 64, get_full += 8;
       if (get == ring + S::kRing) get = ring, get_scales = scales_of, get_full = full_of, get_phase ^= 1;
     };
-    look_up(true, true);
-#pragma unroll 1
-    for (int i = 0; i < S::kUnits / 2; ++i) {
-      issue_keys();
-      issue_values();
-    }
-
     uint32_t q[kCols][D / 16][2];                            // head lr (+ 8): two and two channels for each product
-    float to_log2[kCols][2];                                 // of a product of the tensor cores; here and below: heads 2 lc, 2 lc + 1 (+ 8)
-    float q_bias[kCols][2];                                  // I8: what the sums of products begin with
-    float most[kCols][2], sum[kCols][2];                     // sum: of this lane's tokens
-    float base[kCols][2];                                    // most, or 0 where there is none
-    float acc[D / 16][kCols][4];                             // two channels of each of the two heads
-    float v_ref = 1.f, inv_ref = 1.f;                        // I8: acc is in units of it
-    bool from_start;
-
-    auto begin_row = [&]() {
+    auto load_q = [&]() {
       int heads;
       const int h0 = first_head<NH>(p, at.r, heads);
 #pragma unroll
@@ -539,6 +522,27 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
           }
           q[n][s][0] = x.x, q[n][s][1] = x.y;
         }
+      }
+    };
+    load_q();                                // before the first copies: behind those of all CTAs they come 2 us later (16 sequences of up to 300 tokens 8.9 -> 8.6 us)
+    look_up(true, true);
+#pragma unroll 1
+    for (int i = 0; i < S::kUnits / 2; ++i) {
+      issue_keys();
+      issue_values();
+    }
+
+    float to_log2[kCols][2];                                 // of a product of the tensor cores; here and below: heads 2 lc, 2 lc + 1 (+ 8)
+    float q_bias[kCols][2];                                  // I8: what the sums of products begin with
+    float most[kCols][2], sum[kCols][2];                     // sum: of this lane's tokens
+    float base[kCols][2];                                    // most, or 0 where there is none
+    float acc[D / 16][kCols][4];                             // two channels of each of the two heads
+    float v_ref = 1.f, inv_ref = 1.f;                        // I8: acc is in units of it
+    bool from_start;
+
+    auto begin_row = [&]() {
+#pragma unroll
+      for (int n = 0; n < kCols; ++n) {
         float scale = p.scale_log2, bias = 0.f;
         if constexpr (I8) {
           // bf16 as binary16: times a power of two that brings the head's largest below 4.  What becomes subnormal there is
@@ -800,8 +804,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
         for (int n = 0; n < kCols; ++n) {
           const int head = 2 * lc + 8 * n;
           if (lr == 0) {
-            part.most(head) = make_float2(most[n][0], most[n][1]);
-            part.total(head) = make_float2(sum[n][0], sum[n][1]);
+            *reinterpret_cast<float2*>(&s_most[2 * warp + (more ? 0 : 1)][head]) = make_float2(most[n][0], most[n][1]);
+            *reinterpret_cast<float2*>(&s_total[2 * warp + (more ? 0 : 1)][head]) = make_float2(sum[n][0], sum[n][1]);
           }
 #pragma unroll
           for (int d = 0; d < D / 16; ++d) {
@@ -817,7 +821,10 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     bool fresh = true;
 #pragma unroll 1
     for (int i = 0; i < count && sound; ++i) {
-      if (fresh) begin_row();
+      if (fresh) {
+        if (i > 0) load_q();
+        begin_row();
+      }
       add_tile();
       fresh = at.left == 1;
       if (fresh || i + 1 == count) end_row(fresh, i + 1 < count);
@@ -842,7 +849,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   const uint32_t parts_of_own = __match_any_sync(0xffffffffu, own.x);
   for (int head = warp; head < NH; head += S::kWarps) {
     float m = kNegInf;
-    if (own.x >= 0) m = part_of(lane).at[NH * D + head];
+    if (own.x >= 0) m = s_most[lane][head];
     // the largest of the row's: as whole numbers that have the order of the floats
     const int bits = __float_as_int(m), key = bits ^ (bits >> 31 & 0x7fffffff);
     const int most_key = __reduce_max_sync(parts_of_own, key);
@@ -881,10 +888,9 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
         const int i = of ? __ffs(of) - 1 : leader;
         const float on = of ? 1.f : 0.f;
         of &= of - 1;
-        const Part<D, NH> part = part_of(i);
         f[u] = *reinterpret_cast<const float4*>(&s_weight[i][head]) * make_float4(on, on, on, on);
-        t[u] = part.total4(head);
-        v[u] = part.four(place);
+        t[u] = *reinterpret_cast<const float4*>(&s_total[i][head]);
+        v[u] = part_of(i).four(place);
       }
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) total_p = total_p + f[u] * t[u], sums = sums + f[u] * v[u];
