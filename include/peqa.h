@@ -514,7 +514,8 @@ typedef struct {
  * the binary32 values: scale = max|y| / 127 over the head (1 where all are 0),
  * code = rint(y / scale), in IEEE binary32.  v is not rotated.  Inputs of an 8-bit
  * cache are finite; a head with a value that is not gets a scale that is not either.
- *   q      in   [n_tokens, n_heads, head_dim]; NULL together with q_out: keys and values alone
+ *   q      in   [n_tokens, n_heads, head_dim]; NULL together with q_out: keys and values alone.  n_heads + 2 n_kv_heads is at most
+ *               2^18 (else PEQA_ERR_TOO_LARGE)
  *   k, v   in   [n_tokens, n_kv_heads, head_dim]
  *   q_out  out  [n_tokens, n_heads, head_dim]; q itself (the same strides too) or memory apart from it, and apart from k and v
  *   cos_sin  in  fp32 [n_positions, R]

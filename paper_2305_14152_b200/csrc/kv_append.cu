@@ -83,8 +83,7 @@ int check_rows(const peqa_rows_t* r, int rows, int heads, int dim, bool written)
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kBatch = 16;             // tokens whose places are resolved together
+constexpr int kThreads = 128;
 
 struct Rows {
   uint16_t* data;
@@ -249,6 +248,31 @@ __device__ __forceinline__ void put_row(const AppendParams& p, const Head<D>& he
   }
 }
 
+// The sequence of a row: the first that ends behind it, if it has begun there, else -1.  By a warp, 32 ends at a time ...
+__device__ __forceinline__ int sequence_by_warp(const AppendParams& p, int t) {
+  if (!p.starts) return t;
+  int lo = 0, n = p.cache.n_seqs;            // among n sequences from lo on
+  for (;;) {
+    const int step = (n + 31) / 32;
+    const uint32_t end = min(lo + ((threadIdx.x & 31) + 1) * step, (uint32_t)(lo + n));
+    const int before = __popc(__ballot_sync(0xffffffffu, ptx::ld_global(p.starts + end) <= t)) * step;
+    if (before >= n) return -1;
+    lo += before, n = min(step, n - before);
+    if (step == 1) break;
+  }
+  return ptx::ld_global(p.starts + lo) <= t && t < ptx::ld_global(p.starts + lo + 1) ? lo : -1;
+}
+// ... and by a thread, for many rows at once.
+__device__ __forceinline__ int sequence_of(const AppendParams& p, int t) {
+  if (!p.starts) return t;
+  int lo = 0, hi = p.cache.n_seqs;
+  while (lo < hi) {
+    const int mid = lo + (hi - lo) / 2;
+    if (ptx::ld_global(p.starts + mid + 1) <= t) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo < p.cache.n_seqs && ptx::ld_global(p.starts + lo) <= t ? lo : -1;
+}
 // A token's position: -1 if it is left out.
 __device__ __forceinline__ int position_of(const AppendParams& p, int t, int b) {
   const int len = b < 0 ? 0 : ptx::ld_global(p.seq_lens + b);
@@ -269,38 +293,31 @@ __device__ __forceinline__ int place_of(const AppendParams& p, int b, int positi
   return 1;
 }
 
-// Few items: a CTA for each, which finds the token's place while its row is on its way.
+// A CTA for each item, which finds the token's place while its row is on its way.  (Of 128 threads: with 256, 512 tokens of 96 rows of 128
+// 6.7 us, now 6.1.  A search of all `starts` for the row's sequence by the CTA's threads together: 4096 tokens of 80 rows in 1024 pieces 39.2 us, by
+// warps 37.8, by each thread alone 44.1.)
 template <int D, bool I8>
-__global__ void __launch_bounds__(kThreads) kv_append_few_kernel(const AppendParams p) {
-  __shared__ int s_seq;
+__global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams p) {
   const int t = blockIdx.x;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const Head<D> head(p, blockIdx.y, t);
   uint4 x0 = make_uint4(0, 0, 0, 0), x1 = x0;
   head.load(x0, x1);
-  int b = t;
-  if (p.starts) {
-    if (threadIdx.x == 0) s_seq = -1;
-    __syncthreads();
-    for (int k = threadIdx.x; k < p.cache.n_seqs; k += kThreads)
-      if (ptx::ld_global(p.starts + k) <= t && t < ptx::ld_global(p.starts + k + 1)) s_seq = k;
-    __syncthreads();
-    b = s_seq;
-  }
-  const int position = position_of(p, t, b);
+  const int b = sequence_by_warp(p, t), position = position_of(p, t, b);
   if (position < 0) return;
   uint32_t unit, scale;
   const int state = place_of(p, b, position, unit, scale);
   put_row<D, I8>(p, head, x0, x1, p.cos_sin + (long long)position * p.rotary, state, unit, scale);
 }
 
-// Many: items are numbered through the tokens, then the passes, and the CTAs take equal runs.  So a thread has the same head of one token
-// after another: where it reads and writes moves by a stride.  A CTA resolves the places of its next kBatch tokens together and copies their
-// angles to shared memory; the row of the next token is asked for before the one at hand is used.  With one CTA for every item 4096 tokens of
-// 192 rows of 128 took 79 us, and 2048 of 96 into 8 bits 34 us.
-template <int D, bool I8>
-__global__ void __launch_bounds__(kThreads, 4) kv_append_kernel(const AppendParams p) {
-  __shared__ int s_seq[kBatch], s_position[kBatch], s_state[kBatch];
+// Many items of an 8-bit cache, whose codes take more instructions than the copies leave time for: items are numbered through the
+// tokens, then the passes, and the CTAs take equal runs.  So a thread has the same head of one token after another: where it reads and writes moves by
+// a stride.  A CTA resolves the places of its next kBatch tokens together (4096 tokens of 80 rows: by eights 39.3 us, 16 36.6, 32 34.0) and copies
+// their angles to shared memory; the row of the next token is asked for before the one at hand is used.
+template <int D>
+__global__ void __launch_bounds__(kThreads, 8) kv_append_runs_kernel(const AppendParams p) {
+  constexpr int kBatch = D <= 64 ? 64 : D <= 128 ? 32 : 16;    // tokens whose places are resolved together
+  __shared__ int s_position[kBatch], s_state[kBatch];
   __shared__ uint32_t s_unit[kBatch], s_scale[kBatch];
   __shared__ __align__(16) float s_angles[kBatch][D];
   const int tid = threadIdx.x;
@@ -318,18 +335,9 @@ __global__ void __launch_bounds__(kThreads, 4) kv_append_kernel(const AppendPara
       // ---- the places of the next tokens
       const int n = min(kBatch, tokens);
       __syncthreads();                                         // those of the ones before have been read
-      if (p.starts) {
-        if (tid < kBatch) s_seq[tid] = -1;
-        __syncthreads();
-        for (int k = tid; k < p.cache.n_seqs; k += kThreads) {
-          const int lo = max(ptx::ld_global(p.starts + k), t), hi = min(ptx::ld_global(p.starts + k + 1), t + n);
-          for (int e = lo; e < hi; ++e) s_seq[e - t] = k;
-        }
-        __syncthreads();
-      }
       int b = -1, position = -1;
       if (tid < n) {
-        b = p.starts ? s_seq[tid] : t + tid;
+        b = sequence_of(p, t + tid);
         position = position_of(p, t + tid, b);
         s_position[tid] = max(position, 0);
       }
@@ -345,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, 4) kv_append_kernel(const AppendPara
         const uint4 y0 = x0, y1 = x1;
         head.from += head.from_step;
         if (--tokens > 0) head.load(x0, x1);
-        put_row<D, I8>(p, head, y0, y1, s_angles[e], s_state[e], s_unit[e], s_scale[e]);
+        put_row<D, true>(p, head, y0, y1, s_angles[e], s_state[e], s_unit[e], s_scale[e]);
         head.to_q += (uint64_t)p.q_out.row * 2;
       }
       t += n;
@@ -360,6 +368,7 @@ int launch(AppendParams& p, cudaStream_t st) {
   const long long items = (long long)p.n_tokens * p.passes, sms = sm_count_or(148);
   if (items > 0x7fffffffll) return PEQA_ERR_TOO_LARGE;
   cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(p.n_tokens, p.passes, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -367,14 +376,15 @@ int launch(AppendParams& p, cudaStream_t st) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  // 256 tokens of 80 rows (768 items): a CTA for each 3.4 us, runs of items 5.4; 512 of 96 (1536): 6.7 and 7.8; 2048 of 96 into 8 bits 34 and 23.
-  if (items <= 12 * sms && p.passes <= 65535) {
-    cfg.gridDim = dim3(p.n_tokens, p.passes, 1);
-    PEQA_CUDA(cudaLaunchKernelEx(&cfg, kv_append_few_kernel<D, I8>, p));
-  } else {
-    cfg.gridDim = dim3((unsigned)min(items, 4 * sms), 1, 1);   // as many as can be at once
-    PEQA_CUDA(cudaLaunchKernelEx(&cfg, kv_append_kernel<D, I8>, p));
-  }
+  // A CTA for each item / runs of items, us.  8 bits: 700 tokens of 96 rows of 128 (4200 items) 9.7 / 11.4, 1400 (8400) 18.3 / 18.1, 2600 31.5 / 28.6; 1400 of
+  // 80 rows 14.5 / 15.2, 1700 (8500) 16.9 / 16.7, 4000 35.3 / 31.9.  bf16: 4000 of 96 37.6 / 38.6, 4096 of 192 71.0 / 73.3, of 96 rows of 64 21.4 / 22.7.
+  if constexpr (I8)
+    if (items > 56 * sms) {
+      cfg.gridDim = dim3((unsigned)min(items, 8 * sms), 1, 1);   // as many as can be at once
+      PEQA_CUDA(cudaLaunchKernelEx(&cfg, kv_append_runs_kernel<D>, p));
+      return PEQA_OK;
+    }
+  PEQA_CUDA(cudaLaunchKernelEx(&cfg, kv_append_kernel<D, I8>, p));
   return PEQA_OK;
 }
 
@@ -406,7 +416,7 @@ extern "C" int peqa_kv_append(const peqa_kv_cache_t* c, const peqa_rows_t* q, in
   if (n_tokens < 1 || n_positions < 1 || (!starts && n_tokens != c->n_seqs)) return PEQA_ERR_BAD_SHAPE;
   if (rotary_dim < 16 || rotary_dim % 16 != 0 || rotary_dim > c->head_dim) return PEQA_ERR_BAD_SHAPE;
   if (q && n_heads < 1) return PEQA_ERR_BAD_SHAPE;
-  if (n_heads > (1 << 20) || c->n_kv_heads > (1 << 20)) return PEQA_ERR_TOO_LARGE;
+  if ((q ? n_heads : 0) + 2ll * c->n_kv_heads > (1 << 18)) return PEQA_ERR_TOO_LARGE;
   if (q) {
     PEQA_TRY(check_rows(q, n_tokens, n_heads, c->head_dim, false));
     PEQA_TRY(check_rows(q_out, n_tokens, n_heads, c->head_dim, true));

@@ -329,3 +329,62 @@ def test_captured_pieces_follow_their_starts():
         want = binding.kv_append(fresh, q, k, v, cos_sin, lens, starts)
         assert torch.equal(q_out, want) and torch.equal(cache.k, fresh.k) and torch.equal(cache.v, fresh.v)
     binding.check_status()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.int8])
+@pytest.mark.parametrize("dim,tokens", [(64, 2900), (128, 1500), (256, 800)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_many_heads_of_many_tokens(dtype, dim, tokens, interleaved):
+    """Enough for 8-bit caches to take tokens in runs; a part of the channels turns."""
+    check(Batch(dim, [tokens + 300, 9, 0, 40], [tokens, 1, 0, 40], 70, 13, dim, 16, dtype, rotary=dim - 16, before=2, behind=1), interleaved)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seqs", [31, 32, 33, 1023, 1025, 2100])
+def test_one_token_of_many_sequences_and_pieces(seqs):
+    """With and without starts, sequences of none among them; the search for a row's sequence ends at 32, 1024, ..."""
+    counts = [(5 * i) % 3 for i in range(seqs)]
+    check(Batch(seqs, [c + i % 7 if c else 0 for i, c in enumerate(counts)], counts, 2, 1, 64, 4, before=3, behind=2))
+    check(Batch(seqs, [(3 * i) % 5 for i in range(seqs)], [1] * seqs, 2, 1, 64, 4, ragged=False))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ragged", [False, True])
+def test_many_sequences_of_an_8_bit_cache_in_runs(ragged):
+    n = 1500
+    counts = [1 if i % 9 else 0 for i in range(n)] if ragged else [1] * n
+    check(Batch(13, [c + i % 4 if c else 0 for i, c in enumerate(counts)], counts, 80, 16, 128, 8, torch.int8, ragged=ragged))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("what", ["in place", "page too high", "page below 0", "length too high", "length below 0", "length below the new tokens"])
+def test_runs_of_an_8_bit_cache(what):
+    """In place, and with one sequence that is out of range (a page: some of its tokens)."""
+    batch = Batch(14, [900, 300, 900], [800, 290, 700], 64, 8, 128, 16, torch.int8, behind=3)
+    cache, (q, k, v, cos_sin, lens, starts) = batch.on_gpu(), batch.args()
+    good = batch.on_gpu()
+    want = binding.kv_append(good, q, k, v, cos_sin, lens, starts)
+    binding.check_status()
+    if what == "in place":
+        kept = q.clone()
+        binding.kv_append(cache, q, k, v, cos_sin, lens, starts, q_out=q)
+        assert torch.equal(q[:-3], want[:-3]) and torch.equal(q[-3:], kept[-3:])
+    else:
+        if what.startswith("page"):
+            cache.page_table[1, 5] = cache.k.shape[0] if what.endswith("high") else -1
+        else:
+            lens[1] = {"h": cache.page_table.shape[1] * 16 + 1, "0": -25, "s": 289}[what[-1]]
+        got = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+        binding.kv_append(cache, q, k, v, cos_sin, lens, starts, q_out=got)
+        with pytest.raises(binding.PeqaError) as err:
+            binding.check_status()
+        assert err.value.status == -10
+        for first, end in ((0, 800), (1090, 1790)):
+            assert torch.equal(got[first:end], want[first:end])
+        if what.startswith("length") and what[-1] != "s":
+            assert (got[800:1090] == 7).all()
+    for b in (0, 2) if what != "in place" else (0, 1, 2):
+        page, at = places(batch.table, b, range(batch.lengths[b]), 16)
+        assert torch.equal(cache.k[page, at], good.k[page, at]) and torch.equal(cache.v[page, at], good.v[page, at])
+    binding.check_status()

@@ -114,3 +114,11 @@ def test_refusals_of_the_binding_need_no_gpu():
         binding.kv_append(cache, q, q[:, :2], q[:, :2], torch.zeros(9, 64), lens)
     with pytest.raises(AttributeError):
         binding.attn_decode(None, q, lens)
+
+
+def test_heads_of_an_append_are_bounded(L, p):
+    rows = lambda *a: ctypes.byref(binding._Rows(*a))
+    call = lambda heads, kv: L.peqa_kv_append(_cache(p, n_kv_heads=kv, head_stride=64, token_stride=kv * 64, page_stride=kv * 64 * 16),
+                                              rows(p, heads * 64, 64), heads, rows(p, kv * 64, 64), rows(p, kv * 64, 64), 3, p, 9, 64, 0, p, 0,
+                                              rows(p, heads * 64, 64), 0)
+    assert call((1 << 18) - 3, 2) == -9 and call(1, 1 << 17) == -9
