@@ -53,7 +53,7 @@ struct AttnParams {
   float* lse;
   int4* headers;                     // [2 * CTAs]: row, whether its last tile is in the part
   float* parts;                      // [2 * CTAs][Shape::kPart]
-  float* first_parts;                // [CTAs][warps][Shape::kPart]
+  float* first_parts;                // [CTAs][warps][D][NH]
   int* status;
 };
 
@@ -79,7 +79,7 @@ struct Shape {
   static constexpr int kRing = kUnits * kUnit;
   static constexpr int kSmem = kWarps * (kRing + (I8 ? kUnits * 64 : 0));            // and the scales of a unit's 16 tokens
   static constexpr int kPart = NH * (D + 2);                    // floats of a part: sums, maxima, sums of p
-  static_assert(kFit >= 3 && kRing >= kPart * 4 && kRing % 1024 == 0 && kPart % 4 == 0, "shared memory");
+  static_assert(kFit >= 3 && kRing >= 2 * NH * D * 4 && kRing % 1024 == 0 && kPart % 4 == 0, "shared memory");
 };
 
 // A box of 16 tokens from token y on: channels from x on of head `head` in page `page`.
@@ -286,9 +286,9 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   const int tid = threadIdx.x, lane = tid & 31, warp = ptx::warp_index();
   const int lr = lane >> 2, lc = lane & 3;
   const uint32_t ring = ptx::smem_u32(smem) + warp * S::kRing;
-  // a warp's parts of rows: one that it goes on from lies in the workspace, its last in its ring
-  const auto first_part = [&](int w) { return Part<D, NH>{p.first_parts + ((long long)blockIdx.x * S::kWarps + w) * S::kPart}; };
-  const auto last_part = [&](int w) { return Part<D, NH>{reinterpret_cast<float*>(smem + w * S::kRing)}; };
+  // a warp's parts of rows in its ring, when that is free: the one that it began with (i even; until then it lies in the workspace), its last
+  const auto part_of = [&](int i) { return Part<D, NH>{reinterpret_cast<float*>(smem + (i >> 1) * S::kRing) + (i & 1 ? 0 : NH * D)}; };
+  const auto first_part = [&]() { return Part<D, NH>{p.first_parts + ((long long)blockIdx.x * S::kWarps + warp) * (NH * D)}; };
 
   volatile int* const abort_flag = s_abort;
   if (tid < 2 * S::kWarps) s_head[tid] = make_int4(-1, 0, 0, 0);
@@ -538,7 +538,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     float base[kCols][2];                                    // most, or 0 where there is none
     float acc[D / 16][kCols][4];                             // two channels of each of the two heads
     float v_ref = 1.f, inv_ref = 1.f;                        // I8: acc is in units of it
-    bool from_start;
+    bool from_start, behind = false;         // behind: this warp has the end of a row that the ones before began
 
     auto begin_row = [&]() {
 #pragma unroll
@@ -798,7 +798,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       }
       if (!more) asm volatile("cp.async.wait_group 0;" ::: "memory");   // the ring is no longer filled
       __syncwarp();
-      const Part<D, NH> part = more ? first_part(warp) : last_part(warp);
+      behind = behind || more;
+      const Part<D, NH> part = more ? first_part() : part_of(2 * warp + 1);
       if (NH > 4 || lc < 2)
 #pragma unroll
         for (int n = 0; n < kCols; ++n) {
@@ -830,6 +831,15 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       if (fresh || i + 1 == count) end_row(fresh, i + 1 < count);
       at.next(p);
     }
+    // The join below reads parts again and again: from shared memory, as the loads from here come while the other warps have tiles left.
+    if (behind) {
+      constexpr int kEach = NH * D / 128;
+      float4 x[kEach];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) x[i] = first_part().four(i * 32 + lane);
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) part_of(2 * warp).four(i * 32 + lane) = x[i];
+    }
   }
   __syncthreads();
   if (S::WHOLE && *abort_flag) {
@@ -845,7 +855,6 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   // of all parts for a head, then takes 128 sums of a row at a time, a lane four heads of a channel.
   constexpr int kSlices = NH * D / 128;
   const int4 own = lane < 2 * S::kWarps ? s_head[lane] : make_int4(-1, 0, 0, 0);
-  auto part_of = [&](int i) { return i & 1 ? last_part(i >> 1) : first_part(i >> 1); };
   const uint32_t parts_of_own = __match_any_sync(0xffffffffu, own.x);
   for (int head = warp; head < NH; head += S::kWarps) {
     float m = kNegInf;
@@ -925,6 +934,7 @@ __global__ void __launch_bounds__(kMaxCtas) attn_join_kernel(const AttnParams p,
   __shared__ float4 s_weight[kMaxCtas], s_top[kWarps], s_total[kWarps], s_sums[kWarps][32];
   __shared__ int s_stop;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (tid == 0) s_stop = 0x7fffffff;
   __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -1047,7 +1057,7 @@ int launch_heads(const AttnParams& p, int nh, bool codes, cudaStream_t st) {
 
 // headers, parts of CTAs, parts of warps
 size_t workspace_bytes(int dim, int nh) {
-  return (size_t)attn_ctas() * (2 * sizeof(int4) + (2 + warps_of(dim, nh)) * (size_t)nh * (dim + 2) * sizeof(float));
+  return (size_t)attn_ctas() * (2 * sizeof(int4) + (2 * (size_t)(dim + 2) + (size_t)warps_of(dim, nh) * dim) * nh * sizeof(float));
 }
 
 }  // namespace
