@@ -51,8 +51,10 @@ struct AttnParams {
   bool row_each;                     // a CTA has a row to itself
   uint16_t* out;
   float* lse;
-  int4* headers;                     // [2 * CTAs]: row, whether its last tile is in the part
-  float* parts;                      // [2 * CTAs][Shape::kPart]
+  // [CTAs][2]: row that an earlier CTA began, row that a later one goes on with (-1: none).  (Whole sectors: one that is written in part is
+  // filled from memory before it is read, 0.4 to 0.7 us of every call.)
+  int4* headers;
+  float* parts;                      // [CTAs][2][Shape::kPart]: of those rows
   float* first_parts;                // [CTAs][warps][D][NH]
   int* status;
 };
@@ -281,6 +283,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   __shared__ __align__(16) float s_weight[32][NH], s_most[32][NH], s_total[32][NH];   // of a part and head; s_most: at last of its row
   __shared__ int4 s_head[2 * S::kWarps];   // of a warp's parts: row (-1: none), 1 if it begins its row + 2 if it ends it + 4 times its heads, its first head's place in out
   __shared__ __align__(8) uint64_t s_full[S::WHOLE ? S::kWarps * S::kUnits : 1];
+  __shared__ uint32_t s_empty;             // of sequences blockIdx.x + i gridDim.x, i < 32: those without tiles
   __shared__ int s_abort[2];               // as the bounded waits of sm100_ptx.cuh have it
 
   const int tid = threadIdx.x, lane = tid & 31, warp = ptx::warp_index();
@@ -306,8 +309,13 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  // ---- the tiles of all sequences, and this warp's share of them: [begin, end)
   const int B = p.cache.n_seqs;
+  if (warp == S::kWarps - 1) {               // at the end their lengths would be waited for once more
+    const long long b = blockIdx.x + (long long)lane * gridDim.x;
+    const uint32_t empty = __ballot_sync(0xffffffffu, b < B && span_of(p, (int)b).tiles() == 0);
+    if (lane == 0) s_empty = empty;
+  }
+  // ---- the tiles of all sequences, and this warp's share of them: [begin, end)
   int total = 0, begin = 0, end = 0;
   auto among_warps = [&](int first, int n) {
     const int each = n / S::kWarps, more = n - each * S::kWarps;           // the first `more` warps have one more
@@ -872,10 +880,9 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   const uint32_t leaders = __ballot_sync(0xffffffffu, own.x >= 0 && lane == __ffs(parts_of_own) - 1);
   if (warp == 0 && !p.row_each) {
     const uint32_t behind = __ballot_sync(0xffffffffu, own.x >= 0 && !run_starts), before = __ballot_sync(0xffffffffu, own.x >= 0 && run_starts && !run_ends);
-    const int row0 = __shfl_sync(0xffffffffu, own.x, behind ? __ffs(behind) - 1 : 0), ends0 = __shfl_sync(0xffffffffu, run_ends, behind ? __ffs(behind) - 1 : 0);
-    const int row1 = __shfl_sync(0xffffffffu, own.x, before ? __ffs(before) - 1 : 0);
+    const int row0 = __shfl_sync(0xffffffffu, own.x, behind ? __ffs(behind) - 1 : 0), row1 = __shfl_sync(0xffffffffu, own.x, before ? __ffs(before) - 1 : 0);
     if (lane == 0) {
-      p.headers[2 * blockIdx.x] = make_int4(behind ? row0 : -1, ends0, 0, 0);
+      p.headers[2 * blockIdx.x] = make_int4(behind ? row0 : -1, 0, 0, 0);
       p.headers[2 * blockIdx.x + 1] = make_int4(before ? row1 : -1, 0, 0, 0);
     }
   }
@@ -915,12 +922,12 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   }
 
   // ---- sequences that are not there have outputs all the same
-  for (int b = blockIdx.x; b < B; b += gridDim.x)
-    if (span_of(p, b).tiles() == 0) {
-      for (int i = tid; i < p.n_heads * (D / 8); i += kThreads)
-        reinterpret_cast<uint4*>(p.out)[(long long)b * p.n_heads * (D / 8) + i] = make_uint4(0, 0, 0, 0);
+  for (int i = 0, b = blockIdx.x; b < B; b += gridDim.x, ++i)
+    if (i < 32 ? s_empty >> i & 1 : span_of(p, b).tiles() == 0) {
+      for (int at = tid; at < p.n_heads * (D / 8); at += kThreads)
+        reinterpret_cast<uint4*>(p.out)[(long long)b * p.n_heads * (D / 8) + at] = make_uint4(0, 0, 0, 0);
       if (p.lse)
-        for (int i = tid; i < p.n_heads; i += kThreads) p.lse[(long long)b * p.n_heads + i] = kNegInf;
+        for (int at = tid; at < p.n_heads; at += kThreads) p.lse[(long long)b * p.n_heads + at] = kNegInf;
     }
 }
 
@@ -932,25 +939,22 @@ template <int D, int NH>
 __global__ void __launch_bounds__(kMaxCtas) attn_join_kernel(const AttnParams p, const int ctas) {
   constexpr int kPart = NH * (D + 2), kWarps = kMaxCtas / 32;
   __shared__ float4 s_weight[kMaxCtas], s_top[kWarps], s_total[kWarps], s_sums[kWarps][32];
-  __shared__ int s_stop;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if (tid == 0) s_stop = 0x7fffffff;
-  __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int row = ptx::behind_wait(p.headers)[2 * blockIdx.x + 1].x;
-  if (row < 0) return;
-  // parts of the row: the own one, then the first ones of the CTAs behind, up to the one that has the row's end
-  const int c = blockIdx.x + 1 + tid;
-  const int4 h = c < ctas ? ptx::behind_wait(p.headers)[2 * c] : make_int4(-1, 1, 0, 0);
-  const uint32_t stops = __ballot_sync(0xffffffffu, h.x != row || h.y);
-  if (stops && lane == __ffs(stops) - 1) atomicMin(&s_stop, 2 * tid + (h.x != row));
-  __syncthreads();
-  const int n = min(ctas, 1 + (s_stop >> 1) + (s_stop & 1 ? 0 : 1));
-  const int group = blockIdx.y % (NH / 4), d = blockIdx.y / (NH / 4) * 32 + lane, head = group * 4;
+  // The row's parts: the own one, then the first ones of the CTAs behind that have it too.  Thread i sees to part i + 1, the last thread (there are
+  // fewer parts) to part 0.  What a warp sums first is asked for before it is known whether the row has it.
+  const int4* const headers = ptx::behind_wait(p.headers);
+  const int group = blockIdx.y % (NH / 4), d = blockIdx.y / (NH / 4) * 32 + lane, head = group * 4, place = d * (NH / 4) + group;
   auto part_of = [&](int i) { return Part<D, NH>{p.parts + (i == 0 ? 2ll * blockIdx.x + 1 : 2ll * (blockIdx.x + i)) * kPart}; };
-  float4 m = make_float4(kNegInf, kNegInf, kNegInf, kNegInf), total = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (tid < n) m = part_of(tid).most4(head), total = part_of(tid).total4(head);
+  const int row = headers[2 * blockIdx.x + 1].x, c = blockIdx.x + 1 + tid;
+  const int its_row = c < ctas ? headers[2 * c].x : -1;
+  float4 sums = make_float4(0.f, 0.f, 0.f, 0.f), m = make_float4(kNegInf, kNegInf, kNegInf, kNegInf), total = sums;
+  if ((int)blockIdx.x + warp < ctas) sums = part_of(warp).four(place);
+  if (row < 0) return;
+  const int own = tid == kMaxCtas - 1 ? 0 : tid + 1;
+  if (own == 0 || its_row == row) m = part_of(own).most4(head), total = part_of(own).total4(head);
+  const int n = 1 + __syncthreads_count(its_row == row);
   float4 top = m;
 #pragma unroll
   for (int o = 16; o; o >>= 1) top = larger(top, shuffled(top, o));
@@ -959,15 +963,15 @@ __global__ void __launch_bounds__(kMaxCtas) attn_join_kernel(const AttnParams p,
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) top = larger(top, s_top[w]);
   const float4 f = make_float4(weight(m.x, top.x), weight(m.y, top.y), weight(m.z, top.z), weight(m.w, top.w));
-  s_weight[tid] = f;
+  s_weight[own] = f;
   total = total * f;
 #pragma unroll
   for (int o = 16; o; o >>= 1) total = total + shuffled(total, o);
   if (lane == 0) s_total[warp] = total;
   __syncthreads();
-  float4 sums = make_float4(0.f, 0.f, 0.f, 0.f);
+  sums = warp < n ? s_weight[warp] * sums : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int i = warp; i < n; i += kWarps) sums = sums + s_weight[i] * part_of(i).four(d * (NH / 4) + group);
+  for (int i = warp + kWarps; i < n; i += kWarps) sums = sums + s_weight[i] * part_of(i).four(place);
   s_sums[warp][lane] = sums;
   __syncthreads();
   if (warp > 0) return;
