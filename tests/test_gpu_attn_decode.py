@@ -305,3 +305,13 @@ def test_windows_where_the_work_is_dealt_out(dtype, dim, window):
 def test_about_as_many_rows_as_ctas(heads, kv_heads, n):
     lengths = [(37 * i) % 300 for i in range(n)]
     check(Case(n, lengths, heads, kv_heads, 64, 16))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.int8])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("order", ["heads", "tokens"])
+@pytest.mark.parametrize("window", [0, 9])
+def test_many_rows_of_few_tokens(dtype, dim, order, window):
+    """Last tiles of 1 to 16 tokens, and cut on both sides by the window; what lies behind is no number."""
+    check(Case(dim + window, [1 + (7 * i) % 41 for i in range(100)] + [0, 8, 16, 24], 6, 3, dim, 16, dtype, order, window=window))
