@@ -3,10 +3,11 @@
 //   out[b,h] = sum_t p_t v_t,   p_t = exp(s_t - lse),   s_t = scale <q[b,h], k_t>,   lse = log sum_t exp(s_t)
 //
 // Every cached key and value is read once, by one warp, for all query heads that share it (a row of work: a sequence, a
-// key-value head and up to NH = 8 or 16 of its query heads).  4 NH flops per cached element are too few to bind anything
+// key-value head and up to NH = 4, 8 or 16 of its query heads).  4 NH flops per cached element are too few to bind anything
 // but memory, and the rest is laid out to keep copies in flight:
 //   * A tile is 16 tokens of a row.  Tiles are numbered through all sequences, heads and lengths, and dealt evenly: every CTA
-//     takes an equal run of them, every warp an equal run of its CTA's.  Nothing depends on how uneven the lengths are.
+//     takes an equal run of them, every warp an equal run of its CTA's.  Nothing depends on how uneven the lengths are.  (With few
+//     and short rows a CTA has a row to itself.)
 //   * A warp copies its own tiles into its own ring of shared memory, several units of 16 keys or values ahead (tensor copies, or
 //     cp.async where pages end within tiles), and reads them with ldmatrix as the 16-row operand of the tensor cores' m16n8k16 product, the
 //     heads as its 8 columns:
@@ -1109,11 +1110,11 @@ extern "C" int peqa_attn_decode(const peqa_kv_cache_t* c, const peqa_rows_t* q, 
   p.seq_lens = seq_lens;
   p.n_heads = n_heads;
   // A CTA for every row needs no second kernel, but is as long as the longest row.  Rows of T tiles, rows x T: dealt out evenly / a CTA each, us:
-  // 8 x 9 9.5 / 8.0, 8 x 16 9.5 / 11.0, 8 x 64 10.4 / 13.9; 32 x 9 9.0 / 7.4, 32 x 64 12.7 / 12.5; 128 x 9 10.0 / 7.4, 128 x 64 19.9 / 15.9, 128 x
-  // 128 26.4 / 22.8 (four sequences of uneven lengths).  What is known here of the lengths is what they can be at most.
+  // 8 x 9 8.0 / 5.6, 8 x 16 7.9 / 6.9, 8 x 32 7.9 / 8.0, 8 x 64 8.4 / 9.9; 32 x 9 8.0 / 5.5, 32 x 32 8.2 / 7.5, 32 x 64 9.3 / 9.4; 128 x 9 8.5 / 5.6, 128 x
+  // 64 16.1 / 12.5, 128 x 128 22.4 / 19.4 (four sequences of uneven lengths).  What is known here of the lengths is what they can be at most.
   const long long ctas = attn_ctas(), capacity = p.cache.capacity;
   const long long most = (min(capacity, window > 0 ? window + kTile - 1ll : capacity) + kTile - 1) / kTile;
-  p.row_each = rows <= ctas && (most <= 9 || (4 * rows >= ctas && most * (ctas - rows) <= 48 * ctas && most <= 129));
+  p.row_each = rows <= ctas && (most < 32 || (4 * rows >= ctas && most * (ctas - rows) <= 48 * ctas && most <= 129));
   // A row's last tile is half empty on average, which rows of few tiles feel: 256 sequences of up to 16 tokens, 32 heads, 19.8 -> 18.6 us, of up to 50
   // 40.7 -> 39.0, of up to 513 219.4 -> 217.6.  (8 bits: by the registers that it takes 64 of up to 300 16.9 -> 17.9.)
   p.halves = c->type == PEQA_KV_BF16 && !p.row_each && most <= 64;

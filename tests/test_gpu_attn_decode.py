@@ -315,3 +315,10 @@ def test_about_as_many_rows_as_ctas(heads, kv_heads, n):
 def test_many_rows_of_few_tokens(dtype, dim, order, window):
     """Last tiles of 1 to 16 tokens, and cut on both sides by the window; what lies behind is no number."""
     check(Case(dim + window, [1 + (7 * i) % 41 for i in range(100)] + [0, 8, 16, 24], 6, 3, dim, 16, dtype, order, window=window))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.int8])
+@pytest.mark.parametrize("longest", [495, 496, 497, 513])
+def test_few_rows_of_about_32_tiles(dtype, longest):
+    check(Case(longest, [longest, 300, 0, 17], 4, 2, 64, 16, dtype))
