@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   }
   Cursor in;                                // of the copies; the sums follow with `at`
   in.b = in.r = in.t0 = in.left = in.span.first = in.span.end = 0;
-  int before = 0;                           // tiles of the sequences before this round's
+  int before = 0;                           // tiles of the sequences before these
   if (p.row_each) {
     const int b = blockIdx.x / p.rows_of_seq, r = blockIdx.x - b * p.rows_of_seq;
     const int tiles = span_of(p, b).tiles();
