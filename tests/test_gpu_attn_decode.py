@@ -322,3 +322,11 @@ def test_many_rows_of_few_tokens(dtype, dim, order, window):
 @pytest.mark.parametrize("longest", [495, 496, 497, 513])
 def test_few_rows_of_about_32_tiles(dtype, longest):
     check(Case(longest, [longest, 300, 0, 17], 4, 2, 64, 16, dtype))
+
+
+@pytest.mark.gpu
+def test_more_sequences_than_a_list_of_the_empty_ones_holds():
+    lengths = [(i % 5 - 2) * (i % 7 == 3) * (i % 5 > 2) for i in range(5200)]
+    out, lse = check(Case(17, lengths, 2, 1, 64, 16))
+    none = torch.tensor(lengths, device="cuda") == 0
+    assert (out[none] == 0).all() and (lse[none] == -math.inf).all() and (lse[~none] > -math.inf).all()

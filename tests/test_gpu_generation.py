@@ -90,3 +90,58 @@ def test_prompt_and_tokens(dtype, worst):
             want = torch.einsum("kgt,tkd->kgd", s.softmax(-1), dense[b][1]).reshape(-1) @ lin[3][2].t()
             got = torch.from_numpy(dev_to_f64(y[b]))
             assert (got - want).norm() <= worst * want.norm(), (step, b, float((got - want).norm() / want.norm()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seqs,length", [(3, 100), (16, 900)])
+def test_captured_steps_follow_one_another(seqs, length):
+    """Projections, append, attention and output projection of two layers in one graph, each kernel's launch under the one before: replayed, the bits
+    of the same calls one at a time.  Few rows, and more than there are CTAs."""
+    lin = _linears(5)
+    gen = torch.Generator().manual_seed(6)
+    kv = KV if seqs < 10 else HEADS + 2                      # (the second: a cache of its own width, its keys and values not projected)
+    heads = HEADS if seqs < 10 else HEADS + 2
+    pages = -(-length // 16)
+    tables = [torch.randperm(seqs * pages, generator=gen).to(torch.int32).view(seqs, pages).cuda() for _ in range(2)]
+    caches = [binding.alloc_kv_cache(seqs * pages, 16, kv, DIM, t) for t in tables]
+    for c in caches:
+        for x in (c.k, c.v):
+            x.copy_(torch.randn(x.shape, generator=gen).bfloat16())
+    start = [(c.k.clone(), c.v.clone()) for c in caches]
+    cos_sin, ws = angles(length, DIM).cuda(), binding.alloc_attn_workspace(caches[0], heads)
+    x = torch.randn(seqs, WIDTH, generator=gen).bfloat16().cuda()
+    lens = torch.randint(1, length + 1, (seqs,), generator=gen).to(torch.int32).cuda()
+    more = torch.randn(seqs, 3, 2, DIM, generator=gen).bfloat16().cuda()
+
+    def step(between):
+        y = x
+        for c in caches:
+            q, k, v = (binding.qlinear_decode_prepared(lin[i][0], lin[i][1], y).view(seqs, -1, DIM) for i in range(3))
+            if kv != KV:
+                k, v, q = torch.cat([q, more[:, 0]], 1), torch.cat([q, more[:, 1]], 1), torch.cat([q, more[:, 2]], 1)
+            between()
+            q = binding.kv_append(c, q, k, v, cos_sin, lens)
+            between()
+            o = binding.attn_decode(c, q, lens, workspace=ws)
+            between()
+            y = binding.qlinear_decode_prepared(lin[3][0], lin[3][1], o[:, :HEADS].contiguous().view(seqs, WIDTH))
+            between()
+        return y
+
+    want = step(torch.cuda.synchronize)
+    wrote = [(c.k.clone(), c.v.clone()) for c in caches]
+    step(lambda: None)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(lambda: None)
+    for _ in range(3):
+        for c, (k, v) in zip(caches, start):
+            c.k.copy_(k)
+            c.v.copy_(v)
+        got.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        for c, (k, v) in zip(caches, wrote):
+            assert torch.equal(c.k, k) and torch.equal(c.v, v)
+    binding.check_status()
