@@ -298,7 +298,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   const auto first_part = [&]() { return Part<D, NH>{p.first_parts + ((long long)blockIdx.x * S::kWarps + warp) * (NH * D)}; };
 
   volatile int* const abort_flag = s_abort;
-  if (tid < 2 * S::kWarps) s_head[tid] = make_int4(-1, 0, 0, 0);
+  if (lane < 2) s_head[2 * warp + lane] = make_int4(-1, 0, 0, 0);   // each warp its own: no barrier is sure to come before its parts
+  __syncwarp();
   if constexpr (S::WHOLE) {
     if (lane < S::kUnits) ptx::mbar_init(ptx::smem_u32(&s_full[warp * S::kUnits + lane]), 1);
     ptx::fence_mbar_init();
