@@ -385,18 +385,27 @@ struct HeadRows {
 
 struct Cache {
   peqa_kv_cache_t c = {};
+  static void check_scales(PyObject* o, const at::Tensor& k, const char* name) {
+    const at::Tensor& t = tensor(o, name);
+    if (t.dim() != 3 || t.size(0) != k.size(0) || t.size(1) != k.size(2) || t.size(2) != k.size(1))
+      refuse(name, "[n_pages, n_kv_heads, page_size]");
+  }
   explicit Cache(PyObject* o) {
     const Ref pk(PyObject_GetAttr(o, s_k)), pv(PyObject_GetAttr(o, s_v_cache)), pt(PyObject_GetAttr(o, s_page_table)),
         pks(PyObject_GetAttr(o, s_k_scales)), pvs(PyObject_GetAttr(o, s_v_scales));
     const at::Tensor &k = tensor(pk.p, "k"), &v = tensor(pv.p, "v");
-    here(k, "cache.k");
-    here(v, "cache.v");
     const bool codes = k.scalar_type() == at::kChar;
     if ((!codes && k.scalar_type() != at::kBFloat16) || k.dim() != 4 || k.stride(3) != 1)
       refuse("cache.k", "a torch.bfloat16 or torch.int8 tensor [n_pages, page_size, n_kv_heads, head_dim] with dense channels");
     if (v.scalar_type() != k.scalar_type() || v.sizes() != k.sizes()) refuse("cache.v", "a tensor of cache.k's type and shape");
     for (int d = 0; d < 4; ++d)
       if (k.size(d) != 1 && k.stride(d) != v.stride(d)) refuse("cache.v", "cache.k's strides");
+    if (codes) {                           // as many values in another order would be taken for other tokens' scales
+      check_scales(pks.p, k, "cache.k_scales");
+      check_scales(pvs.p, k, "cache.v_scales");
+    }
+    here(k, "cache.k");
+    here(v, "cache.v");
     c.type = codes ? PEQA_KV_INT8 : PEQA_KV_BF16;
     c.n_pages = size32(k, 0, "cache.k");
     c.page_size = size32(k, 1, "cache.k");
