@@ -564,7 +564,8 @@ def kv_append(cache: KVCache, q, k: torch.Tensor, v: torch.Tensor, cos_sin: torc
     cos_sin fp32 [n_positions, rotary_dim], cosines before sines; seq_lens int32 [n_seqs], WITH the new tokens.
     Without ``starts`` row b is the one new token of sequence b; with it (int32 [n_seqs + 1]) rows starts[b] to
     starts[b + 1] - 1 are the last tokens of sequence b.  Rows of no sequence, or of one of length 0, are left out: q_out
-    (q itself, or memory apart from it) keeps what it has there, and a new one has zeros."""
+    keeps what it has there, and a new one has zeros.  q_out is q itself or apart from it, and apart from k and v (in the rows of
+    one matrix they may lie side by side); what would be read while others write it is refused."""
     return (_native or _load_native()).kv_append(cache, q, k, v, cos_sin, seq_lens, starts, q_out, interleaved)
 
 

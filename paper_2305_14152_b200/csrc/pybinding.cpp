@@ -6,8 +6,10 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <optional>
 #include <vector>
 
 #include <ATen/ATen.h>
@@ -370,18 +372,74 @@ int size32(const at::Tensor& t, int dim, const char* name) {
 struct HeadRows {
   peqa_rows_t r;
   int rows, heads;
-  HeadRows(PyObject* o, int head_dim, const char* name) {
-    const at::Tensor& t = tensor(o, name);
-    here(t, name);
-    if (t.scalar_type() != at::kBFloat16 || t.dim() != 3 || t.size(2) != head_dim || t.stride(2) != 1)
-      refuse(name, "a torch.bfloat16 tensor [rows, heads, head_dim] with dense channels");
+  int64_t dim;
+  const at::Tensor& t;
+  const char* name;
+  HeadRows(PyObject* o, const char* what) : t(tensor(o, what)), name(what) {
+    if (t.scalar_type() != at::kBFloat16 || t.dim() != 3 || t.stride(2) != 1) refuse();
     r.data = t.data_ptr();
     r.row_stride = t.stride(0);
     r.head_stride = t.stride(1);
     rows = size32(t, 0, name);
     heads = size32(t, 1, name);
+    dim = t.size(2);
   }
+  void belong_to(const peqa_kv_cache_t& c) const {
+    here(t, name);
+    if (dim != c.head_dim) refuse();
+  }
+  [[noreturn]] void refuse() const { ::refuse(name, "a torch.bfloat16 tensor [rows, heads, head_dim] with dense channels"); }
 };
+
+// The places of HeadRows as an arithmetic of elements: n steps of a stride, one where the stride says nothing.
+struct Steps {
+  int64_t n, stride;
+  Steps(int64_t count, int64_t by) : n(by == 0 ? 1 : count), stride(n > 1 ? by : 0) {}
+  int64_t span() const { return (n - 1) * stride; }
+};
+
+int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b < 0); }          // b > 0
+
+bool same_places(const HeadRows& a, const HeadRows& b) {
+  const Steps ra(a.rows, a.r.row_stride), rb(b.rows, b.r.row_stride), ha(a.heads, a.r.head_stride), hb(b.heads, b.r.head_stride);
+  return a.r.data == b.r.data && ra.n == rb.n && ra.stride == rb.stride && ha.n == hb.n && ha.stride == hb.stride;
+}
+
+// Whether heads of a and heads of b have an element in common, b's rows being as long as a's.  Exact where the rows of both follow in one
+// stride (as parts of the rows of one matrix do) or their extents lie apart; what else lies within one extent counts as common.
+bool meet(const HeadRows& a, const HeadRows& b) {
+  if (a.t.numel() == 0 || b.t.numel() == 0) return false;
+  const int64_t size = 2, dim = a.dim * size;                                    // from here on in bytes
+  const Steps ra(a.rows, a.r.row_stride * size), rb(b.rows, b.r.row_stride * size), ha(a.heads, a.r.head_stride * size),
+      hb(b.heads, b.r.head_stride * size);
+  const intptr_t at = reinterpret_cast<intptr_t>(b.r.data) - reinterpret_cast<intptr_t>(a.r.data);
+  if (at >= ra.span() + ha.span() + dim || -at >= rb.span() + hb.span() + dim) return false;
+  if (ra.n > 1 && rb.n > 1 && ra.stride != rb.stride) return true;
+  const int64_t row = ra.n > 1 ? ra.stride : rb.stride;
+  if (row > 0) {                                                                 // b's heads beside a's in every row
+    const int64_t from = at - floor_div(at, row) * row;
+    if (ha.span() + dim <= from && from + hb.span() + dim <= row) return false;
+  }
+  // heads j of a and l of b, i rows behind: j ha - l hb + i row - at is where the one begins in the other
+  const bool one_stride = ha.n == 1 || hb.n == 1 || ha.stride == hb.stride;      // then j ha - l hb is a multiple of it
+  const int64_t head = ha.n > 1 ? ha.stride : hb.stride;
+  if (!one_stride && ha.n * hb.n > (1 << 20)) return true;
+  auto common = [&](int64_t apart) {
+    apart -= at;
+    if (row == 0) return -dim < apart && apart < dim;
+    const int64_t first = std::max(-(rb.n - 1), floor_div(-dim - apart, row) + 1);   // least i with i row + apart > -dim
+    return first <= ra.n - 1 && first * row + apart < dim;
+  };
+  if (one_stride) {
+    for (int64_t d = -(hb.n - 1); d < ha.n; ++d)
+      if (common(d * head)) return true;
+    return false;
+  }
+  for (int64_t j = 0; j < ha.n; ++j)
+    for (int64_t l = 0; l < hb.n; ++l)
+      if (common(j * ha.stride - l * hb.stride)) return true;
+  return false;
+}
 
 struct Cache {
   peqa_kv_cache_t c = {};
@@ -434,10 +492,25 @@ struct Cache {
 PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   arity(n, 9);
+  const HeadRows k(a[2], "k"), v(a[3], "v");
+  if (v.heads != k.heads || v.rows != k.rows || v.dim != k.dim) refuse("v", "k's shape");
+  std::optional<HeadRows> q, to;
+  if (a[1] != Py_None) {
+    q.emplace(a[1], "q");
+    if (q->rows != k.rows || q->dim != k.dim) refuse("q", "k's rows");
+  }
+  if (a[7] != Py_None) {
+    if (!q) refuse("q_out", "q beside it");
+    to.emplace(a[7], "q_out");
+    if (to->rows != q->rows || to->heads != q->heads || to->dim != q->dim) refuse("q_out", "q's shape");
+    // a CTA reads rows that others write
+    if (!same_places(*to, *q) && meet(*to, *q)) refuse("q_out", "q itself or memory apart from q");
+    if (meet(*to, k) || meet(*to, v)) refuse("q_out", "memory apart from k and v");
+  }
   const Cache cache(a[0]);
-  const HeadRows k(a[2], cache.c.head_dim, "k"), v(a[3], cache.c.head_dim, "v");
+  k.belong_to(cache.c);
+  v.belong_to(cache.c);
   if (k.heads != cache.c.n_kv_heads) refuse("k", "the cache's heads");
-  if (v.heads != k.heads || v.rows != k.rows) refuse("v", "k's shape");
   const at::Tensor& table = dev(a[4], at::kFloat, "cos_sin");
   here(table, "cos_sin");
   if (table.dim() != 2) refuse("cos_sin", "[n_positions, rotary_dim]");
@@ -452,8 +525,7 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (interleaved < 0) fail();
   void* st = stream();
   const float* angles = static_cast<const float*>(table.data_ptr());
-  if (a[1] == Py_None) {
-    if (a[7] != Py_None) refuse("q_out", "q beside it");
+  if (!q) {
     check(unlocked([&] {
             return peqa_kv_append(&cache.c, nullptr, 0, &k.r, &v.r, k.rows, angles, positions, rotary, interleaved, lens, starts,
                                   nullptr, st);
@@ -461,22 +533,21 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
           "peqa_kv_append");
     Py_RETURN_NONE;
   }
-  const HeadRows q(a[1], cache.c.head_dim, "q");
-  if (q.rows != k.rows) refuse("q", "k's rows");
+  q->belong_to(cache.c);
   PyObject* made = a[7];
-  if (made == Py_None) {
+  if (!to) {
     // rows that are left out keep what their memory had: a new tensor has zeros there
-    made = THPVariable_Wrap(at::zeros({q.rows, q.heads, cache.c.head_dim}, tensor(a[1], "q").options()));
+    made = THPVariable_Wrap(at::zeros({q->rows, q->heads, cache.c.head_dim}, q->t.options()));
     if (!made) fail();
   } else {
+    to->belong_to(cache.c);
     Py_INCREF(made);
   }
   Ref out(made);
-  const HeadRows to(out.p, cache.c.head_dim, "q_out");
-  if (to.rows != q.rows || to.heads != q.heads) refuse("q_out", "q's shape");
+  if (!to) to.emplace(out.p, "q_out");
   check(unlocked([&] {
-          return peqa_kv_append(&cache.c, &q.r, q.heads, &k.r, &v.r, k.rows, angles, positions, rotary, interleaved, lens, starts,
-                                &to.r, st);
+          return peqa_kv_append(&cache.c, &q->r, q->heads, &k.r, &v.r, k.rows, angles, positions, rotary, interleaved, lens, starts,
+                                &to->r, st);
         }),
         "peqa_kv_append");
   Py_INCREF(out.p);
@@ -489,7 +560,8 @@ PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   arity(n, 8);
   const Cache cache(a[0]);
-  const HeadRows q(a[1], cache.c.head_dim, "q");
+  const HeadRows q(a[1], "q");
+  q.belong_to(cache.c);
   if (q.rows != cache.c.n_seqs) refuse("q", "one row per sequence");
   const int32_t* lens = static_cast<const int32_t*>(values(a[2], at::kInt, cache.c.n_seqs, "seq_lens").data_ptr());
   const float scale = a[3] == Py_None ? (float)(1.0 / std::sqrt((double)cache.c.head_dim)) : as_float(a[3]);
