@@ -561,11 +561,12 @@ size_t peqa_attn_workspace_bytes(const peqa_kv_cache_t* cache, int n_heads);
 int peqa_probe_read(const void* src, size_t bytes, uint32_t* sink, size_t sink_bytes, void* stream);
 
 /*
- * Synchronises `stream`, then reads and clears the status word of that stream.
+ * Synchronises `stream`, then reads the status word of that stream and clears what it returns.
  * Returns PEQA_OK, PEQA_ERR_DEVICE_TIMEOUT (a bounded wait of a kernel launched on
  * `stream` expired since the last check; its outputs are undefined),
  * PEQA_ERR_DEVICE_INDEX (a kernel of the key-value cache met a length, page number
- * or position out of range, and left out what it stands for) or PEQA_ERR_CUDA.  Status words live in the library's device image, one per stream
+ * or position out of range, and left out what it stands for) or PEQA_ERR_CUDA.  Where both were found
+ * the time-out is returned, and the index by the next call.  Status words live in the library's device image, one per stream
  * (the first 31 streams seen on a device get a word of their own, any further
  * streams share one); entry points without a workspace argument have nowhere
  * else to report to.  The table is initialised by the first call of any entry

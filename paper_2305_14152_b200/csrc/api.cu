@@ -643,13 +643,12 @@ extern "C" int peqa_check_status(void* stream) {
   int host[kStatusInts] = {};
   PEQA_CUDA(cudaMemcpyAsync(host, dev, sizeof(host), cudaMemcpyDeviceToHost, st));
   PEQA_CUDA(cudaStreamSynchronize(st));
-  if (host[0] != 0 || host[kStatusIndexWord] != 0) {
-    PEQA_CUDA(cudaMemsetAsync(dev, 0, 4 * sizeof(int), st));
-    PEQA_CUDA(cudaMemsetAsync(dev + kStatusIndexWord, 0, sizeof(int), st));
-    PEQA_CUDA(cudaStreamSynchronize(st));
-    return host[0] != 0 ? PEQA_ERR_DEVICE_TIMEOUT : PEQA_ERR_DEVICE_INDEX;
-  }
-  return PEQA_OK;
+  // one finding a call: what is not reported stays for the next
+  if (host[0] == 0 && host[kStatusIndexWord] == 0) return PEQA_OK;
+  if (host[0] != 0) PEQA_CUDA(cudaMemsetAsync(dev, 0, 4 * sizeof(int), st));
+  else PEQA_CUDA(cudaMemsetAsync(dev + kStatusIndexWord, 0, sizeof(int), st));
+  PEQA_CUDA(cudaStreamSynchronize(st));
+  return host[0] != 0 ? PEQA_ERR_DEVICE_TIMEOUT : PEQA_ERR_DEVICE_INDEX;
 }
 
 extern "C" int peqa_selftest_configure(int wait_limit_us, int starve_forward) {
