@@ -533,7 +533,8 @@ int peqa_kv_append(const peqa_kv_cache_t* cache, const peqa_rows_t* q, int n_hea
  *   out[b,h] = sum_t p_t v_t,  p = softmax over t of scale * <q[b,h], k_t>,
  *   t from max(0, seq_lens[b] - window) (from 0 if window is 0) to seq_lens[b] - 1,
  * k_t and v_t of head h / (n_heads / n_kv_heads); n_heads is a multiple of n_kv_heads.
- * A sequence of length 0 gets zeros, and -inf as lse.  What lies behind a sequence's end in its
+ * A sequence of length 0 gets zeros, and -inf as lse.  An infinite value in a bf16 cache makes its channel of the outputs that infinity, NaN
+ * where both signs meet or its p is below 2^-110.  What lies behind a sequence's end in its
  * last page, or before the window, is not read into the result.
  *   q    in   bf16 [n_seqs, n_heads, head_dim]
  *   out  out  bf16 [n_seqs, n_heads, head_dim], dense (binary32 sums, rounded to nearest even); apart from q, whose

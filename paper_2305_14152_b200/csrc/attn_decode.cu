@@ -17,8 +17,9 @@
 //   * With bf16 up to four query heads stand in the columns twice, and p's two numbers (below) in the two places.
 //   * Running maximum and sum per row, as the softmax allows: the sums are rescaled only when the maximum has risen by more than
 //     kSlack (a factor of 2^8 that the binary32 sums carry easily).
-//   * With bf16 values p goes into the second product as the sum of two of them: with one, its rounding (2^-9 of p) would double the
-//     error variance that the rounding of the output has.  8-bit codes are exact in binary16, and p in it is off by 2^-12 (3 % of that variance).
+//   * With bf16 values p goes into the second product as the sum of two of them (off by 2^-16 of p): with one, its rounding (2^-8 of p at most) would
+//     double the error variance that the rounding of the output has.  8-bit codes are exact in binary16, and p in it is off by 2^-11 of itself at
+//     most, an eighth of that (the error of outputs against 64 bits grows by 0.6 % of itself; a second binary16 for the rest costs 4 to 6 % of time).
 //   * A row that a warp has from its first tile to its last is written out.  Parts of rows are joined within the CTA in shared
 //     memory, and what crosses CTAs by a second kernel, which stands ready when the first ends.
 #include "common.cuh"
@@ -160,21 +161,19 @@ __device__ __forceinline__ uint32_t codes(uint32_t x, uint32_t which) {
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 
-// Two numbers rounded to 16 bits, and what that leaves of them; lower half: p0.
-template <bool F16>
-__device__ __forceinline__ uint32_t round16(float& p0, float& p1) {
-  uint32_t w;
-  if constexpr (F16) {
-    const __half2 h = __floats2half2_rn(p0, p1);
-    const float2 f = __half22float2(h);
-    p0 -= f.x, p1 -= f.y;
-    w = *reinterpret_cast<const uint32_t*>(&h);
-  } else {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
-    w = *reinterpret_cast<const uint32_t*>(&h);
-    p0 -= __uint_as_float(w << 16), p1 -= __uint_as_float(w & 0xffff0000u);
-  }
-  return w;
+// Two numbers as 16 bits; lower half: p0.
+__device__ __forceinline__ uint32_t half_pair(float p0, float p1) {
+  const __half2 h = __floats2half2_rn(p0, p1);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// The upper 16 bits of two numbers that are not negative, as bf16, and what they leave.  Cut and not rounded, and with the lowest bit set: both
+// parts are then above 0 wherever p is (from 2^-110 on), so that p times an infinite value is that infinity, and not 0 inf or inf - inf.  What
+// is left, below 2^-7 of p, is rounded to bf16 where it is used: 2^-16 of p at most.
+__device__ __forceinline__ uint32_t upper_halves(float& p0, float& p1) {
+  const uint32_t a = __float_as_uint(p0), b = __float_as_uint(p1);
+  p0 = __uint_as_float(a | 1u) - __uint_as_float(a & 0xffff0000u);
+  p1 = __uint_as_float(b | 1u) - __uint_as_float(b & 0xffff0000u);
+  return __byte_perm(a, b, 0x7632);
 }
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
@@ -737,8 +736,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
       for (int n = 0; n < kCols; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          hi[n][i] = round16<I8>(x[n][2 * i], x[n][2 * i + 1]);
-          lo[n][i] = I8 ? 0u : round16<I8>(x[n][2 * i], x[n][2 * i + 1]);
+          hi[n][i] = I8 ? half_pair(x[n][2 * i], x[n][2 * i + 1]) : upper_halves(x[n][2 * i], x[n][2 * i + 1]);
+          lo[n][i] = I8 ? 0u : bf16_pair(x[n][2 * i], x[n][2 * i + 1]);
           if (S::kHalves && lc >= 2) hi[n][i] = lo[n][i];
           hi[n][i] = transposed(hi[n][i]);
           if constexpr (!I8 && !S::kHalves) lo[n][i] = transposed(lo[n][i]);
@@ -903,16 +902,18 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
     const int place = task % kSlices * 32 + lane, head = place * 4 % NH, d = place * 4 / NH;
     float4 total_p = make_float4(0.f, 0.f, 0.f, 0.f), sums = total_p;
     for (uint32_t of = parts; of;) {
-      constexpr int kAtOnce = 2;               // parts at once; one that is not there is the leader with no weight
+      constexpr int kAtOnce = 2;               // parts at once; for one that is not there the leader is read, and counts as 0 (its sums may be infinite)
+      const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
       float4 f[kAtOnce], t[kAtOnce], v[kAtOnce];
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
-        const int i = of ? __ffs(of) - 1 : leader;
-        const float on = of ? 1.f : 0.f;
+        const bool there = of != 0;
+        const int i = there ? __ffs(of) - 1 : leader;
         of &= of - 1;
-        f[u] = *reinterpret_cast<const float4*>(&s_weight[i][head]) * make_float4(on, on, on, on);
+        f[u] = *reinterpret_cast<const float4*>(&s_weight[i][head]);
         t[u] = *reinterpret_cast<const float4*>(&s_total[i][head]);
         v[u] = part_of(i).four(place);
+        if (!there) f[u] = v[u] = none;
       }
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) total_p = total_p + f[u] * t[u], sums = sums + f[u] * v[u];
