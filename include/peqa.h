@@ -580,7 +580,8 @@ int peqa_check_status(void* stream);
  * kernels launched afterwards on the current device, the bound of a single
  * device-side wait to wait_limit_us microseconds (0 restores the default of two
  * seconds) and, when starve_forward is non-zero, makes the kernels of peqa_qlinear_fwd
- * announce one byte more than their copies deliver, so that the
+ * announce one byte more than their copies deliver, and that of peqa_attn_decode (where it takes
+ * tensor copies) expect an arrival that does not come, so that the
  * first stage never fills: the kernel must then leave through its time-out path,
  * free its tensor memory and report PEQA_ERR_DEVICE_TIMEOUT through
  * peqa_check_status, leaving the context usable.  Synchronises the device and

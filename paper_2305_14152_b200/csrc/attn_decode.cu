@@ -300,7 +300,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, 1) attn_decode_kernel(const At
   if (lane < 2) s_head[2 * warp + lane] = make_int4(-1, 0, 0, 0);   // each warp its own: no barrier is sure to come before its parts
   __syncwarp();
   if constexpr (S::WHOLE) {
-    if (lane < S::kUnits) ptx::mbar_init(ptx::smem_u32(&s_full[warp * S::kUnits + lane]), 1);
+    // self-test knob (peqa_selftest_configure): one arrival more than will come, so that no unit is ever full
+    if (lane < S::kUnits) ptx::mbar_init(ptx::smem_u32(&s_full[warp * S::kUnits + lane]), p.status[5] ? 2 : 1);
     ptx::fence_mbar_init();
     if (tid == 0) {
       s_abort[0] = 0;
