@@ -540,6 +540,10 @@ int peqa_kv_append(const peqa_kv_cache_t* cache, const peqa_rows_t* q, int n_hea
  *   out  out  bf16 [n_seqs, n_heads, head_dim], dense (binary32 sums, rounded to nearest even); apart from q, whose
  *             rows are read by several warps, the last perhaps when the first has written
  *   lse  out  fp32 [n_seqs, n_heads], log of the sum of exp(scale * <q, k_t>); may be NULL
+ * Scores that are all -inf give what the formula does, 0/0: NaN, and -inf as lse.
+ * Bits, beside the roundings of binary32 and of out: bf16, p_t is off by 2^-16 of itself.  8 bits: p_t times its value's scale is one binary16, off by 2^-11 of
+ * itself (out by 2^-11 of the sum of p_t |v_t| at most; its own rounding is 2^-8 of out), or by 2^-31 of the largest scale; q is a binary16 in units of its head's
+ * largest channel, off by 2^-25 of that; the sums of scores carry 128 times the sum of q along, which costs them two bits of binary32's 24.
  * workspace: peqa_attn_workspace_bytes(cache, n_heads), 256-byte aligned, in use until the call's
  * work has ended; its contents before do not matter.  The work is dealt out evenly whatever the lengths are;
  * the same lengths on the same device give the same bits.  For a page number or a length out

@@ -2,9 +2,9 @@
 //
 //   out[b,h] = sum_t p_t v_t,   p_t = exp(s_t - lse),   s_t = scale <q[b,h], k_t>,   lse = log sum_t exp(s_t)
 //
-// Every cached key and value is read once, by one warp, for all query heads that share it (a row of work: a sequence, a
-// key-value head and up to NH = 4, 8 or 16 of its query heads).  4 NH flops per cached element are too few to bind anything
-// but memory, and the rest is laid out to keep copies in flight:
+// Every cached key and value of a row of work is read once, by one warp.  A row is a sequence, a key-value head and up to NH = 4, 8 or 16 of the
+// query heads that share it (8 where D is 256): a larger group is several rows, ceil(group / NH) readings.  4 NH flops per cached element are too few to
+// bind anything but memory, and the rest is laid out to keep copies in flight:
 //   * A tile is 16 tokens of a row.  Tiles are numbered through all sequences, heads and lengths, and dealt evenly: every CTA
 //     takes an equal run of them, every warp an equal run of its CTA's.  Nothing depends on how uneven the lengths are.  (With few
 //     and short rows a CTA has a row to itself.)
