@@ -556,6 +556,29 @@ int peqa_attn_decode(const peqa_kv_cache_t* cache, const peqa_rows_t* q, int n_h
 size_t peqa_attn_workspace_bytes(const peqa_kv_cache_t* cache, int n_heads);
 
 /*
+ * Loss of a training step (App. A trains with the language model's): softmax cross entropy of the logits
+ * X * W^T over a vocabulary of V tokens, and its gradient with respect to X.  W is the head, frozen in bf16 as
+ * everything but the scales is, so there is no other gradient.
+ *   loss[t] = log sum_v exp(<X[t], W[v]>) - <X[t], W[labels[t]]>
+ *   dX[t]   = weight[t] * (sum_v p[t,v] W[v] - W[labels[t]]),  p the softmax
+ * A token with a negative label counts nothing: its loss and its row of dX are 0, and its work is left out.  A
+ * label of V or more is treated alike and noted (PEQA_ERR_DEVICE_INDEX).  loss is not multiplied by weight, which is the gradient
+ * with respect to each token's loss: 1 / (tokens that count) times a loss scale, for the mean.
+ *   X       in   bf16 [T, K]       W  in  bf16 [V, K]       labels  in  int32 [T]
+ *   weight  in   fp32 [T], or NULL: 1 for every token (not read without dX)
+ *   loss    out  fp32 [T]
+ *   dX      out  bf16 [T, K], X itself or memory apart from it; NULL: the losses alone
+ * K is a multiple of 8; T and V at most 2^24, K 2^20 (else PEQA_ERR_TOO_LARGE).  The logits exist in tensor memory
+ * only; of a piece of the vocabulary at a time their exponentials, rounded to bf16 (off by 2^-8 of themselves at most), are kept for dX, whose sums are binary32.
+ * workspace: peqa_head_loss_workspace_bytes(T, V, K, dX != NULL) bytes, 256-byte aligned, in use until the call's work has ended;
+ * its contents before do not matter.  The same inputs on the same device give the same bits.  X and W that are not finite, or
+ * whose products are not, give losses and gradients that are not, in their rows (a row of W: in all).
+ */
+int peqa_head_loss(const void* X_bf16, const void* W_bf16, const int32_t* labels, const float* weight, int T, int V, int K,
+                   float* loss, void* dX_bf16, void* workspace, size_t workspace_bytes, void* stream);
+size_t peqa_head_loss_workspace_bytes(int T, int V, int K, int need_grad);
+
+/*
  * Measurement aid (the paper has no counterpart): reads `bytes` bytes (a
  * multiple of 16, 16-byte aligned) with one CTA per SM, each CTA a contiguous
  * range, and does nothing else.  Its duration is the ceiling for any kernel that

@@ -144,6 +144,10 @@ def lib() -> ctypes.CDLL:
         L.peqa_attn_decode.restype = ctypes.c_int
         L.peqa_attn_workspace_bytes.argtypes = [cp, i32]
         L.peqa_attn_workspace_bytes.restype = sz
+        L.peqa_head_loss.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.peqa_head_loss.restype = ctypes.c_int
+        L.peqa_head_loss_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.peqa_head_loss_workspace_bytes.restype = sz
         for name in ("peqa_quantize_rtn", "peqa_pack", "peqa_unpack", "peqa_qlinear_fwd",
                      "peqa_qlinear_bwd", "peqa_qlinear_decode", "peqa_scale_adamw",
                      "peqa_train_step_host", "peqa_check_status"):
@@ -575,6 +579,25 @@ def attn_decode(cache: KVCache, q: torch.Tensor, seq_lens: torch.Tensor, scale: 
     [n_seqs, n_heads, head_dim], scale 1/sqrt(head_dim) unless given; out, if given, apart from q.  Sequences of length 0 get zeros (and -inf as lse).
     Returns out bf16 [n_seqs, n_heads, head_dim], with return_lse also log(sum(exp(scores))) fp32 [n_seqs, n_heads]."""
     return (_native or _load_native()).attn_decode(cache, q, seq_lens, scale, window, out, workspace, return_lse)
+
+
+def alloc_head_loss_workspace(X: torch.Tensor, W: torch.Tensor, need_grad: bool = True) -> torch.Tensor:
+    """Scratch of head_loss for as many tokens as X has."""
+    n = int(lib().peqa_head_loss_workspace_bytes(X.shape[0], W.shape[0], W.shape[1], 1 if need_grad else 0))
+    if n == 0:
+        raise PeqaError(-3, "peqa_head_loss_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=X.device)
+
+
+def head_loss(X: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, weight=None, need_grad: bool = True, loss=None, dX=None,
+              workspace=None):
+    """Softmax cross entropy of the logits X @ W.T, each token's, and the gradient of their sum weighted by ``weight`` with
+    respect to X; the logits are not kept.
+
+    X bf16 [tokens, features], W bf16 [vocabulary, features] (frozen), labels int32 [tokens]; tokens with a negative label
+    count nothing.  weight fp32 [tokens] is the gradient with respect to each token's loss (1 unless given; it does not multiply the loss).
+    dX may be X itself.  Returns loss fp32 [tokens] and dX bf16 [tokens, features], or None without need_grad."""
+    return (_native or _load_native()).head_loss(X, W, labels, weight, need_grad, loss, dX, workspace)
 
 
 def probe_read(buf: torch.Tensor, sink: torch.Tensor) -> None:

@@ -1,0 +1,814 @@
+// Softmax cross entropy of the vocabulary projection, with its gradient, in pieces of the vocabulary:
+//
+//   l[t,v] = sum_j X[t,j] W[v,j]          loss[t] = log sum_v exp(l[t,v] - l[t,y_t])
+//   dX[t]  = g[t] * (sum_v p[t,v] W[v] - W[y_t]),   p = softmax of l[t]
+//
+// W [V, K] is the frozen head in bf16, so dX is all there is to a gradient.  The logits are formed once and never stored:
+// a contraction costs 2 T V K operations, and with a second one for the gradient these two are all.  What allows that is a reference
+// r[t] that is known before the first logit is: r = l[t,y_t], the label's own, one dot product per token.  With e[t,v] = exp(l[t,v] - r[t]),
+// the label left out, and s[t] their sum,
+//
+//   loss[t] = r[t] - l[t,y_t] + log(s[t] + exp(l[t,y_t] - r[t]))       (= log1p(s[t]) when r is the label's logit)
+//   dX[t]   = g[t] * (sum_{v != y_t} e[t,v] W[v] - s[t] W[y_t]) / (s[t] + exp(l[t,y_t] - r[t]))
+//
+// and neither cancels: a token whose label is all but certain keeps the relative precision of its loss and gradient.  e is rounded to bf16 for
+// the second contraction (off by 2^-8 of itself at most, whatever its size, since bf16 has binary32's exponents; s is summed in binary32 before
+// that).  Nothing overflows while no logit lies more than kFarAbove above r.  Where one does, the epilogue notes the row's largest and raises
+// the chunk's flag, and the chunk's launches, which follow once more and otherwise return at once, repeat it with that as r.
+//
+// Launches.  loss_gather_kernel copies the tokens that count (labels of instruction samples are mostly ignored) side by
+// side and takes r.  Then, piece by piece of the vocabulary, head_loss_kernel works through two kinds of tiles of 256 x 256: logits
+// of piece p, whose epilogue leaves e in bf16 and its sums, and the gradient's sums over piece p - 1, added to binary32 [T, K].  Both
+// kinds in one launch share out evenly where one would leave a last round half empty; no CTA waits for another but for the
+// one that it shares its tiles with.  loss_finish_kernel adds up s and writes loss and dX.
+//
+// A tile belongs to a pair of CTAs (cta_group::2), operands come by TMA through a ring of six stages of 64, and two accumulators of
+// 256 columns fill tensor memory, so that one tile's epilogue runs under the next one's contraction.
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+#include "kv_cache.cuh"
+#include "sm100_ptx.cuh"
+#include "tensor_map.cuh"
+
+namespace peqa {
+
+namespace {
+
+using namespace ptx;
+
+constexpr int kTile = 256;                      // tokens, and vocabulary entries or features, of a tile
+constexpr int kDepth = 64;                      // contraction elements of a stage
+constexpr int kStages = 6;
+constexpr int kOperandBytes = 128 * kDepth * 2;     // this CTA's half of a stage's A or B
+constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kLossThreads = 384;               // warps: 0 TMA, 1 MMA, 2 tensor memory, 4-11 epilogue
+constexpr int kStagingBytes = 4096;             // of an epilogue warp
+constexpr int kLossSmem = kStages * kStageBytes + 8 * kStagingBytes + 1024 + 512;
+constexpr int kRowsOfBlock = 8;                 // tokens of a CTA of the kernels before and behind
+constexpr float kFarAbove = 60.0f;              // exp(60) V |W| is far below binary32's largest number
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kChunkRows = 8192;
+
+struct LossBarriers {
+  uint64_t full[kStages];        // leader: both CTAs' operands landed
+  uint64_t empty[kStages];       // each CTA: MMAs that read the stage completed
+  uint64_t acc_full[2];          // each CTA
+  uint64_t acc_empty[2];         // leader: both CTAs' epilogues drained it
+  uint32_t tmem_base;
+  int abort_flag;
+  int wait_limit_us;             // must follow abort_flag (read by the bounded waits)
+};
+
+// What the kernel before leaves of the tokens that count, in their order.
+struct LiveTokens {
+  int* count;        // [1]
+  int* index;        // token
+  int* label;
+  float* ref;        // logit of the label
+  int* above;        // bits of the largest l - ref beyond kFarAbove, 0 if there is none
+};
+
+struct LossParams {
+  LiveTokens live;
+  int* again;            // the chunk's flag
+  bool second;           // the repetition
+  float* sums;           // [halves of tiles, rows]: s, or (without gradient) pairs of largest logit and sum relative to it
+  int row0, rows;        // first live token of the chunk, rows that its buffers have (a multiple of 256)
+  int V, K, k_blocks;    // stages of a tile of logits
+  int tile0, tiles;      // tiles of the vocabulary in this launch's piece
+  int back0, back_tiles; // those of the piece before, whose gradient is summed; back_tiles 0: none
+  bool first_back;       // nothing has been summed yet
+  int splits;            // parts that the sum over a piece is cut into, each with sums of its own
+  int group;             // blocks of 256 tokens whose tiles are worked through together
+  int* status;
+};
+
+struct Item {
+  bool grad;
+  int row;               // block of 256 tokens of the chunk
+  int col;               // tile of the piece (logits), 256 features (gradient)
+  int split;
+  int kb0, kbs;          // stages of 64: the first (gradient), how many
+};
+
+// A pair's items, one after the other.  Tiles of the gradient, the longer ones as a rule, are dealt out first; the pairs that get one less
+// begin with as many tiles of logits as take its time, and the others are dealt to all.
+struct Walk {
+  int pair, pairs, n1, n2, n2_mine, lo_first, lo_pairs, lo_mine, lo_total;
+  int rows, features, splits, back_blocks;
+  __device__ __forceinline__ Walk(const LossParams& p, int rows_live) {
+    pair = blockIdx.x >> 1;
+    pairs = gridDim.x >> 1;
+    rows = (rows_live + kTile - 1) / kTile;
+    features = (p.K + kTile - 1) / kTile;
+    splits = p.splits;
+    back_blocks = p.back_tiles * (kTile / kDepth);
+    n1 = rows * p.tiles;
+    n2 = p.back_tiles ? rows * features * splits : 0;
+    n2_mine = n2 > pair ? (n2 - pair - 1) / pairs + 1 : 0;
+    lo_first = n2 % pairs;
+    lo_pairs = lo_first ? pairs - lo_first : 0;
+    const int each = lo_pairs ? (back_blocks / splits + p.k_blocks / 2) / p.k_blocks : 0;
+    lo_total = min(n1, each * lo_pairs);
+    const int e = pair - lo_first;
+    lo_mine = lo_pairs && e >= 0 && lo_total > e ? (lo_total - e - 1) / lo_pairs + 1 : 0;
+  }
+  __device__ __forceinline__ bool get(const LossParams& p, int i, Item& it) const {
+    if (i < n2_mine) {
+      int e = pair + i * pairs;
+      it.grad = true;
+      it.col = e % features;
+      e /= features;
+      it.row = e % rows;
+      it.split = e / rows;
+      it.kb0 = (int)((long long)it.split * back_blocks / splits);
+      it.kbs = (int)((long long)(it.split + 1) * back_blocks / splits) - it.kb0;
+      return true;
+    }
+    i -= n2_mine;
+    int e;
+    if (i < lo_mine) {
+      e = pair - lo_first + i * lo_pairs;
+    } else {
+      const long long at = (long long)lo_total + pair + (long long)(i - lo_mine) * pairs;
+      if (at >= n1) return false;
+      e = (int)at;
+    }
+    // groups of token blocks, in them tile by tile of the vocabulary: what the pairs read at a time stays in L2
+    const int g = e / (p.group * p.tiles), first = g * p.group, in_group = min(p.group, rows - first);
+    e -= first * p.tiles;
+    it.grad = false;
+    it.col = e / in_group;
+    it.row = first + e - it.col * in_group;
+    it.split = 0;
+    it.kb0 = 0;
+    it.kbs = p.k_blocks;
+    return true;
+  }
+};
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&b);
+}
+__device__ __forceinline__ void tma_add_2d(const CUtensorMap* m, uint32_t src_smem, int x, int y) {
+  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3}], [%1];"
+               ::"l"(reinterpret_cast<uint64_t>(m)), "r"(src_smem), "r"(x), "r"(y)
+               : "memory");
+}
+__device__ __forceinline__ void wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_kernel_behind_in() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// Reference of a live token: the label's logit, or in the repetition the row's largest if that is far above.
+__device__ __forceinline__ float above_of(const LiveTokens& live, int row) { return __int_as_float(ld_global(live.above + row)); }
+
+template <bool GRAD>
+__global__ void __launch_bounds__(kLossThreads, 1)
+head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w,
+                 const __grid_constant__ CUtensorMap tmap_wt, const __grid_constant__ CUtensorMap tmap_e_out,
+                 const __grid_constant__ CUtensorMap tmap_e_in, const __grid_constant__ CUtensorMap tmap_sum, const LossParams p) {
+  if (GRAD && p.second) {
+    wait_for_kernel_before();
+    if (ld_global(p.again) == 0) {
+      let_kernel_behind_in();
+      return;
+    }
+  }
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint8_t* staging = base + kStages * kStageBytes;
+  LossBarriers* bars = reinterpret_cast<LossBarriers*>(staging + 8 * kStagingBytes);
+  const int warp = warp_index(), lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const bool leader = rank == 0;
+  volatile int* abort_flag = &bars->abort_flag;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(smem_u32(&bars->full[s]), 1);
+      mbar_init(smem_u32(&bars->empty[s]), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(smem_u32(&bars->acc_full[b]), 1);
+      mbar_init(smem_u32(&bars->acc_empty[b]), 16);          // 8 epilogue warps in each CTA
+    }
+    bars->abort_flag = 0;
+    bars->wait_limit_us = p.status[4];
+    fence_mbar_init();
+    prefetch_tmap(&tmap_x);
+    prefetch_tmap(&tmap_w);
+    if (GRAD) {
+      prefetch_tmap(&tmap_wt);
+      prefetch_tmap(&tmap_e_out);
+      prefetch_tmap(&tmap_e_in);
+      prefetch_tmap(&tmap_sum);
+    }
+  }
+  if (warp == 2) {
+    tmem_alloc_pair(smem_u32(&bars->tmem_base), 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  wait_for_kernel_before();
+  let_next_in(false);
+  const uint32_t tmem_base = bars->tmem_base;
+  const int rows_live = min(p.rows, ld_global(p.live.count) - p.row0);     // none or fewer: no items
+  const Walk walk(p, rows_live > 0 ? rows_live : 0);
+
+  if (warp == 0) {
+    // ------------------------------------------ operands (one lane)
+    if (elect_lane() == 0) {
+      uint32_t it = 0;
+      bool ok = true;
+      Item item;
+      // self-test knob (peqa_selftest_configure): one byte more is announced than will arrive
+      const uint32_t starve = p.status[5] != 0 ? 1u : 0u;
+      for (int i = 0; ok && walk.get(p, i, item); ++i) {
+        const int row = item.row * kTile + (int)rank * 128;
+        for (int kb = 0; kb < item.kbs; ++kb, ++it) {
+          const int s = it % kStages;
+          if (!mbar_wait_cluster(smem_u32(&bars->empty[s]), ((it / kStages) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+          if (leader) mbar_arrive_expect_tx(smem_u32(&bars->full[s]), 2 * kStageBytes + starve);
+          const uint32_t bar = mapa_shared(smem_u32(&bars->full[s]), 0), a = smem_u32(base + s * kStageBytes);
+          if (!item.grad) {
+            tma_load_2d_pair(a, &tmap_x, bar, kb * kDepth, p.row0 + row);
+            tma_load_2d_pair(a + kOperandBytes, &tmap_w, bar, kb * kDepth, (p.tile0 + item.col) * kTile + (int)rank * 128);
+          } else if (GRAD) {
+            const int k = (item.kb0 + kb) * kDepth, n0 = item.col * kTile + (int)rank * 128;
+            tma_load_2d_pair(a, &tmap_e_in, bar, k, row);
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+              tma_load_2d_pair(a + kOperandBytes + m * 8192, &tmap_wt, bar, n0 + 64 * m, p.back0 * kTile + k);
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------ MMA issuer (leader CTA, one lane)
+    if (leader) if (elect_lane() == 0) {
+      constexpr uint32_t idesc_logits = idesc_bf16_f32(256, 256, 0, 0), idesc_grad = idesc_bf16_f32(256, 256, 0, 1);
+      const uint32_t a0 = smem_u32(base);
+      const uint64_t adesc0 = smem_desc_sw128(a0, 16, 1024);
+      const uint64_t bdesc_logits = smem_desc_sw128(a0 + kOperandBytes, 16, 1024);
+      const uint64_t bdesc_grad = smem_desc_sw128(a0 + kOperandBytes, 8192, 1024);
+      uint32_t s = 0, ph = 0;
+      bool ok = true;
+      Item item;
+      for (int i = 0; ok && walk.get(p, i, item); ++i) {
+        const int buf = i & 1;
+        if (!mbar_wait_cluster(smem_u32(&bars->acc_empty[buf]), ((i >> 1) & 1u) ^ 1u, abort_flag)) break;
+        tc_fence_after();
+        const uint32_t d = tmem_base + buf * 256;
+        for (int kb = 0; kb < item.kbs; ++kb) {
+          if (!mbar_wait_cluster(smem_u32(&bars->full[s]), ph, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint64_t adesc = adesc0 + s * (kStageBytes >> 4);
+          const uint32_t at = s;
+          if (!item.grad) {
+            const uint64_t bdesc = bdesc_logits + s * (kStageBytes >> 4);
+#pragma unroll
+            for (int k = 0; k < kDepth / 16; ++k)
+              mma_bf16_ss_pair(d, adesc + k * (32 / 16), bdesc + k * (32 / 16), idesc_logits, (kb | k) != 0 ? 1u : 0u);
+          } else if (GRAD) {
+            const uint64_t bdesc = bdesc_grad + s * (kStageBytes >> 4);
+#pragma unroll
+            for (int k = 0; k < kDepth / 16; ++k)
+              mma_bf16_ss_pair(d, adesc + k * (32 / 16), bdesc + k * (16 * 128 / 16), idesc_grad, (kb | k) != 0 ? 1u : 0u);
+          }
+          if (++s == kStages) {
+            s = 0;
+            ph ^= 1u;
+          }
+          mma_commit_pair(smem_u32(&bars->empty[at]), 3);
+        }
+        if (ok) mma_commit_pair(smem_u32(&bars->acc_full[buf]), 3);
+      }
+    }
+  } else if (warp >= 4) {
+    // ------------------------------------------ epilogue: thread = token, 128 of the tile's columns
+    const int quarter = warp & 3, half = (warp - 4) >> 2;
+    uint8_t* mine = staging + (warp - 4) * kStagingBytes;
+    Item item;
+    for (int i = 0; walk.get(p, i, item); ++i) {
+      const int buf = i & 1;
+      const int row_w = item.row * kTile + (int)rank * 128 + quarter * 32, row = row_w + lane;
+      const bool live = row < rows_live;
+      const uint32_t from = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * 256 + half * 128;
+      const uint32_t acc_empty = mapa_shared(smem_u32(&bars->acc_empty[buf]), 0);
+      float ref = 0.0f;
+      int label = -1, cols = 0;                             // both counted from this half tile's first entry
+      const int entry0 = (p.tile0 + item.col) * kTile + half * 128;
+      if (!item.grad) {
+        cols = p.V - entry0;
+        if (live) {
+          ref = ld_global(p.live.ref + p.row0 + row);
+          if (GRAD && p.second) ref += above_of(p.live, p.row0 + row);
+          label = ld_global(p.live.label + p.row0 + row) - entry0;
+        }
+      }
+      if (!warp_wait_cluster(smem_u32(&bars->acc_full[buf]), (uint32_t)(i >> 1) & 1u, abort_flag)) break;
+      tc_fence_after();
+      float most = -INFINITY, sum = 0.0f;
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        uint32_t v[32];
+        tmem_ld_32x32(from + c * 32, v);
+        tmem_ld_wait();
+        if (c == 3) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(acc_empty);
+        }
+        if (!item.grad) {
+          // entries beyond the vocabulary, and the label's own, are not among the others
+          if (cols < c * 32 + 32) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (c * 32 + j >= cols) v[j] = __float_as_uint(-INFINITY);
+          }
+          if ((unsigned)(label - c * 32) < 32u) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (c * 32 + j == label) v[j] = __float_as_uint(-INFINITY);
+          }
+          float here = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) here = fmaxf(here, __uint_as_float(v[j]));
+          if (!GRAD) {
+            // sums relative to the largest so far; a number that is not finite makes both so
+            const float next = fmaxf(most, here), by = next == -INFINITY ? 0.0f : next;
+            sum *= exp2_approx((most - by) * kLog2e);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sum += exp2_approx((__uint_as_float(v[j]) - by) * kLog2e);
+            most = next;
+          } else {
+            most = fmaxf(most, here);
+            uint8_t* at = mine + (c & 1) * 2048;
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            __syncwarp();
+            uint8_t* out = at + lane * 64;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float e[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                e[j] = exp2_approx((__uint_as_float(v[8 * q + j]) - ref) * kLog2e);
+                sum += e[j];
+              }
+              *reinterpret_cast<uint4*>(out + ((q ^ ((lane >> 1) & 3)) << 4)) =
+                  make_uint4(bf16_pair(e[0], e[1]), bf16_pair(e[2], e[3]), bf16_pair(e[4], e[5]), bf16_pair(e[6], e[7]));
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              if (row_w < rows_live) tma_store_2d(&tmap_e_out, smem_u32(at), item.col * kTile + half * 128 + c * 32, row_w);
+              bulk_commit_group();
+            }
+          }
+        } else if (GRAD) {
+          if (lane == 0) bulk_wait_group_read0();
+          __syncwarp();
+          uint8_t* out = mine + lane * 128;
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            *reinterpret_cast<uint4*>(out + ((q ^ (lane & 7)) << 4)) = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            const int x = item.col * kTile + half * 128 + c * 32, y = item.split * p.rows + row_w;
+            if (row_w < rows_live && x < p.K) {
+              if (p.first_back) tma_store_2d(&tmap_sum, smem_u32(mine), x, y);
+              else tma_add_2d(&tmap_sum, smem_u32(mine), x, y);
+            }
+            bulk_commit_group();
+          }
+        }
+      }
+      if (!item.grad) {
+        const size_t slot = ((size_t)(p.tile0 + item.col) * 2 + half) * p.rows + row;
+        if (!GRAD) {
+          reinterpret_cast<float2*>(p.sums)[slot] = make_float2(most, sum);
+        } else {
+          p.sums[slot] = sum;
+          if (live && !p.second && most - ref > kFarAbove) {
+            atomicMax(p.live.above + p.row0 + row, __float_as_int(most - ref));
+            *p.again = 1;
+          }
+          // the halves of the staging memory change hands by turns of c; the next tile may be of the other kind
+          if (lane == 0) bulk_wait_group_read0();
+          __syncwarp();
+        }
+      }
+    }
+    if (lane == 0) bulk_wait_group0();
+  }
+
+  if (*abort_flag) {
+    // let copies and MMAs already in flight finish before memory is released
+    for (int i = 0; i < 64; ++i) __nanosleep(1000);
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  if (warp == 2) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem_base, 512);
+  }
+  if (threadIdx.x == 0 && bars->abort_flag) {
+    atomicExch(p.status, (int)PEQA_ERR_DEVICE_TIMEOUT);
+    p.status[1] = (int)blockIdx.x;
+  }
+}
+
+struct GatherParams {
+  const __nv_bfloat16* X;
+  const __nv_bfloat16* W;
+  const int32_t* labels;
+  int T, V, K;
+  LiveTokens live;
+  __nv_bfloat16* rows;     // live tokens' X, side by side
+  int* again;              // flags of the chunks
+  int chunks;
+  float* loss;
+  __nv_bfloat16* dX;       // or nullptr
+  int* status;
+};
+
+// A warp a token: its place among those that count, its row beside theirs, and the logit of its label.  A CTA counts the tokens before its
+// own itself (16 KB of labels at 4096 tokens).
+__global__ void __launch_bounds__(kRowsOfBlock * 32) loss_gather_kernel(const GatherParams p) {
+  wait_for_kernel_before();
+  let_kernel_behind_in();
+  __shared__ int part[kRowsOfBlock];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t0 = blockIdx.x * kRowsOfBlock;
+  int before = 0;
+  for (int t = threadIdx.x; t < t0; t += kRowsOfBlock * 32) before += (unsigned)ld_global(p.labels + t) < (unsigned)p.V;
+  before = __reduce_add_sync(0xffffffffu, before);
+  if (lane == 0) part[warp] = before;
+  const int32_t near = lane < kRowsOfBlock && t0 + lane < p.T ? ld_global(p.labels + t0 + lane) : -1;
+  const uint32_t alive = __ballot_sync(0xffffffffu, (unsigned)near < (unsigned)p.V);
+  __syncthreads();
+  before = 0;
+#pragma unroll
+  for (int w = 0; w < kRowsOfBlock; ++w) before += part[w];
+  if (blockIdx.x == 0)
+    for (int c = threadIdx.x; c < p.chunks; c += kRowsOfBlock * 32) p.again[c] = 0;
+  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *p.live.count = before + __popc(alive);
+
+  const int t = t0 + warp;
+  if (t >= p.T) return;
+  const int label = __shfl_sync(0xffffffffu, near, warp);
+  const size_t own = (size_t)t * p.K;
+  if (!(alive >> warp & 1u)) {
+    if (lane == 0) {
+      if (label >= p.V) note_bad_index(p.status);
+      p.loss[t] = 0.0f;
+    }
+    if (p.dX)
+      for (int c = lane * 8; c < p.K; c += 256) *reinterpret_cast<uint4*>(p.dX + own + c) = make_uint4(0u, 0u, 0u, 0u);
+    return;
+  }
+  const int at = before + __popc(alive & ((1u << warp) - 1u));
+  const __nv_bfloat16* w = p.W + (size_t)label * p.K;
+  __nv_bfloat16* row = p.rows + (size_t)at * p.K;
+  float dot = 0.0f;
+#pragma unroll 4
+  for (int c = lane * 8; c < p.K; c += 256) {
+    const uint4 a = ld_global(reinterpret_cast<const uint4*>(p.X + own + c)), b = ld_global(reinterpret_cast<const uint4*>(w + c));
+    *reinterpret_cast<uint4*>(row + c) = a;
+    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      dot = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), dot);
+      dot = fmaf(__uint_as_float(x[e] & 0xFFFF0000u), __uint_as_float(y[e] & 0xFFFF0000u), dot);
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+  if (lane == 0) {
+    p.live.index[at] = t;
+    p.live.label[at] = label;
+    p.live.ref[at] = dot;
+    p.live.above[at] = 0;
+  }
+}
+
+struct FinishParams {
+  LiveTokens live;
+  const float* sums;
+  int halves;              // of tiles of the vocabulary
+  int row0, rows;
+  const float* grads;      // [splits, rows, K]
+  int splits, K;
+  const __nv_bfloat16* W;
+  const float* weight;     // or nullptr
+  float* loss;
+  __nv_bfloat16* dX;
+};
+
+// Eight tokens a CTA: their sums over the vocabulary, added in one order whatever the timing, then a warp a token.
+template <bool GRAD>
+__global__ void __launch_bounds__(kRowsOfBlock * 32) loss_finish_kernel(const FinishParams p) {
+  wait_for_kernel_before();
+  let_kernel_behind_in();
+  __shared__ float2 part[32][kRowsOfBlock];
+  const int row_b = blockIdx.x * kRowsOfBlock, live = min(p.rows, ld_global(p.live.count) - p.row0);
+  if (row_b >= live) return;
+  {
+    const int r = threadIdx.x & (kRowsOfBlock - 1), first = threadIdx.x / kRowsOfBlock;
+    float most = -INFINITY, sum = 0.0f;
+    for (int h = first; h < p.halves; h += 32) {
+      const size_t at = (size_t)h * p.rows + row_b + r;
+      if (GRAD) {
+        sum += ld_global(p.sums + at);
+      } else {
+        const float2 v = ld_global(reinterpret_cast<const float2*>(p.sums) + at);
+        const float next = fmaxf(most, v.x), by = next == -INFINITY ? 0.0f : next;
+        sum = sum * exp2_approx((most - by) * kLog2e) + v.y * exp2_approx((v.x - by) * kLog2e);
+        most = next;
+      }
+    }
+    part[first][r] = make_float2(most, sum);
+  }
+  __syncthreads();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = row_b + warp;
+  if (row >= live) return;
+  const float2 v = part[lane][warp];
+  float sum = v.y, most = v.x;
+  if (!GRAD) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    sum *= exp2_approx((v.x - (most == -INFINITY ? 0.0f : most)) * kLog2e);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+
+  const int token = ld_global(p.live.index + p.row0 + row);
+  // the reference above the label's logit, and the label's term
+  const float above = GRAD ? above_of(p.live, p.row0 + row) : most - ld_global(p.live.ref + p.row0 + row);
+  const float own = expf(-above);
+  if (lane == 0) {
+    float loss;
+    if (GRAD) loss = above == 0.0f ? log1pf(sum) : above + logf(sum + own);
+    else loss = above <= 0.0f ? log1pf(sum * expf(above)) : above + logf(sum + own);
+    p.loss[token] = loss;
+  }
+  if (!GRAD) return;
+  const float by = (p.weight ? ld_global(p.weight + token) : 1.0f) / (sum + own);
+  const __nv_bfloat16* w = p.W + (size_t)ld_global(p.live.label + p.row0 + row) * p.K;
+  const float* g = p.grads + (size_t)row * p.K;
+  const size_t per_split = (size_t)p.rows * p.K;
+  __nv_bfloat16* out = p.dX + (size_t)token * p.K;
+#pragma unroll 2
+  for (int c = lane * 8; c < p.K; c += 256) {
+    float4 lo = ld_global(reinterpret_cast<const float4*>(g + c)), hi = ld_global(reinterpret_cast<const float4*>(g + c + 4));
+    for (int s = 1; s < p.splits; ++s) {
+      const float4 a = ld_global(reinterpret_cast<const float4*>(g + s * per_split + c));
+      const float4 b = ld_global(reinterpret_cast<const float4*>(g + s * per_split + c + 4));
+      lo.x += a.x; lo.y += a.y; lo.z += a.z; lo.w += a.w;
+      hi.x += b.x; hi.y += b.y; hi.z += b.z; hi.w += b.w;
+    }
+    const uint4 b = ld_global(reinterpret_cast<const uint4*>(w + c));
+    const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    const uint32_t y[4] = {b.x, b.y, b.z, b.w};
+    uint32_t o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      o[e] = bf16_pair(fmaf(-sum, __uint_as_float(y[e] << 16), v[2 * e]) * by,
+                       fmaf(-sum, __uint_as_float(y[e] & 0xFFFF0000u), v[2 * e + 1]) * by);
+    *reinterpret_cast<uint4*>(out + c) = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+}
+
+// ------------------------------------------------------------- host side
+
+struct LossPlan {
+  int rows;                  // live tokens of a chunk at most, a multiple of 256
+  int chunks;
+  int tiles, pieces, splits;
+  int group;
+  // offsets into the workspace
+  size_t count, again, index, label, ref, above, x, sums, e[2], grads, bytes;
+  int piece_tile(int i) const { return (int)((long long)tiles * i / pieces); }
+  int piece_width() const { return ((tiles + pieces - 1) / pieces) * kTile; }     // entries of the widest
+};
+
+// Sizes and cuts, by the sizes of the call alone.
+LossPlan plan_loss(int T, int V, int K, bool grad, int sms) {
+  LossPlan c = {};
+  const int pairs = sms / 2 > 0 ? sms / 2 : 1;
+  // tokens of a chunk: their sums of the gradient are 256 MB at most (or 256 tokens')
+  long long most = ((1ll << 26) / K) & ~255ll;
+  most = most < 256 ? 256 : most > kChunkRows ? kChunkRows : most;
+  const long long all = ((long long)T + 255) & ~255ll;
+  c.rows = (int)(all < most ? all : most);
+  c.chunks = (int)((all + c.rows - 1) / c.rows);
+  c.tiles = (int)(((long long)V + kTile - 1) / kTile);
+  c.pieces = 1;
+  c.splits = 1;
+  // token blocks that share an L2 with a tile or two of the vocabulary for each pair
+  c.group = (int)((32ll << 20) / (512ll * K));
+  c.group = c.group < 4 ? 4 : c.group;
+  if (grad) {
+    // 64 MB of exponentials a piece
+    const long long wide = (64ll << 20) / (512ll * c.rows);
+    c.pieces = (int)((c.tiles + wide - 1) / wide);
+    const int back = (c.rows / kTile) * ((K + kTile - 1) / kTile);
+    if (back < pairs) {
+      c.splits = pairs / back;
+      const int least = c.tiles / c.pieces * (kTile / kDepth);
+      if (c.splits > least) c.splits = least;
+      if (c.splits > 16) c.splits = 16;
+    }
+  }
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at = (at + bytes + 255) & ~(size_t)255;
+    return here;
+  };
+  const size_t rows_all = (size_t)c.chunks * c.rows;
+  c.count = take(4);
+  c.again = take((size_t)c.chunks * 4);
+  c.index = take(rows_all * 4);
+  c.label = take(rows_all * 4);
+  c.ref = take(rows_all * 4);
+  c.above = take(rows_all * 4);
+  c.x = take(rows_all * K * 2);
+  c.sums = take((size_t)c.tiles * 2 * c.rows * (grad ? 4 : 8));
+  if (grad) {
+    c.e[0] = take((size_t)c.rows * c.piece_width() * 2);
+    c.e[1] = c.pieces > 1 ? take((size_t)c.rows * c.piece_width() * 2) : c.e[0];
+    c.grads = take((size_t)c.splits * c.rows * K * 4);
+  }
+  c.bytes = at;
+  return c;
+}
+
+int loss_map(CUtensorMap* m, CUtensorMapDataType type, const void* base, uint64_t inner, uint64_t outer, int size, uint32_t box_x,
+             uint32_t box_y, CUtensorMapSwizzle swizzle) {
+  EncodeTiledFn enc = nullptr;
+  PEQA_TRY(tensor_map_encoder(&enc));
+  cuuint64_t dims[2] = {inner, outer};
+  cuuint64_t strides[1] = {inner * size};
+  cuuint32_t box[2] = {box_x, box_y};
+  cuuint32_t estr[2] = {1, 1};
+  if (enc(m, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return cuda_fail(cudaErrorInvalidValue);
+  return PEQA_OK;
+}
+int bf16_map(CUtensorMap* m, const void* base, uint64_t inner, uint64_t outer, uint32_t box_y) {
+  return loss_map(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, inner, outer, 2, 64, box_y, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+template <bool GRAD>
+int launch_loss(const CUtensorMap (&maps)[6], const LossParams& p, int pairs, cudaStream_t st) {
+  auto kern = head_loss_kernel<GRAD>;
+  static std::atomic<uint64_t> done{0};
+  PEQA_TRY(allow_smem(kern, kLossSmem, done));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * pairs, 1, 1);
+  cfg.blockDim = dim3(kLossThreads, 1, 1);
+  cfg.dynamicSmemBytes = kLossSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  PEQA_CUDA(cudaLaunchKernelEx(&cfg, kern, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], p));
+  return PEQA_OK;
+}
+
+}  // namespace
+
+}  // namespace peqa
+
+using namespace peqa;
+
+static bool loss_shape_ok(int T, int V, int K) { return T > 0 && V > 0 && K > 0 && K % 8 == 0; }
+// K and V so that no count below passes 31 bits
+static bool loss_size_ok(int T, int V, int K) { return T <= (1 << 24) && V <= (1 << 24) && K <= (1 << 20); }
+
+extern "C" size_t peqa_head_loss_workspace_bytes(int T, int V, int K, int need_grad) {
+  if (!loss_shape_ok(T, V, K) || !loss_size_ok(T, V, K)) return 0;
+  return plan_loss(T, V, K, need_grad != 0, sm_count_or(148)).bytes;
+}
+
+extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* labels, const float* weight, int T, int V, int K,
+                              float* loss, void* dX, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!X || !W || !labels || !loss) return PEQA_ERR_NULL;
+  if (!loss_shape_ok(T, V, K)) return PEQA_ERR_BAD_SHAPE;
+  if (!loss_size_ok(T, V, K)) return PEQA_ERR_TOO_LARGE;
+  if (!aligned16(X) || !aligned16(W) || !aligned16(labels) || !aligned16(loss) || !aligned16(dX) || !aligned16(weight))
+    return PEQA_ERR_ALIGNMENT;
+  PEQA_TRY(check_arch());
+  const int sms = sm_count_or(148), pairs = sms / 2;
+  const LossPlan c = plan_loss(T, V, K, dX != nullptr, sms);
+  if (!workspace || workspace_bytes < c.bytes) return PEQA_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return PEQA_ERR_ALIGNMENT;
+  cudaStream_t st = as_stream(stream);
+  char* ws = static_cast<char*>(workspace);
+  int* status = nullptr;
+  PEQA_TRY(status_word(st, &status));
+
+  LiveTokens live;
+  live.count = reinterpret_cast<int*>(ws + c.count);
+  live.index = reinterpret_cast<int*>(ws + c.index);
+  live.label = reinterpret_cast<int*>(ws + c.label);
+  live.ref = reinterpret_cast<float*>(ws + c.ref);
+  live.above = reinterpret_cast<int*>(ws + c.above);
+
+  LossParams p = {};
+  p.live = live;
+  p.sums = reinterpret_cast<float*>(ws + c.sums);
+  p.rows = c.rows;
+  p.V = V;
+  p.K = K;
+  p.k_blocks = (K + kDepth - 1) / kDepth;
+  p.splits = c.splits;
+  p.group = c.group;
+  p.status = status;
+  const uint64_t width = c.piece_width();
+  CUtensorMap maps[6], e_out[2], e_in[2];
+  PEQA_TRY(bf16_map(&maps[0], ws + c.x, K, (uint64_t)c.chunks * c.rows, 128));
+  PEQA_TRY(bf16_map(&maps[1], W, K, V, 128));
+  PEQA_TRY(bf16_map(&maps[2], W, K, V, 64));
+  maps[3] = maps[4] = maps[5] = maps[0];
+  if (dX) {
+    for (int b = 0; b < 2; ++b) {
+      PEQA_TRY(loss_map(&e_out[b], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, ws + c.e[b], width, c.rows, 2, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B));
+      PEQA_TRY(bf16_map(&e_in[b], ws + c.e[b], width, c.rows, 128));
+    }
+    PEQA_TRY(loss_map(&maps[5], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, ws + c.grads, K, (uint64_t)c.splits * c.rows, 4, 32, 32,
+                      CU_TENSOR_MAP_SWIZZLE_128B));
+  }
+
+  GatherParams gp = {};
+  gp.X = static_cast<const __nv_bfloat16*>(X);
+  gp.W = static_cast<const __nv_bfloat16*>(W);
+  gp.labels = labels;
+  gp.T = T;
+  gp.V = V;
+  gp.K = K;
+  gp.live = live;
+  gp.rows = reinterpret_cast<__nv_bfloat16*>(ws + c.x);
+  gp.again = reinterpret_cast<int*>(ws + c.again);
+  gp.chunks = c.chunks;
+  gp.loss = loss;
+  gp.dX = static_cast<__nv_bfloat16*>(dX);
+  gp.status = status;
+  PEQA_TRY(launch_after(loss_gather_kernel, (T + kRowsOfBlock - 1) / kRowsOfBlock, kRowsOfBlock * 32, st, gp));
+
+  FinishParams fp = {};
+  fp.live = live;
+  fp.sums = p.sums;
+  fp.halves = 2 * c.tiles;
+  fp.rows = c.rows;
+  fp.grads = reinterpret_cast<const float*>(ws + c.grads);
+  fp.splits = c.splits;
+  fp.K = K;
+  fp.W = gp.W;
+  fp.weight = weight;
+  fp.loss = loss;
+  fp.dX = gp.dX;
+  for (int ch = 0; ch < c.chunks; ++ch) {
+    p.row0 = fp.row0 = ch * c.rows;
+    p.again = gp.again + ch;
+    for (int turn = 0; turn < (dX ? 2 : 1); ++turn) {
+      p.second = turn == 1;
+      for (int i = 0; i <= (dX ? c.pieces : 0); ++i) {
+        p.tile0 = i < c.pieces ? c.piece_tile(i) : 0;
+        p.tiles = i < c.pieces ? c.piece_tile(i + 1) - p.tile0 : 0;
+        p.back0 = i > 0 ? c.piece_tile(i - 1) : 0;
+        p.back_tiles = i > 0 ? c.piece_tile(i) - p.back0 : 0;
+        p.first_back = i == 1;
+        if (dX) {
+          maps[3] = e_out[i & 1];
+          maps[4] = e_in[(i & 1) ^ 1];
+          PEQA_TRY(launch_loss<true>(maps, p, pairs, st));
+        } else {
+          PEQA_TRY(launch_loss<false>(maps, p, pairs, st));
+        }
+      }
+    }
+    const int blocks = (c.rows < T ? c.rows : T + kRowsOfBlock - 1) / kRowsOfBlock;
+    PEQA_TRY(launch_after(dX ? loss_finish_kernel<true> : loss_finish_kernel<false>, blocks, kRowsOfBlock * 32, st, fp));
+  }
+  return PEQA_OK;
+}

@@ -250,6 +250,69 @@ PyObject* qlinear_decode_prepared(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// A tensor [rows, cols] of this type on `like`'s device, or the caller's.
+at::Tensor matrix(PyObject* given, const at::Tensor& like, at::IntArrayRef shape, at::ScalarType dtype, const char* name) {
+  if (given == Py_None) return at::empty(shape, like.options().dtype(dtype));
+  const at::Tensor& t = dev(given, dtype, name);
+  if (t.sizes() != shape || t.device() != like.device()) {
+    PyErr_Format(PyExc_ValueError, "%s: not of the shape, or on the device, that the call writes", name);
+    fail();
+  }
+  return t;
+}
+
+// (X, W, labels, weight, need_grad, loss, dX, workspace) -> (loss, dX)
+PyObject* head_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  arity(n, 8);
+  const at::Tensor &X = dev(a[0], at::kBFloat16, "X"), &W = dev(a[1], at::kBFloat16, "W"), &labels = dev(a[2], at::kInt, "labels");
+  const int64_t T = X.dim() == 2 ? X.size(0) : 0, K = X.dim() == 2 ? X.size(1) : 0, V = W.dim() == 2 ? W.size(0) : 0;
+  if (X.dim() != 2 || W.dim() != 2 || W.size(1) != K || labels.dim() != 1 || labels.size(0) != T) {
+    PyErr_SetString(PyExc_ValueError, "X [tokens, features], W [vocabulary, features] and labels [tokens] do not belong together");
+    fail();
+  }
+  if (X.get_device() != c10::cuda::current_device() || W.device() != X.device() || labels.device() != X.device()) {
+    PyErr_SetString(PyExc_ValueError, "X, W and labels: expected tensors on the current CUDA device");
+    fail();
+  }
+  const int grad = PyObject_IsTrue(a[4]);
+  if (grad < 0) fail();
+  const float* weight = nullptr;
+  if (a[3] != Py_None) {
+    const at::Tensor& w = dev(a[3], at::kFloat, "weight");
+    if (w.dim() != 1 || w.size(0) != T || w.device() != X.device()) {
+      PyErr_SetString(PyExc_ValueError, "weight: expected one value per token, on the device of X");
+      fail();
+    }
+    weight = w.data_ptr<float>();
+  }
+  at::Tensor loss = matrix(a[5], X, {T}, at::kFloat, "loss"), dX;
+  if (grad) dX = matrix(a[6], X, {T, K}, at::kBFloat16, "dX");
+  const Workspace given(a[7]);
+  at::Tensor own;
+  void* wp = given.p;
+  size_t wb = given.bytes;
+  const bool fits = T <= INT32_MAX && V <= INT32_MAX && K <= INT32_MAX;
+  if (a[7] == Py_None && fits) {
+    wb = peqa_head_loss_workspace_bytes((int)T, (int)V, (int)K, grad);
+    if (wb > 0) {
+      own = at::empty({(int64_t)wb}, X.options().dtype(at::kByte));
+      wp = own.data_ptr();
+    }
+  }
+  void *x = X.data_ptr(), *w = W.data_ptr(), *dx = grad ? dX.data_ptr() : nullptr, *st = stream();
+  const int32_t* lab = labels.data_ptr<int32_t>();
+  float* out = loss.data_ptr<float>();
+  check(fits ? unlocked([&] { return peqa_head_loss(x, w, lab, weight, (int)T, (int)V, (int)K, out, dx, wp, wb, st); })
+             : (int)PEQA_ERR_TOO_LARGE,
+        "peqa_head_loss");
+  Ref first(THPVariable_Wrap(std::move(loss)));
+  if (!grad) return PyTuple_Pack(2, first.p, Py_None);
+  Ref second(THPVariable_Wrap(std::move(dX)));
+  return PyTuple_Pack(2, first.p, second.p);
+  END_HANDLE_TH_ERRORS
+}
+
 // (values, gradient, m, v, lr, beta1, beta2, eps, weight_decay, step), for the scales or the zero-points
 template <typename F>
 PyObject* adamw(PyObject* const* a, Py_ssize_t n, const char* values, const char* grad, F entry, const char* where) {
@@ -612,6 +675,7 @@ PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {FAST(qlinear_fwd),       FAST(qlinear_fwd_zf), FAST(qlinear_decode), FAST(qlinear_decode_prepared),
+                          FAST(head_loss),
                           FAST(scale_adamw),       FAST(zero_adamw),     FAST(layer_train_step),
                           FAST(kv_append),         FAST(attn_decode),
                           {"bind_error", bind_error, METH_O, nullptr},   {nullptr, nullptr, 0, nullptr}};
