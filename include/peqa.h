@@ -454,6 +454,26 @@ int peqa_qlinear_decode_prepared(const peqa_qweight_t* w, const uint32_t* prepar
                                  void* stream);
 
 /*
+ * The gated feed-forward block of a decoder layer, H = act(X Wg^T) * (X Wu^T) with gate and up projection quantized (Eq. 2), up to
+ * the down projection.  Both projections are ONE quantized linear w of out_features = 2F rows, F a multiple of 8: rows
+ * 16i .. 16i + 7 are the gate's rows 8i .. 8i + 7, rows 16i + 8 .. 16i + 15 the up projection's rows 8i .. 8i + 7 (quantization works row by
+ * row, so this can be done before or after it).  All that takes a linear takes the block: with dY of peqa_glu_bwd the gradients
+ * (peqa_qlinear_bwd, whose dX is then the sum over both projections, and the calls beside it), AdamW, peqa_decode_prepare.
+ *   peqa_qglu_fwd: Y = X W_hat^T, H[t,c] = act(Y[t, gate row of c]) * Y[t, up row of c] (of Y before it is rounded)
+ *     X in bf16 [T, K];  Y out bf16 [T, 2F], for the backward pass, or NULL;  H out bf16 [T, F].
+ *     K % 64 == 0, with 3 bits K % 128 == 0; T >= 1.  Y's bits are peqa_qlinear_fwd's.
+ *   peqa_glu_bwd: dY from Y and dH in bf16 [T, F]; dY out bf16 [T, 2F], Y itself or memory apart from it.
+ *   peqa_qglu_decode_prepared: H [M, F] of 1 to 16 tokens from the prepared weights; arguments, shapes and the time at which
+ *     `prepared` has to be final as with peqa_qlinear_decode_prepared.
+ * activation: silu, x / (1 + exp(-x)), or gelu in its tanh form, x/2 (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))); evaluated in binary32.
+ */
+typedef enum { PEQA_ACT_SILU = 0, PEQA_ACT_GELU_TANH = 1 } peqa_activation;
+int peqa_qglu_fwd(const peqa_qweight_t* w, int activation, const void* X_bf16, int T, void* Y_bf16, void* H_bf16, void* stream);
+int peqa_glu_bwd(int activation, const void* Y_bf16, const void* dH_bf16, int T, int F, void* dY_bf16, void* stream);
+int peqa_qglu_decode_prepared(const peqa_qweight_t* w, int activation, const uint32_t* prepared, const void* X_bf16, int M,
+                              void* H_bf16, const float* scale_table, int n_tasks, const int32_t* task_ids, void* stream);
+
+/*
  * Token generation around the quantized linears (Sec. 3.1): between the q, k and v
  * projections of a decoder layer and its output projection stand the rotation of
  * the new queries and keys by their positions, the cache of keys and values, and

@@ -144,6 +144,12 @@ def lib() -> ctypes.CDLL:
         L.peqa_attn_decode.restype = ctypes.c_int
         L.peqa_attn_workspace_bytes.argtypes = [cp, i32]
         L.peqa_attn_workspace_bytes.restype = sz
+        L.peqa_qglu_fwd.argtypes = [qp, i32, vp, i32, vp, vp, vp]
+        L.peqa_qglu_fwd.restype = ctypes.c_int
+        L.peqa_glu_bwd.argtypes = [i32, vp, vp, i32, i32, vp, vp]
+        L.peqa_glu_bwd.restype = ctypes.c_int
+        L.peqa_qglu_decode_prepared.argtypes = [qp, i32, vp, vp, i32, vp, vp, i32, vp, vp]
+        L.peqa_qglu_decode_prepared.restype = ctypes.c_int
         L.peqa_head_loss.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, sz, vp]
         L.peqa_head_loss.restype = ctypes.c_int
         L.peqa_head_loss_workspace_bytes.argtypes = [i32, i32, i32, i32]
@@ -527,6 +533,49 @@ def qlinear_decode_prepared(w: QWeight, prepared: torch.Tensor, X: torch.Tensor,
     """Decode from the prepared weights; with scale_table [n_tasks, N, G] and task_ids [M] every
     token uses the scales of its own task."""
     return (_native or _load_native()).qlinear_decode_prepared(w, prepared, X, Y, scale_table, task_ids)
+
+
+def glu_rows(gate: torch.Tensor, up: torch.Tensor) -> torch.Tensor:
+    """Rows of the gate and of the up projection (weights, codes, zero-points, scales, or their gradients), in the order of the gated block: runs
+    of eight by turns."""
+    if gate.shape != up.shape or gate.shape[0] % 8:
+        raise ValueError("gate and up: expected one shape, rows a multiple of 8")
+    return torch.stack([gate.unflatten(0, (-1, 8)), up.unflatten(0, (-1, 8))], 1).flatten(0, 2)
+
+
+def glu_split(rows: torch.Tensor):
+    """The inverse of glu_rows: (gate, up)."""
+    if rows.shape[0] % 16:
+        raise ValueError("rows: expected a multiple of 16")
+    halves = rows.unflatten(0, (-1, 2, 8))
+    return halves[:, 0].flatten(0, 1), halves[:, 1].flatten(0, 1)
+
+
+def glu_interleave(gate: QWeight, up: QWeight) -> QWeight:
+    """The gated block of two quantized projections: one linear of the rows of both."""
+    if (gate.bits, gate.K, gate.G) != (up.bits, up.K, up.G):
+        raise ValueError("gate and up: expected one number of bits, input width and group size")
+    return QWeight(gate.bits, gate.N + up.N, gate.K, gate.group_size, glu_rows(gate.qweight, up.qweight), glu_rows(gate.zeros, up.zeros),
+                   glu_rows(gate.scales, up.scales))
+
+
+def qglu_fwd(w: QWeight, X: torch.Tensor, activation: str = "silu", keep: bool = True, Y=None, H=None):
+    """Forward of a gated block (rows as glu_rows puts them): H = act(gate) * up bf16 [tokens, N / 2] and, with ``keep`` or a Y to
+    write, the sums Y bf16 [tokens, N] that glu_bwd wants; activation "silu" or "gelu_tanh".  Returns (H, Y or None)."""
+    return (_native or _load_native()).qglu_fwd(w, X, activation, keep, Y, H)
+
+
+def glu_bwd(Y: torch.Tensor, dH: torch.Tensor, activation: str = "silu", dY=None):
+    """dY bf16 [tokens, N] of a gated block from Y and dH bf16 [tokens, N / 2]; dY may be Y itself.  The block's own gradients are those
+    of its linear: qlinear_bwd(w, X, dY) and the calls beside it."""
+    return (_native or _load_native()).glu_bwd(Y, dH, activation, dY)
+
+
+def qglu_decode_prepared(w: QWeight, prepared: torch.Tensor, X: torch.Tensor, activation: str = "silu", H=None, scale_table=None,
+                         task_ids=None):
+    """Outputs of a gated block for 1 to 16 tokens, bf16 [tokens, N / 2], from its prepared weights (decode_prepare); scale_table and
+    task_ids as in qlinear_decode_prepared."""
+    return (_native or _load_native()).qglu_decode_prepared(w, prepared, X, activation, H, scale_table, task_ids)
 
 
 @dataclass

@@ -5,6 +5,7 @@
 #include <atomic>
 #include <math.h>
 
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -218,8 +219,11 @@ int launch_ds_channel(const peqa_qweight_t* w, const float* ds_part, int slots, 
                       cudaStream_t st);
 bool fwd_pair_supported(const peqa_qweight_t* w);
 // ds_part != nullptr (one scale per channel): sums of dY * u per channel, see fwd_pair_sm100.cu
+// glu != nullptr: a gated block (glu.cuh), whose Y may be nullptr
+struct GluOut;
 int launch_fwd_pair(const peqa_qweight_t* w, const float* zeros_f, int g, const void* X, int T,
-                    void* Y, const void* dY, float* ds_part, cudaStream_t st, Side side);
+                    void* Y, const void* dY, float* ds_part, cudaStream_t st, Side side, const GluOut* glu = nullptr);
+int launch_glu_fwd(const peqa_qweight_t* w, int g, const void* X, int T, void* Y, const GluOut& glu, cudaStream_t st);
 bool dx_pair_supported(const peqa_qweight_t* w);
 int launch_dx_pair(const peqa_qweight_t* w, const float* zeros_f, int g, const void* dY, int T,
                    void* dX, Side side, cudaStream_t st);
@@ -232,7 +236,8 @@ bool split_is_faster(const peqa_qweight_t* w, int T, bool trans, bool channel_sc
 int split_ds_slots(const peqa_qweight_t* w, int T);
 int split_part_tokens(const peqa_qweight_t* w, int T_call, bool trans);
 int launch_split(const peqa_qweight_t* w, const float* zeros_f, int g, const void* act, int T, void* out,
-                 bool trans, const void* dY, float* ds_part, cudaStream_t st, int T_call, int t0, Side side = kInOrder);
+                 bool trans, const void* dY, float* ds_part, cudaStream_t st, int T_call, int t0, Side side = kInOrder,
+                 const GluOut* glu = nullptr);
 // adam != nullptr: the AdamW step on (w->scales, m, v) is applied where dS is produced
 struct DsAdam {
   AdamWConsts c;

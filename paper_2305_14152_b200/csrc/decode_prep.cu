@@ -93,6 +93,7 @@
 
 #include "common.cuh"
 #include "dequant.cuh"
+#include "glu.cuh"
 #include "sm100_ptx.cuh"
 
 namespace peqa {
@@ -146,6 +147,7 @@ struct PrepParams {
   int row_bytes;            // of the canonical matrix
   int cshift;               // log2 of the CTAs that share a range of rows, each with a slice of K
   uint32_t m_magic[2];      // quotient_magic of M and of (M + 1) / 2
+  GluOut glu;               // H != nullptr: a gated block, H [M, N / 2] instead of Y
   int* status;
 };
 
@@ -1183,6 +1185,18 @@ decode_prep_kernel(const PrepParams p) {
         mine[at1] = sum[1];
         continue;
       }
+      if (p.glu.H) {
+        // the pair's sixteen rows are eight gate rows and their up rows, in the halves of half a warp (which is in step: its
+        // lanes differ in lr alone); a CTA's ranges are whole pairs then
+        const uint32_t half = 0xFFFFu << (threadIdx.x & 16);
+        const float up0 = __shfl_xor_sync(half, sum[0], 8), up1 = __shfl_xor_sync(half, sum[1], 8);
+        if (lr < 8) {
+          __nv_bfloat16* at = p.glu.H + (size_t)m * (p.N >> 1) + (pair_rg(lp) >> 1) * kGluRun + lr;
+          at[0] = __float2bfloat16_rn(glu_value(sum[0], up0, p.glu.act));
+          if (m + 1 < p.M) at[p.N >> 1] = __float2bfloat16_rn(glu_value(sum[1], up1, p.glu.act));
+        }
+        continue;
+      }
       p.Y[(size_t)m * p.N + row] = __float2bfloat16_rn(sum[0]);
       if (m + 1 < p.M) p.Y[(size_t)(m + 1) * p.N + row] = __float2bfloat16_rn(sum[1]);
     }
@@ -1209,6 +1223,12 @@ decode_prep_kernel(const PrepParams p) {
         for (int r = 0; r < 4; ++r) v[r] = rh + r < csize ? ld_cluster_f32(mapa_shared(at, (uint32_t)(rh + r))) : 0.0f;
 #pragma unroll
         for (int r = 0; r < 4; ++r) sum += v[r];
+      }
+      if (p.glu.H) {
+        const float up = __shfl_xor_sync(0xFFFFu << (threadIdx.x & 16), sum, 8);
+        if (lr < 8)
+          p.glu.H[(size_t)m * (p.N >> 1) + (pair_rg(lp) >> 1) * kGluRun + lr] = __float2bfloat16_rn(glu_value(sum, up, p.glu.act));
+        continue;
       }
       p.Y[(size_t)m * p.N + pair_rg(lp) * 8 + lr] = __float2bfloat16_rn(sum);
     }
@@ -1354,7 +1374,8 @@ int x_pitch_for(int steps) {
 //
 // i8 (one or two tokens): the plan of the integer kernel, whose activations take four bytes each and are all
 // staged at once, at most four steps to a half-warp.
-int plan_prep(int N, int K, int M, int bits, int gcols, bool canon, bool i8, bool tasks, PrepPlan* plan) {
+// whole_pairs: the CTAs' ranges are pairs of row groups (the gated block, whose gate and up rows share one).
+int plan_prep(int N, int K, int M, int bits, int gcols, bool canon, bool i8, bool tasks, PrepPlan* plan, bool whole_pairs = false) {
   const int sms = sm_count_or(148);
   const int rgs = N / 8;
   const int NT = M <= 8 ? 1 : 2, TOKP = 8 * NT;
@@ -1376,6 +1397,7 @@ int plan_prep(int N, int K, int M, int bits, int gcols, bool canon, bool i8, boo
       if (ci > 0 && (c.T < (1 << ci) || active[ci] < 1 || !(grouped || one_group))) continue;
       const int Tl = (c.T + (1 << ci) - 1) >> ci;                     // most steps of a CTA
       c.rg_per_cta = (rgs + active[ci] * waves - 1) / (active[ci] * waves);
+      if (whole_pairs) c.rg_per_cta = (c.rg_per_cta + 1) & ~1;
       c.grid = ((rgs + c.rg_per_cta - 1) / c.rg_per_cta) << ci;
       // a range that starts and ends at an odd row group holds the most pairs
       c.pairs = c.rg_per_cta / 2 + 1;
@@ -1505,9 +1527,11 @@ bool prep_group_supported(int K, int g) {
   return g == K || g % kStepCols == 0 || g == 64 || g == 128 || g == 256;
 }
 
-// One launch over prepared or canonical weights, or (prepared ones) two of at most eight tokens each.
+// One launch over prepared or canonical weights, or (prepared ones) two of at most eight tokens each.  glu (prepared): the outputs of a gated
+// block in place of Y.
 int run_decode(const peqa_qweight_t* w, const void* weights, bool canon, int g, const void* X, int M, void* Y,
-               const float* scale_table, int n_tasks, const int32_t* task_ids, cudaStream_t st) {
+               const float* scale_table, int n_tasks, const int32_t* task_ids, cudaStream_t st, const GluOut& glu = {}) {
+  const bool pairs = glu.H != nullptr;
   PrepPlan plan;
   bool two = false;
   // A row that is one group of 64, 128 or 256 columns is taken for one with groups inside the step, but for canonical rows with a
@@ -1515,11 +1539,11 @@ int run_decode(const peqa_qweight_t* w, const void* weights, bool canon, int g, 
   const int gcols = canon && task_ids && g < kStepCols ? kStepCols : g;
   if (M > 8) {
     PrepPlan half;
-    PEQA_TRY(plan_prep(w->out_features, w->in_features, (M + 1) / 2, w->bits, g, false, false, task_ids != nullptr, &half));
-    two = task_ids || plan_prep(w->out_features, w->in_features, M, w->bits, g, false, false, false, &plan) != PEQA_OK ||
+    PEQA_TRY(plan_prep(w->out_features, w->in_features, (M + 1) / 2, w->bits, g, false, false, task_ids != nullptr, &half, pairs));
+    two = task_ids || plan_prep(w->out_features, w->in_features, M, w->bits, g, false, false, false, &plan, pairs) != PEQA_OK ||
           2 * half.ns < plan.ns;
-  } else if (M > 2 || plan_prep(w->out_features, w->in_features, M, w->bits, gcols, canon, true, task_ids != nullptr, &plan) != PEQA_OK) {
-    PEQA_TRY(plan_prep(w->out_features, w->in_features, M, w->bits, gcols, canon, false, task_ids != nullptr, &plan));
+  } else if (M > 2 || plan_prep(w->out_features, w->in_features, M, w->bits, gcols, canon, true, task_ids != nullptr, &plan, pairs) != PEQA_OK) {
+    PEQA_TRY(plan_prep(w->out_features, w->in_features, M, w->bits, gcols, canon, false, task_ids != nullptr, &plan, pairs));
   }
   if (two) {
     // Two launches of at most eight tokens each, the second of which finds the weights in L2: with a
@@ -1529,10 +1553,11 @@ int run_decode(const peqa_qweight_t* w, const void* weights, bool canon, int g, 
     // for 9; of 4-bit weights, whose rings are larger, 70000, 103000 and 131000; with 512 columns about 1.9 times as many).
     const int h = (M + 1) / 2;
     const size_t K = (size_t)w->in_features, N = (size_t)w->out_features;
-    PEQA_TRY(run_decode(w, weights, false, g, X, h, Y, scale_table, n_tasks, task_ids, st));
+    const GluOut behind = {pairs ? glu.H + (size_t)h * (N / 2) : nullptr, glu.act};
+    PEQA_TRY(run_decode(w, weights, false, g, X, h, Y, scale_table, n_tasks, task_ids, st, glu));
     return run_decode(w, weights, false, g, static_cast<const char*>(X) + (size_t)h * K * 2, M - h,
-                      static_cast<char*>(Y) + (size_t)h * N * 2, scale_table, n_tasks,
-                      task_ids ? task_ids + h : nullptr, st);
+                      pairs ? nullptr : static_cast<char*>(Y) + (size_t)h * N * 2, scale_table, n_tasks,
+                      task_ids ? task_ids + h : nullptr, st, behind);
   }
   PrepParams p;
   p.P = static_cast<const uint8_t*>(weights);
@@ -1557,6 +1582,7 @@ int run_decode(const peqa_qweight_t* w, const void* weights, bool canon, int g, 
   p.pairs_per_cta = plan.pairs;
   p.cshift = plan.cshift;
   p.row_bytes = p.K / 8 * w->bits;
+  p.glu = glu;
   p.m_magic[0] = quotient_magic(M);
   p.m_magic[1] = quotient_magic((M + 1) / 2);
   PEQA_TRY(status_word(st, &p.status));
@@ -1626,14 +1652,11 @@ extern "C" int peqa_decode_unprepare(const peqa_qweight_t* w, const uint32_t* pr
   return run_layout(w, prepared, qweight_out, false, stream);
 }
 
-extern "C" int peqa_qlinear_decode_prepared(const peqa_qweight_t* w, const uint32_t* prepared,
-                                            const void* X, int M, void* Y,
-                                            const float* scale_table, int n_tasks,
-                                            const int32_t* task_ids, void* stream) {
+static int check_decode_prepared(const peqa_qweight_t* w, const uint32_t* prepared, const void* X, int M, const void* out,
+                                 const float* scale_table, int n_tasks, const int32_t* task_ids) {
   PEQA_TRY(check_prep_layer(w));
-  if (!prepared || !X || !Y || !w->zeros) return PEQA_ERR_NULL;
-  const int g = effective_group(w->in_features, w->group_size);
-  if (!prep_group_supported(w->in_features, g)) return PEQA_ERR_BAD_SHAPE;
+  if (!prepared || !X || !out || !w->zeros) return PEQA_ERR_NULL;
+  if (!prep_group_supported(w->in_features, effective_group(w->in_features, w->group_size))) return PEQA_ERR_BAD_SHAPE;
   if (M < 1 || M > 16) return PEQA_ERR_BAD_SHAPE;
   if (task_ids) {
     if (!scale_table) return PEQA_ERR_NULL;
@@ -1641,7 +1664,26 @@ extern "C" int peqa_qlinear_decode_prepared(const peqa_qweight_t* w, const uint3
   } else if (!w->scales) {
     return PEQA_ERR_NULL;
   }
-  if (!aligned16(prepared) || !aligned16(X) || !aligned16(Y)) return PEQA_ERR_ALIGNMENT;
+  if (!aligned16(prepared) || !aligned16(X) || !aligned16(out)) return PEQA_ERR_ALIGNMENT;
+  return PEQA_OK;
+}
+
+extern "C" int peqa_qlinear_decode_prepared(const peqa_qweight_t* w, const uint32_t* prepared,
+                                            const void* X, int M, void* Y,
+                                            const float* scale_table, int n_tasks,
+                                            const int32_t* task_ids, void* stream) {
+  PEQA_TRY(check_decode_prepared(w, prepared, X, M, Y, scale_table, n_tasks, task_ids));
   PEQA_TRY(check_arch());
+  const int g = effective_group(w->in_features, w->group_size);
   return run_decode(w, prepared, false, g, X, M, Y, scale_table, n_tasks, task_ids, as_stream(stream));
+}
+
+extern "C" int peqa_qglu_decode_prepared(const peqa_qweight_t* w, int activation, const uint32_t* prepared, const void* X, int M, void* H,
+                                         const float* scale_table, int n_tasks, const int32_t* task_ids, void* stream) {
+  PEQA_TRY(check_decode_prepared(w, prepared, X, M, H, scale_table, n_tasks, task_ids));
+  if (w->out_features % 16 != 0 || !glu_act_ok(activation)) return PEQA_ERR_BAD_SHAPE;
+  PEQA_TRY(check_arch());
+  const GluOut glu = {static_cast<__nv_bfloat16*>(H), activation};
+  const int g = effective_group(w->in_features, w->group_size);
+  return run_decode(w, prepared, false, g, X, M, nullptr, scale_table, n_tasks, task_ids, as_stream(stream), glu);
 }

@@ -27,6 +27,7 @@
 
 #include "common.cuh"
 #include "dequant.cuh"
+#include "glu.cuh"
 #include "sm100_ptx.cuh"
 #include "tensor_map.cuh"
 
@@ -74,6 +75,8 @@ struct PairParams {
   Side side;            // see common.cuh
   const __nv_bfloat16* dY;   // DS: [T, N]
   float* ds_part;            // DS: [2 * ceil(T / 256)][N]
+  GluOut glu;                // GLU; `out` may be nullptr then
+  bool glu_wide;             // GLU: rows of H begin at multiples of 32 bytes
   int* status;
 };
 
@@ -88,7 +91,10 @@ __device__ __forceinline__ int pair_group_of(const PairParams& p, int col) {
 // (2 T N K flop).  A warp multiplies its 32 tokens x 32 channels by dY and folds them over its
 // lanes; the four warps of a token block are added through their staging tiles in warp order and
 // stored to ds_part; ds_channel_kernel adds the blocks.
-template <int BITS, bool FOLD, bool ZF, bool DS>
+//
+// GLU (glu.cuh): a thread holds both sums of its token's channels and writes their H itself, 32 bytes of a
+// row at a time, which are whole sectors; Y goes by way of the staging tile as ever, if it is wanted.
+template <int BITS, bool FOLD, bool ZF, bool DS, bool GLU>
 __global__ void __launch_bounds__(kPairThreads, 1)
 qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_q,
                  const __grid_constant__ CUtensorMap tmap_y, const PairParams p) {
@@ -121,7 +127,7 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
     fence_mbar_init();
     prefetch_tmap(&tmap_x);
     prefetch_tmap(&tmap_q);
-    prefetch_tmap(&tmap_y);
+    if (!GLU || p.out) prefetch_tmap(&tmap_y);
   }
   if (warp == 2) {
     tmem_alloc_pair(smem_u32(&bars->tmem_base), P_TMEM_COLS);
@@ -307,6 +313,31 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
             const float u = __uint_as_float(v[j]);
             return FOLD ? u : u * __shfl_sync(0xffffffffu, scale, h * W + j);
           };
+          if constexpr (GLU) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(scaled(j));
+            uint32_t o[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const int j = (q >> 2) * 16 + (q & 3) * 2;      // gate of channels 2q and 2q + 1, their up sums eight further
+              const __nv_bfloat162 b =
+                  __floats2bfloat162_rn(glu_value(__uint_as_float(v[j]), __uint_as_float(v[j + 8]), p.glu.act),
+                                        glu_value(__uint_as_float(v[j + 1]), __uint_as_float(v[j + 9]), p.glu.act));
+              o[q] = *reinterpret_cast<const uint32_t*>(&b);
+            }
+            if (row0 + lane < p.T) {
+              __nv_bfloat16* at = p.glu.H + (size_t)(row0 + lane) * (p.N >> 1) + (c0 >> 1);
+              if (p.glu_wide) {
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(o[0]), "r"(o[1]), "r"(o[2]),
+                             "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
+              } else {
+                *reinterpret_cast<uint4*>(at) = make_uint4(o[0], o[1], o[2], o[3]);
+                if (c0 + 16 < p.N) *reinterpret_cast<uint4*>(at + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+              }
+            }
+            if (!p.out) continue;
+          }
+          auto output = [&](int j) { return GLU ? __uint_as_float(v[j]) : scaled(j); };
           // the previous store must have finished reading the staging tile
           if (h == 0) {
             if (lane == 0) bulk_wait_group_read0();
@@ -316,10 +347,10 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
           for (int q = 0; q < W / 8; ++q) {
             uint4 o;
             __nv_bfloat162 b;
-            b = __floats2bfloat162_rn(scaled(8 * q + 0), scaled(8 * q + 1)); o.x = *reinterpret_cast<uint32_t*>(&b);
-            b = __floats2bfloat162_rn(scaled(8 * q + 2), scaled(8 * q + 3)); o.y = *reinterpret_cast<uint32_t*>(&b);
-            b = __floats2bfloat162_rn(scaled(8 * q + 4), scaled(8 * q + 5)); o.z = *reinterpret_cast<uint32_t*>(&b);
-            b = __floats2bfloat162_rn(scaled(8 * q + 6), scaled(8 * q + 7)); o.w = *reinterpret_cast<uint32_t*>(&b);
+            b = __floats2bfloat162_rn(output(8 * q + 0), output(8 * q + 1)); o.x = *reinterpret_cast<uint32_t*>(&b);
+            b = __floats2bfloat162_rn(output(8 * q + 2), output(8 * q + 3)); o.y = *reinterpret_cast<uint32_t*>(&b);
+            b = __floats2bfloat162_rn(output(8 * q + 4), output(8 * q + 5)); o.z = *reinterpret_cast<uint32_t*>(&b);
+            b = __floats2bfloat162_rn(output(8 * q + 6), output(8 * q + 7)); o.w = *reinterpret_cast<uint32_t*>(&b);
             *reinterpret_cast<uint4*>(srow + (((h * (W / 8) + q) ^ sw) << 4)) = o;
           }
           if constexpr (DS) {
@@ -347,6 +378,7 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
             half_sum[h] = __uint_as_float(v[0]) + __shfl_xor_sync(0xffffffffu, __uint_as_float(v[0]), 16);
           }
         }
+        if (GLU && !p.out) continue;
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0 && row0 < p.T) {
@@ -520,10 +552,10 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
   }
 }
 
-template <int BITS, bool FOLD, bool ZF, bool DS>
+template <int BITS, bool FOLD, bool ZF, bool DS, bool GLU = false>
 int launch_pair_t(const CUtensorMap& tx, const CUtensorMap& tq, const CUtensorMap& ty, const PairParams& p,
                   int pairs, cudaStream_t st) {
-  auto kern = qfwd_pair_kernel<BITS, FOLD, ZF, DS>;
+  auto kern = qfwd_pair_kernel<BITS, FOLD, ZF, DS, GLU>;
   static std::atomic<uint64_t> done{0};
   PEQA_TRY(allow_smem(kern, P_SMEM_BYTES, done));
   cudaLaunchConfig_t cfg = {};
@@ -555,8 +587,10 @@ bool fwd_pair_supported(const peqa_qweight_t* w) {
 }
 
 int launch_fwd_pair(const peqa_qweight_t* w, const float* zeros_f, int g, const void* X, int T,
-                    void* Y, const void* dY, float* ds_part, cudaStream_t st, Side side) {
+                    void* Y, const void* dY, float* ds_part, cudaStream_t st, Side side, const GluOut* glu) {
   PairParams p;
+  p.glu = glu ? *glu : GluOut{};
+  p.glu_wide = w->out_features % 32 == 0 && reinterpret_cast<uintptr_t>(p.glu.H) % 32 == 0;
   p.side = side;
   p.zeros = w->zeros;
   p.zeros_f = zeros_f;
@@ -578,8 +612,8 @@ int launch_fwd_pair(const peqa_qweight_t* w, const float* zeros_f, int g, const 
   PEQA_TRY(status_word(st, &p.status));
   EncodeTiledFn enc = nullptr;
   PEQA_TRY(tensor_map_encoder(&enc));
-  CUtensorMap tx, tq, ty;
-  {
+  CUtensorMap tx, tq, ty = {};
+  if (Y) {
     // output Y [T, N]: boxes of 32 channels x 32 tokens, 64-byte swizzle (the epilogue's staging tile)
     cuuint64_t dims[2] = {(cuuint64_t)p.N, (cuuint64_t)T};
     cuuint64_t strides[1] = {(cuuint64_t)p.N * 2};
@@ -619,6 +653,12 @@ int launch_fwd_pair(const peqa_qweight_t* w, const float* zeros_f, int g, const 
   const int pairs = tiles < max_pairs ? tiles : max_pairs;
   p.items = make_pair_items(p.n_tiles, p.t_tiles, T, pairs);
   const bool fold = p.G > 1;
+  if (glu) {
+    if (fold) return w->bits == 4 ? launch_pair_t<4, true, false, false, true>(tx, tq, ty, p, pairs, st)
+                                  : launch_pair_t<3, true, false, false, true>(tx, tq, ty, p, pairs, st);
+    return w->bits == 4 ? launch_pair_t<4, false, false, false, true>(tx, tq, ty, p, pairs, st)
+                        : launch_pair_t<3, false, false, false, true>(tx, tq, ty, p, pairs, st);
+  }
   if (zeros_f)   // a real-valued zero-point is folded into the operand whatever the group size
     return w->bits == 4 ? launch_pair_t<4, true, true, false>(tx, tq, ty, p, pairs, st)
                         : launch_pair_t<3, true, true, false>(tx, tq, ty, p, pairs, st);

@@ -1019,6 +1019,12 @@ int launch_fwd(const peqa_qweight_t* w, const float* zeros_f, int g, const void*
   return launch_qgemm(w, zeros_f, g, X, T, Y, false, st);
 }
 
+int launch_glu_fwd(const peqa_qweight_t* w, int g, const void* X, int T, void* Y, const GluOut& glu, cudaStream_t st) {
+  if (split_is_faster(w, T, false, g == w->in_features))
+    return launch_split(w, nullptr, g, X, T, Y, false, nullptr, nullptr, st, T, 0, kInOrder, &glu);
+  return launch_fwd_pair(w, nullptr, g, X, T, Y, nullptr, nullptr, st, kInOrder, &glu);
+}
+
 int launch_dx(const peqa_qweight_t* w, const float* zeros_f, int g, const void* dY, int T, void* dX,
               cudaStream_t st, int T_call, int t0, Side side) {
   if (dx_pair_supported(w) && split_is_faster(w, T_call, true, false))

@@ -1,0 +1,31 @@
+// The gated feed-forward block, H = act(X Wg^T) * (X Wu^T), as the kernels see it: gate and up projection are one quantized
+// linear of 2 F rows, in which runs of eight gate rows alternate with the eight up rows of the same channels.  So the two sums of a
+// channel are made by one tile, wherever the tile begins, and mostly in one thread; and all that is done with a linear (its
+// gradients, AdamW, the prepared copy) is done with the block.
+#pragma once
+
+#include "common.cuh"
+
+namespace peqa {
+
+constexpr int kGluRun = 8;       // rows of a run
+
+// What a forward kernel makes of the block's sums beside storing them.
+struct GluOut {
+  __nv_bfloat16* H;              // [tokens, F]; nullptr: an ordinary linear
+  int act;                       // peqa_activation
+};
+
+inline bool glu_act_ok(int act) { return act == PEQA_ACT_SILU || act == PEQA_ACT_GELU_TANH; }
+
+#ifdef __CUDACC__
+// Both activations are x p(v) with p the logistic function: v = x, or 2 sqrt(2/pi) (x + 0.044715 x^3), since (1 + tanh(u)) / 2 =
+// p(2u).  Exponential and reciprocal are the approximate ones (2^-21 of p for |v| up to 88), far below bf16's step.
+constexpr float kGeluInner = 1.5957691216057308f, kGeluCubic = 0.044715f;
+__device__ __forceinline__ float glu_value(float x, float up, int act) {
+  const float v = act == PEQA_ACT_SILU ? x : kGeluInner * fmaf(kGeluCubic * x * x, x, x);
+  return __fdividef(x, 1.0f + __expf(-v)) * up;
+}
+#endif
+
+}  // namespace peqa

@@ -261,6 +261,105 @@ at::Tensor matrix(PyObject* given, const at::Tensor& like, at::IntArrayRef shape
   return t;
 }
 
+int activation(PyObject* o) {
+  if (PyUnicode_Check(o)) {
+    if (PyUnicode_CompareWithASCIIString(o, "silu") == 0) return PEQA_ACT_SILU;
+    if (PyUnicode_CompareWithASCIIString(o, "gelu_tanh") == 0) return PEQA_ACT_GELU_TANH;
+  }
+  PyErr_Format(PyExc_ValueError, "activation: expected 'silu' or 'gelu_tanh', got %R", o);
+  fail();
+}
+
+// X [tokens, K] of a gated block on the current device, and its tokens.
+int64_t glu_tokens(const at::Tensor& X, const peqa_qweight_t& w) {
+  if (X.dim() != 2 || X.size(1) != w.in_features || X.get_device() != c10::cuda::current_device()) {
+    PyErr_SetString(PyExc_ValueError, "X: expected [tokens, in_features] on the current CUDA device");
+    fail();
+  }
+  if (X.size(0) > INT32_MAX) check(PEQA_ERR_TOO_LARGE, "peqa_qglu");
+  return X.size(0);
+}
+
+// (w, X, activation, keep, Y, H) -> (H, Y)
+PyObject* qglu_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  arity(n, 6);
+  const peqa_qweight_t w = weight(a[0]);
+  const at::Tensor& X = dev(a[1], at::kBFloat16, "X");
+  const int64_t T = glu_tokens(X, w);
+  const int act = activation(a[2]), keep = PyObject_IsTrue(a[3]);
+  if (keep < 0) fail();
+  at::Tensor H = matrix(a[5], X, {T, w.out_features / 2}, at::kBFloat16, "H"), Y;
+  if (keep || a[4] != Py_None) Y = matrix(a[4], X, {T, w.out_features}, at::kBFloat16, "Y");
+  void *x = X.data_ptr(), *h = H.data_ptr(), *y = Y.defined() ? Y.data_ptr() : nullptr, *st = stream();
+  check(unlocked([&] { return peqa_qglu_fwd(&w, act, x, (int)T, y, h, st); }), "peqa_qglu_fwd");
+  Ref first(THPVariable_Wrap(std::move(H)));
+  if (!y) return PyTuple_Pack(2, first.p, Py_None);
+  Ref second(THPVariable_Wrap(std::move(Y)));
+  return PyTuple_Pack(2, first.p, second.p);
+  END_HANDLE_TH_ERRORS
+}
+
+// (Y, dH, activation, dY) -> dY
+PyObject* glu_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  arity(n, 4);
+  const at::Tensor &Y = dev(a[0], at::kBFloat16, "Y"), &dH = dev(a[1], at::kBFloat16, "dH");
+  if (Y.dim() != 2 || dH.dim() != 2 || dH.size(0) != Y.size(0) || 2 * dH.size(1) != Y.size(1) || dH.device() != Y.device() ||
+      Y.get_device() != c10::cuda::current_device()) {
+    PyErr_SetString(PyExc_ValueError, "Y [tokens, 2F] and dH [tokens, F]: expected on the current CUDA device");
+    fail();
+  }
+  const int act = activation(a[2]);
+  const bool fits = Y.size(0) <= INT32_MAX && Y.size(1) <= INT32_MAX;
+  at::Tensor dY = matrix(a[3], Y, Y.sizes(), at::kBFloat16, "dY");
+  void *y = Y.data_ptr(), *dh = dH.data_ptr(), *dy = dY.data_ptr(), *st = stream();
+  const int T = (int)Y.size(0), F = (int)dH.size(1);
+  check(fits ? unlocked([&] { return peqa_glu_bwd(act, y, dh, T, F, dy, st); }) : (int)PEQA_ERR_TOO_LARGE, "peqa_glu_bwd");
+  return THPVariable_Wrap(std::move(dY));
+  END_HANDLE_TH_ERRORS
+}
+
+// (w, prepared, X, activation, H, scale_table, task_ids) -> H
+PyObject* qglu_decode_prepared(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  arity(n, 7);
+  const peqa_qweight_t w = weight(a[0]);
+  const at::Tensor &prepared = dev(a[1], at::kInt, "prepared"), &X = dev(a[2], at::kBFloat16, "X");
+  const int64_t M = glu_tokens(X, w);
+  const int act = activation(a[3]);
+  if ((size_t)prepared.numel() * 4 < peqa_decode_prepared_bytes(&w) || prepared.device() != X.device()) {
+    PyErr_SetString(PyExc_ValueError, "prepared: not the prepared copy of this block, or on another device than X");
+    fail();
+  }
+  const float* table = nullptr;
+  const int32_t* ids = nullptr;
+  int n_tasks = 0;
+  if ((a[5] == Py_None) != (a[6] == Py_None)) {
+    PyErr_SetString(PyExc_ValueError, "scale_table and task_ids come together");
+    fail();
+  }
+  if (a[6] != Py_None) {
+    const at::Tensor &t = dev(a[5], at::kFloat, "scale_table"), &i = dev(a[6], at::kInt, "task_ids");
+    const int64_t G = w.group_size > 0 && w.in_features % w.group_size == 0 ? w.in_features / w.group_size : 1;
+    if (t.dim() < 2 || t.size(0) < 1 || t.size(0) > INT32_MAX || t.numel() / t.size(0) != w.out_features * G || i.dim() != 1 ||
+        i.size(0) != M || t.device() != X.device() || i.device() != X.device()) {
+      PyErr_SetString(PyExc_ValueError, "scale_table [tasks, out_features, groups] and task_ids [tokens] do not belong to this block and X");
+      fail();
+    }
+    table = t.data_ptr<float>();
+    ids = i.data_ptr<int32_t>();
+    n_tasks = (int)t.size(0);
+  }
+  at::Tensor H = matrix(a[4], X, {M, w.out_features / 2}, at::kBFloat16, "H");
+  void *x = X.data_ptr(), *h = H.data_ptr(), *st = stream();
+  const uint32_t* from = static_cast<const uint32_t*>(prepared.data_ptr());
+  check(unlocked([&] { return peqa_qglu_decode_prepared(&w, act, from, x, (int)M, h, table, n_tasks, ids, st); }),
+        "peqa_qglu_decode_prepared");
+  return THPVariable_Wrap(std::move(H));
+  END_HANDLE_TH_ERRORS
+}
+
 // (X, W, labels, weight, need_grad, loss, dX, workspace) -> (loss, dX)
 PyObject* head_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -675,7 +774,7 @@ PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {FAST(qlinear_fwd),       FAST(qlinear_fwd_zf), FAST(qlinear_decode), FAST(qlinear_decode_prepared),
-                          FAST(head_loss),
+                          FAST(head_loss),         FAST(qglu_fwd),      FAST(glu_bwd),        FAST(qglu_decode_prepared),
                           FAST(scale_adamw),       FAST(zero_adamw),     FAST(layer_train_step),
                           FAST(kv_append),         FAST(attn_decode),
                           {"bind_error", bind_error, METH_O, nullptr},   {nullptr, nullptr, 0, nullptr}};

@@ -31,6 +31,7 @@
 
 #include "common.cuh"
 #include "dequant.cuh"
+#include "glu.cuh"
 #include "sm100_ptx.cuh"
 #include "tensor_map.cuh"
 
@@ -83,6 +84,7 @@ struct SplitParams {
   int q, cshift;          // tiles per cluster, log2 of the CTAs per cluster (q <= 1 << cshift)
   const __nv_bfloat16* dY;   // DS: [T, N]
   float* ds_part;            // DS: [token tiles * passes][N]
+  GluOut glu;                // GLU; `out` may be nullptr then
   Side side;                 // see common.cuh
   int* status;
 };
@@ -125,7 +127,8 @@ __device__ __forceinline__ UnitZS split_load_zs(const SplitParams& p, int i, int
 // DS (forward with one scale per channel): where the fp32 sums of a tile are complete they are also
 // multiplied by dY and summed over the tile's tokens, dS[i] = sum_t dY[t,i] * u[t,i] (see the
 // pair kernel).
-template <int BITS, bool TRANS, bool FOLD, bool ZF, bool DS>
+// GLU (forward): the outputs of a gated block beside or instead of Y, see glu.cuh.
+template <int BITS, bool TRANS, bool FOLD, bool ZF, bool DS, bool GLU>
 __global__ void __launch_bounds__(kSplitThreads, 1)
 qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constant__ CUtensorMap tmap_pk,
               const SplitParams p) {
@@ -501,6 +504,26 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
             const float4 sc = ld_global(reinterpret_cast<const float4*>(p.scales + row));   // one scale per channel
             a.x *= sc.x; a.y *= sc.y; a.z *= sc.z; a.w *= sc.w;
           }
+          if constexpr (GLU) {
+            // A CTA finishes a multiple of 16 rows, four lanes' vectors: gate, gate, up, up of eight channels of a token.  The four have
+            // come here together.
+            const uint32_t four = 0xFu << (lane & 28);
+            float4 up;
+            up.x = __shfl_xor_sync(four, a.x, 2);
+            up.y = __shfl_xor_sync(four, a.y, 2);
+            up.z = __shfl_xor_sync(four, a.z, 2);
+            up.w = __shfl_xor_sync(four, a.w, 2);
+            if (!(lane & 2)) {
+              const __nv_bfloat162 b0 = __floats2bfloat162_rn(glu_value(a.x, up.x, p.glu.act), glu_value(a.y, up.y, p.glu.act));
+              const __nv_bfloat162 b1 = __floats2bfloat162_rn(glu_value(a.z, up.z, p.glu.act), glu_value(a.w, up.w, p.glu.act));
+              uint2 o;
+              o.x = *reinterpret_cast<const uint32_t*>(&b0);
+              o.y = *reinterpret_cast<const uint32_t*>(&b1);
+              const int channel = (row >> 4) * kGluRun + (row & 7);
+              *reinterpret_cast<uint2*>(p.glu.H + (size_t)(t0 + t) * (p.R >> 1) + channel) = o;
+            }
+            if (!p.out) continue;
+          }
           __nv_bfloat162 h0 = __floats2bfloat162_rn(a.x, a.y), h1 = __floats2bfloat162_rn(a.z, a.w);
           uint2 o;
           o.x = *reinterpret_cast<uint32_t*>(&h0);
@@ -555,10 +578,10 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
   if (beside && blockIdx.x == 0 && threadIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-template <int BITS, bool TRANS, bool FOLD, bool ZF, bool DS = false>
+template <int BITS, bool TRANS, bool FOLD, bool ZF, bool DS = false, bool GLU = false>
 int launch_split_t(const CUtensorMap& ta, const CUtensorMap& tp, const SplitParams& p, size_t smem,
                    cudaStream_t st) {
-  auto kern = qsplit_kernel<BITS, TRANS, FOLD, ZF, DS>;
+  auto kern = qsplit_kernel<BITS, TRANS, FOLD, ZF, DS, GLU>;
   static std::atomic<uint64_t> done{0};
   PEQA_TRY(allow_smem(kern, SM_SMEM_LIMIT, done));
   cudaLaunchConfig_t cfg = {};
@@ -701,8 +724,9 @@ int split_part_tokens(const peqa_qweight_t* w, int T_call, bool trans) {
 // The T tokens from t0 on of a call of T_call tokens (act, out: of the part).  Plan and cut are those of the
 // whole call, so a token's sums are added in the same order in whichever part it comes.
 int launch_split(const peqa_qweight_t* w, const float* zeros_f, int g, const void* act, int T, void* out,
-                 bool trans, const void* dY, float* ds_part, cudaStream_t st, int T_call, int t0, Side side) {
+                 bool trans, const void* dY, float* ds_part, cudaStream_t st, int T_call, int t0, Side side, const GluOut* glu) {
   SplitParams p;
+  p.glu = glu ? *glu : GluOut{};
   p.side = side;
   p.zeros = w->zeros;
   p.zeros_f = zeros_f;
@@ -773,6 +797,12 @@ int launch_split(const peqa_qweight_t* w, const float* zeros_f, int g, const voi
       return cuda_fail(cudaErrorInvalidValue);
   }
   const bool b4 = w->bits == 4;
+  if (glu) {
+    if (p.G > 1) return b4 ? launch_split_t<4, false, true, false, false, true>(ta, tp, p, smem, st)
+                           : launch_split_t<3, false, true, false, false, true>(ta, tp, p, smem, st);
+    return b4 ? launch_split_t<4, false, false, false, false, true>(ta, tp, p, smem, st)
+              : launch_split_t<3, false, false, false, false, true>(ta, tp, p, smem, st);
+  }
   if (trans) {
     if (zeros_f) return b4 ? launch_split_t<4, true, true, true>(ta, tp, p, smem, st)
                            : launch_split_t<3, true, true, true>(ta, tp, p, smem, st);

@@ -1,0 +1,204 @@
+"""The gated feed-forward block against its definition in 64 bits: forward, backward, single tokens, and a step of them together."""
+import pytest
+import torch
+
+from glu_util import backward, block, forward
+from loss_util import assert_within
+from paper_2305_14152_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+#: tokens, channels, columns: tiles cut everywhere, few and many tokens (both kernels), rows of H that begin at 16 bytes and at 32
+SHAPES = [(1, 8, 128), (5, 24, 256), (16, 136, 384), (17, 40, 128), (77, 1000, 512), (200, 264, 1024), (513, 1048, 128), (300, 2048, 640),
+          (1030, 520, 256), (2100, 1376, 512)]
+
+
+def rows(T, K, seed):
+    return torch.randn((T, K), generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").bfloat16()
+
+
+@pytest.mark.parametrize("bits", [3, 4])
+@pytest.mark.parametrize("group", [0, 32, 128])
+@pytest.mark.parametrize("T,F,K", SHAPES)
+def test_forward(T, F, K, group, bits):
+    w, W, _ = block(F, K, bits, group, seed=F + K)
+    X = rows(T, K, T)
+    act = "silu" if (T + bits) % 2 else "gelu_tanh"
+    H, Y = binding.qglu_fwd(w, X, act)
+    alone, none = binding.qglu_fwd(w, X, act, keep=False)
+    assert none is None and torch.equal(H, alone)
+    assert torch.equal(Y, binding.qlinear_fwd(w, X))
+    binding.check_status()
+    want, want_Y, tol, tol_Y = forward(X, W, act, w.G > 1)
+    assert_within(Y, want_Y, tol_Y, "Y")
+    assert_within(H, want, tol, "H")
+
+
+@pytest.mark.parametrize("T,F,K", [(9, 40, 64), (100, 88, 192), (700, 72, 320)])
+def test_forward_of_odd_multiples_of_64_columns(T, F, K):
+    w, W, _ = block(F, K, 4, 64, seed=3)
+    X = rows(T, K, 4)
+    H, Y = binding.qglu_fwd(w, X)
+    want, want_Y, tol, tol_Y = forward(X, W, "silu", w.G > 1)
+    assert_within(Y, want_Y, tol_Y, "Y")
+    assert_within(H, want, tol, "H")
+
+
+@pytest.mark.parametrize("T,F", [(40, 520), (1500, 520), (40, 264), (1500, 264)])
+def test_forward_writes_what_it_is_given_and_no_more(T, F):
+    """Outputs inside larger buffers, H at an odd multiple of 16 bytes."""
+    w, _, _ = block(F, 256, 4, 0, seed=5)
+    X = rows(T, 256, 6)
+    want, want_Y = binding.qglu_fwd(w, X)
+    for lead in (8, 16):
+        buf = torch.full((lead + T * F + 64,), 7.0, dtype=torch.bfloat16, device="cuda")
+        buf_Y = torch.full((lead + 2 * T * F + 64,), 7.0, dtype=torch.bfloat16, device="cuda")
+        H, Y = buf[lead:lead + T * F].view(T, F), buf_Y[lead:lead + 2 * T * F].view(T, 2 * F)
+        binding.qglu_fwd(w, X, Y=Y, H=H)
+        assert torch.equal(H, want) and torch.equal(Y, want_Y)
+        for b, n in ((buf, T * F), (buf_Y, 2 * T * F)):
+            assert (b[:lead] == 7).all() and (b[lead + n:] == 7).all()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
+@pytest.mark.parametrize("T,F", [(1, 8), (3, 1000), (1001, 264), (64, 4096)])
+def test_backward_of_the_activation(T, F, act):
+    gen = torch.Generator(device="cuda").manual_seed(T + F)
+    Y = (2 * torch.randn((T, 2 * F), generator=gen, device="cuda")).bfloat16()
+    dH = torch.randn((T, F), generator=gen, device="cuda").bfloat16()
+    # where exponentials over- and underflow, and where nothing happens
+    odd = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 80.0, -80.0, 1e4, -1e4, 3e19, -3e19, 1e-3, -1.28, -5.5, 5.5, -0.75, 0.75], device="cuda")
+    for i, v in enumerate(odd.tolist()):
+        Y[i % T, (16 * i + i % 8) % (2 * F)] = v
+    dY = binding.glu_bwd(Y, dH, act)
+    want, tol = backward(Y, dH, act)
+    assert not dY.isnan().any()
+    fine = want.isfinite()                                    # autograd's own inf * 0 far out
+    assert_within(torch.where(fine, dY, 0), torch.where(fine, want, 0), torch.where(fine, tol, 0), "dY")
+    over = Y.clone()
+    assert binding.glu_bwd(over, dH, act, dY=over).data_ptr() == over.data_ptr()
+    assert torch.equal(over, dY)
+
+
+@pytest.mark.parametrize("bits", [3, 4])
+@pytest.mark.parametrize("group", [0, 64, 128, 256, 512])
+@pytest.mark.parametrize("F,K", [(8, 512), (24, 1024), (1000, 512), (5504, 2048)])
+def test_decode(F, K, group, bits):
+    w, W, _ = block(F, K, bits, group, seed=F + group)
+    prepared = binding.decode_prepare(w)
+    torch.cuda.synchronize()
+    for M in (1, 2, 3, 7, 8, 9, 13, 16):
+        X = rows(M, K, M)
+        act = "gelu_tanh" if M % 2 else "silu"
+        H = binding.qglu_decode_prepared(w, prepared, X, act)
+        want, _, tol, _ = forward(X, W, act, False)
+        assert_within(H, want, tol, f"H of {M}")
+    binding.check_status()
+
+
+@pytest.mark.parametrize("bits,group", [(3, 0), (3, 128), (4, 64), (4, 256)])
+@pytest.mark.parametrize("F,K", [(40, 512), (3000, 1024)])
+def test_decode_of_several_tasks(F, K, bits, group):
+    w, _, codes = block(F, K, bits, group, seed=8)
+    from glu_util import weights
+    table = torch.stack([w.scales, 2 * w.scales, w.scales.flip(0)]).contiguous()
+    prepared = binding.decode_prepare(w)
+    torch.cuda.synchronize()
+    for M in (1, 2, 5, 8, 11, 16):
+        X = rows(M, K, M)
+        ids = torch.arange(M, device="cuda", dtype=torch.int32) * 2 % 3
+        H = binding.qglu_decode_prepared(w, prepared, X, scale_table=table, task_ids=ids)
+        for t in range(3):
+            mine = ids == t
+            want, _, tol, _ = forward(X[mine], weights(codes, w.zeros, table[t]), "silu", False)
+            assert_within(H[mine], want, tol, f"H of task {t}")
+
+
+def test_rows_of_two_projections():
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    Wg, Wu = (torch.randn((48, 256), generator=gen, device="cuda") for _ in range(2))
+    gate, up = binding.quantize_rtn(Wg, 4, 64), binding.quantize_rtn(Wu, 4, 64)
+    both = binding.glu_interleave(gate, up)
+    whole = binding.quantize_rtn(binding.glu_rows(Wg, Wu), 4, 64)
+    for a, b in ((both.qweight, whole.qweight), (both.zeros, whole.zeros), (both.scales, whole.scales)):
+        assert torch.equal(a, b)
+    assert all(torch.equal(a, b) for a, b in zip(binding.glu_split(both.scales), (gate.scales, up.scales)))
+    X = rows(33, 256, 2)
+    H, Y = binding.qglu_fwd(both, X)
+    Yg, Yu = binding.glu_split(Y.T.contiguous())
+    # the same sums in another order: a step of bf16 of Y, at most
+    for got, one in ((Yg.T, gate), (Yu.T, up)):
+        assert (got.double() - binding.qlinear_fwd(one, X).double()).abs().max() <= 2.0 ** -7 * Y.abs().max()
+
+
+def _rel(got, want):
+    return float((got.double() - want).norm() / want.norm())
+
+
+@pytest.mark.parametrize("bits,group", [(4, 0), (3, 128)])
+def test_a_training_step_to_the_loss(bits, group):
+    """Block, down projection, residual, loss and back, the scales stepped; against autograd in 64 bits.  A dozen bf16 roundings, each
+    off by 2^-9 in the mean, add up to less than 12 * 2^-9 of the whole; folded scales take two more a product."""
+    T, K, F, V = 300, 256, 512, 3000
+    w, W, codes = block(F, K, bits, group, seed=20)
+    down_codes = torch.randint(2 ** bits, (K, F), device="cuda", generator=torch.Generator(device="cuda").manual_seed(21)).to(torch.uint8)
+    G = 1 if group == 0 else F // group
+    down = binding.QWeight(bits, K, F, group, binding.pack(down_codes, bits), torch.full((K, G), 2 ** (bits - 1), dtype=torch.uint8, device="cuda"),
+                           torch.full((K, G), F ** -0.5 * 3.5 / 2 ** bits, device="cuda"))
+    X = rows(T, K, 22)
+    head = (rows(V, K, 23).float() * K ** -0.5).bfloat16()
+    labels = torch.randint(V, (T,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(24)).int()
+    labels[::3] = -1
+    weight = torch.full((T,), 1.0 / int((labels >= 0).sum()), device="cuda")
+
+    H, Y = binding.qglu_fwd(w, X)
+    Z = binding.qlinear_fwd(down, H) + X
+    loss, dZ = binding.head_loss(Z, head, labels, weight)
+    dH, dS_down = binding.qlinear_bwd(down, H, dZ)
+    dY = binding.glu_bwd(Y, dH, dY=Y)
+    dX, dS = binding.qlinear_bwd(w, X, dY)
+    dX = dX + dZ
+    binding.check_status()
+
+    from glu_util import act, halves, weights
+    s, s_down = w.scales.double().requires_grad_(), down.scales.double().requires_grad_()
+    x = X.double().requires_grad_()
+
+    def linear(x, codes, zeros, s):
+        n, g = zeros.shape
+        q = codes.double().view(n, g, -1) - zeros.double()[:, :, None]
+        return x @ (q * s[:, :, None]).view(n, -1).T
+
+    gate, up = halves(linear(x, codes, w.zeros, s))
+    z = linear(act(gate, "silu") * up, down_codes, down.zeros, s_down) + x
+    live = labels >= 0
+    each = torch.nn.functional.cross_entropy((z @ head.double().T)[live], labels[live].long(), reduction="none")
+    (each * weight[live].double()).sum().backward()
+    assert _rel(loss[live], each.detach()) < 12 * 2.0 ** -9
+    for got, want in ((dX, x.grad), (dS, s.grad), (dS_down, s_down.grad)):
+        assert _rel(got, want) < 16 * 2.0 ** -9
+    m, v = torch.zeros_like(w.scales), torch.zeros_like(w.scales)
+    before = w.scales.clone()
+    binding.qlinear_bwd_ds_adamw(w, X, dY, m, v, lr=1e-5)
+    assert not torch.equal(before, w.scales) and w.scales.isfinite().all()
+
+
+def test_captured_decode_beside_another_stream():
+    w, _, _ = block(1024, 1024, 3, 64, seed=30)
+    prepared = binding.decode_prepare(w)
+    torch.cuda.synchronize()
+    X, other = rows(4, 1024, 31), rows(300, 1024, 32)
+    want, want_other = binding.qglu_decode_prepared(w, prepared, X).clone(), binding.qglu_fwd(w, other)[0].clone()
+    H = torch.empty_like(want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.qglu_decode_prepared(w, prepared, X, H=H)
+    side = torch.cuda.Stream()
+    for _ in range(5):
+        H.zero_()
+        graph.replay()
+        with torch.cuda.stream(side):
+            got = binding.qglu_fwd(w, other)[0]
+        torch.cuda.synchronize()
+        assert torch.equal(H, want) and torch.equal(got, want_other)
