@@ -131,7 +131,7 @@ struct PrepParams {
   const uint8_t* zeros;     // [N, G]
   const float* scales;      // [N, G] or table [n_tasks, N, G]
   const __nv_bfloat16* X;   // [M, K]
-  __nv_bfloat16* Y;         // [M, N]
+  __nv_bfloat16* Y;         // [M, N], GLU: H [M, N / 2]
   const int32_t* task_ids;  // nullptr: one task
   int n_tasks;
   int N, K, G, M;
@@ -144,10 +144,13 @@ struct PrepParams {
   int sps;                  // steps per slot (1 or 2)
   int x_pitch;              // bytes between staged token rows
   int pairs_per_cta;
-  int row_bytes;            // of the canonical matrix
+  // (Parameters of another size move registers in two of three instances, some to 30 bytes more of spills: the two are never both wanted.)
+  union {
+    int row_bytes;          // of the canonical matrix
+    int act;                // GLU: peqa_activation
+  };
   int cshift;               // log2 of the CTAs that share a range of rows, each with a slice of K
   uint32_t m_magic[2];      // quotient_magic of M and of (M + 1) / 2
-  GluOut glu;               // H != nullptr: a gated block, H [M, N / 2] instead of Y
   int* status;
 };
 
@@ -370,7 +373,9 @@ struct CanonRow {
 // numbers of up to 31 bits times a power of two, cut into four signed digits, and the MMA's eight columns
 // are two tokens x four digits, which fp16 operands would leave idle.  An MMA covers twice the columns,
 // the codes are cheaper to take out (i8_string), and the sums of a group are exact.
-template <int BITS, int NT, int GSH, bool TASKS, bool CANON, bool I8, int V>
+//
+// GLU: the outputs of a gated block (glu.cuh) in place of Y.
+template <int BITS, int NT, int GSH, bool TASKS, bool CANON, bool I8, int V, bool GLU>
 __global__ void __launch_bounds__(kPThreads, 1)
 decode_prep_kernel(const PrepParams p) {
   constexpr int C = BITS;                            // 16-byte chunks per lane, step and group
@@ -1185,15 +1190,15 @@ decode_prep_kernel(const PrepParams p) {
         mine[at1] = sum[1];
         continue;
       }
-      if (p.glu.H) {
+      if constexpr (GLU) {
         // the pair's sixteen rows are eight gate rows and their up rows, in the halves of half a warp (which is in step: its
         // lanes differ in lr alone); a CTA's ranges are whole pairs then
         const uint32_t half = 0xFFFFu << (threadIdx.x & 16);
         const float up0 = __shfl_xor_sync(half, sum[0], 8), up1 = __shfl_xor_sync(half, sum[1], 8);
         if (lr < 8) {
-          __nv_bfloat16* at = p.glu.H + (size_t)m * (p.N >> 1) + (pair_rg(lp) >> 1) * kGluRun + lr;
-          at[0] = __float2bfloat16_rn(glu_value(sum[0], up0, p.glu.act));
-          if (m + 1 < p.M) at[p.N >> 1] = __float2bfloat16_rn(glu_value(sum[1], up1, p.glu.act));
+          __nv_bfloat16* at = p.Y + (size_t)m * (p.N >> 1) + (pair_rg(lp) >> 1) * kGluRun + lr;
+          at[0] = __float2bfloat16_rn(glu_value(sum[0], up0, p.act));
+          if (m + 1 < p.M) at[p.N >> 1] = __float2bfloat16_rn(glu_value(sum[1], up1, p.act));
         }
         continue;
       }
@@ -1224,10 +1229,10 @@ decode_prep_kernel(const PrepParams p) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) sum += v[r];
       }
-      if (p.glu.H) {
+      if constexpr (GLU) {
         const float up = __shfl_xor_sync(0xFFFFu << (threadIdx.x & 16), sum, 8);
         if (lr < 8)
-          p.glu.H[(size_t)m * (p.N >> 1) + (pair_rg(lp) >> 1) * kGluRun + lr] = __float2bfloat16_rn(glu_value(sum, up, p.glu.act));
+          p.Y[(size_t)m * (p.N >> 1) + (pair_rg(lp) >> 1) * kGluRun + lr] = __float2bfloat16_rn(glu_value(sum, up, p.act));
         continue;
       }
       p.Y[(size_t)m * p.N + pair_rg(lp) * 8 + lr] = __float2bfloat16_rn(sum);
@@ -1457,9 +1462,9 @@ int plan_prep(int N, int K, int M, int bits, int gcols, bool canon, bool i8, boo
   return plan->ns < 0 ? PEQA_ERR_TOO_LARGE : PEQA_OK;
 }
 
-template <int BITS, int NT, int GSH, bool TASKS, bool CANON, bool I8, int V>
-int launch_prep_t(const PrepParams& p, int grid, size_t smem, cudaStream_t st) {
-  auto kern = decode_prep_kernel<BITS, NT, GSH, TASKS, CANON, I8, V>;
+template <int BITS, int NT, int GSH, bool TASKS, bool CANON, bool I8, int V, bool GLU>
+int launch_prep_k(const PrepParams& p, int grid, size_t smem, cudaStream_t st) {
+  auto kern = decode_prep_kernel<BITS, NT, GSH, TASKS, CANON, I8, V, GLU>;
   static std::atomic<uint64_t> done{0};
   PEQA_TRY(allow_smem(kern, kPSmemLimit, done));
   cudaLaunchConfig_t cfg = {};
@@ -1480,8 +1485,15 @@ int launch_prep_t(const PrepParams& p, int grid, size_t smem, cudaStream_t st) {
   return PEQA_OK;
 }
 
+template <int BITS, int NT, int GSH, bool TASKS, bool CANON, bool I8, int V>
+int launch_prep_t(const PrepParams& p, bool glu, int grid, size_t smem, cudaStream_t st) {
+  if constexpr (!CANON)
+    if (glu) return launch_prep_k<BITS, NT, GSH, TASKS, CANON, I8, V, true>(p, grid, smem, st);
+  return launch_prep_k<BITS, NT, GSH, TASKS, CANON, I8, V, false>(p, grid, smem, st);
+}
+
 template <int BITS, int NT, bool TASKS, bool CANON, bool I8>
-int launch_prep_g(const PrepParams& p, int gsh, int grid, size_t smem, cudaStream_t st) {
+int launch_prep_g(const PrepParams& p, bool glu, int gsh, int grid, size_t smem, cudaStream_t st) {
   // A step holds 8, 4 or 2 groups of a row; vectors of them where every row's groups start on one and are whole ones
   // (a row of 11008 columns has 172 groups of 64 and 86 of 128).
   auto in_vectors = [&](int v) {
@@ -1490,28 +1502,28 @@ int launch_prep_g(const PrepParams& p, int gsh, int grid, size_t smem, cudaStrea
   switch (gsh) {
     case 1:
       if constexpr (!CANON)
-        return in_vectors(4) ? launch_prep_t<BITS, NT, 1, TASKS, CANON, I8, 4>(p, grid, smem, st)
-                             : launch_prep_t<BITS, NT, 1, TASKS, CANON, I8, 1>(p, grid, smem, st);
+        return in_vectors(4) ? launch_prep_t<BITS, NT, 1, TASKS, CANON, I8, 4>(p, glu, grid, smem, st)
+                             : launch_prep_t<BITS, NT, 1, TASKS, CANON, I8, 1>(p, glu, grid, smem, st);
       return PEQA_ERR_BAD_SHAPE;
     case 2:
-      return in_vectors(4)   ? launch_prep_t<BITS, NT, 2, TASKS, CANON, I8, 4>(p, grid, smem, st)
-             : in_vectors(2) ? launch_prep_t<BITS, NT, 2, TASKS, CANON, I8, 2>(p, grid, smem, st)
-                             : launch_prep_t<BITS, NT, 2, TASKS, CANON, I8, 1>(p, grid, smem, st);
-    case 3: return launch_prep_t<BITS, NT, 3, TASKS, CANON, I8, 1>(p, grid, smem, st);   // two groups a step
-    default: return launch_prep_t<BITS, NT, 0, false, CANON, I8, 1>(p, grid, smem, st);   // tasks: looked up per row
+      return in_vectors(4)   ? launch_prep_t<BITS, NT, 2, TASKS, CANON, I8, 4>(p, glu, grid, smem, st)
+             : in_vectors(2) ? launch_prep_t<BITS, NT, 2, TASKS, CANON, I8, 2>(p, glu, grid, smem, st)
+                             : launch_prep_t<BITS, NT, 2, TASKS, CANON, I8, 1>(p, glu, grid, smem, st);
+    case 3: return launch_prep_t<BITS, NT, 3, TASKS, CANON, I8, 1>(p, glu, grid, smem, st);   // two groups a step
+    default: return launch_prep_t<BITS, NT, 0, false, CANON, I8, 1>(p, glu, grid, smem, st);   // tasks: looked up per row
   }
 }
 
 template <int BITS, bool CANON>
-int launch_prep_b(const PrepParams& p, bool i8, int gsh, int grid, size_t smem, cudaStream_t st) {
+int launch_prep_b(const PrepParams& p, bool glu, bool i8, int gsh, int grid, size_t smem, cudaStream_t st) {
   if constexpr (!CANON) {                              // (canonical rows: at most eight tokens, see decode_rows_supported)
-    if (p.M > 8) return launch_prep_g<BITS, 2, false, false, false>(p, gsh, grid, smem, st);
+    if (p.M > 8) return launch_prep_g<BITS, 2, false, false, false>(p, glu, gsh, grid, smem, st);
     if (p.task_ids)
-      return i8 ? launch_prep_g<BITS, 1, true, false, true>(p, gsh, grid, smem, st)
-                : launch_prep_g<BITS, 1, true, false, false>(p, gsh, grid, smem, st);
+      return i8 ? launch_prep_g<BITS, 1, true, false, true>(p, glu, gsh, grid, smem, st)
+                : launch_prep_g<BITS, 1, true, false, false>(p, glu, gsh, grid, smem, st);
   }
-  return i8 ? launch_prep_g<BITS, 1, false, CANON, true>(p, gsh, grid, smem, st)
-            : launch_prep_g<BITS, 1, false, CANON, false>(p, gsh, grid, smem, st);
+  return i8 ? launch_prep_g<BITS, 1, false, CANON, true>(p, glu, gsh, grid, smem, st)
+            : launch_prep_g<BITS, 1, false, CANON, false>(p, glu, gsh, grid, smem, st);
 }
 
 int check_prep_layer(const peqa_qweight_t* w) {
@@ -1564,7 +1576,7 @@ int run_decode(const peqa_qweight_t* w, const void* weights, bool canon, int g, 
   p.zeros = w->zeros;
   p.scales = task_ids ? scale_table : w->scales;
   p.X = static_cast<const __nv_bfloat16*>(X);
-  p.Y = static_cast<__nv_bfloat16*>(Y);
+  p.Y = pairs ? glu.H : static_cast<__nv_bfloat16*>(Y);
   p.task_ids = task_ids;
   p.n_tasks = n_tasks;
   p.N = w->out_features;
@@ -1581,17 +1593,17 @@ int run_decode(const peqa_qweight_t* w, const void* weights, bool canon, int g, 
   p.x_pitch = plan.x_pitch;
   p.pairs_per_cta = plan.pairs;
   p.cshift = plan.cshift;
-  p.row_bytes = p.K / 8 * w->bits;
-  p.glu = glu;
+  if (pairs) p.act = glu.act;
+  else p.row_bytes = p.K / 8 * w->bits;
   p.m_magic[0] = quotient_magic(M);
   p.m_magic[1] = quotient_magic((M + 1) / 2);
   PEQA_TRY(status_word(st, &p.status));
   const int gsh = gcols == 64 ? 1 : gcols == 128 ? 2 : gcols == 256 ? 3 : 0;
   if (canon)
-    return w->bits == 3 ? launch_prep_b<3, true>(p, plan.i8, gsh, plan.grid, plan.smem, st)
-                        : launch_prep_b<4, true>(p, plan.i8, gsh, plan.grid, plan.smem, st);
-  return w->bits == 3 ? launch_prep_b<3, false>(p, plan.i8, gsh, plan.grid, plan.smem, st)
-                      : launch_prep_b<4, false>(p, plan.i8, gsh, plan.grid, plan.smem, st);
+    return w->bits == 3 ? launch_prep_b<3, true>(p, false, plan.i8, gsh, plan.grid, plan.smem, st)
+                        : launch_prep_b<4, true>(p, false, plan.i8, gsh, plan.grid, plan.smem, st);
+  return w->bits == 3 ? launch_prep_b<3, false>(p, pairs, plan.i8, gsh, plan.grid, plan.smem, st)
+                      : launch_prep_b<4, false>(p, pairs, plan.i8, gsh, plan.grid, plan.smem, st);
 }
 
 }  // namespace

@@ -73,10 +73,18 @@ struct PairParams {
   int n_tiles, t_tiles, k_blocks;   // 256-channel tiles, 512-token tiles, 64-deep stages
   PairItems items;
   Side side;            // see common.cuh
-  const __nv_bfloat16* dY;   // DS: [T, N]
-  float* ds_part;            // DS: [2 * ceil(T / 256)][N]
-  GluOut glu;                // GLU; `out` may be nullptr then
-  bool glu_wide;             // GLU: rows of H begin at multiples of 32 bytes
+  // (One size of the parameters for all: see PrepParams in decode_prep.cu.)
+  union {
+    const __nv_bfloat16* dY; // DS: [T, N]
+    __nv_bfloat16* H;        // GLU: [T, N / 2]; `out` may be nullptr then
+  };
+  union {
+    float* ds_part;          // DS: [2 * ceil(T / 256)][N]
+    struct {
+      int act;               // GLU: peqa_activation
+      int wide;              // GLU: rows of H begin at multiples of 32 bytes
+    } glu;
+  };
   int* status;
 };
 
@@ -326,8 +334,8 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
               o[q] = *reinterpret_cast<const uint32_t*>(&b);
             }
             if (row0 + lane < p.T) {
-              __nv_bfloat16* at = p.glu.H + (size_t)(row0 + lane) * (p.N >> 1) + (c0 >> 1);
-              if (p.glu_wide) {
+              __nv_bfloat16* at = p.H + (size_t)(row0 + lane) * (p.N >> 1) + (c0 >> 1);
+              if (p.glu.wide) {
                 asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(o[0]), "r"(o[1]), "r"(o[2]),
                              "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
               } else {
@@ -589,8 +597,6 @@ bool fwd_pair_supported(const peqa_qweight_t* w) {
 int launch_fwd_pair(const peqa_qweight_t* w, const float* zeros_f, int g, const void* X, int T,
                     void* Y, const void* dY, float* ds_part, cudaStream_t st, Side side, const GluOut* glu) {
   PairParams p;
-  p.glu = glu ? *glu : GluOut{};
-  p.glu_wide = w->out_features % 32 == 0 && reinterpret_cast<uintptr_t>(p.glu.H) % 32 == 0;
   p.side = side;
   p.zeros = w->zeros;
   p.zeros_f = zeros_f;
@@ -598,6 +604,11 @@ int launch_fwd_pair(const peqa_qweight_t* w, const float* zeros_f, int g, const 
   p.out = static_cast<__nv_bfloat16*>(Y);
   p.dY = static_cast<const __nv_bfloat16*>(dY);
   p.ds_part = ds_part;
+  if (glu) {
+    p.H = glu->H;
+    p.glu.act = glu->act;
+    p.glu.wide = w->out_features % 32 == 0 && reinterpret_cast<uintptr_t>(glu->H) % 32 == 0;
+  }
   p.N = w->out_features;
   p.K = w->in_features;
   p.g = g;

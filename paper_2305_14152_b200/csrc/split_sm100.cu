@@ -82,9 +82,15 @@ struct SplitParams {
   int region;             // bytes of the stage buffers, which the partial sums take over
   int acc2, a_col;        // tensor-memory columns of the second accumulator and of the weights (forward)
   int q, cshift;          // tiles per cluster, log2 of the CTAs per cluster (q <= 1 << cshift)
-  const __nv_bfloat16* dY;   // DS: [T, N]
-  float* ds_part;            // DS: [token tiles * passes][N]
-  GluOut glu;                // GLU; `out` may be nullptr then
+  // (One size of the parameters for all: see PrepParams in decode_prep.cu.)
+  union {
+    const __nv_bfloat16* dY; // DS: [T, N]
+    __nv_bfloat16* H;        // GLU: [T, N / 2]; `out` may be nullptr then
+  };
+  union {
+    float* ds_part;          // DS: [token tiles * passes][N]
+    int act;                 // GLU: peqa_activation
+  };
   Side side;                 // see common.cuh
   int* status;
 };
@@ -514,13 +520,13 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
             up.z = __shfl_xor_sync(four, a.z, 2);
             up.w = __shfl_xor_sync(four, a.w, 2);
             if (!(lane & 2)) {
-              const __nv_bfloat162 b0 = __floats2bfloat162_rn(glu_value(a.x, up.x, p.glu.act), glu_value(a.y, up.y, p.glu.act));
-              const __nv_bfloat162 b1 = __floats2bfloat162_rn(glu_value(a.z, up.z, p.glu.act), glu_value(a.w, up.w, p.glu.act));
+              const __nv_bfloat162 b0 = __floats2bfloat162_rn(glu_value(a.x, up.x, p.act), glu_value(a.y, up.y, p.act));
+              const __nv_bfloat162 b1 = __floats2bfloat162_rn(glu_value(a.z, up.z, p.act), glu_value(a.w, up.w, p.act));
               uint2 o;
               o.x = *reinterpret_cast<const uint32_t*>(&b0);
               o.y = *reinterpret_cast<const uint32_t*>(&b1);
               const int channel = (row >> 4) * kGluRun + (row & 7);
-              *reinterpret_cast<uint2*>(p.glu.H + (size_t)(t0 + t) * (p.R >> 1) + channel) = o;
+              *reinterpret_cast<uint2*>(p.H + (size_t)(t0 + t) * (p.R >> 1) + channel) = o;
             }
             if (!p.out) continue;
           }
@@ -726,7 +732,6 @@ int split_part_tokens(const peqa_qweight_t* w, int T_call, bool trans) {
 int launch_split(const peqa_qweight_t* w, const float* zeros_f, int g, const void* act, int T, void* out,
                  bool trans, const void* dY, float* ds_part, cudaStream_t st, int T_call, int t0, Side side, const GluOut* glu) {
   SplitParams p;
-  p.glu = glu ? *glu : GluOut{};
   p.side = side;
   p.zeros = w->zeros;
   p.zeros_f = zeros_f;
@@ -734,6 +739,10 @@ int launch_split(const peqa_qweight_t* w, const float* zeros_f, int g, const voi
   p.out = static_cast<__nv_bfloat16*>(out);
   p.dY = static_cast<const __nv_bfloat16*>(dY);
   p.ds_part = ds_part;
+  if (glu) {
+    p.H = glu->H;
+    p.act = glu->act;
+  }
   p.N = w->out_features;
   p.K = w->in_features;
   p.g = g;
