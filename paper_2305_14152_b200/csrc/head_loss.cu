@@ -46,7 +46,7 @@ constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kLossThreads = 384;               // warps: 0 TMA, 1 MMA, 2 tensor memory, 4-11 epilogue
 constexpr int kStagingBytes = 4096;             // of an epilogue warp
 constexpr int kLossSmem = kStages * kStageBytes + 8 * kStagingBytes + 1024 + 512;
-constexpr int kRowsOfBlock = 8;                 // tokens of a CTA of the kernels before and behind
+constexpr int kSideThreads = 256;               // of the kernels before and behind
 constexpr float kFarAbove = 60.0f;              // exp(60) V |W| is far below binary32's largest number
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kChunkRows = 8192;
@@ -77,11 +77,12 @@ struct LossParams {
   float* sums;           // [halves of tiles, rows]: s, or (without gradient) pairs of largest logit and sum relative to it
   int row0, rows;        // first live token of the chunk, rows that its buffers have (a multiple of 256)
   int V, K, k_blocks;    // stages of a tile of logits
+  int width;             // entries of a tile of the vocabulary, a multiple of 32
   int tile0, tiles;      // tiles of the vocabulary in this launch's piece
-  int back0, back_tiles; // those of the piece before, whose gradient is summed; back_tiles 0: none
+  int back0, back_blocks;    // first entry and stages of the piece before, whose gradient is summed; 0 stages: none
   bool first_back;       // nothing has been summed yet
   int splits;            // parts that the sum over a piece is cut into, each with sums of its own
-  int group;             // blocks of 256 tokens whose tiles are worked through together
+  int group, back_group; // blocks of 256 tokens whose tiles are worked through together
   int* status;
 };
 
@@ -97,34 +98,38 @@ struct Item {
 // begin with as many tiles of logits as take its time, and the others are dealt to all.
 struct Walk {
   int pair, pairs, n1, n2, n2_mine, lo_first, lo_pairs, lo_mine, lo_total;
-  int rows, features, splits, back_blocks;
+  int rows, features, splits;
   __device__ __forceinline__ Walk(const LossParams& p, int rows_live) {
     pair = blockIdx.x >> 1;
     pairs = gridDim.x >> 1;
     rows = (rows_live + kTile - 1) / kTile;
     features = (p.K + kTile - 1) / kTile;
     splits = p.splits;
-    back_blocks = p.back_tiles * (kTile / kDepth);
     n1 = rows * p.tiles;
-    n2 = p.back_tiles ? rows * features * splits : 0;
+    n2 = p.back_blocks ? rows * features * splits : 0;
     n2_mine = n2 > pair ? (n2 - pair - 1) / pairs + 1 : 0;
     lo_first = n2 % pairs;
     lo_pairs = lo_first ? pairs - lo_first : 0;
-    const int each = lo_pairs ? (back_blocks / splits + p.k_blocks / 2) / p.k_blocks : 0;
+    const int each = lo_pairs ? (p.back_blocks / splits + p.k_blocks / 2) / p.k_blocks : 0;
     lo_total = min(n1, each * lo_pairs);
     const int e = pair - lo_first;
     lo_mine = lo_pairs && e >= 0 && lo_total > e ? (lo_total - e - 1) / lo_pairs + 1 : 0;
+  }
+  // Groups of token blocks, in them column by column of tiles: what the pairs read at a time stays in L2.
+  __device__ __forceinline__ void deal(int e, int group, int cols, Item& it) const {
+    const int g = e / (group * cols), first = g * group, in_group = min(group, rows - first);
+    e -= first * cols;
+    it.col = e / in_group;
+    it.row = first + e - it.col * in_group;
   }
   __device__ __forceinline__ bool get(const LossParams& p, int i, Item& it) const {
     if (i < n2_mine) {
       int e = pair + i * pairs;
       it.grad = true;
-      it.col = e % features;
-      e /= features;
-      it.row = e % rows;
-      it.split = e / rows;
-      it.kb0 = (int)((long long)it.split * back_blocks / splits);
-      it.kbs = (int)((long long)(it.split + 1) * back_blocks / splits) - it.kb0;
+      it.split = e / (rows * features);
+      deal(e - it.split * rows * features, p.back_group, features, it);
+      it.kb0 = (int)((long long)it.split * p.back_blocks / splits);
+      it.kbs = (int)((long long)(it.split + 1) * p.back_blocks / splits) - it.kb0;
       return true;
     }
     i -= n2_mine;
@@ -136,12 +141,8 @@ struct Walk {
       if (at >= n1) return false;
       e = (int)at;
     }
-    // groups of token blocks, in them tile by tile of the vocabulary: what the pairs read at a time stays in L2
-    const int g = e / (p.group * p.tiles), first = g * p.group, in_group = min(p.group, rows - first);
-    e -= first * p.tiles;
     it.grad = false;
-    it.col = e / in_group;
-    it.row = first + e - it.col * in_group;
+    deal(e, p.group, p.tiles, it);
     it.split = 0;
     it.kb0 = 0;
     it.kbs = p.k_blocks;
@@ -233,22 +234,23 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
       Item item;
       // self-test knob (peqa_selftest_configure): one byte more is announced than will arrive
       const uint32_t starve = p.status[5] != 0 ? 1u : 0u;
+      const uint32_t logits_bytes = 2 * kOperandBytes + p.width * (kDepth * 2);      // of both CTAs
       for (int i = 0; ok && walk.get(p, i, item); ++i) {
         const int row = item.row * kTile + (int)rank * 128;
         for (int kb = 0; kb < item.kbs; ++kb, ++it) {
           const int s = it % kStages;
           if (!mbar_wait_cluster(smem_u32(&bars->empty[s]), ((it / kStages) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-          if (leader) mbar_arrive_expect_tx(smem_u32(&bars->full[s]), 2 * kStageBytes + starve);
+          if (leader) mbar_arrive_expect_tx(smem_u32(&bars->full[s]), (item.grad ? 2 * kStageBytes : logits_bytes) + starve);
           const uint32_t bar = mapa_shared(smem_u32(&bars->full[s]), 0), a = smem_u32(base + s * kStageBytes);
           if (!item.grad) {
             tma_load_2d_pair(a, &tmap_x, bar, kb * kDepth, p.row0 + row);
-            tma_load_2d_pair(a + kOperandBytes, &tmap_w, bar, kb * kDepth, (p.tile0 + item.col) * kTile + (int)rank * 128);
+            tma_load_2d_pair(a + kOperandBytes, &tmap_w, bar, kb * kDepth, (p.tile0 + item.col) * p.width + (int)rank * (p.width >> 1));
           } else if (GRAD) {
             const int k = (item.kb0 + kb) * kDepth, n0 = item.col * kTile + (int)rank * 128;
             tma_load_2d_pair(a, &tmap_e_in, bar, k, row);
 #pragma unroll
             for (int m = 0; m < 2; ++m)
-              tma_load_2d_pair(a + kOperandBytes + m * 8192, &tmap_wt, bar, n0 + 64 * m, p.back0 * kTile + k);
+              tma_load_2d_pair(a + kOperandBytes + m * 8192, &tmap_wt, bar, n0 + 64 * m, p.back0 + k);
           }
         }
       }
@@ -256,7 +258,8 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
   } else if (warp == 1) {
     // ------------------------------------------ MMA issuer (leader CTA, one lane)
     if (leader) if (elect_lane() == 0) {
-      constexpr uint32_t idesc_logits = idesc_bf16_f32(256, 256, 0, 0), idesc_grad = idesc_bf16_f32(256, 256, 0, 1);
+      const uint32_t idesc_logits = idesc_bf16_f32(256, p.width, 0, 0);
+      constexpr uint32_t idesc_grad = idesc_bf16_f32(256, 256, 0, 1);
       const uint32_t a0 = smem_u32(base);
       const uint64_t adesc0 = smem_desc_sw128(a0, 16, 1024);
       const uint64_t bdesc_logits = smem_desc_sw128(a0 + kOperandBytes, 16, 1024);
@@ -307,9 +310,10 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
       const uint32_t acc_empty = mapa_shared(smem_u32(&bars->acc_empty[buf]), 0);
       float ref = 0.0f;
       int label = -1, cols = 0;                             // both counted from this half tile's first entry
-      const int entry0 = (p.tile0 + item.col) * kTile + half * 128;
+      const int entry0 = (p.tile0 + item.col) * p.width + half * 128;
+      const int chunks = item.grad ? 4 : min(4, (p.width - half * 128) >> 5);      // none: 0 or less
       if (!item.grad) {
-        cols = p.V - entry0;
+        cols = min(p.V - entry0, chunks * 32);
         if (live) {
           ref = ld_global(p.live.ref + p.row0 + row);
           if (GRAD && p.second) ref += above_of(p.live, p.row0 + row);
@@ -320,11 +324,11 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
       tc_fence_after();
       float most = -INFINITY, sum = 0.0f;
 #pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < chunks; ++c) {
         uint32_t v[32];
         tmem_ld_32x32(from + c * 32, v);
         tmem_ld_wait();
-        if (c == 3) {
+        if (c + 1 == chunks) {
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(acc_empty);
@@ -371,7 +375,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
-              if (row_w < rows_live) tma_store_2d(&tmap_e_out, smem_u32(at), item.col * kTile + half * 128 + c * 32, row_w);
+              if (row_w < rows_live) tma_store_2d(&tmap_e_out, smem_u32(at), item.col * p.width + half * 128 + c * 32, row_w);
               bulk_commit_group();
             }
           }
@@ -393,6 +397,11 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
             bulk_commit_group();
           }
         }
+      }
+      if (chunks <= 0) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(acc_empty);
       }
       if (!item.grad) {
         const size_t slot = ((size_t)(p.tile0 + item.col) * 2 + half) * p.rows + row;
@@ -444,58 +453,73 @@ struct GatherParams {
   int* status;
 };
 
-// A warp a token: its place among those that count, its row beside theirs, and the logit of its label.  A CTA counts the tokens before its
-// own itself (16 KB of labels at 4096 tokens).
-__global__ void __launch_bounds__(kRowsOfBlock * 32) loss_gather_kernel(const GatherParams p) {
+// Sum over the CTA (kSideThreads), in one order, to all threads.  part: 8 floats of shared memory that nobody reads any more.
+template <typename V, typename F>
+__device__ __forceinline__ V over_block(V v, V* part, F&& join) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = join(v, __shfl_xor_sync(0xffffffffu, v, o));
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = part[0];
+#pragma unroll
+  for (int w = 1; w < kSideThreads / 32; ++w) v = join(v, part[w]);
+  return v;
+}
+__device__ __forceinline__ float add_floats(float a, float b) { return a + b; }
+
+// ROWS tokens a CTA, 8 / ROWS warps a token: its place among those that count, its row beside theirs, and the logit of its label.
+// A CTA counts the tokens before its own itself (16 KB of labels at 4096 tokens).  One token a CTA where there are few.
+template <int ROWS>
+__global__ void __launch_bounds__(kSideThreads) loss_gather_kernel(const GatherParams p) {
   wait_for_kernel_before();
   let_kernel_behind_in();
-  __shared__ int part[kRowsOfBlock];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t0 = blockIdx.x * kRowsOfBlock;
-  int before = 0;
-  for (int t = threadIdx.x; t < t0; t += kRowsOfBlock * 32) before += (unsigned)ld_global(p.labels + t) < (unsigned)p.V;
-  before = __reduce_add_sync(0xffffffffu, before);
-  if (lane == 0) part[warp] = before;
-  const int32_t near = lane < kRowsOfBlock && t0 + lane < p.T ? ld_global(p.labels + t0 + lane) : -1;
+  constexpr int kSpan = kSideThreads / ROWS;         // threads of a token
+  __shared__ int counts[8];
+  __shared__ float dots[8];
+  const int lane = threadIdx.x & 31, t0 = blockIdx.x * ROWS, mine = threadIdx.x / kSpan, at_thread = threadIdx.x % kSpan;
+  const int32_t near = lane < ROWS && t0 + lane < p.T ? ld_global(p.labels + t0 + lane) : -1;
   const uint32_t alive = __ballot_sync(0xffffffffu, (unsigned)near < (unsigned)p.V);
-  __syncthreads();
-  before = 0;
-#pragma unroll
-  for (int w = 0; w < kRowsOfBlock; ++w) before += part[w];
+  const int t = t0 + mine, label = __shfl_sync(0xffffffffu, near, mine);
+  const bool live = alive >> mine & 1u;
+  const size_t own = (size_t)t * p.K;
+  int before = 0;
+  for (int i = threadIdx.x; i < t0; i += kSideThreads) before += (unsigned)ld_global(p.labels + i) < (unsigned)p.V;
+  before = over_block(before, counts, [](int a, int b) { return a + b; });
   if (blockIdx.x == 0)
-    for (int c = threadIdx.x; c < p.chunks; c += kRowsOfBlock * 32) p.again[c] = 0;
+    for (int c = threadIdx.x; c < p.chunks; c += kSideThreads) p.again[c] = 0;
   if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *p.live.count = before + __popc(alive);
 
-  const int t = t0 + warp;
-  if (t >= p.T) return;
-  const int label = __shfl_sync(0xffffffffu, near, warp);
-  const size_t own = (size_t)t * p.K;
-  if (!(alive >> warp & 1u)) {
-    if (lane == 0) {
+  const int at = before + __popc(alive & ((1u << mine) - 1u));
+  float dot = 0.0f;
+  if (live) {
+    const __nv_bfloat16* w = p.W + (size_t)label * p.K;
+    __nv_bfloat16* row = p.rows + (size_t)at * p.K;
+#pragma unroll 4
+    for (int c = at_thread * 8; c < p.K; c += kSpan * 8) {
+      const uint4 a = ld_global(reinterpret_cast<const uint4*>(p.X + own + c)), b = ld_global(reinterpret_cast<const uint4*>(w + c));
+      *reinterpret_cast<uint4*>(row + c) = a;
+      const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        dot = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), dot);
+        dot = fmaf(__uint_as_float(x[e] & 0xFFFF0000u), __uint_as_float(y[e] & 0xFFFF0000u), dot);
+      }
+    }
+  } else if (t < p.T) {
+    if (at_thread == 0) {
       if (label >= p.V) note_bad_index(p.status);
       p.loss[t] = 0.0f;
     }
     if (p.dX)
-      for (int c = lane * 8; c < p.K; c += 256) *reinterpret_cast<uint4*>(p.dX + own + c) = make_uint4(0u, 0u, 0u, 0u);
-    return;
+      for (int c = at_thread * 8; c < p.K; c += kSpan * 8) *reinterpret_cast<uint4*>(p.dX + own + c) = make_uint4(0u, 0u, 0u, 0u);
   }
-  const int at = before + __popc(alive & ((1u << warp) - 1u));
-  const __nv_bfloat16* w = p.W + (size_t)label * p.K;
-  __nv_bfloat16* row = p.rows + (size_t)at * p.K;
-  float dot = 0.0f;
-#pragma unroll 4
-  for (int c = lane * 8; c < p.K; c += 256) {
-    const uint4 a = ld_global(reinterpret_cast<const uint4*>(p.X + own + c)), b = ld_global(reinterpret_cast<const uint4*>(w + c));
-    *reinterpret_cast<uint4*>(row + c) = a;
-    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+  if constexpr (ROWS == 1) {
+    dot = over_block(dot, dots, add_floats);
+  } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      dot = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), dot);
-      dot = fmaf(__uint_as_float(x[e] & 0xFFFF0000u), __uint_as_float(y[e] & 0xFFFF0000u), dot);
-    }
+    for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-  if (lane == 0) {
+  if (live && at_thread == 0) {
     p.live.index[at] = t;
     p.live.label[at] = label;
     p.live.ref[at] = dot;
@@ -516,48 +540,61 @@ struct FinishParams {
   __nv_bfloat16* dX;
 };
 
-// Eight tokens a CTA: their sums over the vocabulary, added in one order whatever the timing, then a warp a token.
-template <bool GRAD>
-__global__ void __launch_bounds__(kRowsOfBlock * 32) loss_finish_kernel(const FinishParams p) {
+// A largest logit and a sum relative to it.
+struct LogSum {
+  float most, sum;
+};
+__device__ __forceinline__ LogSum join_sums(LogSum a, LogSum b) {
+  const float most = fmaxf(a.most, b.most), by = most == -INFINITY ? 0.0f : most;
+  return {most, a.sum * exp2_approx((a.most - by) * kLog2e) + b.sum * exp2_approx((b.most - by) * kLog2e)};
+}
+
+// ROWS tokens a CTA: their sums over the vocabulary, added in one order whatever the timing, then 8 / ROWS warps a token.
+template <bool GRAD, int ROWS>
+__global__ void __launch_bounds__(kSideThreads) loss_finish_kernel(const FinishParams p) {
   wait_for_kernel_before();
   let_kernel_behind_in();
-  __shared__ float2 part[32][kRowsOfBlock];
-  const int row_b = blockIdx.x * kRowsOfBlock, live = min(p.rows, ld_global(p.live.count) - p.row0);
+  constexpr int kSpan = kSideThreads / ROWS, kParts = kSideThreads / ROWS;
+  __shared__ LogSum part[kParts][ROWS];
+  const int row_b = blockIdx.x * ROWS, live = min(p.rows, ld_global(p.live.count) - p.row0);
   if (row_b >= live) return;
   {
-    const int r = threadIdx.x & (kRowsOfBlock - 1), first = threadIdx.x / kRowsOfBlock;
-    float most = -INFINITY, sum = 0.0f;
-    for (int h = first; h < p.halves; h += 32) {
+    const int r = threadIdx.x % ROWS, first = threadIdx.x / ROWS;
+    LogSum v = {-INFINITY, 0.0f};
+    for (int h = first; h < p.halves; h += kParts) {
       const size_t at = (size_t)h * p.rows + row_b + r;
       if (GRAD) {
-        sum += ld_global(p.sums + at);
+        v.sum += ld_global(p.sums + at);
       } else {
-        const float2 v = ld_global(reinterpret_cast<const float2*>(p.sums) + at);
-        const float next = fmaxf(most, v.x), by = next == -INFINITY ? 0.0f : next;
-        sum = sum * exp2_approx((most - by) * kLog2e) + v.y * exp2_approx((v.x - by) * kLog2e);
-        most = next;
+        const float2 u = ld_global(reinterpret_cast<const float2*>(p.sums) + at);
+        v = join_sums(v, {u.x, u.y});
       }
     }
-    part[first][r] = make_float2(most, sum);
+    part[first][r] = v;
   }
   __syncthreads();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = row_b + warp;
+  const int mine = threadIdx.x / kSpan, at_thread = threadIdx.x % kSpan, lane = threadIdx.x & 31, row = row_b + mine;
   if (row >= live) return;
-  const float2 v = part[lane][warp];
-  float sum = v.y, most = v.x;
-  if (!GRAD) {
+  LogSum v = {-INFINITY, 0.0f};
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-    sum *= exp2_approx((v.x - (most == -INFINITY ? 0.0f : most)) * kLog2e);
+  for (int h = 0; h < kParts; h += 32) {
+    const LogSum u = part[h + lane][mine];
+    if (GRAD) v.sum += u.sum;
+    else v = join_sums(v, u);
   }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  for (int o = 16; o > 0; o >>= 1) {
+    const LogSum u = {__shfl_xor_sync(0xffffffffu, v.most, o), __shfl_xor_sync(0xffffffffu, v.sum, o)};
+    if (GRAD) v.sum += u.sum;
+    else v = join_sums(v, u);
+  }
+  const float sum = v.sum;
 
   const int token = ld_global(p.live.index + p.row0 + row);
   // the reference above the label's logit, and the label's term
-  const float above = GRAD ? above_of(p.live, p.row0 + row) : most - ld_global(p.live.ref + p.row0 + row);
+  const float above = GRAD ? above_of(p.live, p.row0 + row) : v.most - ld_global(p.live.ref + p.row0 + row);
   const float own = expf(-above);
-  if (lane == 0) {
+  if (at_thread == 0) {
     float loss;
     if (GRAD) loss = above == 0.0f ? log1pf(sum) : above + logf(sum + own);
     else loss = above <= 0.0f ? log1pf(sum * expf(above)) : above + logf(sum + own);
@@ -570,22 +607,23 @@ __global__ void __launch_bounds__(kRowsOfBlock * 32) loss_finish_kernel(const Fi
   const size_t per_split = (size_t)p.rows * p.K;
   __nv_bfloat16* out = p.dX + (size_t)token * p.K;
 #pragma unroll 2
-  for (int c = lane * 8; c < p.K; c += 256) {
+  for (int c = at_thread * 8; c < p.K; c += kSpan * 8) {
     float4 lo = ld_global(reinterpret_cast<const float4*>(g + c)), hi = ld_global(reinterpret_cast<const float4*>(g + c + 4));
+    const uint4 b = ld_global(reinterpret_cast<const uint4*>(w + c));
+#pragma unroll 4
     for (int s = 1; s < p.splits; ++s) {
       const float4 a = ld_global(reinterpret_cast<const float4*>(g + s * per_split + c));
-      const float4 b = ld_global(reinterpret_cast<const float4*>(g + s * per_split + c + 4));
+      const float4 d = ld_global(reinterpret_cast<const float4*>(g + s * per_split + c + 4));
       lo.x += a.x; lo.y += a.y; lo.z += a.z; lo.w += a.w;
-      hi.x += b.x; hi.y += b.y; hi.z += b.z; hi.w += b.w;
+      hi.x += d.x; hi.y += d.y; hi.z += d.z; hi.w += d.w;
     }
-    const uint4 b = ld_global(reinterpret_cast<const uint4*>(w + c));
-    const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    const float v8[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
     const uint32_t y[4] = {b.x, b.y, b.z, b.w};
     uint32_t o[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      o[e] = bf16_pair(fmaf(-sum, __uint_as_float(y[e] << 16), v[2 * e]) * by,
-                       fmaf(-sum, __uint_as_float(y[e] & 0xFFFF0000u), v[2 * e + 1]) * by);
+      o[e] = bf16_pair(fmaf(-sum, __uint_as_float(y[e] << 16), v8[2 * e]) * by,
+                       fmaf(-sum, __uint_as_float(y[e] & 0xFFFF0000u), v8[2 * e + 1]) * by);
     *reinterpret_cast<uint4*>(out + c) = make_uint4(o[0], o[1], o[2], o[3]);
   }
 }
@@ -595,12 +633,12 @@ __global__ void __launch_bounds__(kRowsOfBlock * 32) loss_finish_kernel(const Fi
 struct LossPlan {
   int rows;                  // live tokens of a chunk at most, a multiple of 256
   int chunks;
-  int tiles, pieces, splits;
-  int group;
+  int width, tiles, pieces, splits;      // width: entries of a tile
+  int group, back_group;
   // offsets into the workspace
   size_t count, again, index, label, ref, above, x, sums, e[2], grads, bytes;
   int piece_tile(int i) const { return (int)((long long)tiles * i / pieces); }
-  int piece_width() const { return ((tiles + pieces - 1) / pieces) * kTile; }     // entries of the widest
+  int piece_width() const { return ((tiles + pieces - 1) / pieces) * width; }     // entries of the widest
 };
 
 // Sizes and cuts, by the sizes of the call alone.
@@ -613,20 +651,38 @@ LossPlan plan_loss(int T, int V, int K, bool grad, int sms) {
   const long long all = ((long long)T + 255) & ~255ll;
   c.rows = (int)(all < most ? all : most);
   c.chunks = (int)((all + c.rows - 1) / c.rows);
-  c.tiles = (int)(((long long)V + kTile - 1) / kTile);
-  c.pieces = 1;
+  const int blocks = c.rows / kTile;
+  // 64 MB of exponentials a piece
+  const long long wide = (64ll << 20) / (2ll * c.rows);
+  c.pieces = grad ? (int)((V + wide - 1) / wide) : 1;
+  // Where all tiles of logits are one launch's, they are as wide as shares them out best: rounds of the pairs, each a tile's contraction,
+  // which takes a time proportional to its width, and a sixteenth of a full one's for what does not.
+  c.width = kTile;
+  if (c.pieces == 1) {
+    long long best = 0;
+    for (int width = kTile; width >= 128; width -= 32) {
+      const long long rounds = ((long long)blocks * ((V + width - 1) / width) + pairs - 1) / pairs, cost = rounds * (width + 16);
+      if (best == 0 || cost < best) {
+        best = cost;
+        c.width = width;
+      }
+    }
+  }
+  c.tiles = (int)(((long long)V + c.width - 1) / c.width);
+  if (c.pieces > c.tiles) c.pieces = c.tiles;
   c.splits = 1;
-  // token blocks that share an L2 with a tile or two of the vocabulary for each pair
-  c.group = (int)((32ll << 20) / (512ll * K));
-  c.group = c.group < 4 ? 4 : c.group;
+  // token blocks whose operands, 32 MB, share the L2 with a few tiles of the other side
+  auto group_of = [](long long depth) {
+    const int g = (int)((32ll << 20) / (512ll * depth));
+    return g < 4 ? 4 : g;
+  };
+  c.group = group_of(K);
+  c.back_group = group_of(c.piece_width());
   if (grad) {
-    // 64 MB of exponentials a piece
-    const long long wide = (64ll << 20) / (512ll * c.rows);
-    c.pieces = (int)((c.tiles + wide - 1) / wide);
-    const int back = (c.rows / kTile) * ((K + kTile - 1) / kTile);
+    const int back = blocks * ((K + kTile - 1) / kTile);
     if (back < pairs) {
       c.splits = pairs / back;
-      const int least = c.tiles / c.pieces * (kTile / kDepth);
+      const int least = c.tiles / c.pieces * c.width / kDepth;
       if (c.splits > least) c.splits = least;
       if (c.splits > 16) c.splits = 16;
     }
@@ -656,11 +712,11 @@ LossPlan plan_loss(int T, int V, int K, bool grad, int sms) {
 }
 
 int loss_map(CUtensorMap* m, CUtensorMapDataType type, const void* base, uint64_t inner, uint64_t outer, int size, uint32_t box_x,
-             uint32_t box_y, CUtensorMapSwizzle swizzle) {
+             uint32_t box_y, CUtensorMapSwizzle swizzle, uint64_t pitch = 0) {
   EncodeTiledFn enc = nullptr;
   PEQA_TRY(tensor_map_encoder(&enc));
   cuuint64_t dims[2] = {inner, outer};
-  cuuint64_t strides[1] = {inner * size};
+  cuuint64_t strides[1] = {pitch ? pitch : inner * size};
   cuuint32_t box[2] = {box_x, box_y};
   cuuint32_t estr[2] = {1, 1};
   if (enc(m, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
@@ -743,17 +799,18 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
   p.k_blocks = (K + kDepth - 1) / kDepth;
   p.splits = c.splits;
   p.group = c.group;
+  p.back_group = c.back_group;
+  p.width = c.width;
   p.status = status;
   const uint64_t width = c.piece_width();
-  CUtensorMap maps[6], e_out[2], e_in[2];
+  CUtensorMap maps[6], e_out[2];
   PEQA_TRY(bf16_map(&maps[0], ws + c.x, K, (uint64_t)c.chunks * c.rows, 128));
-  PEQA_TRY(bf16_map(&maps[1], W, K, V, 128));
+  PEQA_TRY(bf16_map(&maps[1], W, K, V, c.width / 2));
   PEQA_TRY(bf16_map(&maps[2], W, K, V, 64));
   maps[3] = maps[4] = maps[5] = maps[0];
   if (dX) {
     for (int b = 0; b < 2; ++b) {
       PEQA_TRY(loss_map(&e_out[b], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, ws + c.e[b], width, c.rows, 2, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B));
-      PEQA_TRY(bf16_map(&e_in[b], ws + c.e[b], width, c.rows, 128));
     }
     PEQA_TRY(loss_map(&maps[5], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, ws + c.grads, K, (uint64_t)c.splits * c.rows, 4, 32, 32,
                       CU_TENSOR_MAP_SWIZZLE_128B));
@@ -773,7 +830,10 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
   gp.loss = loss;
   gp.dX = static_cast<__nv_bfloat16*>(dX);
   gp.status = status;
-  PEQA_TRY(launch_after(loss_gather_kernel, (T + kRowsOfBlock - 1) / kRowsOfBlock, kRowsOfBlock * 32, st, gp));
+  // one token a CTA while that fills no more than two rounds of the SMs
+  const bool few = T <= 2 * 8 * sms;
+  PEQA_TRY(few ? launch_after(loss_gather_kernel<1>, T, kSideThreads, st, gp)
+               : launch_after(loss_gather_kernel<8>, (T + 7) / 8, kSideThreads, st, gp));
 
   FinishParams fp = {};
   fp.live = live;
@@ -795,20 +855,25 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
       for (int i = 0; i <= (dX ? c.pieces : 0); ++i) {
         p.tile0 = i < c.pieces ? c.piece_tile(i) : 0;
         p.tiles = i < c.pieces ? c.piece_tile(i + 1) - p.tile0 : 0;
-        p.back0 = i > 0 ? c.piece_tile(i - 1) : 0;
-        p.back_tiles = i > 0 ? c.piece_tile(i) - p.back0 : 0;
+        const int before = i > 0 ? c.piece_tile(i - 1) : 0, entries = i > 0 ? (c.piece_tile(i) - before) * c.width : 0;
+        p.back0 = before * c.width;
+        p.back_blocks = (entries + kDepth - 1) / kDepth;
         p.first_back = i == 1;
         if (dX) {
           maps[3] = e_out[i & 1];
-          maps[4] = e_in[(i & 1) ^ 1];
+          // of the piece's own width: what its last stage has beyond that is read as zeros
+          if (i > 0)
+            PEQA_TRY(loss_map(&maps[4], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, ws + c.e[(i & 1) ^ 1], entries, c.rows, 2, 64, 128,
+                              CU_TENSOR_MAP_SWIZZLE_128B, width * 2));
           PEQA_TRY(launch_loss<true>(maps, p, pairs, st));
         } else {
           PEQA_TRY(launch_loss<false>(maps, p, pairs, st));
         }
       }
     }
-    const int blocks = (c.rows < T ? c.rows : T + kRowsOfBlock - 1) / kRowsOfBlock;
-    PEQA_TRY(launch_after(dX ? loss_finish_kernel<true> : loss_finish_kernel<false>, blocks, kRowsOfBlock * 32, st, fp));
+    const int rows = c.rows < T ? c.rows : T;
+    if (few) PEQA_TRY(launch_after(dX ? loss_finish_kernel<true, 1> : loss_finish_kernel<false, 1>, rows, kSideThreads, st, fp));
+    else PEQA_TRY(launch_after(dX ? loss_finish_kernel<true, 8> : loss_finish_kernel<false, 8>, (rows + 7) / 8, kSideThreads, st, fp));
   }
   return PEQA_OK;
 }
