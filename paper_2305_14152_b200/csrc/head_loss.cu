@@ -28,27 +28,35 @@
 #include <cuda_bf16.h>
 
 #include "common.cuh"
+#include "head_loss.cuh"
 #include "kv_cache.cuh"
-#include "sm100_ptx.cuh"
-#include "tensor_map.cuh"
 
 namespace peqa {
+
+int loss::loss_map(CUtensorMap* m, CUtensorMapDataType type, const void* base, uint64_t inner, uint64_t outer, int size, uint32_t box_x,
+             uint32_t box_y, CUtensorMapSwizzle swizzle, uint64_t pitch) {
+  EncodeTiledFn enc = nullptr;
+  PEQA_TRY(tensor_map_encoder(&enc));
+  cuuint64_t dims[2] = {inner, outer};
+  cuuint64_t strides[1] = {pitch ? pitch : inner * size};
+  cuuint32_t box[2] = {box_x, box_y};
+  cuuint32_t estr[2] = {1, 1};
+  if (enc(m, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return cuda_fail(cudaErrorInvalidValue);
+  return PEQA_OK;
+}
 
 namespace {
 
 using namespace ptx;
+using namespace loss;
 
-constexpr int kTile = 256;                      // tokens, and vocabulary entries or features, of a tile
-constexpr int kDepth = 64;                      // contraction elements of a stage
 constexpr int kStages = 6;
-constexpr int kOperandBytes = 128 * kDepth * 2;     // this CTA's half of a stage's A or B
 constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kLossThreads = 384;               // warps: 0 TMA, 1 MMA, 2 tensor memory, 4-11 epilogue
 constexpr int kStagingBytes = 4096;             // of an epilogue warp
 constexpr int kLossSmem = kStages * kStageBytes + 8 * kStagingBytes + 1024 + 512;
 constexpr int kSideThreads = 256;               // of the kernels before and behind
-constexpr float kFarAbove = 60.0f;              // exp(60) V |W| is far below binary32's largest number
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kChunkRows = 8192;
 
 struct LossBarriers {
@@ -59,31 +67,6 @@ struct LossBarriers {
   uint32_t tmem_base;
   int abort_flag;
   int wait_limit_us;             // must follow abort_flag (read by the bounded waits)
-};
-
-// What the kernel before leaves of the tokens that count, in their order.
-struct LiveTokens {
-  int* count;        // [1]
-  int* index;        // token
-  int* label;
-  float* ref;        // logit of the label
-  int* above;        // bits of the largest l - ref beyond kFarAbove, 0 if there is none
-};
-
-struct LossParams {
-  LiveTokens live;
-  int* again;            // the chunk's flag
-  bool second;           // the repetition
-  float* sums;           // [halves of tiles, rows]: s, or (without gradient) pairs of largest logit and sum relative to it
-  int row0, rows;        // first live token of the chunk, rows that its buffers have (a multiple of 256)
-  int V, K, k_blocks;    // stages of a tile of logits
-  int width;             // entries of a tile of the vocabulary, a multiple of 32
-  int tile0, tiles;      // tiles of the vocabulary in this launch's piece
-  int back0, back_blocks;    // first entry and stages of the piece before, whose gradient is summed; 0 stages: none
-  bool first_back;       // nothing has been summed yet
-  int splits;            // parts that the sum over a piece is cut into, each with sums of its own
-  int group, back_group; // blocks of 256 tokens whose tiles are worked through together
-  int* status;
 };
 
 struct Item {
@@ -149,26 +132,6 @@ struct Walk {
     return true;
   }
 };
-
-__device__ __forceinline__ float exp2_approx(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
-  const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&b);
-}
-__device__ __forceinline__ void tma_add_2d(const CUtensorMap* m, uint32_t src_smem, int x, int y) {
-  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3}], [%1];"
-               ::"l"(reinterpret_cast<uint64_t>(m)), "r"(src_smem), "r"(x), "r"(y)
-               : "memory");
-}
-__device__ __forceinline__ void wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void let_kernel_behind_in() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
-// Reference of a live token: the label's logit, or in the repetition the row's largest if that is far above.
-__device__ __forceinline__ float above_of(const LiveTokens& live, int row) { return __int_as_float(ld_global(live.above + row)); }
 
 template <bool GRAD>
 __global__ void __launch_bounds__(kLossThreads, 1)
@@ -530,7 +493,7 @@ __global__ void __launch_bounds__(kSideThreads) loss_gather_kernel(const GatherP
 struct FinishParams {
   LiveTokens live;
   const float* sums;
-  int halves;              // of tiles of the vocabulary
+  int parts;               // that the vocabulary's sums come in
   int row0, rows;
   const float* grads;      // [splits, rows, K]
   int splits, K;
@@ -561,7 +524,7 @@ __global__ void __launch_bounds__(kSideThreads) loss_finish_kernel(const FinishP
   {
     const int r = threadIdx.x % ROWS, first = threadIdx.x / ROWS;
     LogSum v = {-INFINITY, 0.0f};
-    for (int h = first; h < p.halves; h += kParts) {
+    for (int h = first; h < p.parts; h += kParts) {
       const size_t at = (size_t)h * p.rows + row_b + r;
       if (GRAD) {
         v.sum += ld_global(p.sums + at);
@@ -635,6 +598,7 @@ struct LossPlan {
   int chunks;
   int width, tiles, pieces, splits;      // width: entries of a tile
   int group, back_group;
+  bool few;                  // head_loss_few.cu
   // offsets into the workspace
   size_t count, again, index, label, ref, above, x, sums, e[2], grads, bytes;
   int piece_tile(int i) const { return (int)((long long)tiles * i / pieces); }
@@ -652,6 +616,7 @@ LossPlan plan_loss(int T, int V, int K, bool grad, int sms) {
   c.rows = (int)(all < most ? all : most);
   c.chunks = (int)((all + c.rows - 1) / c.rows);
   const int blocks = c.rows / kTile;
+  c.few = T <= kFewTokens;
   // 64 MB of exponentials a piece
   const long long wide = (64ll << 20) / (2ll * c.rows);
   c.pieces = grad ? (int)((V + wide - 1) / wide) : 1;
@@ -678,7 +643,19 @@ LossPlan plan_loss(int T, int V, int K, bool grad, int sms) {
   };
   c.group = group_of(K);
   c.back_group = group_of(c.piece_width());
-  if (grad) {
+  if (grad && c.few) {
+    // rounds of the pairs, each the stages of a part and eight stages' time for what does not grow with them, one more for each part
+    const long long features = (K + kTile - 1) / kTile, stages = (long long)c.piece_width() / kDepth;
+    const int least = c.tiles / c.pieces * c.width / kDepth;
+    long long best = 0;
+    for (int splits = 1; splits <= 16 && splits <= least; ++splits) {
+      const long long cost = (features * splits + pairs - 1) / pairs * (stages / splits + 8) + splits;
+      if (best == 0 || cost < best) {
+        best = cost;
+        c.splits = splits;
+      }
+    }
+  } else if (grad) {
     const int back = blocks * ((K + kTile - 1) / kTile);
     if (back < pairs) {
       c.splits = pairs / back;
@@ -701,7 +678,7 @@ LossPlan plan_loss(int T, int V, int K, bool grad, int sms) {
   c.ref = take(rows_all * 4);
   c.above = take(rows_all * 4);
   c.x = take(rows_all * K * 2);
-  c.sums = take((size_t)c.tiles * 2 * c.rows * (grad ? 4 : 8));
+  c.sums = take((size_t)c.tiles * (c.few ? kFewParts : 2) * c.rows * (grad ? 4 : 8));
   if (grad) {
     c.e[0] = take((size_t)c.rows * c.piece_width() * 2);
     c.e[1] = c.pieces > 1 ? take((size_t)c.rows * c.piece_width() * 2) : c.e[0];
@@ -709,23 +686,6 @@ LossPlan plan_loss(int T, int V, int K, bool grad, int sms) {
   }
   c.bytes = at;
   return c;
-}
-
-int loss_map(CUtensorMap* m, CUtensorMapDataType type, const void* base, uint64_t inner, uint64_t outer, int size, uint32_t box_x,
-             uint32_t box_y, CUtensorMapSwizzle swizzle, uint64_t pitch = 0) {
-  EncodeTiledFn enc = nullptr;
-  PEQA_TRY(tensor_map_encoder(&enc));
-  cuuint64_t dims[2] = {inner, outer};
-  cuuint64_t strides[1] = {pitch ? pitch : inner * size};
-  cuuint32_t box[2] = {box_x, box_y};
-  cuuint32_t estr[2] = {1, 1};
-  if (enc(m, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
-          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-    return cuda_fail(cudaErrorInvalidValue);
-  return PEQA_OK;
-}
-int bf16_map(CUtensorMap* m, const void* base, uint64_t inner, uint64_t outer, uint32_t box_y) {
-  return loss_map(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, inner, outer, 2, 64, box_y, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 template <bool GRAD>
@@ -838,7 +798,7 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
   FinishParams fp = {};
   fp.live = live;
   fp.sums = p.sums;
-  fp.halves = 2 * c.tiles;
+  fp.parts = (c.few ? kFewParts : 2) * c.tiles;
   fp.rows = c.rows;
   fp.grads = reinterpret_cast<const float*>(ws + c.grads);
   fp.splits = c.splits;
@@ -859,7 +819,12 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
         p.back0 = before * c.width;
         p.back_blocks = (entries + kDepth - 1) / kDepth;
         p.first_back = i == 1;
-        if (dX) {
+        if (c.few) {
+          const FewBuffers few = {gp.rows, W, reinterpret_cast<__nv_bfloat16*>(ws + c.e[i & 1]),
+                                  reinterpret_cast<const __nv_bfloat16*>(ws + c.e[(i & 1) ^ 1]), (int)width, entries,
+                                  reinterpret_cast<float*>(ws + c.grads), T};
+          PEQA_TRY(launch_few(p, few, dX != nullptr, pairs, st));
+        } else if (dX) {
           maps[3] = e_out[i & 1];
           // of the piece's own width: what its last stage has beyond that is read as zeros
           if (i > 0)

@@ -1,0 +1,91 @@
+// What the kernels of the vocabulary projection's loss share (head_loss.cu, and head_loss_few.cu for few tokens).
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+#include "sm100_ptx.cuh"
+#include "tensor_map.cuh"
+
+namespace peqa {
+namespace loss {
+
+using namespace ptx;
+
+constexpr int kTile = 256;                      // tokens, and vocabulary entries or features, of a tile
+constexpr int kDepth = 64;                      // contraction elements of a stage
+constexpr int kOperandBytes = 128 * kDepth * 2;     // this CTA's half of a stage's A or B
+constexpr int kLossThreads = 384;               // warps: 0 TMA, 1 MMA, 2 tensor memory, 4-11 epilogue
+constexpr float kFarAbove = 60.0f;              // exp(60) V |W| is far below binary32's largest number
+constexpr float kLog2e = 1.4426950408889634f;
+
+// What the kernel before leaves of the tokens that count, in their order.
+struct LiveTokens {
+  int* count;        // [1]
+  int* index;        // token
+  int* label;
+  float* ref;        // logit of the label
+  int* above;        // bits of the largest l - ref beyond kFarAbove, 0 if there is none
+};
+
+struct LossParams {
+  LiveTokens live;
+  int* again;            // the chunk's flag
+  bool second;           // the repetition
+  float* sums;           // [halves (few tokens: eighths) of tiles, rows]: s, or (without gradient) pairs of largest logit and sum relative to it
+  int row0, rows;        // first live token of the chunk, rows that its buffers have (a multiple of 256)
+  int V, K, k_blocks;    // stages of a tile of logits
+  int width;             // entries of a tile of the vocabulary, a multiple of 32
+  int tile0, tiles;      // tiles of the vocabulary in this launch's piece
+  int back0, back_blocks;    // first entry and stages of the piece before, whose gradient is summed; 0 stages: none
+  bool first_back;       // nothing has been summed yet
+  int splits;            // parts that the sum over a piece is cut into, each with sums of its own
+  int group, back_group; // blocks of 256 tokens whose tiles are worked through together
+  int* status;
+};
+
+int loss_map(CUtensorMap* m, CUtensorMapDataType type, const void* base, uint64_t inner, uint64_t outer, int size, uint32_t box_x,
+             uint32_t box_y, CUtensorMapSwizzle swizzle, uint64_t pitch = 0);
+inline int bf16_map(CUtensorMap* m, const void* base, uint64_t inner, uint64_t outer, uint32_t box_y, uint64_t pitch = 0) {
+  return loss_map(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, inner, outer, 2, 64, box_y, CU_TENSOR_MAP_SWIZZLE_128B, pitch);
+}
+
+// Few tokens (head_loss_few.cu): tokens at most, partial sums of a tile, its buffers.
+constexpr int kFewTokens = 256;
+constexpr int kFewParts = 8;
+struct FewBuffers {
+  const void* rows;            // live tokens' X, [256, K]
+  const void* W;
+  __nv_bfloat16* out;          // exponentials of this piece [256, pitch]
+  const __nv_bfloat16* in;     // and of the piece before
+  int pitch, in_entries;
+  float* grads;                // [splits, 256, K]
+  int tokens;                  // T
+};
+int launch_few(const LossParams& p, const FewBuffers& b, bool grad, int pairs, cudaStream_t st);
+
+#ifdef __CUDACC__
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&b);
+}
+__device__ __forceinline__ void tma_add_2d(const CUtensorMap* m, uint32_t src_smem, int x, int y) {
+  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3}], [%1];"
+               ::"l"(reinterpret_cast<uint64_t>(m)), "r"(src_smem), "r"(x), "r"(y)
+               : "memory");
+}
+__device__ __forceinline__ void wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_kernel_behind_in() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// Reference of a live token: the label's logit, or in the repetition the row's largest if that is far above.
+__device__ __forceinline__ float above_of(const LiveTokens& live, int row) { return __int_as_float(ld_global(live.above + row)); }
+#endif
+
+}  // namespace loss
+}  // namespace peqa
