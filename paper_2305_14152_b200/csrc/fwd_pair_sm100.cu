@@ -88,6 +88,8 @@ struct PairParams {
   int* status;
 };
 
+static_assert(sizeof(PairBarriers) <= 512, "the scales lie behind the barriers");
+
 __device__ __forceinline__ int pair_group_of(const PairParams& p, int col) {
   if (p.G == 1) return 0;
   return p.g_shift >= 0 ? (col >> p.g_shift) : (col / p.g);
@@ -112,6 +114,7 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
   uint8_t* sm_q = base + PSTAGES * PSTAGE_BYTES;          // PQ_SLOTS x 4 KiB, plain 32-byte rows
   uint8_t* sm_e = sm_q + PQ_SLOTS * PQ_BYTES;             // 8 epilogue warps x 2 KiB, 64-byte swizzle
   PairBarriers* bars = reinterpret_cast<PairBarriers*>(sm_e + 8 * PE_BYTES);
+  float* sm_scales = reinterpret_cast<float*>(sm_e + 8 * PE_BYTES + 512);     // GLU with one scale per channel: the tile's 256
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const bool leader = rank == 0;
@@ -266,6 +269,90 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
       pair_item(p.items, tile, p.T, n_tile, tt0, blocks);
       const int n0 = n_tile * 256;
       const int row0 = tt0 + m * 256 + (int)rank * 128 + quarter * 32;   // first token of this warp
+      if constexpr (GLU) {
+        // Sixteen columns at a time, eight channels' gate and up sums, the next sixteen on their way from tensor memory meanwhile.  Scales come
+        // from shared memory, four a read that all lanes share.  (All warps of a CTA come by here as often, whether or not a wait runs out: a tile's
+        // accumulators are full for all or for none.)
+        if (!FOLD) {
+          const int c = (warp - 4) * 32 + lane;
+          named_barrier_sync(2, 256);              // the last tile's have been read
+          sm_scales[c] = n0 + c < p.N ? ld_global(p.scales + n0 + c) : 0.0f;
+          named_barrier_sync(2, 256);
+        }
+        if (!warp_wait_cluster(smem_u32(&bars->acc_full), (uint32_t)(local & 1), abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const int units = m < blocks ? min(16, (p.N - n0) / 16) : 0;
+        const uint32_t acc = tmem_base + ((uint32_t)(quarter * 32) << 16) + m * 256;
+        const bool live = row0 + lane < p.T;
+        __nv_bfloat16* h_row = p.H + (size_t)(row0 + lane) * (p.N >> 1) + (n0 >> 1);
+        uint32_t v[16], next[16], o[8];
+        if (units > 0) tmem_ld_32x16(acc, v);
+#pragma unroll 1
+        for (int u = 0; u < units; u += 2) {
+#pragma unroll
+          for (int side = 0; side < 2; ++side) {
+            const int at = u + side;
+            if (at < units) {
+              uint32_t (&here)[16] = side == 0 ? v : next;
+              uint32_t (&after)[16] = side == 0 ? next : v;
+              tmem_ld_wait(here);
+              if (at + 1 < units) {
+                tmem_ld_32x16(acc + (at + 1) * 16, after);
+              } else {
+                // nothing of this tile is left in tensor memory for this warp
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(acc_empty_leader);
+              }
+              float y[16];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float4 sc = FOLD ? make_float4(1.0f, 1.0f, 1.0f, 1.0f) : *reinterpret_cast<const float4*>(sm_scales + at * 16 + 4 * e);
+                const float s4[4] = {sc.x, sc.y, sc.z, sc.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) y[4 * e + k] = FOLD ? __uint_as_float(here[4 * e + k]) : __uint_as_float(here[4 * e + k]) * s4[k];
+              }
+              if (p.glu.act == PEQA_ACT_SILU) glu_pack<PEQA_ACT_SILU>(y, o + 4 * side);
+              else glu_pack<PEQA_ACT_GELU_TANH>(y, o + 4 * side);
+              if (p.out) {
+                if (side == 0) {
+                  if (lane == 0) bulk_wait_group_read0();
+                  __syncwarp();
+                }
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                  *reinterpret_cast<uint4*>(srow + (((side * 2 + q) ^ sw) << 4)) =
+                      make_uint4(bf16_pair(y[8 * q], y[8 * q + 1]), bf16_pair(y[8 * q + 2], y[8 * q + 3]),
+                                 bf16_pair(y[8 * q + 4], y[8 * q + 5]), bf16_pair(y[8 * q + 6], y[8 * q + 7]));
+              }
+            }
+          }
+          if (p.out) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0 && row0 < p.T) {
+              tma_store_2d(&tmap_y, smem_u32(stage), n0 + u * 16, row0);
+              bulk_commit_group();
+            }
+          }
+          if (live) {
+            __nv_bfloat16* to = h_row + u * 8;
+            if (p.glu.wide) {
+              asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(o[0]), "r"(o[1]), "r"(o[2]),
+                           "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
+            } else {
+              *reinterpret_cast<uint4*>(to) = make_uint4(o[0], o[1], o[2], o[3]);
+              if (u + 1 < units) *reinterpret_cast<uint4*>(to + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+            }
+          }
+        }
+        if (units <= 0) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(acc_empty_leader);
+        }
+        continue;
+      }
       const __nv_bfloat16* dy_row = p.dY + (size_t)(row0 + lane) * p.N + n0;
       float ds_sum[8];
       if (DS) {
@@ -321,31 +408,6 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
             const float u = __uint_as_float(v[j]);
             return FOLD ? u : u * __shfl_sync(0xffffffffu, scale, h * W + j);
           };
-          if constexpr (GLU) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(scaled(j));
-            uint32_t o[8];
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-              const int j = (q >> 2) * 16 + (q & 3) * 2;      // gate of channels 2q and 2q + 1, their up sums eight further
-              const __nv_bfloat162 b =
-                  __floats2bfloat162_rn(glu_value(__uint_as_float(v[j]), __uint_as_float(v[j + 8]), p.glu.act),
-                                        glu_value(__uint_as_float(v[j + 1]), __uint_as_float(v[j + 9]), p.glu.act));
-              o[q] = *reinterpret_cast<const uint32_t*>(&b);
-            }
-            if (row0 + lane < p.T) {
-              __nv_bfloat16* at = p.H + (size_t)(row0 + lane) * (p.N >> 1) + (c0 >> 1);
-              if (p.glu.wide) {
-                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(o[0]), "r"(o[1]), "r"(o[2]),
-                             "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
-              } else {
-                *reinterpret_cast<uint4*>(at) = make_uint4(o[0], o[1], o[2], o[3]);
-                if (c0 + 16 < p.N) *reinterpret_cast<uint4*>(at + 8) = make_uint4(o[4], o[5], o[6], o[7]);
-              }
-            }
-            if (!p.out) continue;
-          }
-          auto output = [&](int j) { return GLU ? __uint_as_float(v[j]) : scaled(j); };
           // the previous store must have finished reading the staging tile
           if (h == 0) {
             if (lane == 0) bulk_wait_group_read0();
@@ -355,10 +417,10 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
           for (int q = 0; q < W / 8; ++q) {
             uint4 o;
             __nv_bfloat162 b;
-            b = __floats2bfloat162_rn(output(8 * q + 0), output(8 * q + 1)); o.x = *reinterpret_cast<uint32_t*>(&b);
-            b = __floats2bfloat162_rn(output(8 * q + 2), output(8 * q + 3)); o.y = *reinterpret_cast<uint32_t*>(&b);
-            b = __floats2bfloat162_rn(output(8 * q + 4), output(8 * q + 5)); o.z = *reinterpret_cast<uint32_t*>(&b);
-            b = __floats2bfloat162_rn(output(8 * q + 6), output(8 * q + 7)); o.w = *reinterpret_cast<uint32_t*>(&b);
+            b = __floats2bfloat162_rn(scaled(8 * q + 0), scaled(8 * q + 1)); o.x = *reinterpret_cast<uint32_t*>(&b);
+            b = __floats2bfloat162_rn(scaled(8 * q + 2), scaled(8 * q + 3)); o.y = *reinterpret_cast<uint32_t*>(&b);
+            b = __floats2bfloat162_rn(scaled(8 * q + 4), scaled(8 * q + 5)); o.z = *reinterpret_cast<uint32_t*>(&b);
+            b = __floats2bfloat162_rn(scaled(8 * q + 6), scaled(8 * q + 7)); o.w = *reinterpret_cast<uint32_t*>(&b);
             *reinterpret_cast<uint4*>(srow + (((h * (W / 8) + q) ^ sw) << 4)) = o;
           }
           if constexpr (DS) {
@@ -386,7 +448,6 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
             half_sum[h] = __uint_as_float(v[0]) + __shfl_xor_sync(0xffffffffu, __uint_as_float(v[0]), 16);
           }
         }
-        if (GLU && !p.out) continue;
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0 && row0 < p.T) {
@@ -565,11 +626,12 @@ int launch_pair_t(const CUtensorMap& tx, const CUtensorMap& tq, const CUtensorMa
                   int pairs, cudaStream_t st) {
   auto kern = qfwd_pair_kernel<BITS, FOLD, ZF, DS, GLU>;
   static std::atomic<uint64_t> done{0};
-  PEQA_TRY(allow_smem(kern, P_SMEM_BYTES, done));
+  constexpr int kSmem = P_SMEM_BYTES + (GLU && !FOLD ? 1024 : 0);
+  PEQA_TRY(allow_smem(kern, kSmem, done));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * pairs, 1, 1);
   cfg.blockDim = dim3(kPairThreads, 1, 1);
-  cfg.dynamicSmemBytes = P_SMEM_BYTES;
+  cfg.dynamicSmemBytes = kSmem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;

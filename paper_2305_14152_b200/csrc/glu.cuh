@@ -20,11 +20,27 @@ inline bool glu_act_ok(int act) { return act == PEQA_ACT_SILU || act == PEQA_ACT
 
 #ifdef __CUDACC__
 // Both activations are x p(v) with p the logistic function: v = x, or 2 sqrt(2/pi) (x + 0.044715 x^3), since (1 + tanh(u)) / 2 =
-// p(2u).  Exponential and reciprocal are the approximate ones (2^-21 of p for |v| up to 88), far below bf16's step.
+// p(2u).  Exponential and reciprocal are the approximate ones (good to 2^-18 of p for |v| up to 88), far below bf16's step.
 constexpr float kGeluInner = 1.5957691216057308f, kGeluCubic = 0.044715f;
+template <int ACT>
+__device__ __forceinline__ float glu_value(float x, float up) {
+  const float v = ACT == PEQA_ACT_SILU ? x : kGeluInner * fmaf(kGeluCubic * x * x, x, x);
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + __expf(-v)));      // 0 where the exponential is too large
+  return x * r * up;
+}
 __device__ __forceinline__ float glu_value(float x, float up, int act) {
-  const float v = act == PEQA_ACT_SILU ? x : kGeluInner * fmaf(kGeluCubic * x * x, x, x);
-  return __fdividef(x, 1.0f + __expf(-v)) * up;
+  return act == PEQA_ACT_SILU ? glu_value<PEQA_ACT_SILU>(x, up) : glu_value<PEQA_ACT_GELU_TANH>(x, up);
+}
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&b);
+}
+// Eight channels: their gate sums, then their up sums, in y.
+template <int ACT>
+__device__ __forceinline__ void glu_pack(const float (&y)[16], uint32_t* o) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) o[q] = bf16_pair(glu_value<ACT>(y[2 * q], y[2 * q + 8]), glu_value<ACT>(y[2 * q + 1], y[2 * q + 9]));
 }
 #endif
 

@@ -521,9 +521,31 @@ __global__ void __launch_bounds__(kSideThreads) loss_finish_kernel(const FinishP
   __shared__ LogSum part[kParts][ROWS];
   const int row_b = blockIdx.x * ROWS, live = min(p.rows, ld_global(p.live.count) - p.row0);
   if (row_b >= live) return;
+  // everything that the sums are not needed for is asked for before them
+  const int mine = threadIdx.x / kSpan, at_thread = threadIdx.x % kSpan, lane = threadIdx.x & 31, row = min(row_b + mine, live - 1);
+  const int token = ld_global(p.live.index + p.row0 + row), label = ld_global(p.live.label + p.row0 + row);
+  const float ref = GRAD ? above_of(p.live, p.row0 + row) : ld_global(p.live.ref + p.row0 + row);
+  const float weight = GRAD && p.weight ? ld_global(p.weight + token) : 1.0f;
+  const __nv_bfloat16* w = p.W + (size_t)label * p.K;
+  const float* g = p.grads + (size_t)row * p.K;
+  const size_t per_split = (size_t)p.rows * p.K;
+  struct Eight {
+    float v[8];       // the first part's sums
+    uint4 w;          // the label's row of the head
+  };
+  auto load = [&](int c) {
+    Eight e = {};
+    if (GRAD && c < p.K) {
+      const float4 a = ld_global(reinterpret_cast<const float4*>(g + c)), b = ld_global(reinterpret_cast<const float4*>(g + c + 4));
+      e = {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, ld_global(reinterpret_cast<const uint4*>(w + c))};
+    }
+    return e;
+  };
+  Eight now = load(at_thread * 8);
   {
     const int r = threadIdx.x % ROWS, first = threadIdx.x / ROWS;
     LogSum v = {-INFINITY, 0.0f};
+#pragma unroll 4
     for (int h = first; h < p.parts; h += kParts) {
       const size_t at = (size_t)h * p.rows + row_b + r;
       if (GRAD) {
@@ -536,8 +558,7 @@ __global__ void __launch_bounds__(kSideThreads) loss_finish_kernel(const FinishP
     part[first][r] = v;
   }
   __syncthreads();
-  const int mine = threadIdx.x / kSpan, at_thread = threadIdx.x % kSpan, lane = threadIdx.x & 31, row = row_b + mine;
-  if (row >= live) return;
+  if (row_b + mine >= live) return;
   LogSum v = {-INFINITY, 0.0f};
 #pragma unroll
   for (int h = 0; h < kParts; h += 32) {
@@ -552,10 +573,8 @@ __global__ void __launch_bounds__(kSideThreads) loss_finish_kernel(const FinishP
     else v = join_sums(v, u);
   }
   const float sum = v.sum;
-
-  const int token = ld_global(p.live.index + p.row0 + row);
   // the reference above the label's logit, and the label's term
-  const float above = GRAD ? above_of(p.live, p.row0 + row) : v.most - ld_global(p.live.ref + p.row0 + row);
+  const float above = GRAD ? ref : v.most - ref;
   const float own = expf(-above);
   if (at_thread == 0) {
     float loss;
@@ -564,30 +583,26 @@ __global__ void __launch_bounds__(kSideThreads) loss_finish_kernel(const FinishP
     p.loss[token] = loss;
   }
   if (!GRAD) return;
-  const float by = (p.weight ? ld_global(p.weight + token) : 1.0f) / (sum + own);
-  const __nv_bfloat16* w = p.W + (size_t)ld_global(p.live.label + p.row0 + row) * p.K;
-  const float* g = p.grads + (size_t)row * p.K;
-  const size_t per_split = (size_t)p.rows * p.K;
+  const float by = weight / (sum + own);
   __nv_bfloat16* out = p.dX + (size_t)token * p.K;
-#pragma unroll 2
+#pragma unroll 1
   for (int c = at_thread * 8; c < p.K; c += kSpan * 8) {
-    float4 lo = ld_global(reinterpret_cast<const float4*>(g + c)), hi = ld_global(reinterpret_cast<const float4*>(g + c + 4));
-    const uint4 b = ld_global(reinterpret_cast<const uint4*>(w + c));
+    const Eight next = load(c + kSpan * 8);
 #pragma unroll 4
     for (int s = 1; s < p.splits; ++s) {
       const float4 a = ld_global(reinterpret_cast<const float4*>(g + s * per_split + c));
-      const float4 d = ld_global(reinterpret_cast<const float4*>(g + s * per_split + c + 4));
-      lo.x += a.x; lo.y += a.y; lo.z += a.z; lo.w += a.w;
-      hi.x += d.x; hi.y += d.y; hi.z += d.z; hi.w += d.w;
+      const float4 b = ld_global(reinterpret_cast<const float4*>(g + s * per_split + c + 4));
+      now.v[0] += a.x; now.v[1] += a.y; now.v[2] += a.z; now.v[3] += a.w;
+      now.v[4] += b.x; now.v[5] += b.y; now.v[6] += b.z; now.v[7] += b.w;
     }
-    const float v8[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-    const uint32_t y[4] = {b.x, b.y, b.z, b.w};
+    const uint32_t y[4] = {now.w.x, now.w.y, now.w.z, now.w.w};
     uint32_t o[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      o[e] = bf16_pair(fmaf(-sum, __uint_as_float(y[e] << 16), v8[2 * e]) * by,
-                       fmaf(-sum, __uint_as_float(y[e] & 0xFFFF0000u), v8[2 * e + 1]) * by);
+      o[e] = bf16_pair(fmaf(-sum, __uint_as_float(y[e] << 16), now.v[2 * e]) * by,
+                       fmaf(-sum, __uint_as_float(y[e] & 0xFFFF0000u), now.v[2 * e + 1]) * by);
     *reinterpret_cast<uint4*>(out + c) = make_uint4(o[0], o[1], o[2], o[3]);
+    now = next;
   }
 }
 
@@ -764,11 +779,21 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
   p.status = status;
   const uint64_t width = c.piece_width();
   CUtensorMap maps[6], e_out[2];
-  PEQA_TRY(bf16_map(&maps[0], ws + c.x, K, (uint64_t)c.chunks * c.rows, 128));
-  PEQA_TRY(bf16_map(&maps[1], W, K, V, c.width / 2));
-  PEQA_TRY(bf16_map(&maps[2], W, K, V, 64));
-  maps[3] = maps[4] = maps[5] = maps[0];
-  if (dX) {
+  if (!c.few) {
+    PEQA_TRY(bf16_map(&maps[0], ws + c.x, K, (uint64_t)c.chunks * c.rows, 128));
+    PEQA_TRY(bf16_map(&maps[1], W, K, V, c.width / 2));
+    PEQA_TRY(bf16_map(&maps[2], W, K, V, 64));
+    maps[3] = maps[4] = maps[5] = maps[0];
+  }
+  FewCall few = {};
+  if (c.few) {
+    few.grads = reinterpret_cast<float*>(ws + c.grads);
+    few.pitch = (int)width;
+    few.tokens = T;
+    for (int b = 0; b < 2; ++b) few.e[b] = ws + c.e[b];
+    PEQA_TRY(few_maps(few, ws + c.x, W, c.width, V, K, dX != nullptr));
+  }
+  if (dX && !c.few) {
     for (int b = 0; b < 2; ++b) {
       PEQA_TRY(loss_map(&e_out[b], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, ws + c.e[b], width, c.rows, 2, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B));
     }
@@ -791,9 +816,9 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
   gp.dX = static_cast<__nv_bfloat16*>(dX);
   gp.status = status;
   // one token a CTA while that fills no more than two rounds of the SMs
-  const bool few = T <= 2 * 8 * sms;
-  PEQA_TRY(few ? launch_after(loss_gather_kernel<1>, T, kSideThreads, st, gp)
-               : launch_after(loss_gather_kernel<8>, (T + 7) / 8, kSideThreads, st, gp));
+  const bool alone = T <= 2 * 8 * sms;
+  PEQA_TRY(alone ? launch_after(loss_gather_kernel<1>, T, kSideThreads, st, gp)
+                 : launch_after(loss_gather_kernel<8>, (T + 7) / 8, kSideThreads, st, gp));
 
   FinishParams fp = {};
   fp.live = live;
@@ -820,10 +845,7 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
         p.back_blocks = (entries + kDepth - 1) / kDepth;
         p.first_back = i == 1;
         if (c.few) {
-          const FewBuffers few = {gp.rows, W, reinterpret_cast<__nv_bfloat16*>(ws + c.e[i & 1]),
-                                  reinterpret_cast<const __nv_bfloat16*>(ws + c.e[(i & 1) ^ 1]), (int)width, entries,
-                                  reinterpret_cast<float*>(ws + c.grads), T};
-          PEQA_TRY(launch_few(p, few, dX != nullptr, pairs, st));
+          PEQA_TRY(launch_few(p, few, i & 1, entries, dX != nullptr, pairs, st));
         } else if (dX) {
           maps[3] = e_out[i & 1];
           // of the piece's own width: what its last stage has beyond that is read as zeros
@@ -837,7 +859,7 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
       }
     }
     const int rows = c.rows < T ? c.rows : T;
-    if (few) PEQA_TRY(launch_after(dX ? loss_finish_kernel<true, 1> : loss_finish_kernel<false, 1>, rows, kSideThreads, st, fp));
+    if (alone) PEQA_TRY(launch_after(dX ? loss_finish_kernel<true, 1> : loss_finish_kernel<false, 1>, rows, kSideThreads, st, fp));
     else PEQA_TRY(launch_after(dX ? loss_finish_kernel<true, 8> : loss_finish_kernel<false, 8>, (rows + 7) / 8, kSideThreads, st, fp));
   }
   return PEQA_OK;

@@ -54,16 +54,15 @@ inline int bf16_map(CUtensorMap* m, const void* base, uint64_t inner, uint64_t o
 // Few tokens (head_loss_few.cu): tokens at most, partial sums of a tile, its buffers.
 constexpr int kFewTokens = 256;
 constexpr int kFewParts = 8;
-struct FewBuffers {
-  const void* rows;            // live tokens' X, [256, K]
-  const void* W;
-  __nv_bfloat16* out;          // exponentials of this piece [256, pitch]
-  const __nv_bfloat16* in;     // and of the piece before
-  int pitch, in_entries;
+struct FewCall {
   float* grads;                // [splits, 256, K]
-  int tokens;                  // T
+  void* e[2];                  // exponentials of a piece [256, pitch]; by turns, if there are several
+  int pitch, tokens;
+  CUtensorMap w, x, wt, e_out[2];
 };
-int launch_few(const LossParams& p, const FewBuffers& b, bool grad, int pairs, cudaStream_t st);
+int few_maps(FewCall& call, const void* rows, const void* W, int width, int V, int K, bool grad);
+// turn: which of e this piece's exponentials go to; in_entries: of the piece before, in the other
+int launch_few(const LossParams& p, const FewCall& call, int turn, int in_entries, bool grad, int pairs, cudaStream_t st);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ float exp2_approx(float x) {

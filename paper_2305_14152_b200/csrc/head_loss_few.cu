@@ -29,13 +29,12 @@ struct FewBarriers {
   float ref[kFewTokens];
   int label[kFewTokens];         // -1 where there is no token
 };
-constexpr int kFewSmemFixed = 1024 + (int)((sizeof(FewBarriers) + 127) / 128 * 128);
+constexpr int kFewStaging = 2048;        // of an epilogue warp: 32 tokens x 16 entries, twice
+constexpr int kFewSmemFixed = 1024 + 8 * kFewStaging + (int)((sizeof(FewBarriers) + 127) / 128 * 128);
 
 struct FewParams {
   LossParams p;
-  __nv_bfloat16* out;            // exponentials [256, pitch]
   float* grads;                  // [splits, 256, K]
-  int pitch;
   int nt;                        // columns: tokens, a multiple of 16
   int stages, stage_bytes;
 };
@@ -43,7 +42,7 @@ struct FewParams {
 // Items of a launch: the gradient's, then logits, dealt out in turns.
 struct FewItem {
   bool grad;
-  int col, kb0, kbs, split;
+  int col, kbs, split;
 };
 struct FewWalk {
   int n1, n2, features;
@@ -59,12 +58,10 @@ struct FewWalk {
     if (it.grad) {
       it.split = e / features;
       it.col = e - it.split * features;
-      it.kb0 = (int)((long long)it.split * p.back_blocks / p.splits);
-      it.kbs = (int)((long long)(it.split + 1) * p.back_blocks / p.splits) - it.kb0;
+      it.kbs = (p.back_blocks - it.split + p.splits - 1) / p.splits;
     } else {
       it.split = 0;
       it.col = e - n2;
-      it.kb0 = 0;
       it.kbs = p.k_blocks;
     }
     return true;
@@ -89,7 +86,8 @@ __device__ __forceinline__ float fold32(float (&v)[32], int lane, F&& join) {
 template <bool GRAD>
 __global__ void __launch_bounds__(kLossThreads, 1)
 head_loss_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
-                     const __grid_constant__ CUtensorMap tmap_wt, const __grid_constant__ CUtensorMap tmap_e, const FewParams q) {
+                     const __grid_constant__ CUtensorMap tmap_wt, const __grid_constant__ CUtensorMap tmap_e,
+                     const __grid_constant__ CUtensorMap tmap_e_out, const FewParams q) {
   const LossParams& p = q.p;
   if (GRAD && p.second) {
     wait_for_kernel_before();
@@ -100,7 +98,8 @@ head_loss_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
   }
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  FewBarriers* bars = reinterpret_cast<FewBarriers*>(base + q.stages * q.stage_bytes);
+  uint8_t* staging = base + q.stages * q.stage_bytes;
+  FewBarriers* bars = reinterpret_cast<FewBarriers*>(staging + 8 * kFewStaging);
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const bool leader = rank == 0;
@@ -123,6 +122,7 @@ head_loss_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
     if (GRAD) {
       prefetch_tmap(&tmap_wt);
       prefetch_tmap(&tmap_e);
+      prefetch_tmap(&tmap_e_out);
     }
   }
   if (warp == 2) {
@@ -156,7 +156,8 @@ head_loss_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
           if (!mbar_wait_cluster(smem_u32(&bars->empty[s]), ph ^ 1u, abort_flag)) { ok = false; break; }
           if (leader) mbar_arrive_expect_tx(smem_u32(&bars->full[s]), bytes);
           const uint32_t bar = mapa_shared(smem_u32(&bars->full[s]), 0), a = smem_u32(base + s * q.stage_bytes);
-          const int k = (item.kb0 + kb) * kDepth;
+          // All parts of the gradient's sum go through the piece together, from its end: what the logits were made of last is still in L2.
+          const int k = (item.grad ? p.back_blocks - 1 - item.split - kb * p.splits : kb) * kDepth;
           if (!item.grad) {
             tma_load_2d_pair(a, &tmap_w, bar, k, (p.tile0 + item.col) * p.width + (int)rank * half_entries);
             tma_load_2d_pair(a + kOperandBytes, &tmap_x, bar, k, (int)rank * half_tokens);
@@ -283,11 +284,21 @@ head_loss_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
                 }
               }
             }
-            if (mine) {
-              __nv_bfloat16* at = q.out + (size_t)t0 * q.pitch + in_piece;
+            // [token][entry] in two boxes of 16 entries, which a CTA's share of a tile is a multiple of
+            if (lane == 0) bulk_wait_group_read0();
+            __syncwarp();
+            uint8_t* at = staging + (warp - 4) * kFewStaging + (lane >> 4) * 1024 + (lane & 15) * 2;
 #pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (t0 + j < live) at[(size_t)j * q.pitch] = __float2bfloat16_rn(v[j]);
+            for (int j = 0; j < 32; ++j) *reinterpret_cast<__nv_bfloat16*>(at + j * 32) = __float2bfloat16_rn(v[j]);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              const int first = in_piece;                     // of the warp's entries
+#pragma unroll
+              for (int b = 0; b < 2; ++b)
+                if (t0 < live && quarter * 32 + b * 16 < half_entries)
+                  tma_store_2d(&tmap_e_out, smem_u32(staging + (warp - 4) * kFewStaging + b * 1024), first + b * 16, t0);
+              bulk_commit_group();
             }
             p.sums[slot] = fold32(v, lane, [](float a, float b) { return a + b; });
           }
@@ -309,6 +320,7 @@ head_loss_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
         if (lane == 0) mbar_arrive_cluster(acc_empty);
       }
     }
+    if (GRAD && lane == 0) bulk_wait_group0();
   }
 
   if (*abort_flag) {
@@ -329,7 +341,8 @@ head_loss_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
 }
 
 template <bool GRAD>
-int launch_few_t(const CUtensorMap (&m)[4], const FewParams& q, int pairs, size_t smem, cudaStream_t st) {
+int launch_few_t(const CUtensorMap& w, const CUtensorMap& x, const CUtensorMap& wt, const CUtensorMap& e_in, const CUtensorMap& e_out,
+                 const FewParams& q, int pairs, size_t smem, cudaStream_t st) {
   auto kern = head_loss_few_kernel<GRAD>;
   static std::atomic<uint64_t> done{0};
   PEQA_TRY(allow_smem(kern, kFewSmemLimit, done));
@@ -347,33 +360,37 @@ int launch_few_t(const CUtensorMap (&m)[4], const FewParams& q, int pairs, size_
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  PEQA_CUDA(cudaLaunchKernelEx(&cfg, kern, m[0], m[1], m[2], m[3], q));
+  PEQA_CUDA(cudaLaunchKernelEx(&cfg, kern, w, x, wt, e_in, e_out, q));
   return PEQA_OK;
 }
 
 }  // namespace
 
-int loss::launch_few(const LossParams& p, const FewBuffers& b, bool grad, int pairs, cudaStream_t st) {
+int loss::few_maps(FewCall& call, const void* rows, const void* W, int width, int V, int K, bool grad) {
+  const uint32_t half_tokens = ((call.tokens + 15) & ~15) / 2;
+  PEQA_TRY(bf16_map(&call.w, W, K, V, width / 2));
+  PEQA_TRY(bf16_map(&call.x, rows, K, kFewTokens, half_tokens));
+  if (!grad) return PEQA_OK;
+  PEQA_TRY(bf16_map(&call.wt, W, K, V, 64));
+  for (int b = 0; b < (call.e[0] == call.e[1] ? 1 : 2); ++b)
+    PEQA_TRY(loss_map(&call.e_out[b], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, call.e[b], call.pitch, kFewTokens, 2, 16, 32, CU_TENSOR_MAP_SWIZZLE_NONE));
+  return PEQA_OK;
+}
+
+int loss::launch_few(const LossParams& p, const FewCall& call, int turn, int in_entries, bool grad, int pairs, cudaStream_t st) {
   FewParams q;
   q.p = p;
-  q.out = b.out;
-  q.grads = b.grads;
-  q.pitch = b.pitch;
-  q.nt = (b.tokens + 15) & ~15;
+  q.grads = call.grads;
+  q.nt = (call.tokens + 15) & ~15;
   q.stage_bytes = kOperandBytes + q.nt / 2 * (kDepth * 2);
   q.stages = (kFewSmemLimit - kFewSmemFixed) / q.stage_bytes;
   if (q.stages > kMaxStages) q.stages = kMaxStages;
-  CUtensorMap m[4];
-  PEQA_TRY(bf16_map(&m[0], b.W, p.K, p.V, p.width / 2));
-  PEQA_TRY(bf16_map(&m[1], b.rows, p.K, kFewTokens, q.nt / 2));
-  m[2] = m[3] = m[0];
-  if (grad) {
-    PEQA_TRY(bf16_map(&m[2], b.W, p.K, p.V, 64));
-    // of the piece's own width: what its last stage has beyond that is read as zeros
-    if (b.in_entries > 0) PEQA_TRY(bf16_map(&m[3], b.in, b.in_entries, kFewTokens, q.nt / 2, (uint64_t)b.pitch * 2));
-  }
   const size_t smem = (size_t)q.stages * q.stage_bytes + kFewSmemFixed;
-  return grad ? launch_few_t<true>(m, q, pairs, smem, st) : launch_few_t<false>(m, q, pairs, smem, st);
+  if (!grad) return launch_few_t<false>(call.w, call.x, call.w, call.w, call.w, q, pairs, smem, st);
+  CUtensorMap e_in = call.w;
+  // of the piece's own width: what its last stage has beyond that is read as zeros
+  if (in_entries > 0) PEQA_TRY(bf16_map(&e_in, call.e[turn ^ 1], in_entries, kFewTokens, q.nt / 2, (uint64_t)call.pitch * 2));
+  return launch_few_t<true>(call.w, call.x, call.wt, e_in, call.e_out[call.e[0] == call.e[1] ? 0 : turn], q, pairs, smem, st);
 }
 
 }  // namespace peqa
