@@ -270,8 +270,8 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
       const int n0 = n_tile * 256;
       const int row0 = tt0 + m * 256 + (int)rank * 128 + quarter * 32;   // first token of this warp
       if constexpr (GLU) {
-        // Sixteen columns at a time, eight channels' gate and up sums, the next sixteen on their way from tensor memory meanwhile.  Scales come
-        // from shared memory, four a read that all lanes share.  (All warps of a CTA come by here as often, whether or not a wait runs out: a tile's
+        // Sixteen columns at a time, eight channels' gate and up sums.  (The next sixteen asked for meanwhile took registers that the dequant warps'
+        // code went without: 1024 columns, us, so / as it is 175.6 / 169.3.)  Scales come from shared memory, four a read that all lanes share.  (All warps of a CTA come by here as often, whether or not a wait runs out: a tile's
         // accumulators are full for all or for none.)
         if (!FOLD) {
           const int c = (warp - 4) * 32 + lane;
@@ -285,20 +285,16 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
         const uint32_t acc = tmem_base + ((uint32_t)(quarter * 32) << 16) + m * 256;
         const bool live = row0 + lane < p.T;
         __nv_bfloat16* h_row = p.H + (size_t)(row0 + lane) * (p.N >> 1) + (n0 >> 1);
-        uint32_t v[16], next[16], o[8];
-        if (units > 0) tmem_ld_32x16(acc, v);
+        uint32_t v[16], o[8];
 #pragma unroll 1
         for (int u = 0; u < units; u += 2) {
 #pragma unroll
           for (int side = 0; side < 2; ++side) {
             const int at = u + side;
             if (at < units) {
-              uint32_t (&here)[16] = side == 0 ? v : next;
-              uint32_t (&after)[16] = side == 0 ? next : v;
-              tmem_ld_wait(here);
-              if (at + 1 < units) {
-                tmem_ld_32x16(acc + (at + 1) * 16, after);
-              } else {
+              tmem_ld_32x16(acc + at * 16, v);
+              tmem_ld_wait();
+              if (at + 1 == units) {
                 // nothing of this tile is left in tensor memory for this warp
                 tc_fence_before();
                 __syncwarp();
@@ -310,7 +306,7 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
                 const float4 sc = FOLD ? make_float4(1.0f, 1.0f, 1.0f, 1.0f) : *reinterpret_cast<const float4*>(sm_scales + at * 16 + 4 * e);
                 const float s4[4] = {sc.x, sc.y, sc.z, sc.w};
 #pragma unroll
-                for (int k = 0; k < 4; ++k) y[4 * e + k] = FOLD ? __uint_as_float(here[4 * e + k]) : __uint_as_float(here[4 * e + k]) * s4[k];
+                for (int k = 0; k < 4; ++k) y[4 * e + k] = FOLD ? __uint_as_float(v[4 * e + k]) : __uint_as_float(v[4 * e + k]) * s4[k];
               }
               if (p.glu.act == PEQA_ACT_SILU) glu_pack<PEQA_ACT_SILU>(y, o + 4 * side);
               else glu_pack<PEQA_ACT_GELU_TANH>(y, o + 4 * side);

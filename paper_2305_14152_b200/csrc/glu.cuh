@@ -22,12 +22,19 @@ inline bool glu_act_ok(int act) { return act == PEQA_ACT_SILU || act == PEQA_ACT
 // Both activations are x p(v) with p the logistic function: v = x, or 2 sqrt(2/pi) (x + 0.044715 x^3), since (1 + tanh(u)) / 2 =
 // p(2u).  Exponential and reciprocal are the approximate ones (good to 2^-18 of p for |v| up to 88), far below bf16's step.
 constexpr float kGeluInner = 1.5957691216057308f, kGeluCubic = 0.044715f;
+__device__ __forceinline__ float rcp_approx(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// v of x
+template <int ACT>
+__device__ __forceinline__ float glu_inner(float x) {
+  return ACT == PEQA_ACT_SILU ? x : kGeluInner * fmaf(kGeluCubic * x * x, x, x);
+}
 template <int ACT>
 __device__ __forceinline__ float glu_value(float x, float up) {
-  const float v = ACT == PEQA_ACT_SILU ? x : kGeluInner * fmaf(kGeluCubic * x * x, x, x);
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + __expf(-v)));      // 0 where the exponential is too large
-  return x * r * up;
+  return x * rcp_approx(1.0f + __expf(-glu_inner<ACT>(x))) * up;      // (0 where the exponential is too large)
 }
 __device__ __forceinline__ float glu_value(float x, float up, int act) {
   return act == PEQA_ACT_SILU ? glu_value<PEQA_ACT_SILU>(x, up) : glu_value<PEQA_ACT_GELU_TANH>(x, up);
@@ -36,7 +43,8 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&b);
 }
-// Eight channels: their gate sums, then their up sums, in y.
+// Eight channels: their gate sums, then their up sums, in y.  (One reciprocal for four of them, 1/a = bcd / abcd, is three quarters of the
+// special functions and more multiplications: 4096 tokens at 22016 x 1024, where the epilogue shows, 169 -> 174 us.)
 template <int ACT>
 __device__ __forceinline__ void glu_pack(const float (&y)[16], uint32_t* o) {
 #pragma unroll
