@@ -69,6 +69,44 @@ struct LossBarriers {
   int wait_limit_us;             // must follow abort_flag (read by the bounded waits)
 };
 
+// How the tokens that count share a chunk's buffers and pairs, known where they have been counted.  Where they fill half of the buffers, a
+// quarter or an eighth, as of instruction samples, of which the answers count alone, several pieces of the vocabulary are taken at once, and where their tiles
+// of the gradient are fewer than the pairs, the sum over a piece is cut into parts with sums of their own.
+constexpr int kFolds = 4;
+struct Share {
+  int blocks;            // of 256 tokens
+  int fold;              // log2 of the pieces taken at once
+  int splits;            // parts
+};
+struct ShareRule {
+  int blocks, pieces, features, pairs;     // features: tiles of 256
+  int splits;            // parts that the buffer has room for when all tokens count
+  int least;             // stages of the narrowest piece
+};
+__host__ __device__ inline Share share_of(const ShareRule& r, int rows_live) {
+  Share s = {(rows_live + kTile - 1) / kTile, 0, 1};
+  if (s.blocks == 0) return s;
+  while (s.fold + 1 < kFolds && (2 << s.fold) * s.blocks <= r.blocks && (1 << s.fold) < r.pieces) ++s.fold;
+  const int tiles = s.blocks * r.features, room = r.splits * r.blocks / s.blocks;
+  if (tiles < r.pairs) s.splits = r.pairs / tiles;
+  s.splits = s.splits < 16 ? s.splits : 16;
+  s.splits = s.splits < r.least ? s.splits : r.least;
+  s.splits = s.splits < room ? s.splits : room;
+  return s;
+}
+
+// What a launch of the ordinary kernel is given beside LossParams, whose piece is its own here.
+struct LossLaunch {
+  ShareRule rule;
+  int number;            // of the launch: logits of piece `number`, the gradient's sum over the one before (pieces as many as are taken at once)
+  int all_tiles, pieces;
+  __host__ __device__ int piece_tile(int i) const { return (int)((long long)all_tiles * (i < pieces ? i : pieces) / pieces); }
+};
+struct LossMaps {
+  CUtensorMap x, w, wt, sum;
+  CUtensorMap e_out[kFolds], e_in[kFolds];
+};
+
 struct Item {
   bool grad;
   int row;               // block of 256 tokens of the chunk
@@ -81,19 +119,28 @@ struct Item {
 // begin with as many tiles of logits as take its time, and the others are dealt to all.
 struct Walk {
   int pair, pairs, n1, n2, n2_mine, lo_first, lo_pairs, lo_mine, lo_total;
-  int rows, features, splits;
-  __device__ __forceinline__ Walk(const LossParams& p, int rows_live) {
+  int rows, features, splits, fold, back_group;
+  int tile0, tiles, back0, back_blocks;
+  __device__ __forceinline__ Walk(const LossParams& p, const LossLaunch& l, int rows_live) {
+    const Share share = share_of(l.rule, rows_live);
     pair = blockIdx.x >> 1;
     pairs = gridDim.x >> 1;
-    rows = (rows_live + kTile - 1) / kTile;
-    features = (p.K + kTile - 1) / kTile;
-    splits = p.splits;
-    n1 = rows * p.tiles;
-    n2 = p.back_blocks ? rows * features * splits : 0;
+    rows = share.blocks;
+    features = l.rule.features;
+    splits = share.splits;
+    fold = share.fold;
+    back_group = max(4, p.back_group >> fold);
+    const int before = l.piece_tile((l.number - 1) << fold), behind = l.piece_tile((l.number + 1) << fold);
+    tile0 = l.piece_tile(l.number << fold);
+    tiles = behind - tile0;
+    back0 = before * p.width;
+    back_blocks = l.number > 0 ? ((tile0 - before) * p.width + kDepth - 1) / kDepth : 0;
+    n1 = rows * tiles;
+    n2 = back_blocks ? rows * features * splits : 0;
     n2_mine = n2 > pair ? (n2 - pair - 1) / pairs + 1 : 0;
     lo_first = n2 % pairs;
     lo_pairs = lo_first ? pairs - lo_first : 0;
-    const int each = lo_pairs ? (p.back_blocks / splits + p.k_blocks / 2) / p.k_blocks : 0;
+    const int each = lo_pairs ? (back_blocks / splits + p.k_blocks / 2) / p.k_blocks : 0;
     lo_total = min(n1, each * lo_pairs);
     const int e = pair - lo_first;
     lo_mine = lo_pairs && e >= 0 && lo_total > e ? (lo_total - e - 1) / lo_pairs + 1 : 0;
@@ -110,9 +157,9 @@ struct Walk {
       int e = pair + i * pairs;
       it.grad = true;
       it.split = e / (rows * features);
-      deal(e - it.split * rows * features, p.back_group, features, it);
-      it.kb0 = (int)((long long)it.split * p.back_blocks / splits);
-      it.kbs = (int)((long long)(it.split + 1) * p.back_blocks / splits) - it.kb0;
+      deal(e - it.split * rows * features, back_group, features, it);
+      it.kb0 = (int)((long long)it.split * back_blocks / splits);
+      it.kbs = (int)((long long)(it.split + 1) * back_blocks / splits) - it.kb0;
       return true;
     }
     i -= n2_mine;
@@ -125,7 +172,7 @@ struct Walk {
       e = (int)at;
     }
     it.grad = false;
-    deal(e, p.group, p.tiles, it);
+    deal(e, p.group, tiles, it);
     it.split = 0;
     it.kb0 = 0;
     it.kbs = p.k_blocks;
@@ -135,9 +182,7 @@ struct Walk {
 
 template <bool GRAD>
 __global__ void __launch_bounds__(kLossThreads, 1)
-head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w,
-                 const __grid_constant__ CUtensorMap tmap_wt, const __grid_constant__ CUtensorMap tmap_e_out,
-                 const __grid_constant__ CUtensorMap tmap_e_in, const __grid_constant__ CUtensorMap tmap_sum, const LossParams p) {
+head_loss_kernel(const __grid_constant__ LossMaps maps, const LossParams p, const LossLaunch l) {
   if (GRAD && p.second) {
     wait_for_kernel_before();
     if (ld_global(p.again) == 0) {
@@ -166,13 +211,11 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
     bars->abort_flag = 0;
     bars->wait_limit_us = p.status[4];
     fence_mbar_init();
-    prefetch_tmap(&tmap_x);
-    prefetch_tmap(&tmap_w);
+    prefetch_tmap(&maps.x);
+    prefetch_tmap(&maps.w);
     if (GRAD) {
-      prefetch_tmap(&tmap_wt);
-      prefetch_tmap(&tmap_e_out);
-      prefetch_tmap(&tmap_e_in);
-      prefetch_tmap(&tmap_sum);
+      prefetch_tmap(&maps.wt);
+      prefetch_tmap(&maps.sum);
     }
   }
   if (warp == 2) {
@@ -187,7 +230,8 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
   let_next_in(false);
   const uint32_t tmem_base = bars->tmem_base;
   const int rows_live = min(p.rows, ld_global(p.live.count) - p.row0);     // none or fewer: no items
-  const Walk walk(p, rows_live > 0 ? rows_live : 0);
+  const Walk walk(p, l, rows_live > 0 ? rows_live : 0);
+  const CUtensorMap *tmap_e_out = &maps.e_out[walk.fold], *tmap_e_in = &maps.e_in[walk.fold];
 
   if (warp == 0) {
     // ------------------------------------------ operands (one lane)
@@ -206,14 +250,14 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
           if (leader) mbar_arrive_expect_tx(smem_u32(&bars->full[s]), (item.grad ? 2 * kStageBytes : logits_bytes) + starve);
           const uint32_t bar = mapa_shared(smem_u32(&bars->full[s]), 0), a = smem_u32(base + s * kStageBytes);
           if (!item.grad) {
-            tma_load_2d_pair(a, &tmap_x, bar, kb * kDepth, p.row0 + row);
-            tma_load_2d_pair(a + kOperandBytes, &tmap_w, bar, kb * kDepth, (p.tile0 + item.col) * p.width + (int)rank * (p.width >> 1));
+            tma_load_2d_pair(a, &maps.x, bar, kb * kDepth, p.row0 + row);
+            tma_load_2d_pair(a + kOperandBytes, &maps.w, bar, kb * kDepth, (walk.tile0 + item.col) * p.width + (int)rank * (p.width >> 1));
           } else if (GRAD) {
             const int k = (item.kb0 + kb) * kDepth, n0 = item.col * kTile + (int)rank * 128;
-            tma_load_2d_pair(a, &tmap_e_in, bar, k, row);
+            tma_load_2d_pair(a, tmap_e_in, bar, k, row);
 #pragma unroll
             for (int m = 0; m < 2; ++m)
-              tma_load_2d_pair(a + kOperandBytes + m * 8192, &tmap_wt, bar, n0 + 64 * m, p.back0 + k);
+              tma_load_2d_pair(a + kOperandBytes + m * 8192, &maps.wt, bar, n0 + 64 * m, walk.back0 + k);
           }
         }
       }
@@ -273,7 +317,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
       const uint32_t acc_empty = mapa_shared(smem_u32(&bars->acc_empty[buf]), 0);
       float ref = 0.0f;
       int label = -1, cols = 0;                             // both counted from this half tile's first entry
-      const int entry0 = (p.tile0 + item.col) * p.width + half * 128;
+      const int entry0 = (walk.tile0 + item.col) * p.width + half * 128;
       const int chunks = item.grad ? 4 : min(4, (p.width - half * 128) >> 5);      // none: 0 or less
       if (!item.grad) {
         cols = min(p.V - entry0, chunks * 32);
@@ -338,7 +382,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
-              if (row_w < rows_live) tma_store_2d(&tmap_e_out, smem_u32(at), item.col * p.width + half * 128 + c * 32, row_w);
+              if (row_w < rows_live) tma_store_2d(tmap_e_out, smem_u32(at), item.col * p.width + half * 128 + c * 32, row_w);
               bulk_commit_group();
             }
           }
@@ -352,10 +396,10 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
-            const int x = item.col * kTile + half * 128 + c * 32, y = item.split * p.rows + row_w;
+            const int x = item.col * kTile + half * 128 + c * 32, y = item.split * walk.rows * kTile + row_w;
             if (row_w < rows_live && x < p.K) {
-              if (p.first_back) tma_store_2d(&tmap_sum, smem_u32(mine), x, y);
-              else tma_add_2d(&tmap_sum, smem_u32(mine), x, y);
+              if (l.number == 1) tma_store_2d(&maps.sum, smem_u32(mine), x, y);
+              else tma_add_2d(&maps.sum, smem_u32(mine), x, y);
             }
             bulk_commit_group();
           }
@@ -367,7 +411,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
         if (lane == 0) mbar_arrive_cluster(acc_empty);
       }
       if (!item.grad) {
-        const size_t slot = ((size_t)(p.tile0 + item.col) * 2 + half) * p.rows + row;
+        const size_t slot = ((size_t)(walk.tile0 + item.col) * 2 + half) * p.rows + row;
         if (!GRAD) {
           reinterpret_cast<float2*>(p.sums)[slot] = make_float2(most, sum);
         } else {
@@ -495,8 +539,9 @@ struct FinishParams {
   const float* sums;
   int parts;               // that the vocabulary's sums come in
   int row0, rows;
-  const float* grads;      // [splits, rows, K]
-  int splits, K;
+  const float* grads;      // [splits, rows, K]: rows of the blocks of 256 that count
+  ShareRule rule;
+  int splits, K;           // splits: of few tokens, whose sums are 256 rows each; 0: by the rule
   const __nv_bfloat16* W;
   const float* weight;     // or nullptr
   float* loss;
@@ -528,7 +573,8 @@ __global__ void __launch_bounds__(kSideThreads) loss_finish_kernel(const FinishP
   const float weight = GRAD && p.weight ? ld_global(p.weight + token) : 1.0f;
   const __nv_bfloat16* w = p.W + (size_t)label * p.K;
   const float* g = p.grads + (size_t)row * p.K;
-  const size_t per_split = (size_t)p.rows * p.K;
+  const Share share = GRAD && !p.splits ? share_of(p.rule, live) : Share{1, 0, p.splits};
+  const size_t per_split = (size_t)share.blocks * kTile * p.K;
   struct Eight {
     float v[8];       // the first part's sums
     uint4 w;          // the label's row of the head
@@ -589,7 +635,7 @@ __global__ void __launch_bounds__(kSideThreads) loss_finish_kernel(const FinishP
   for (int c = at_thread * 8; c < p.K; c += kSpan * 8) {
     const Eight next = load(c + kSpan * 8);
 #pragma unroll 4
-    for (int s = 1; s < p.splits; ++s) {
+    for (int s = 1; s < share.splits; ++s) {
       const float4 a = ld_global(reinterpret_cast<const float4*>(g + s * per_split + c));
       const float4 b = ld_global(reinterpret_cast<const float4*>(g + s * per_split + c + 4));
       now.v[0] += a.x; now.v[1] += a.y; now.v[2] += a.z; now.v[3] += a.w;
@@ -616,6 +662,9 @@ struct LossPlan {
   bool few;                  // head_loss_few.cu
   // offsets into the workspace
   size_t count, again, index, label, ref, above, x, sums, e[2], grads, bytes;
+  ShareRule rule(int K, int pairs) const {
+    return {rows / kTile, pieces, (K + kTile - 1) / kTile, pairs, splits, tiles / pieces * width / kDepth};
+  }
   int piece_tile(int i) const { return (int)((long long)tiles * i / pieces); }
   int piece_width() const { return ((tiles + pieces - 1) / pieces) * width; }     // entries of the widest
 };
@@ -704,7 +753,7 @@ LossPlan plan_loss(int T, int V, int K, bool grad, int sms) {
 }
 
 template <bool GRAD>
-int launch_loss(const CUtensorMap (&maps)[6], const LossParams& p, int pairs, cudaStream_t st) {
+int launch_loss(const LossMaps& maps, const LossParams& p, const LossLaunch& l, int pairs, cudaStream_t st) {
   auto kern = head_loss_kernel<GRAD>;
   static std::atomic<uint64_t> done{0};
   PEQA_TRY(allow_smem(kern, kLossSmem, done));
@@ -722,7 +771,7 @@ int launch_loss(const CUtensorMap (&maps)[6], const LossParams& p, int pairs, cu
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  PEQA_CUDA(cudaLaunchKernelEx(&cfg, kern, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], p));
+  PEQA_CUDA(cudaLaunchKernelEx(&cfg, kern, maps, p, l));
   return PEQA_OK;
 }
 
@@ -778,13 +827,7 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
   p.width = c.width;
   p.status = status;
   const uint64_t width = c.piece_width();
-  CUtensorMap maps[6], e_out[2];
-  if (!c.few) {
-    PEQA_TRY(bf16_map(&maps[0], ws + c.x, K, (uint64_t)c.chunks * c.rows, 128));
-    PEQA_TRY(bf16_map(&maps[1], W, K, V, c.width / 2));
-    PEQA_TRY(bf16_map(&maps[2], W, K, V, 64));
-    maps[3] = maps[4] = maps[5] = maps[0];
-  }
+  LossMaps maps = {};
   FewCall few = {};
   if (c.few) {
     few.grads = reinterpret_cast<float*>(ws + c.grads);
@@ -792,14 +835,24 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
     few.tokens = T;
     for (int b = 0; b < 2; ++b) few.e[b] = ws + c.e[b];
     PEQA_TRY(few_maps(few, ws + c.x, W, c.width, V, K, dX != nullptr));
-  }
-  if (dX && !c.few) {
-    for (int b = 0; b < 2; ++b) {
-      PEQA_TRY(loss_map(&e_out[b], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, ws + c.e[b], width, c.rows, 2, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B));
+  } else {
+    PEQA_TRY(bf16_map(&maps.x, ws + c.x, K, (uint64_t)c.chunks * c.rows, 128));
+    PEQA_TRY(bf16_map(&maps.w, W, K, V, c.width / 2));
+    if (dX) {
+      PEQA_TRY(bf16_map(&maps.wt, W, K, V, 64));
+      PEQA_TRY(loss_map(&maps.sum, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, ws + c.grads, K, (uint64_t)c.splits * c.rows, 4, 32, 32,
+                        CU_TENSOR_MAP_SWIZZLE_128B));
     }
-    PEQA_TRY(loss_map(&maps[5], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, ws + c.grads, K, (uint64_t)c.splits * c.rows, 4, 32, 32,
-                      CU_TENSOR_MAP_SWIZZLE_128B));
   }
+  // [turn][fold]; several pieces' entries are whole stages, one's may not be: what its last stage has beyond it is read as zeros
+  CUtensorMap e_out[2][kFolds] = {}, e_in[2][kFolds] = {};
+  if (dX && !c.few)
+    for (int b = 0; b < (c.pieces > 1 ? 2 : 1); ++b)
+      for (int f = 0; f < kFolds && c.rows / kTile >> f > 0; ++f) {
+        PEQA_TRY(loss_map(&e_out[b][f], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, ws + c.e[b], width << f, c.rows >> f, 2, 32, 32,
+                          CU_TENSOR_MAP_SWIZZLE_64B));
+        PEQA_TRY(bf16_map(&e_in[b][f], ws + c.e[b], width << f, c.rows >> f, 128));
+      }
 
   GatherParams gp = {};
   gp.X = static_cast<const __nv_bfloat16*>(X);
@@ -826,7 +879,9 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
   fp.parts = (c.few ? kFewParts : 2) * c.tiles;
   fp.rows = c.rows;
   fp.grads = reinterpret_cast<const float*>(ws + c.grads);
-  fp.splits = c.splits;
+  fp.splits = c.few ? c.splits : 0;
+  const ShareRule rule = c.rule(K, pairs);
+  fp.rule = rule;
   fp.K = K;
   fp.W = gp.W;
   fp.weight = weight;
@@ -838,23 +893,25 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
     for (int turn = 0; turn < (dX ? 2 : 1); ++turn) {
       p.second = turn == 1;
       for (int i = 0; i <= (dX ? c.pieces : 0); ++i) {
-        p.tile0 = i < c.pieces ? c.piece_tile(i) : 0;
-        p.tiles = i < c.pieces ? c.piece_tile(i + 1) - p.tile0 : 0;
-        const int before = i > 0 ? c.piece_tile(i - 1) : 0, entries = i > 0 ? (c.piece_tile(i) - before) * c.width : 0;
-        p.back0 = before * c.width;
-        p.back_blocks = (entries + kDepth - 1) / kDepth;
-        p.first_back = i == 1;
         if (c.few) {
+          p.tile0 = i < c.pieces ? c.piece_tile(i) : 0;
+          p.tiles = i < c.pieces ? c.piece_tile(i + 1) - p.tile0 : 0;
+          const int before = i > 0 ? c.piece_tile(i - 1) : 0, entries = i > 0 ? (c.piece_tile(i) - before) * c.width : 0;
+          p.back0 = before * c.width;
+          p.back_blocks = (entries + kDepth - 1) / kDepth;
+          p.first_back = i == 1;
           PEQA_TRY(launch_few(p, few, i & 1, entries, dX != nullptr, pairs, st));
-        } else if (dX) {
-          maps[3] = e_out[i & 1];
-          // of the piece's own width: what its last stage has beyond that is read as zeros
-          if (i > 0)
-            PEQA_TRY(loss_map(&maps[4], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, ws + c.e[(i & 1) ^ 1], entries, c.rows, 2, 64, 128,
-                              CU_TENSOR_MAP_SWIZZLE_128B, width * 2));
-          PEQA_TRY(launch_loss<true>(maps, p, pairs, st));
+          continue;
+        }
+        const LossLaunch l = {rule, i, c.tiles, c.pieces};
+        if (dX) {
+          for (int f = 0; f < kFolds; ++f) {
+            maps.e_out[f] = e_out[c.pieces > 1 ? i & 1 : 0][f];
+            maps.e_in[f] = e_in[c.pieces > 1 ? (i & 1) ^ 1 : 0][f];
+          }
+          PEQA_TRY(launch_loss<true>(maps, p, l, pairs, st));
         } else {
-          PEQA_TRY(launch_loss<false>(maps, p, pairs, st));
+          PEQA_TRY(launch_loss<false>(maps, p, l, pairs, st));
         }
       }
     }

@@ -44,6 +44,15 @@ def test_tokens_that_count_nothing(T, ignored):
     assert not loss[off].any() and not dX[off].any()
 
 
+@pytest.mark.parametrize("T,V,K,ignored", [(5000, 20000, 64, 0.45), (5000, 20000, 64, 0.7), (5000, 20000, 64, 0.93), (5000, 20000, 1000, 0.99),
+                                           (9000, 12000, 72, 0.8), (1900, 40000, 64, 0.6), (3000, 30001, 264, 0.5)])
+def test_mostly_ignored(T, V, K, ignored):
+    """Where a half, a quarter or an eighth of a chunk counts, two, four or eight pieces of the vocabulary are taken at once."""
+    X, W, labels, weight = inputs(T, V, K, seed=T + K, ignored=ignored)
+    check(X, W, labels, weight)
+    check(X, W, labels, weight, grad=False)
+
+
 @pytest.mark.parametrize("T", [40, 200, 600])
 @pytest.mark.parametrize("grad", [True, False])
 def test_labels_far_below_the_largest_logit(T, grad):
