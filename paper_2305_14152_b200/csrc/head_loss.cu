@@ -548,15 +548,6 @@ struct FinishParams {
   __nv_bfloat16* dX;
 };
 
-// A largest logit and a sum relative to it.
-struct LogSum {
-  float most, sum;
-};
-__device__ __forceinline__ LogSum join_sums(LogSum a, LogSum b) {
-  const float most = fmaxf(a.most, b.most), by = most == -INFINITY ? 0.0f : most;
-  return {most, a.sum * exp2_approx((a.most - by) * kLog2e) + b.sum * exp2_approx((b.most - by) * kLog2e)};
-}
-
 // ROWS tokens a CTA: their sums over the vocabulary, added in one order whatever the timing, then 8 / ROWS warps a token.
 template <bool GRAD, int ROWS>
 __global__ void __launch_bounds__(kSideThreads) loss_finish_kernel(const FinishParams p) {
@@ -619,16 +610,13 @@ __global__ void __launch_bounds__(kSideThreads) loss_finish_kernel(const FinishP
     else v = join_sums(v, u);
   }
   const float sum = v.sum;
-  // the reference above the label's logit, and the label's term
-  const float above = GRAD ? ref : v.most - ref;
-  const float own = expf(-above);
-  if (at_thread == 0) {
-    float loss;
-    if (GRAD) loss = above == 0.0f ? log1pf(sum) : above + logf(sum + own);
-    else loss = above <= 0.0f ? log1pf(sum * expf(above)) : above + logf(sum + own);
-    p.loss[token] = loss;
+  if (!GRAD) {
+    if (at_thread == 0) p.loss[token] = loss_of(v, ref);
+    return;
   }
-  if (!GRAD) return;
+  // the reference above the label's logit, and the label's term
+  const float above = ref, own = expf(-above);
+  if (at_thread == 0) p.loss[token] = above == 0.0f ? log1pf(sum) : above + logf(sum + own);
   const float by = weight / (sum + own);
   __nv_bfloat16* out = p.dX + (size_t)token * p.K;
 #pragma unroll 1
@@ -830,11 +818,17 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
   LossMaps maps = {};
   FewCall few = {};
   if (c.few) {
+    few.labels = labels;
     few.grads = reinterpret_cast<float*>(ws + c.grads);
     few.pitch = (int)width;
     few.tokens = T;
     for (int b = 0; b < 2; ++b) few.e[b] = ws + c.e[b];
-    PEQA_TRY(few_maps(few, ws + c.x, W, c.width, V, K, dX != nullptr));
+    PEQA_TRY(few_maps(few, dX ? ws + c.x : X, W, c.width, V, K, dX != nullptr));
+    if (!dX) {
+      p.tiles = c.tiles;
+      PEQA_TRY(launch_few(p, few, 0, 0, false, pairs, st));
+      return finish_few(p, few, kFewParts * c.tiles, loss, st);
+    }
   } else {
     PEQA_TRY(bf16_map(&maps.x, ws + c.x, K, (uint64_t)c.chunks * c.rows, 128));
     PEQA_TRY(bf16_map(&maps.w, W, K, V, c.width / 2));

@@ -54,7 +54,10 @@ inline int bf16_map(CUtensorMap* m, const void* base, uint64_t inner, uint64_t o
 // Few tokens (head_loss_few.cu): tokens at most, partial sums of a tile, its buffers.
 constexpr int kFewTokens = 256;
 constexpr int kFewParts = 8;
+// Without gradient nothing is known or counted beforehand: the tokens are the call's own, and a label's logit is left in live.ref by the thread that
+// makes it.
 struct FewCall {
+  const int32_t* labels;
   float* grads;                // [splits, 256, K]
   void* e[2];                  // exponentials of a piece [256, pitch]; by turns, if there are several
   int pitch, tokens;
@@ -63,6 +66,7 @@ struct FewCall {
 int few_maps(FewCall& call, const void* rows, const void* W, int width, int V, int K, bool grad);
 // turn: which of e this piece's exponentials go to; in_entries: of the piece before, in the other
 int launch_few(const LossParams& p, const FewCall& call, int turn, int in_entries, bool grad, int pairs, cudaStream_t st);
+int finish_few(const LossParams& p, const FewCall& call, int parts, float* loss, cudaStream_t st);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ float exp2_approx(float x) {
@@ -81,6 +85,20 @@ __device__ __forceinline__ void tma_add_2d(const CUtensorMap* m, uint32_t src_sm
 }
 __device__ __forceinline__ void wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_kernel_behind_in() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// A largest logit and a sum relative to it.
+struct LogSum {
+  float most, sum;
+};
+__device__ __forceinline__ LogSum join_sums(LogSum a, LogSum b) {
+  const float most = fmaxf(a.most, b.most), by = most == -INFINITY ? 0.0f : most;
+  return {most, a.sum * exp2_approx((a.most - by) * kLog2e) + b.sum * exp2_approx((b.most - by) * kLog2e)};
+}
+// loss = log(sum over all entries of exp(l)) - label's logit, from the sum over the others
+__device__ __forceinline__ float loss_of(LogSum others, float label) {
+  const float above = others.most - label;
+  return above <= 0.0f ? log1pf(others.sum * expf(above)) : above + logf(others.sum + expf(-above));
+}
 
 // Reference of a live token: the label's logit, or in the repetition the row's largest if that is far above.
 __device__ __forceinline__ float above_of(const LiveTokens& live, int row) { return __int_as_float(ld_global(live.above + row)); }

@@ -8,6 +8,7 @@
 // An epilogue thread is an entry or a feature.  Sums over the entries go across the lanes: at distance o a lane keeps the tokens that
 // agree with it in bit o and hands the others over, 31 exchanges for 32 tokens.  Every warp of a tile leaves its own.
 #include "head_loss.cuh"
+#include "kv_cache.cuh"
 
 namespace peqa {
 
@@ -35,6 +36,8 @@ constexpr int kFewSmemFixed = 1024 + 8 * kFewStaging + (int)((sizeof(FewBarriers
 struct FewParams {
   LossParams p;
   float* grads;                  // [splits, 256, K]
+  const int32_t* labels;         // without gradient: of the call's tokens, `tokens` of them
+  int tokens;
   int nt;                        // columns: tokens, a multiple of 16
   int stages, stage_bytes;
 };
@@ -136,7 +139,7 @@ head_loss_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
   wait_for_kernel_before();
   let_next_in(false);
   const uint32_t tmem_base = bars->tmem_base;
-  const int live = min(kFewTokens, ld_global(p.live.count));
+  const int live = GRAD ? min(kFewTokens, ld_global(p.live.count)) : q.tokens;
   const FewWalk walk(p, live > 0);
   const int half_entries = p.width >> 1, half_tokens = q.nt >> 1;     // of a CTA
   const uint32_t b_bytes = half_tokens * (kDepth * 2);
@@ -218,11 +221,12 @@ head_loss_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
       const int t = (int)threadIdx.x - 128;
       float ref = 0.0f;
       int label = -1;
-      if (t < live) {
+      if (GRAD && t < live) {
         ref = ld_global(p.live.ref + t);
-        if (GRAD && p.second) ref += above_of(p.live, t);
+        if (p.second) ref += above_of(p.live, t);
         label = ld_global(p.live.label + t);
       }
+      if (!GRAD && t < live) label = ld_global(q.labels + t);
       bars->ref[t] = ref;
       bars->label[t] = label;
       named_barrier_sync(1, 256);
@@ -257,7 +261,11 @@ head_loss_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
           if (!GRAD) {
             float x[32];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = x[j] = valid && bars->label[t0 + j] != entry ? __uint_as_float(r[j]) : -INFINITY;
+            for (int j = 0; j < 32; ++j) {
+              const bool own = bars->label[t0 + j] == entry;
+              if (valid && own) p.live.ref[t0 + j] = __uint_as_float(r[j]);        // one thread of all
+              v[j] = x[j] = valid && !own ? __uint_as_float(r[j]) : -INFINITY;
+            }
             const float most = fold32(v, lane, [](float a, float b) { return fmaxf(a, b); });
             const float by = most == -INFINITY ? 0.0f : most;
 #pragma unroll
@@ -364,12 +372,43 @@ int launch_few_t(const CUtensorMap& w, const CUtensorMap& x, const CUtensorMap& 
   return PEQA_OK;
 }
 
+// The losses of few tokens without gradient, a token a CTA.
+__global__ void __launch_bounds__(256) loss_few_finish_kernel(const float2* sums, int parts, const int32_t* labels, int V, const float* ref,
+                                                              float* loss, int* status) {
+  wait_for_kernel_before();
+  let_kernel_behind_in();
+  __shared__ LogSum part[8];
+  const int token = blockIdx.x, lane = threadIdx.x & 31;
+  const int label = ld_global(labels + token);
+  const float own = ld_global(ref + token);
+  if ((unsigned)label >= (unsigned)V) {
+    if (threadIdx.x == 0) {
+      if (label >= V) note_bad_index(status);
+      loss[token] = 0.0f;
+    }
+    return;
+  }
+  LogSum v = {-INFINITY, 0.0f};
+#pragma unroll 4
+  for (int h = threadIdx.x; h < parts; h += 256) {
+    const float2 u = ld_global(sums + (size_t)h * kFewTokens + token);
+    v = join_sums(v, {u.x, u.y});
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = join_sums(v, {__shfl_xor_sync(0xffffffffu, v.most, o), __shfl_xor_sync(0xffffffffu, v.sum, o)});
+  if (lane == 0) part[threadIdx.x >> 5] = v;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < 8; ++w) v = join_sums(v, part[w]);
+  loss[token] = loss_of(v, own);
+}
+
 }  // namespace
 
 int loss::few_maps(FewCall& call, const void* rows, const void* W, int width, int V, int K, bool grad) {
   const uint32_t half_tokens = ((call.tokens + 15) & ~15) / 2;
   PEQA_TRY(bf16_map(&call.w, W, K, V, width / 2));
-  PEQA_TRY(bf16_map(&call.x, rows, K, kFewTokens, half_tokens));
+  PEQA_TRY(bf16_map(&call.x, rows, K, grad ? kFewTokens : call.tokens, half_tokens));
   if (!grad) return PEQA_OK;
   PEQA_TRY(bf16_map(&call.wt, W, K, V, 64));
   for (int b = 0; b < (call.e[0] == call.e[1] ? 1 : 2); ++b)
@@ -381,6 +420,8 @@ int loss::launch_few(const LossParams& p, const FewCall& call, int turn, int in_
   FewParams q;
   q.p = p;
   q.grads = call.grads;
+  q.labels = call.labels;
+  q.tokens = call.tokens;
   q.nt = (call.tokens + 15) & ~15;
   q.stage_bytes = kOperandBytes + q.nt / 2 * (kDepth * 2);
   q.stages = (kFewSmemLimit - kFewSmemFixed) / q.stage_bytes;
@@ -391,6 +432,11 @@ int loss::launch_few(const LossParams& p, const FewCall& call, int turn, int in_
   // of the piece's own width: what its last stage has beyond that is read as zeros
   if (in_entries > 0) PEQA_TRY(bf16_map(&e_in, call.e[turn ^ 1], in_entries, kFewTokens, q.nt / 2, (uint64_t)call.pitch * 2));
   return launch_few_t<true>(call.w, call.x, call.wt, e_in, call.e_out[call.e[0] == call.e[1] ? 0 : turn], q, pairs, smem, st);
+}
+
+int loss::finish_few(const LossParams& p, const FewCall& call, int parts, float* loss, cudaStream_t st) {
+  return launch_after(loss_few_finish_kernel, call.tokens, 256, st, reinterpret_cast<const float2*>(p.sums), parts, call.labels, p.V,
+                      static_cast<const float*>(p.live.ref), loss, p.status);
 }
 
 }  // namespace peqa
