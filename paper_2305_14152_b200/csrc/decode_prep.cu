@@ -374,10 +374,13 @@ struct CanonRow {
 // are two tokens x four digits, which fp16 operands would leave idle.  An MMA covers twice the columns,
 // the codes are cheaper to take out (i8_string), and the sums of a group are exact.
 //
-// GLU: the outputs of a gated block (glu.cuh) in place of Y.
-template <int BITS, int NT, int GSH, bool TASKS, bool CANON, bool I8, int V, bool GLU>
+// FORM: entries of the vectors that scales and zero-points are read by, and kGluForm for the outputs of a gated block (glu.cuh) in place of Y.
+constexpr int kGluForm = 8;
+template <int BITS, int NT, int GSH, bool TASKS, bool CANON, bool I8, int FORM>
 __global__ void __launch_bounds__(kPThreads, 1)
 decode_prep_kernel(const PrepParams p) {
+  constexpr int V = FORM & (kGluForm - 1);
+  constexpr bool GLU = FORM >= kGluForm;
   constexpr int C = BITS;                            // 16-byte chunks per lane, step and group
   constexpr int BLK = C * 512;                       // bytes of one block (rg, t)
   constexpr int TOKP = 8 * NT;
@@ -1462,9 +1465,9 @@ int plan_prep(int N, int K, int M, int bits, int gcols, bool canon, bool i8, boo
   return plan->ns < 0 ? PEQA_ERR_TOO_LARGE : PEQA_OK;
 }
 
-template <int BITS, int NT, int GSH, bool TASKS, bool CANON, bool I8, int V, bool GLU>
+template <int BITS, int NT, int GSH, bool TASKS, bool CANON, bool I8, int FORM>
 int launch_prep_k(const PrepParams& p, int grid, size_t smem, cudaStream_t st) {
-  auto kern = decode_prep_kernel<BITS, NT, GSH, TASKS, CANON, I8, V, GLU>;
+  auto kern = decode_prep_kernel<BITS, NT, GSH, TASKS, CANON, I8, FORM>;
   static std::atomic<uint64_t> done{0};
   PEQA_TRY(allow_smem(kern, kPSmemLimit, done));
   cudaLaunchConfig_t cfg = {};
@@ -1488,8 +1491,8 @@ int launch_prep_k(const PrepParams& p, int grid, size_t smem, cudaStream_t st) {
 template <int BITS, int NT, int GSH, bool TASKS, bool CANON, bool I8, int V>
 int launch_prep_t(const PrepParams& p, bool glu, int grid, size_t smem, cudaStream_t st) {
   if constexpr (!CANON)
-    if (glu) return launch_prep_k<BITS, NT, GSH, TASKS, CANON, I8, V, true>(p, grid, smem, st);
-  return launch_prep_k<BITS, NT, GSH, TASKS, CANON, I8, V, false>(p, grid, smem, st);
+    if (glu) return launch_prep_k<BITS, NT, GSH, TASKS, CANON, I8, V + kGluForm>(p, grid, smem, st);
+  return launch_prep_k<BITS, NT, GSH, TASKS, CANON, I8, V>(p, grid, smem, st);
 }
 
 template <int BITS, int NT, bool TASKS, bool CANON, bool I8>

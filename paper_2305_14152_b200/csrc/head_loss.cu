@@ -235,7 +235,7 @@ head_loss_kernel(const __grid_constant__ LossMaps maps, const LossParams p, cons
 
   if (warp == 0) {
     // ------------------------------------------ operands (one lane)
-    if (elect_lane() == 0) {
+    if (const uint32_t lane = elect_lane(); lane == 0) {
       uint32_t it = 0;
       bool ok = true;
       Item item;
@@ -264,7 +264,7 @@ head_loss_kernel(const __grid_constant__ LossMaps maps, const LossParams p, cons
     }
   } else if (warp == 1) {
     // ------------------------------------------ MMA issuer (leader CTA, one lane)
-    if (leader) if (elect_lane() == 0) {
+    if (leader) if (const uint32_t lane = elect_lane(); lane == 0) {
       const uint32_t idesc_logits = idesc_bf16_f32(256, p.width, 0, 0);
       constexpr uint32_t idesc_grad = idesc_bf16_f32(256, 256, 0, 1);
       const uint32_t a0 = smem_u32(base);

@@ -146,7 +146,7 @@ head_loss_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
 
   if (warp == 0) {
     // ------------------------------------------ operands (one lane)
-    if (elect_lane() == 0) {
+    if (const uint32_t lane = elect_lane(); lane == 0) {
       int s = 0;
       uint32_t ph = 0;
       bool ok = true;
@@ -179,7 +179,7 @@ head_loss_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
     }
   } else if (warp == 1) {
     // ------------------------------------------ MMA issuer (leader CTA, one lane)
-    if (leader) if (elect_lane() == 0) {
+    if (leader) if (const uint32_t lane = elect_lane(); lane == 0) {
       const uint32_t idesc_logits = idesc_bf16_f32(256, q.nt, 0, 0), idesc_grad = idesc_bf16_f32(256, q.nt, 1, 0);
       const uint32_t a0 = smem_u32(base);
       const uint64_t adesc_logits = smem_desc_sw128(a0, 16, 1024), adesc_grad = smem_desc_sw128(a0, 8192, 1024);
