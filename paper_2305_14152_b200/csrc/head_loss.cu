@@ -499,19 +499,7 @@ __global__ void __launch_bounds__(kSideThreads) loss_gather_kernel(const GatherP
   const int at = before + __popc(alive & ((1u << mine) - 1u));
   float dot = 0.0f;
   if (live) {
-    const __nv_bfloat16* w = p.W + (size_t)label * p.K;
-    __nv_bfloat16* row = p.rows + (size_t)at * p.K;
-#pragma unroll 4
-    for (int c = at_thread * 8; c < p.K; c += kSpan * 8) {
-      const uint4 a = ld_global(reinterpret_cast<const uint4*>(p.X + own + c)), b = ld_global(reinterpret_cast<const uint4*>(w + c));
-      *reinterpret_cast<uint4*>(row + c) = a;
-      const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        dot = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), dot);
-        dot = fmaf(__uint_as_float(x[e] & 0xFFFF0000u), __uint_as_float(y[e] & 0xFFFF0000u), dot);
-      }
-    }
+    dot = dot_share(p.X + own, p.W + (size_t)label * p.K, p.rows + (size_t)at * p.K, p.K, at_thread * 8, kSpan * 8);
   } else if (t < p.T) {
     if (at_thread == 0) {
       if (label >= p.V) note_bad_index(p.status);
@@ -523,8 +511,7 @@ __global__ void __launch_bounds__(kSideThreads) loss_gather_kernel(const GatherP
   if constexpr (ROWS == 1) {
     dot = over_block(dot, dots, add_floats);
   } else {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+    dot = warp_sum(dot);
   }
   if (live && at_thread == 0) {
     p.live.index[at] = t;
@@ -818,12 +805,14 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
   LossMaps maps = {};
   FewCall few = {};
   if (c.few) {
+    few.rows = dX ? ws + c.x : X;
+    few.W = W;
     few.labels = labels;
     few.grads = reinterpret_cast<float*>(ws + c.grads);
     few.pitch = (int)width;
     few.tokens = T;
     for (int b = 0; b < 2; ++b) few.e[b] = ws + c.e[b];
-    PEQA_TRY(few_maps(few, dX ? ws + c.x : X, W, c.width, V, K, dX != nullptr));
+    PEQA_TRY(few_maps(few, c.width, V, K, dX != nullptr));
     if (!dX) {
       p.tiles = c.tiles;
       PEQA_TRY(launch_few(p, few, 0, 0, false, pairs, st));

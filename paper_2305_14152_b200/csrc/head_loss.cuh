@@ -54,16 +54,17 @@ inline int bf16_map(CUtensorMap* m, const void* base, uint64_t inner, uint64_t o
 // Few tokens (head_loss_few.cu): tokens at most, partial sums of a tile, its buffers.
 constexpr int kFewTokens = 256;
 constexpr int kFewParts = 8;
-// Without gradient nothing is known or counted beforehand: the tokens are the call's own, and a label's logit is left in live.ref by the thread that
-// makes it.
+// Without gradient nothing is known or counted beforehand: the tokens are the call's own, and the labels' logits are left in live.ref.
 struct FewCall {
+  const void* rows;            // [256, K], or the call's X
+  const void* W;
   const int32_t* labels;
   float* grads;                // [splits, 256, K]
   void* e[2];                  // exponentials of a piece [256, pitch]; by turns, if there are several
   int pitch, tokens;
   CUtensorMap w, x, wt, e_out[2];
 };
-int few_maps(FewCall& call, const void* rows, const void* W, int width, int V, int K, bool grad);
+int few_maps(FewCall& call, int width, int V, int K, bool grad);
 // turn: which of e this piece's exponentials go to; in_entries: of the piece before, in the other
 int launch_few(const LossParams& p, const FewCall& call, int turn, int in_entries, bool grad, int pairs, cudaStream_t st);
 int finish_few(const LossParams& p, const FewCall& call, int parts, float* loss, cudaStream_t st);
@@ -85,6 +86,31 @@ __device__ __forceinline__ void tma_add_2d(const CUtensorMap* m, uint32_t src_sm
 }
 __device__ __forceinline__ void wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_kernel_behind_in() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// This lane's share of <x, w>, K a multiple of 8: columns first, first + step, ... of eight; copy: where x is to be left too, or nullptr.
+__device__ __forceinline__ float dot_share(const __nv_bfloat16* x, const __nv_bfloat16* w, __nv_bfloat16* copy, int K, int first, int step) {
+  float dot = 0.0f;
+#pragma unroll 4
+  for (int c = first; c < K; c += step) {
+    const uint4 a = ld_global(reinterpret_cast<const uint4*>(x + c)), b = ld_global(reinterpret_cast<const uint4*>(w + c));
+    if (copy) *reinterpret_cast<uint4*>(copy + c) = a;
+    const uint32_t xs[4] = {a.x, a.y, a.z, a.w}, ws[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      dot = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ws[e] << 16), dot);
+      dot = fmaf(__uint_as_float(xs[e] & 0xFFFF0000u), __uint_as_float(ws[e] & 0xFFFF0000u), dot);
+    }
+  }
+  return dot;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ float warp_dot(const __nv_bfloat16* x, const __nv_bfloat16* w, int K, int lane) {
+  return warp_sum(dot_share(x, w, nullptr, K, lane * 8, 256));
+}
 
 // A largest logit and a sum relative to it.
 struct LogSum {

@@ -36,7 +36,10 @@ constexpr int kFewSmemFixed = 1024 + 8 * kFewStaging + (int)((sizeof(FewBarriers
 struct FewParams {
   LossParams p;
   float* grads;                  // [splits, 256, K]
-  const int32_t* labels;         // without gradient: of the call's tokens, `tokens` of them
+  // without gradient: the call's tokens, `tokens` of them, and their labels
+  const int32_t* labels;
+  const __nv_bfloat16* x;
+  const __nv_bfloat16* W;
   int tokens;
   int nt;                        // columns: tokens, a multiple of 16
   int stages, stage_bytes;
@@ -215,6 +218,18 @@ head_loss_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
         if (ok) mma_commit_pair(smem_u32(&bars->acc_full[buf]), 3);
       }
     }
+  } else if (warp == 3) {
+    // ------------------------------------------ without gradient: the labels' logits, while the tiles are worked on.  In binary32: a tile's
+    // sums drop what is below their last bit, always towards zero, which the label's, the largest as a rule, shows most (a loss of 1e-3 off by 3e-5 of
+    // itself).
+    if (!GRAD) {
+      for (int t = blockIdx.x; t < live; t += gridDim.x) {
+        const int label = ld_global(q.labels + t);
+        if ((unsigned)label >= (unsigned)p.V) continue;
+        const float dot = warp_dot(q.x + (size_t)t * p.K, q.W + (size_t)label * p.K, p.K, lane);
+        if (lane == 0) p.live.ref[t] = dot;
+      }
+    }
   } else if (warp >= 4) {
     // ------------------------------------------ epilogue: thread = entry or feature, every other 32 tokens
     {
@@ -261,11 +276,7 @@ head_loss_few_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
           if (!GRAD) {
             float x[32];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const bool own = bars->label[t0 + j] == entry;
-              if (valid && own) p.live.ref[t0 + j] = __uint_as_float(r[j]);        // one thread of all
-              v[j] = x[j] = valid && !own ? __uint_as_float(r[j]) : -INFINITY;
-            }
+            for (int j = 0; j < 32; ++j) v[j] = x[j] = valid && bars->label[t0 + j] != entry ? __uint_as_float(r[j]) : -INFINITY;
             const float most = fold32(v, lane, [](float a, float b) { return fmaxf(a, b); });
             const float by = most == -INFINITY ? 0.0f : most;
 #pragma unroll
@@ -405,12 +416,12 @@ __global__ void __launch_bounds__(256) loss_few_finish_kernel(const float2* sums
 
 }  // namespace
 
-int loss::few_maps(FewCall& call, const void* rows, const void* W, int width, int V, int K, bool grad) {
+int loss::few_maps(FewCall& call, int width, int V, int K, bool grad) {
   const uint32_t half_tokens = ((call.tokens + 15) & ~15) / 2;
-  PEQA_TRY(bf16_map(&call.w, W, K, V, width / 2));
-  PEQA_TRY(bf16_map(&call.x, rows, K, grad ? kFewTokens : call.tokens, half_tokens));
+  PEQA_TRY(bf16_map(&call.w, call.W, K, V, width / 2));
+  PEQA_TRY(bf16_map(&call.x, call.rows, K, grad ? kFewTokens : call.tokens, half_tokens));
   if (!grad) return PEQA_OK;
-  PEQA_TRY(bf16_map(&call.wt, W, K, V, 64));
+  PEQA_TRY(bf16_map(&call.wt, call.W, K, V, 64));
   for (int b = 0; b < (call.e[0] == call.e[1] ? 1 : 2); ++b)
     PEQA_TRY(loss_map(&call.e_out[b], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, call.e[b], call.pitch, kFewTokens, 2, 16, 32, CU_TENSOR_MAP_SWIZZLE_NONE));
   return PEQA_OK;
@@ -421,6 +432,8 @@ int loss::launch_few(const LossParams& p, const FewCall& call, int turn, int in_
   q.p = p;
   q.grads = call.grads;
   q.labels = call.labels;
+  q.x = static_cast<const __nv_bfloat16*>(call.rows);
+  q.W = static_cast<const __nv_bfloat16*>(call.W);
   q.tokens = call.tokens;
   q.nt = (call.tokens + 15) & ~15;
   q.stage_bytes = kOperandBytes + q.nt / 2 * (kDepth * 2);
