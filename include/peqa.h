@@ -460,7 +460,8 @@ int peqa_qlinear_decode_prepared(const peqa_qweight_t* w, const uint32_t* prepar
  * row, so this can be done before or after it).  All that takes a linear takes the block: with dY of peqa_glu_bwd the gradients
  * (peqa_qlinear_bwd, whose dX is then the sum over both projections, and the calls beside it), AdamW, peqa_decode_prepare.
  *   peqa_qglu_fwd: Y = X W_hat^T, H[t,c] = act(Y[t, gate row of c]) * Y[t, up row of c] (of Y before it is rounded)
- *     X in bf16 [T, K];  Y out bf16 [T, 2F], for the backward pass, or NULL;  H out bf16 [T, F].
+ *     X in bf16 [T, K];  Y out bf16 [T, 2F], for the backward pass, or NULL;  H out bf16 [T, F];
+ *     both apart from X and from each other.
  *     K % 64 == 0, with 3 bits K % 128 == 0; T >= 1.  Y's bits are peqa_qlinear_fwd's.
  *   peqa_glu_bwd: dY from Y and dH in bf16 [T, F]; dY out bf16 [T, 2F], Y itself or memory apart from it.
  *   peqa_qglu_decode_prepared: H [M, F] of 1 to 16 tokens from the prepared weights; arguments, shapes and the time at which

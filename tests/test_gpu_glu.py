@@ -183,6 +183,28 @@ def test_a_training_step_to_the_loss(bits, group):
     assert not torch.equal(before, w.scales) and w.scales.isfinite().all()
 
 
+def test_what_is_refused():
+    w, _, _ = block(64, 256, 4, 64, seed=40)
+    X, H = rows(20, 256, 41), torch.zeros((20, 64), dtype=torch.bfloat16, device="cuda")
+    Y = torch.zeros((20, 128), dtype=torch.bfloat16, device="cuda")
+    prepared = binding.decode_prepare(w)
+    torch.cuda.synchronize()
+    few = X[:4].contiguous()
+    for call in (lambda: binding.qglu_fwd(w, X[:, :128].contiguous()), lambda: binding.qglu_fwd(w, X.float()), lambda: binding.qglu_fwd(w, X.cpu()),
+                 lambda: binding.qglu_fwd(w, X, "relu"), lambda: binding.qglu_fwd(w, X, 0), lambda: binding.qglu_fwd(w, X, H=Y),
+                 lambda: binding.qglu_fwd(w, X, Y=H), lambda: binding.glu_bwd(Y, H[:19]), lambda: binding.glu_bwd(Y, Y),
+                 lambda: binding.glu_bwd(Y, H, dY=H), lambda: binding.glu_bwd(Y, H, "gelu"), lambda: binding.glu_bwd(Y[:, :64], H),
+                 lambda: binding.qglu_decode_prepared(w, prepared[:-1], few), lambda: binding.qglu_decode_prepared(w, prepared, few, scale_table=w.scales[None]),
+                 lambda: binding.qglu_decode_prepared(w, prepared, few, scale_table=w.scales[None, :-1].contiguous(), task_ids=torch.zeros(4, dtype=torch.int32, device="cuda")),
+                 lambda: binding.qglu_decode_prepared(w, prepared, few, scale_table=w.scales[None], task_ids=torch.zeros(3, dtype=torch.int32, device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(binding.PeqaError) as e:
+        binding.qglu_decode_prepared(w, prepared, X)
+    assert e.value.status == -3                               # more than 16 tokens
+    binding.check_status()
+
+
 def test_captured_decode_beside_another_stream():
     w, _, _ = block(1024, 1024, 3, 64, seed=30)
     prepared = binding.decode_prepare(w)

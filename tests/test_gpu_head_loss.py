@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 #: chunks of tokens
 SHAPES = [(1, 1, 8), (1, 2, 64), (1, 1000, 64), (3, 257, 72), (17, 5000, 200), (150, 32000, 512), (255, 256, 256), (256, 513, 128),
           (257, 1025, 1000), (513, 2050, 136), (700, 50257, 96), (2048, 999, 2048), (8200, 9000, 64),
-          (5, 140001, 64), (33, 333, 2056), (64, 32000, 128), (129, 8200, 640), (240, 4097, 328)]
+          (300, 1, 8), (300, 3, 40), (5, 270001, 64), (33, 333, 2056), (64, 32000, 128), (129, 8200, 640), (240, 4097, 328)]
 
 
 def check(X, W, labels, weight, grad=True, **more):
@@ -113,14 +113,39 @@ def test_values_that_are_not_finite_stay_in_their_rows():
     assert_within(dX[fine], want_dX, tol_dX, "dX")
 
 
-def test_labels_beyond_the_vocabulary_are_noted():
-    X, W, labels, weight = inputs(40, 500, 64, seed=10)
-    labels[7], labels[8] = 500, 2 ** 31 - 1
-    loss, dX = binding.head_loss(X, W, labels, weight)
+def test_what_is_refused():
+    X, W, labels, weight = inputs(300, 1000, 128, seed=14)
+    for grad in (True, False):
+        ws = binding.alloc_head_loss_workspace(X, W, grad)
+        with pytest.raises(binding.PeqaError) as e:
+            binding.head_loss(X, W, labels, weight, need_grad=grad, workspace=ws[:-256])
+        assert e.value.status == -5
+        with pytest.raises(binding.PeqaError) as e:
+            binding.head_loss(X, W, labels, weight, need_grad=grad, workspace=torch.cat([ws, ws])[16:])
+        assert e.value.status == -4
+    bad = [dict(X=X.float()), dict(X=X[:, :64]), dict(W=W[:, :120].contiguous()), dict(labels=labels.long()), dict(labels=labels[:-1]),
+           dict(labels=labels.cpu()), dict(weight=weight[:-1]), dict(weight=weight.double()), dict(loss=torch.empty(299, device="cuda")),
+           dict(dX=torch.empty_like(X[:299])), dict(dX=torch.empty_like(X, dtype=torch.float32)), dict(X=X[0]), dict(W=W[0])]
+    for more in bad:
+        with pytest.raises(ValueError):
+            binding.head_loss(**({"X": X, "W": W, "labels": labels, "weight": weight} | more))
     with pytest.raises(binding.PeqaError) as e:
-        binding.check_status()
-    assert e.value.status == -10
+        binding.head_loss(X[:, :100].contiguous(), W[:, :100].contiguous(), labels)
+    assert e.value.status == -3
     binding.check_status()
+
+
+@pytest.mark.parametrize("T", [40, 400])
+def test_labels_beyond_the_vocabulary_are_noted(T):
+    X, W, labels, weight = inputs(T, 500, 64, seed=10)
+    labels[7], labels[8] = 500, 2 ** 31 - 1
+    for grad in (False, True):
+        loss, dX = binding.head_loss(X, W, labels, weight, need_grad=grad)
+        with pytest.raises(binding.PeqaError) as e:
+            binding.check_status()
+        assert e.value.status == -10
+        binding.check_status()
+        assert not loss[7:9].any()
     want, want_dX, tol, tol_dX = reference(X, W, labels, weight)
     assert_within(loss, want, tol, "loss")
     assert_within(dX, want_dX, tol_dX, "dX")
