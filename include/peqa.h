@@ -6,8 +6,9 @@
  * layer is W_hat = s * (Q - z) (Eq. 2, Sec. 3.2).  This library is the layer's
  * hot path: quantize once (Eq. 1), forward, backward (dX and the scale
  * gradient dS, without ever materialising dW), small-batch decode, AdamW
- * on the scales, and for token generation the paged key-value cache with the
- * attention that reads it.
+ * on the scales, for token generation the paged key-value cache with the
+ * attention that reads it, and around a training step's linears the gated feed-forward
+ * block and the loss of the vocabulary projection with its gradient.
  *
  * Conventions for every entry point
  *   - All tensor pointers are DEVICE pointers owned by the caller, dense and
@@ -55,7 +56,7 @@ typedef enum {
   PEQA_ERR_CUDA = -7,           /* a CUDA runtime/driver call failed; see peqa_last_cuda_error() */
   PEQA_ERR_DEVICE_TIMEOUT = -8, /* a bounded device-side wait expired */
   PEQA_ERR_TOO_LARGE = -9,      /* size exceeds a documented fixed capacity */
-  PEQA_ERR_DEVICE_INDEX = -10   /* a length, page number or position read on the device is out of range */
+  PEQA_ERR_DEVICE_INDEX = -10   /* a length, page number, position or label read on the device is out of range */
 } peqa_status;
 
 /* Frozen part (Q, z) and trainable scale s of one PEQA linear layer. */
@@ -614,7 +615,7 @@ int peqa_probe_read(const void* src, size_t bytes, uint32_t* sink, size_t sink_b
  * Returns PEQA_OK, PEQA_ERR_DEVICE_TIMEOUT (a bounded wait of a kernel launched on
  * `stream` expired since the last check; its outputs are undefined),
  * PEQA_ERR_DEVICE_INDEX (a kernel of the key-value cache met a length, page number
- * or position out of range, and left out what it stands for) or PEQA_ERR_CUDA.  Where both were found
+ * or position out of range, or one of the loss a label, and left out what it stands for) or PEQA_ERR_CUDA.  Where both were found
  * the time-out is returned, and the index by the next call.  Status words live in the library's device image, one per stream
  * (the first 31 streams seen on a device get a word of their own, any further
  * streams share one); entry points without a workspace argument have nowhere
@@ -628,7 +629,7 @@ int peqa_check_status(void* stream);
  * kernels launched afterwards on the current device, the bound of a single
  * device-side wait to wait_limit_us microseconds (0 restores the default of two
  * seconds) and, when starve_forward is non-zero, makes the kernels of peqa_qlinear_fwd
- * announce one byte more than their copies deliver, and that of peqa_attn_decode (where it takes
+ * (peqa_qglu_fwd, peqa_head_loss) announce one byte more than their copies deliver, and that of peqa_attn_decode (where it takes
  * tensor copies) expect an arrival that does not come, so that the
  * first stage never fills: the kernel must then leave through its time-out path,
  * free its tensor memory and report PEQA_ERR_DEVICE_TIMEOUT through
