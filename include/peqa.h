@@ -75,7 +75,8 @@ typedef enum {
   PEQA_OP_BWD = 1,
   PEQA_OP_DECODE = 2,
   PEQA_OP_BWD_DS_FROM_Y = 3,
-  PEQA_OP_BWD_DSDZ = 4
+  PEQA_OP_BWD_DSDZ = 4,
+  PEQA_OP_GLU_FWD = 5
 } peqa_op;
 
 /* Library version, major*10000 + minor*100 + patch. */
@@ -463,14 +464,17 @@ int peqa_qlinear_decode_prepared(const peqa_qweight_t* w, const uint32_t* prepar
  *   peqa_qglu_fwd: Y = X W_hat^T, H[t,c] = act(Y[t, gate row of c]) * Y[t, up row of c] (of Y before it is rounded)
  *     X in bf16 [T, K];  Y out bf16 [T, 2F], for the backward pass, or NULL;  H out bf16 [T, F];
  *     both apart from X and from each other.
- *     K % 64 == 0, with 3 bits K % 128 == 0; T >= 1.  Y's bits are peqa_qlinear_fwd's.
+ *     K % 64 == 0, with 3 bits K % 128 == 0; T >= 1.  Needs a workspace of peqa_workspace_bytes(PEQA_OP_GLU_FWD, T, w) bytes, 256-byte aligned,
+ *     when that is non-zero: with groups, whose scales go into the operands, these are binary16 (X times a power of two per token, scales times one per row),
+ *     so that Y and H are off by little more than their own rounding.  With one scale per row Y's bits are peqa_qlinear_fwd's.
  *   peqa_glu_bwd: dY from Y and dH in bf16 [T, F]; dY out bf16 [T, 2F], Y itself or memory apart from it.
  *   peqa_qglu_decode_prepared: H [M, F] of 1 to 16 tokens from the prepared weights; arguments, shapes and the time at which
  *     `prepared` has to be final as with peqa_qlinear_decode_prepared.
  * activation: silu, x / (1 + exp(-x)), or gelu in its tanh form, x/2 (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))); evaluated in binary32.
  */
 typedef enum { PEQA_ACT_SILU = 0, PEQA_ACT_GELU_TANH = 1 } peqa_activation;
-int peqa_qglu_fwd(const peqa_qweight_t* w, int activation, const void* X_bf16, int T, void* Y_bf16, void* H_bf16, void* stream);
+int peqa_qglu_fwd(const peqa_qweight_t* w, int activation, const void* X_bf16, int T, void* Y_bf16, void* H_bf16, void* workspace,
+                  size_t workspace_bytes, void* stream);
 int peqa_glu_bwd(int activation, const void* Y_bf16, const void* dH_bf16, int T, int F, void* dY_bf16, void* stream);
 int peqa_qglu_decode_prepared(const peqa_qweight_t* w, int activation, const uint32_t* prepared, const void* X_bf16, int M,
                               void* H_bf16, const float* scale_table, int n_tasks, const int32_t* task_ids, void* stream);

@@ -25,7 +25,7 @@ LIB_PATH = os.path.join(_HERE, "libpeqa_b200.so")
 _lib = None
 _native = None
 
-OP_FWD, OP_BWD, OP_DECODE, OP_BWD_DS_FROM_Y, OP_BWD_DSDZ = 0, 1, 2, 3, 4
+OP_FWD, OP_BWD, OP_DECODE, OP_BWD_DS_FROM_Y, OP_BWD_DSDZ, OP_GLU_FWD = 0, 1, 2, 3, 4, 5
 
 STATUS_NAMES = {
     0: "PEQA_OK", -1: "PEQA_ERR_NULL", -2: "PEQA_ERR_BAD_BITS", -3: "PEQA_ERR_BAD_SHAPE",
@@ -144,7 +144,7 @@ def lib() -> ctypes.CDLL:
         L.peqa_attn_decode.restype = ctypes.c_int
         L.peqa_attn_workspace_bytes.argtypes = [cp, i32]
         L.peqa_attn_workspace_bytes.restype = sz
-        L.peqa_qglu_fwd.argtypes = [qp, i32, vp, i32, vp, vp, vp]
+        L.peqa_qglu_fwd.argtypes = [qp, i32, vp, i32, vp, vp, vp, sz, vp]
         L.peqa_qglu_fwd.restype = ctypes.c_int
         L.peqa_glu_bwd.argtypes = [i32, vp, vp, i32, i32, vp, vp]
         L.peqa_glu_bwd.restype = ctypes.c_int
@@ -559,10 +559,11 @@ def glu_interleave(gate: QWeight, up: QWeight) -> QWeight:
                    glu_rows(gate.scales, up.scales))
 
 
-def qglu_fwd(w: QWeight, X: torch.Tensor, activation: str = "silu", keep: bool = True, Y=None, H=None):
+def qglu_fwd(w: QWeight, X: torch.Tensor, activation: str = "silu", keep: bool = True, Y=None, H=None, workspace=None):
     """Forward of a gated block (rows as glu_rows puts them): H = act(gate) * up bf16 [tokens, N / 2] and, with ``keep`` or a Y to
-    write, the sums Y bf16 [tokens, N] that glu_bwd wants; activation "silu" or "gelu_tanh".  Returns (H, Y or None)."""
-    return (_native or _load_native()).qglu_fwd(w, X, activation, keep, Y, H)
+    write, the sums Y bf16 [tokens, N] that glu_bwd wants; activation "silu" or "gelu_tanh".  A block with groups works in a workspace
+    (alloc_workspace(OP_GLU_FWD, tokens, w), or one of its own).  Returns (H, Y or None)."""
+    return (_native or _load_native()).qglu_fwd(w, X, activation, keep, Y, H, workspace)
 
 
 def glu_bwd(Y: torch.Tensor, dH: torch.Tensor, activation: str = "silu", dY=None):

@@ -150,6 +150,7 @@ extern "C" size_t peqa_workspace_bytes(int op, int T, const peqa_qweight_t* w) {
     case PEQA_OP_BWD: return ds_workspace_bytes(w, g, T);
     case PEQA_OP_DECODE: return decode_workspace_bytes(w, g, T);
     case PEQA_OP_BWD_DSDZ: return dsdz_workspace_bytes(w, g, T);
+    case PEQA_OP_GLU_FWD: return glu_workspace_bytes(w, g, T);
     case PEQA_OP_BWD_DS_FROM_Y: return g == w->in_features ? ds_from_y_workspace_bytes(w, T) : 0;
     default: return 0;
   }

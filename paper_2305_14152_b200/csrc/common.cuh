@@ -223,6 +223,7 @@ bool fwd_pair_supported(const peqa_qweight_t* w);
 struct GluOut;
 int launch_fwd_pair(const peqa_qweight_t* w, const float* zeros_f, int g, const void* X, int T,
                     void* Y, const void* dY, float* ds_part, cudaStream_t st, Side side, const GluOut* glu = nullptr);
+size_t glu_workspace_bytes(const peqa_qweight_t* w, int g, int T);
 int launch_glu_fwd(const peqa_qweight_t* w, int g, const void* X, int T, void* Y, const GluOut& glu, cudaStream_t st);
 bool dx_pair_supported(const peqa_qweight_t* w);
 int launch_dx_pair(const peqa_qweight_t* w, const float* zeros_f, int g, const void* dY, int T,

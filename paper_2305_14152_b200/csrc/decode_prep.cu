@@ -1568,7 +1568,7 @@ int run_decode(const peqa_qweight_t* w, const void* weights, bool canon, int g, 
     // for 9; of 4-bit weights, whose rings are larger, 70000, 103000 and 131000; with 512 columns about 1.9 times as many).
     const int h = (M + 1) / 2;
     const size_t K = (size_t)w->in_features, N = (size_t)w->out_features;
-    const GluOut behind = {pairs ? glu.H + (size_t)h * (N / 2) : nullptr, glu.act};
+    const GluOut behind = {pairs ? glu.H + (size_t)h * (N / 2) : nullptr, glu.act, nullptr};
     PEQA_TRY(run_decode(w, weights, false, g, X, h, Y, scale_table, n_tasks, task_ids, st, glu));
     return run_decode(w, weights, false, g, static_cast<const char*>(X) + (size_t)h * K * 2, M - h,
                       pairs ? nullptr : static_cast<char*>(Y) + (size_t)h * N * 2, scale_table, n_tasks,
@@ -1698,7 +1698,7 @@ extern "C" int peqa_qglu_decode_prepared(const peqa_qweight_t* w, int activation
   PEQA_TRY(check_decode_prepared(w, prepared, X, M, H, scale_table, n_tasks, task_ids));
   if (w->out_features % 16 != 0 || !glu_act_ok(activation)) return PEQA_ERR_BAD_SHAPE;
   PEQA_TRY(check_arch());
-  const GluOut glu = {static_cast<__nv_bfloat16*>(H), activation};
+  const GluOut glu = {static_cast<__nv_bfloat16*>(H), activation, nullptr};
   const int g = effective_group(w->in_features, w->group_size);
   return run_decode(w, prepared, false, g, X, M, nullptr, scale_table, n_tasks, task_ids, as_stream(stream), glu);
 }

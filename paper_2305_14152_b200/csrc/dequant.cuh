@@ -120,15 +120,23 @@ __device__ __forceinline__ void natural_zero_consts(uint32_t z, uint32_t (&zc)[n
   }
 }
 
+// The biases of each kind of pair.  HALF: binary16, whose ten bits of mantissa take a code at bit o with a bias of 2^(10 - o).
+template <int BITS, bool HALF>
+__host__ __device__ constexpr uint32_t natural_bias(int kind) {
+  if (BITS == 4) return HALF ? 0x64006400u : 0x43004300u;
+  return kind == 0 ? (HALF ? 0x58006400u : 0x41804300u) : kind == 1 ? (HALF ? 0x60005C00u : 0x42804200u) : (HALF ? 0x58005400u : 0x41804100u);
+}
+
 // The four biased pairs of block BLK of a unit.
-template <int BITS, int BLK>
+template <int BITS, int BLK, bool HALF = false>
 __device__ __forceinline__ void block8_raw(const uint32_t (&w)[BITS], uint32_t (&x)[4]) {
   if constexpr (BITS == 4) {
+    constexpr uint32_t bias = natural_bias<BITS, HALF>(0);
     const uint32_t v = w[BLK], c = v >> 4;
-    x[0] = lop3_and_or(prmt(v, c, 0x4400u), 0x000F000Fu, 0x43004300u);
-    x[1] = lop3_and_or(prmt(v, c, 0x5511u), 0x000F000Fu, 0x43004300u);
-    x[2] = lop3_and_or(prmt(v, c, 0x6622u), 0x000F000Fu, 0x43004300u);
-    x[3] = lop3_and_or(prmt(v, c, 0x7733u), 0x000F000Fu, 0x43004300u);
+    x[0] = lop3_and_or(prmt(v, c, 0x4400u), 0x000F000Fu, bias);
+    x[1] = lop3_and_or(prmt(v, c, 0x5511u), 0x000F000Fu, bias);
+    x[2] = lop3_and_or(prmt(v, c, 0x6622u), 0x000F000Fu, bias);
+    x[3] = lop3_and_or(prmt(v, c, 0x7733u), 0x000F000Fu, bias);
   } else {
     constexpr int at = 24 * BLK + 4;                        // first bit of the copy
     uint32_t c;
@@ -136,10 +144,10 @@ __device__ __forceinline__ void block8_raw(const uint32_t (&w)[BITS], uint32_t (
     else c = __funnelshift_r(w[at / 32], w[at / 32 + 1], at % 32);
     constexpr int b0 = 3 * BLK, b1 = b0 + 1, b2 = b0 + 2;   // the block's bytes
     // selectors: byte b % 4 of the word in the halves that take it (0 to 3), byte 4 + i of the copy in the others
-    x[0] = lop3_and_or(prmt(w[b0 / 4], c, (b0 % 4) * 0x1111u), 0x00380007u, 0x41804300u);
-    x[1] = lop3_and_or(prmt(w[b1 / 4], c, (b1 % 4) * 0x1100u + 0x0044u), 0x000E001Cu, 0x42804200u);
-    x[2] = lop3_and_or(prmt(w[b1 / 4], c, (b1 % 4) * 0x0011u + 0x5500u), 0x00380070u, 0x41804100u);
-    x[3] = lop3_and_or(prmt(w[b2 / 4], c, (b2 % 4) * 0x0011u + 0x6600u), 0x000E001Cu, 0x42804200u);
+    x[0] = lop3_and_or(prmt(w[b0 / 4], c, (b0 % 4) * 0x1111u), 0x00380007u, natural_bias<BITS, HALF>(0));
+    x[1] = lop3_and_or(prmt(w[b1 / 4], c, (b1 % 4) * 0x1100u + 0x0044u), 0x000E001Cu, natural_bias<BITS, HALF>(1));
+    x[2] = lop3_and_or(prmt(w[b1 / 4], c, (b1 % 4) * 0x0011u + 0x5500u), 0x00380070u, natural_bias<BITS, HALF>(2));
+    x[3] = lop3_and_or(prmt(w[b2 / 4], c, (b2 % 4) * 0x0011u + 0x6600u), 0x000E001Cu, natural_bias<BITS, HALF>(1));
   }
 }
 
@@ -169,6 +177,28 @@ __device__ __forceinline__ void unit32_natural(const uint32_t (&w)[BITS], uint32
   block8_natural<BITS, 1, FOLD>(w, zc, s2, out + 4);
   block8_natural<BITS, 2, FOLD>(w, zc, s2, out + 8);
   block8_natural<BITS, 3, FOLD>(w, zc, s2, out + 12);
+}
+
+// The same in binary16, (q - z) * s with s rounded to it: each rounding is off by 2^-11 at most where bf16's is by 2^-8.  s and z are such that
+// nothing leaves binary16's range.
+template <int BITS>
+__device__ __forceinline__ void unit32_half(const uint32_t (&w)[BITS], uint32_t z, float s, uint32_t (&out)[16]) {
+  constexpr uint32_t step[3] = {BITS == 4 ? 0x00010001u : 0x00080001u, 0x00020004u, 0x00080010u};
+  uint32_t zc[natural_kinds(BITS)], s2;
+#pragma unroll
+  for (int k = 0; k < natural_kinds(BITS); ++k) zc[k] = z * step[k] + natural_bias<BITS, true>(k);
+  asm("cvt.rn.f16x2.f32 %0, %1, %1;" : "=r"(s2) : "f"(s));
+  uint32_t x[4][4];
+  block8_raw<BITS, 0, true>(w, x[0]);
+  block8_raw<BITS, 1, true>(w, x[1]);
+  block8_raw<BITS, 2, true>(w, x[2]);
+  block8_raw<BITS, 3, true>(w, x[3]);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    uint32_t d;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(x[i / 4][i % 4]), "r"(zc[natural_kind(BITS, i % 4)]));
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(out[i]) : "r"(d), "r"(s2));
+  }
 }
 
 // Splits a real-valued zero-point into the integer the exact dequantization can use and

@@ -66,7 +66,7 @@ struct PairBarriers {
 
 struct PairParams {
   const uint8_t* zeros;
-  const float* zeros_f;   // real-valued zero-points (App. K) or nullptr; replaces `zeros`
+  const float* zeros_f;   // real-valued zero-points (App. K) or nullptr; replaces `zeros`; GLU: GluOut::factors
   const float* scales;
   __nv_bfloat16* out;   // Y [T, N]
   int N, K, G, g, g_shift, T;
@@ -108,13 +108,14 @@ template <int BITS, bool FOLD, bool ZF, bool DS, bool GLU>
 __global__ void __launch_bounds__(kPairThreads, 1)
 qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_q,
                  const __grid_constant__ CUtensorMap tmap_y, const PairParams p) {
+  constexpr bool HALF = GLU && FOLD;                      // binary16 operands
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
   uint8_t* sm_q = base + PSTAGES * PSTAGE_BYTES;          // PQ_SLOTS x 4 KiB, plain 32-byte rows
   uint8_t* sm_e = sm_q + PQ_SLOTS * PQ_BYTES;             // 8 epilogue warps x 2 KiB, 64-byte swizzle
   PairBarriers* bars = reinterpret_cast<PairBarriers*>(sm_e + 8 * PE_BYTES);
-  float* sm_scales = reinterpret_cast<float*>(sm_e + 8 * PE_BYTES + 512);     // GLU with one scale per channel: the tile's 256
+  float* sm_scales = reinterpret_cast<float*>(sm_e + 8 * PE_BYTES + 512);     // GLU: what the tile's 256 channels are multiplied by
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const bool leader = rank == 0;
@@ -210,7 +211,7 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
       // One thread issues everything, the MMAs of a stage in a few cycles each (see elect_lane), so the tensor pipe has work
       // while this thread waits for the next stage.  Weights and activations share a barrier, and descriptors are advanced
       // by additions (the address field counts 16-byte units).
-      constexpr uint32_t idesc = idesc_bf16_f32(256, 256, 0, 0);
+      constexpr uint32_t idesc = HALF ? idesc_f16_f32(256, 256, 0, 0) : idesc_bf16_f32(256, 256, 0, 0);
       const uint32_t a0 = smem_u32(base);
       const uint64_t adesc0 = smem_desc_sw128(a0, 16, 1024);
       const uint64_t bdesc0 = smem_desc_sw128(a0 + PA_BYTES, 16, 1024);
@@ -273,12 +274,11 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
         // Sixteen columns at a time, eight channels' gate and up sums.  (The next sixteen asked for meanwhile took registers that the dequant warps'
         // code went without: 1024 columns, us, so / as it is 175.6 / 169.3.)  Scales come from shared memory, four a read that all lanes share.  (All warps of a CTA come by here as often, whether or not a wait runs out: a tile's
         // accumulators are full for all or for none.)
-        if (!FOLD) {
-          const int c = (warp - 4) * 32 + lane;
-          named_barrier_sync(2, 256);              // the last tile's have been read
-          sm_scales[c] = n0 + c < p.N ? ld_global(p.scales + n0 + c) : 0.0f;
-          named_barrier_sync(2, 256);
-        }
+        const int own = (warp - 4) * 32 + lane;
+        named_barrier_sync(2, 256);              // the last tile's have been read
+        sm_scales[own] = n0 + own < p.N ? ld_global((HALF ? p.zeros_f : p.scales) + n0 + own) : 0.0f;
+        named_barrier_sync(2, 256);
+        const float token = HALF && row0 + lane < p.T ? ld_global(p.zeros_f + p.N + row0 + lane) : 1.0f;
         if (!warp_wait_cluster(smem_u32(&bars->acc_full), (uint32_t)(local & 1), abort_flag)) { ok = false; break; }
         tc_fence_after();
         const int units = m < blocks ? min(16, (p.N - n0) / 16) : 0;
@@ -303,10 +303,10 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
               float y[16];
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const float4 sc = FOLD ? make_float4(1.0f, 1.0f, 1.0f, 1.0f) : *reinterpret_cast<const float4*>(sm_scales + at * 16 + 4 * e);
+                const float4 sc = *reinterpret_cast<const float4*>(sm_scales + at * 16 + 4 * e);
                 const float s4[4] = {sc.x, sc.y, sc.z, sc.w};
 #pragma unroll
-                for (int k = 0; k < 4; ++k) y[4 * e + k] = FOLD ? __uint_as_float(v[4 * e + k]) : __uint_as_float(v[4 * e + k]) * s4[k];
+                for (int k = 0; k < 4; ++k) y[4 * e + k] = __uint_as_float(v[4 * e + k]) * (HALF ? s4[k] * token : s4[k]);
               }
               if (p.glu.act == PEQA_ACT_SILU) glu_pack<PEQA_ACT_SILU>(y, o + 4 * side);
               else glu_pack<PEQA_ACT_GELU_TANH>(y, o + 4 * side);
@@ -574,6 +574,9 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
       if constexpr (ZF) {
         dq::unit32_affine<BITS>(w[0], z[0], sc[0], o0);
         dq::unit32_affine<BITS>(w[1], one_group ? z[0] : z[1], s1, o1);
+      } else if constexpr (HALF) {
+        dq::unit32_half<BITS>(w[0], pair_load ? z[0] & 0xFFu : z[0], sc[0], o0);
+        dq::unit32_half<BITS>(w[1], one_group ? z[0] : pair_load ? z[0] >> 8 : z[1], s1, o1);
       } else {
         dq::unit32_natural<BITS, FOLD>(w[0], pair_load ? z[0] & 0xFFu : z[0], sc[0], o0);
         dq::unit32_natural<BITS, FOLD>(w[1], one_group ? z[0] : pair_load ? z[0] >> 8 : z[1], s1, o1);
@@ -622,7 +625,7 @@ int launch_pair_t(const CUtensorMap& tx, const CUtensorMap& tq, const CUtensorMa
                   int pairs, cudaStream_t st) {
   auto kern = qfwd_pair_kernel<BITS, FOLD, ZF, DS, GLU>;
   static std::atomic<uint64_t> done{0};
-  constexpr int kSmem = P_SMEM_BYTES + (GLU && !FOLD ? 1024 : 0);
+  constexpr int kSmem = P_SMEM_BYTES + (GLU ? 1024 : 0);
   PEQA_TRY(allow_smem(kern, kSmem, done));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * pairs, 1, 1);
@@ -663,6 +666,7 @@ int launch_fwd_pair(const peqa_qweight_t* w, const float* zeros_f, int g, const 
   p.dY = static_cast<const __nv_bfloat16*>(dY);
   p.ds_part = ds_part;
   if (glu) {
+    p.zeros_f = glu->factors;
     p.H = glu->H;
     p.glu.act = glu->act;
     p.glu.wide = w->out_features % 32 == 0 && reinterpret_cast<uintptr_t>(glu->H) % 32 == 0;

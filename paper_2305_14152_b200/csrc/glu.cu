@@ -58,13 +58,114 @@ __global__ void __launch_bounds__(kBackThreads) glu_bwd_kernel(const uint4* Y, c
   dY[2 * u + 1] = make_uint4(b[0], b[1], b[2], b[3]);
 }
 
+// Operands of a block with groups, in binary16 (see GluOut).  A CTA a token: its largest channel brought to [2^14, 2^15), so that all that is more than
+// 2^-28 of it keeps its bits.  Behind the tokens' CTAs a warp for eight rows: a row's largest scale brought to [1, 2).  (A warp a token and a
+// warp a row took 7.5 us for 77 tokens and 22016 rows of 32 groups, 16 for 4096 tokens.)
+constexpr int kRowsOfWarp = 8;
+constexpr int kRowsOfCta = kRowsOfWarp * kBackThreads / 32;
+constexpr int kHeld = 4;                          // 16-byte pieces of a token that a thread keeps between the two passes
+
+// 2^e for |e| <= 126, and the exponent that takes the largest of these bits to 2^target; what is not finite stays so.
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+__device__ __forceinline__ int shift_to(uint32_t largest, int target) {
+  const int e = (int)(largest >> 23 & 255u);
+  return e == 255 ? 0 : max(-126, min(126, target + 127 - e));
+}
+__device__ __forceinline__ uint32_t largest_of(const uint4& v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t most = 0u;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) most = max(most, max(w[e] << 16 & 0x7FFF0000u, w[e] & 0x7FFF0000u));
+  return most;
+}
+__device__ __forceinline__ uint4 to_half(const uint4& v, float by) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t o[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(o[q]) : "f"(high(w[q]) * by), "f"(low(w[q]) * by));
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+__global__ void __launch_bounds__(kBackThreads) glu_operands_kernel(const uint4* X, const float* scales, int T, int K, int N, int G,
+                                                                    uint4* halves, float* scaled, float* factors) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (blockIdx.x < T) {
+    __shared__ uint32_t part[kBackThreads / 32];
+    const int pieces = K / 8;
+    const uint4* x = X + (size_t)blockIdx.x * pieces;
+    uint4 held[kHeld];
+    uint32_t most = 0u;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int c = (int)threadIdx.x + i * kBackThreads;
+      held[i] = c < pieces ? ptx::ld_global(x + c) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) most = max(most, largest_of(held[i]));
+    for (int c = (int)threadIdx.x + kHeld * kBackThreads; c < pieces; c += kBackThreads) most = max(most, largest_of(ptx::ld_global(x + c)));
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) part[warp] = most;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kBackThreads / 32; ++w) most = max(most, part[w]);
+    const int e = shift_to(most, 14);
+    const float by = power_of_two(e);
+    uint4* out = halves + (size_t)blockIdx.x * pieces;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int c = (int)threadIdx.x + i * kBackThreads;
+      if (c < pieces) out[c] = to_half(held[i], by);
+    }
+    for (int c = (int)threadIdx.x + kHeld * kBackThreads; c < pieces; c += kBackThreads) out[c] = to_half(ptx::ld_global(x + c), by);
+    if (threadIdx.x == 0) factors[N + blockIdx.x] = power_of_two(-e);
+    return;
+  }
+  const int row0 = ((int)blockIdx.x - T) * kRowsOfCta + warp * kRowsOfWarp;
+  float s[kRowsOfWarp];                           // the first 32 groups of each row, all asked for before the first is used
+#pragma unroll
+  for (int r = 0; r < kRowsOfWarp; ++r) s[r] = row0 + r < N && lane < G ? ptx::ld_global(scales + (size_t)(row0 + r) * G + lane) : 0.0f;
+#pragma unroll
+  for (int r = 0; r < kRowsOfWarp; ++r) {
+    if (row0 + r >= N) break;
+    const float* from = scales + (size_t)(row0 + r) * G;
+    float* to = scaled + (size_t)(row0 + r) * G;
+    uint32_t most = __float_as_uint(s[r]) & 0x7FFFFFFFu;
+    for (int g = lane + 32; g < G; g += 32) most = max(most, __float_as_uint(ptx::ld_global(from + g)) & 0x7FFFFFFFu);
+    const int e = shift_to(__reduce_max_sync(0xffffffffu, most), 0);
+    const float by = power_of_two(e);
+    if (lane < G) to[lane] = s[r] * by;
+    for (int g = lane + 32; g < G; g += 32) to[g] = ptx::ld_global(from + g) * by;
+    if (lane == 0) factors[row0 + r] = power_of_two(-e);
+  }
+}
+
+// The workspace of a block with groups.
+struct GluWorkspace {
+  size_t halves, scaled, factors, bytes;
+};
+GluWorkspace glu_workspace(const peqa_qweight_t* w, int G, int T) {
+  GluWorkspace ws = {};
+  if (G == 1) return ws;
+  auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
+  const size_t N = (size_t)w->out_features;
+  ws.scaled = up((size_t)T * w->in_features * 2);
+  ws.factors = ws.scaled + up(N * G * sizeof(float));
+  ws.bytes = ws.factors + up((N + T) * sizeof(float));
+  return ws;
+}
+
 }  // namespace
+
+size_t glu_workspace_bytes(const peqa_qweight_t* w, int g, int T) { return glu_workspace(w, w->in_features / g, T).bytes; }
 
 }  // namespace peqa
 
 using namespace peqa;
 
-extern "C" int peqa_qglu_fwd(const peqa_qweight_t* w, int activation, const void* X, int T, void* Y, void* H, void* stream) {
+extern "C" int peqa_qglu_fwd(const peqa_qweight_t* w, int activation, const void* X, int T, void* Y, void* H, void* workspace,
+                             size_t workspace_bytes, void* stream) {
   int g = 0, G = 0;
   PEQA_TRY(check_qweight(w, &g, &G));
   if (!X || !H) return PEQA_ERR_NULL;
@@ -72,7 +173,22 @@ extern "C" int peqa_qglu_fwd(const peqa_qweight_t* w, int activation, const void
     return PEQA_ERR_BAD_SHAPE;
   if (!aligned16(X) || !aligned16(Y) || !aligned16(H)) return PEQA_ERR_ALIGNMENT;
   PEQA_TRY(check_arch());
-  return launch_glu_fwd(w, g, X, T, Y, GluOut{static_cast<__nv_bfloat16*>(H), activation}, as_stream(stream));
+  const GluWorkspace at = glu_workspace(w, G, T);
+  GluOut glu = {static_cast<__nv_bfloat16*>(H), activation, nullptr};
+  cudaStream_t st = as_stream(stream);
+  if (at.bytes == 0) return launch_glu_fwd(w, g, X, T, Y, glu, st);
+  if (!workspace || workspace_bytes < at.bytes) return PEQA_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return PEQA_ERR_ALIGNMENT;
+  char* ws = static_cast<char*>(workspace);
+  float *scaled = reinterpret_cast<float*>(ws + at.scaled), *factors = reinterpret_cast<float*>(ws + at.factors);
+  const long long ctas = (long long)T + (w->out_features + kRowsOfCta - 1) / kRowsOfCta;
+  if (ctas > INT32_MAX) return PEQA_ERR_TOO_LARGE;
+  PEQA_TRY(launch_after(glu_operands_kernel, (int)ctas, kBackThreads, st, static_cast<const uint4*>(X), w->scales, T, (int)w->in_features,
+                        (int)w->out_features, G, reinterpret_cast<uint4*>(ws + at.halves), scaled, factors));
+  peqa_qweight_t half = *w;
+  half.scales = scaled;
+  glu.factors = factors;
+  return launch_glu_fwd(&half, g, ws + at.halves, T, Y, glu, st);
 }
 
 extern "C" int peqa_glu_bwd(int activation, const void* Y, const void* dH, int T, int F, void* dY, void* stream) {

@@ -11,9 +11,14 @@ namespace peqa {
 constexpr int kGluRun = 8;       // rows of a run
 
 // What a forward kernel makes of the block's sums beside storing them.
+//
+// Scales of groups lie on the contraction, so they go into the operand, and rounded to bf16 there they and the products are off by 2^-9 of themselves in the
+// mean: two such sums multiplied had twice the error that the rounding of H has.  So with groups the operands are binary16 (2^-12): X times a power of two
+// per token, scales times one per row, which glu_operands_kernel (glu.cu) makes and the epilogue takes off.
 struct GluOut {
   __nv_bfloat16* H;              // [tokens, F]; nullptr: an ordinary linear
   int act;                       // peqa_activation
+  const float* factors;          // groups: what the sums are multiplied by, [2F] and behind them [tokens]
 };
 
 inline bool glu_act_ok(int act) { return act == PEQA_ACT_SILU || act == PEQA_ACT_GELU_TANH; }

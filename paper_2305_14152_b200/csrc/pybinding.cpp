@@ -280,10 +280,10 @@ int64_t glu_tokens(const at::Tensor& X, const peqa_qweight_t& w) {
   return X.size(0);
 }
 
-// (w, X, activation, keep, Y, H) -> (H, Y)
+// (w, X, activation, keep, Y, H, workspace) -> (H, Y)
 PyObject* qglu_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  arity(n, 6);
+  arity(n, 7);
   const peqa_qweight_t w = weight(a[0]);
   const at::Tensor& X = dev(a[1], at::kBFloat16, "X");
   const int64_t T = glu_tokens(X, w);
@@ -291,8 +291,19 @@ PyObject* qglu_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (keep < 0) fail();
   at::Tensor H = matrix(a[5], X, {T, w.out_features / 2}, at::kBFloat16, "H"), Y;
   if (keep || a[4] != Py_None) Y = matrix(a[4], X, {T, w.out_features}, at::kBFloat16, "Y");
+  const Workspace given(a[6]);
+  at::Tensor own;
+  void* wp = given.p;
+  size_t wb = given.bytes;
+  if (a[6] == Py_None) {
+    wb = peqa_workspace_bytes(PEQA_OP_GLU_FWD, (int)T, &w);
+    if (wb > 0) {
+      own = at::empty({(int64_t)wb}, X.options().dtype(at::kByte));
+      wp = own.data_ptr();
+    }
+  }
   void *x = X.data_ptr(), *h = H.data_ptr(), *y = Y.defined() ? Y.data_ptr() : nullptr, *st = stream();
-  check(unlocked([&] { return peqa_qglu_fwd(&w, act, x, (int)T, y, h, st); }), "peqa_qglu_fwd");
+  check(unlocked([&] { return peqa_qglu_fwd(&w, act, x, (int)T, y, h, wp, wb, st); }), "peqa_qglu_fwd");
   Ref first(THPVariable_Wrap(std::move(H)));
   if (!y) return PyTuple_Pack(2, first.p, Py_None);
   Ref second(THPVariable_Wrap(std::move(Y)));

@@ -68,7 +68,7 @@ struct SplitBarriers {
 
 struct SplitParams {
   const uint8_t* zeros;
-  const float* zeros_f;   // real-valued zero-points (App. K) or nullptr; replaces `zeros`
+  const float* zeros_f;   // real-valued zero-points (App. K) or nullptr; replaces `zeros`; GLU: GluOut::factors
   const float* scales;
   __nv_bfloat16* out;     // [T, R]
   int N, K, G, g, g_shift, T;
@@ -260,7 +260,7 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
   } else if (warp == 1) {
     // ------------------------------------------------- MMA issuer (one lane)
     if (const uint32_t lane = elect_lane(); lane == 0) {
-      const uint32_t idesc = idesc_bf16_f32(SM_ROWS, 16, TRANS ? 1 : 0, 0) +
+      const uint32_t idesc = (GLU && FOLD ? idesc_f16_f32(SM_ROWS, 16, TRANS ? 1 : 0, 0) : idesc_bf16_f32(SM_ROWS, 16, TRANS ? 1 : 0, 0)) +
                              ((uint32_t)((p.nt - 16) >> 3) << 17);
       // Descriptors are advanced by additions (the address field counts 16-byte units).
       const uint32_t a0 = smem_u32(base);
@@ -375,6 +375,7 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
         const uint32_t z = one_group ? cur[0].z : cur[k].z;
         const float sc = one_group ? cur[0].s : cur[k].s;
         if constexpr (ZF) dq::unit32_affine<BITS>(w[k], z, sc, o[k]);
+        else if constexpr (GLU && FOLD) dq::unit32_half<BITS>(w[k], z, sc, o[k]);
         else dq::unit32_natural<BITS, FOLD>(w[k], z, sc, o[k]);
       }
       const int s = it % p.stages;
@@ -505,6 +506,11 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
             ds.y = fmaf(a.y, __uint_as_float(y.x & 0xFFFF0000u), ds.y);
             ds.z = fmaf(a.z, __uint_as_float(y.y << 16), ds.z);
             ds.w = fmaf(a.w, __uint_as_float(y.y & 0xFFFF0000u), ds.w);
+          }
+          if constexpr (GLU && FOLD) {
+            const float4 sc = ld_global(reinterpret_cast<const float4*>(p.zeros_f + row));
+            const float token = ld_global(p.zeros_f + p.N + t0 + t);
+            a.x *= sc.x * token; a.y *= sc.y * token; a.z *= sc.z * token; a.w *= sc.w * token;
           }
           if (!FOLD) {
             const float4 sc = ld_global(reinterpret_cast<const float4*>(p.scales + row));   // one scale per channel
@@ -742,6 +748,7 @@ int launch_split(const peqa_qweight_t* w, const float* zeros_f, int g, const voi
   if (glu) {
     p.H = glu->H;
     p.act = glu->act;
+    p.zeros_f = glu->factors;
   }
   p.N = w->out_features;
   p.K = w->in_features;

@@ -37,15 +37,17 @@ def act(x, activation):
 
 
 def forward(X, W, activation, folded):
-    """(H, Y, tolerances of both).  folded: the operand is (Q - z) bf16(s) rounded to bf16 (groups of columns); else codes are exact."""
+    """(H, Y, tolerances of both).  folded: the operand is (Q - z) s in binary16 (groups of columns); else codes are exact."""
     X64 = X.double()
     Y = X64 @ W.T
     K = X.shape[1]
     size = X64.abs() @ W.abs().T
-    # two half steps of bf16 where scales are folded in; a binary32 sum of 16 products at a time, which may drop what is below 2^-23 of the
-    # sum of magnitudes; the scale's own product; few tokens: activations are rounded at 2^-25 of the row's largest
-    d = size * ((2 * 2.0 ** -8 if folded else 0.0) + (K / 16 + 6) * 2.0 ** -23) \
+    # two half steps of binary16 where scales are folded in, in units that the row's largest follows; a binary32 sum of 16 products at a time, which
+    # may drop what is below 2^-23 of the sum of magnitudes; the scale's own product; activations are rounded at 2^-25 of the row's largest
+    d = size * ((2 * 2.0 ** -11 if folded else 0.0) + (K / 16 + 6) * 2.0 ** -23) \
         + 2.0 ** -25 * X64.abs().amax(1, keepdim=True) * W.abs().sum(1)[None]
+    if folded:
+        d = d + 2.0 ** -24 * X64.abs().sum(1, keepdim=True) * W.abs().amax(1)[None]
     gate, up = halves(Y)
     dg, du = halves(d)
     a = act(gate, activation)

@@ -27,7 +27,7 @@ def weight(p, bits=4, N=64, K=256, group=0, **more):
 
 
 def test_forward(L, p):
-    call = lambda w, act=0, X=p, T=4, Y=p, H=p: L.peqa_qglu_fwd(w, act, X, T, Y, H, 0)
+    call = lambda w, act=0, X=p, T=4, Y=p, H=p: L.peqa_qglu_fwd(w, act, X, T, Y, H, p, 1 << 40, 0)
     w = weight(p)
     assert call(w, X=0) == NULL and call(w, H=0) == NULL and call(None) == NULL and call(weight(p, z=0)) == NULL
     assert call(w, X=p + 8) == ALIGN and call(w, H=p + 8) == ALIGN and call(w, Y=p + 8) == ALIGN

@@ -27,7 +27,8 @@ def test_forward(T, F, K, group, bits):
     H, Y = binding.qglu_fwd(w, X, act)
     alone, none = binding.qglu_fwd(w, X, act, keep=False)
     assert none is None and torch.equal(H, alone)
-    assert torch.equal(Y, binding.qlinear_fwd(w, X))
+    if w.G == 1:
+        assert torch.equal(Y, binding.qlinear_fwd(w, X))
     binding.check_status()
     want, want_Y, tol, tol_Y = forward(X, W, act, w.G > 1)
     assert_within(Y, want_Y, tol_Y, "Y")
@@ -42,6 +43,32 @@ def test_forward_of_odd_multiples_of_64_columns(T, F, K):
     want, want_Y, tol, tol_Y = forward(X, W, "silu", w.G > 1)
     assert_within(Y, want_Y, tol_Y, "Y")
     assert_within(H, want, tol, "H")
+
+
+@pytest.mark.parametrize("T", [30, 600])
+def test_forward_of_scales_and_tokens_of_any_size(T):
+    """Rows whose scales are far apart, or all 0; tokens from 2^-100 to 2^100, of zeros, with channels far below the largest."""
+    F, K = 40, 512
+    w, _, codes = block(F, K, 4, 64, seed=50)
+    w.scales *= 2.0 ** (torch.arange(2 * F, device="cuda") % 40 - 20)[:, None]
+    w.scales[:, 1::2] *= 2.0 ** -9
+    w.scales[16:24] = 0
+    from glu_util import weights
+    W = weights(codes, w.zeros, w.scales)
+    X = (rows(T, K, 51) * 2.0 ** (10 * (torch.arange(T, device="cuda") % 5 - 2))[:, None]).bfloat16()
+    X[3] *= 2.0 ** -80
+    X[4] = 0
+    X[5, ::2] *= 2.0 ** -20
+    H, Y = binding.qglu_fwd(w, X)
+    want, want_Y, tol, tol_Y = forward(X, W, "silu", True)
+    assert_within(Y, want_Y, tol_Y + 2.0 ** -126, "Y")
+    near = want_Y.abs().amax(1) < 2.0 ** 60                    # products within binary32
+    assert_within(H[near], want[near], tol[near] + 2.0 ** -126, "H")
+    X[7, 9], X[8, 9] = float("inf"), float("nan")
+    Y2 = binding.qglu_fwd(w, X)[1]
+    assert not Y2[7:9, w.scales.amax(1) > 0].isfinite().all() and Y2[8].isnan().all()
+    keep = [t for t in range(T) if t not in (7, 8)]
+    assert torch.equal(Y2[keep], Y[keep])
 
 
 @pytest.mark.parametrize("T,F", [(40, 520), (1500, 520), (40, 264), (1500, 264)])
@@ -185,6 +212,12 @@ def test_a_training_step_to_the_loss(bits, group):
 
 def test_what_is_refused():
     w, _, _ = block(64, 256, 4, 64, seed=40)
+    X = rows(20, 256, 41)
+    ws = binding.alloc_workspace(binding.OP_GLU_FWD, 20, w)
+    for bad, status in ((ws[:-256], -5), (torch.cat([ws, ws])[16:], -4)):
+        with pytest.raises(binding.PeqaError) as e:
+            binding.qglu_fwd(w, X, workspace=bad)
+        assert e.value.status == status
     X, H = rows(20, 256, 41), torch.zeros((20, 64), dtype=torch.bfloat16, device="cuda")
     Y = torch.zeros((20, 128), dtype=torch.bfloat16, device="cuda")
     prepared = binding.decode_prepare(w)
