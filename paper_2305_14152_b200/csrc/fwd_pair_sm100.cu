@@ -272,8 +272,8 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
       const int row0 = tt0 + m * 256 + (int)rank * 128 + quarter * 32;   // first token of this warp
       if constexpr (GLU) {
         // Sixteen columns at a time, eight channels' gate and up sums.  (The next sixteen asked for meanwhile took registers that the dequant warps'
-        // code went without: 1024 columns, us, so / as it is 175.6 / 169.3.)  Scales come from shared memory, four a read that all lanes share.  (All warps of a CTA come by here as often, whether or not a wait runs out: a tile's
-        // accumulators are full for all or for none.)
+        // code went without: 1024 columns, us, so / as it is 175.6 / 169.3.)  Scales come from shared memory, four a read that all lanes share.
+        // (All warps of a CTA come by these barriers as often, whether or not a wait runs out: a tile's accumulators are full for all or for none.)
         const int own = (warp - 4) * 32 + lane;
         named_barrier_sync(2, 256);              // the last tile's have been read
         sm_scales[own] = n0 + own < p.N ? ld_global((HALF ? p.zeros_f : p.scales) + n0 + own) : 0.0f;

@@ -661,9 +661,10 @@ LossPlan plan_loss(int T, int V, int K, bool grad, int sms) {
   c.chunks = (int)((all + c.rows - 1) / c.rows);
   const int blocks = c.rows / kTile;
   c.few = T <= kFewTokens;
-  // 64 MB of exponentials a piece; few tokens' twice that, since what their launches do is read the head, which one pass over
-  // it, logits, and another, gradient, do best (four pieces of 32000 x 4096, whose second reads would be L2's: 150 tokens 133 -> 172 us)
-  const long long wide = ((c.few ? 128ll : 64ll) << 20) / (2ll * c.rows);
+  // 96 MB of exponentials a piece (4096 tokens at 32000 x 8192, us: 32 MB 3540, 64 3390, 96 3350, 128 3330; every piece's sums of the gradient go to memory
+  // once more); few tokens' 128, since what their launches do is read the head, which one pass over it, logits, and another, gradient, do
+  // best (four pieces of 32000 x 4096, whose second reads would be L2's: 150 tokens 133 -> 172)
+  const long long wide = ((c.few ? 128ll : 96ll) << 20) / (2ll * c.rows);
   c.pieces = grad ? (int)((V + wide - 1) / wide) : 1;
   // Where all tiles of logits are one launch's, they are as wide as shares them out best: rounds of the pairs, each a tile's contraction,
   // which takes a time proportional to its width, and a sixteenth of a full one's for what does not.
