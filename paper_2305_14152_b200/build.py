@@ -16,7 +16,7 @@ NATIVE_SRC = os.path.join(CSRC, "pybinding.cpp")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-Xcompiler", "-fPIC", "-shared", "-Xptxas", "-v",
+    "-Xcompiler", "-fPIC", "-shared", "-Xptxas", "-v", "--threads", "0",
     "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
 
