@@ -58,7 +58,7 @@ struct PairBarriers {
   uint64_t pk_empty[PQ_SLOTS];  // each CTA: the group that owns the slot has read it
   uint64_t acc_full;            // each CTA: both accumulators ready
   uint64_t acc_empty;           // leader: both CTAs' epilogues drained them
-  uint64_t ds_full, ds_free;    // each CTA (DS): the epilogue warps' sums of a tile lie ready / have been read
+  uint64_t ds_full, ds_free;    // each CTA (DS): the epilogue warps' sums of a tile lie ready / have been read; GLU, ds_full: acc_empty of the second block
   uint32_t tmem_base;
   int abort_flag;
   int wait_limit_us;    // must follow abort_flag (read by the bounded waits)
@@ -132,7 +132,7 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
     }
     mbar_init(smem_u32(&bars->acc_full), 1);
     mbar_init(smem_u32(&bars->acc_empty), 16);            // 8 epilogue warps in each CTA
-    mbar_init(smem_u32(&bars->ds_full), 8);
+    mbar_init(smem_u32(&bars->ds_full), GLU ? 16 : 8);
     mbar_init(smem_u32(&bars->ds_free), 8);
     bars->abort_flag = 0;
     bars->wait_limit_us = p.status[4];
@@ -224,7 +224,42 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
         pair_item(p.items, tile, p.T, n_tile, tt0, blocks);
         if (!mbar_wait_cluster(smem_u32(&bars->acc_empty), (uint32_t)(local & 1) ^ 1u, abort_flag)) { ok = false; break; }
         tc_fence_after();
-        for (int kb = 0; kb < p.k_blocks; ++kb) {
+        int kb0 = 0;
+        if constexpr (GLU) {
+          // The first stages multiply the first block of tokens while the second one's last sums are still being worked on, then the second
+          const int ahead = p.k_blocks < PSTAGES ? p.k_blocks : PSTAGES;
+          uint32_t s1 = s, ph1 = ph;
+          for (int m = 0; ok && m < 2; ++m) {
+            if (m == 1) {
+              if (!mbar_wait_cluster(smem_u32(&bars->ds_full), (uint32_t)(local & 1) ^ 1u, abort_flag)) { ok = false; break; }
+              tc_fence_after();
+              s1 = s;
+              ph1 = ph;
+            }
+            for (int kb = 0; kb < ahead; ++kb) {
+              if (m == 0) {
+                if (!mbar_wait_cluster(full0 + s1 * 8, ph1, abort_flag)) { ok = false; break; }
+                tc_fence_after();
+              }
+              const uint64_t adesc = adesc0 + s1 * (PSTAGE_BYTES >> 4) + m * (PBLK_BYTES >> 4), bdesc = bdesc0 + s1 * (PSTAGE_BYTES >> 4);
+              if (m < blocks) {
+#pragma unroll
+                for (int k = 0; k < PK / 16; ++k)
+                  mma_bf16_ss_pair(tmem_base + m * 256, adesc + k * (32 / 16), bdesc + k * (32 / 16), idesc, (kb | k) != 0 ? 1u : 0u);
+              }
+              if (m == 1) mma_commit_pair(empty0 + s1 * 8, 3);
+              if (++s1 == PSTAGES) {
+                s1 = 0;
+                ph1 ^= 1u;
+              }
+            }
+          }
+          if (!ok) break;
+          s = s1;
+          ph = ph1;
+          kb0 = ahead;
+        }
+        for (int kb = kb0; kb < p.k_blocks; ++kb) {
           if (!mbar_wait_cluster(full0 + s * 8, ph, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const uint64_t adesc = adesc0 + s * (PSTAGE_BYTES >> 4), bdesc = bdesc0 + s * (PSTAGE_BYTES >> 4);
@@ -278,74 +313,82 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
         named_barrier_sync(2, 256);              // the last tile's have been read
         sm_scales[own] = n0 + own < p.N ? ld_global((HALF ? p.zeros_f : p.scales) + n0 + own) : 0.0f;
         named_barrier_sync(2, 256);
-        const float token = HALF && row0 + lane < p.T ? ld_global(p.zeros_f + p.N + row0 + lane) : 1.0f;
         if (!warp_wait_cluster(smem_u32(&bars->acc_full), (uint32_t)(local & 1), abort_flag)) { ok = false; break; }
         tc_fence_after();
-        const int units = m < blocks ? min(16, (p.N - n0) / 16) : 0;
-        const uint32_t acc = tmem_base + ((uint32_t)(quarter * 32) << 16) + m * 256;
-        const bool live = row0 + lane < p.T;
-        __nv_bfloat16* h_row = p.H + (size_t)(row0 + lane) * (p.N >> 1) + (n0 >> 1);
-        uint32_t v[16], o[8];
+        // All warps take the first block of tokens, then the second, 128 columns each, so that the next tile's products for the first may begin under
+        // the second's epilogue.
+        const uint32_t second_empty_leader = mapa_shared(smem_u32(&bars->ds_full), 0);
+        const int first = m * 128, units = max(0, min(8, (p.N - n0 - first) / 16));
 #pragma unroll 1
-        for (int u = 0; u < units; u += 2) {
+        for (int b = 0; b < 2; ++b) {
+          const int rows = tt0 + b * 256 + (int)rank * 128 + quarter * 32, mine = b < blocks ? units : 0;
+          const uint32_t acc = tmem_base + ((uint32_t)(quarter * 32) << 16) + b * 256 + first;
+          const bool live = rows + lane < p.T;
+          const float token = HALF && live ? ld_global(p.zeros_f + p.N + rows + lane) : 1.0f;
+          __nv_bfloat16* h_row = p.H + (size_t)(rows + lane) * (p.N >> 1) + ((n0 + first) >> 1);
+          const uint32_t drained = b == 0 ? acc_empty_leader : second_empty_leader;
+          uint32_t v[16], o[8];
+#pragma unroll 1
+          for (int u = 0; u < mine; u += 2) {
 #pragma unroll
-          for (int side = 0; side < 2; ++side) {
-            const int at = u + side;
-            if (at < units) {
-              tmem_ld_32x16(acc + at * 16, v);
-              tmem_ld_wait();
-              if (at + 1 == units) {
-                // nothing of this tile is left in tensor memory for this warp
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(acc_empty_leader);
-              }
-              float y[16];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float4 sc = *reinterpret_cast<const float4*>(sm_scales + at * 16 + 4 * e);
-                const float s4[4] = {sc.x, sc.y, sc.z, sc.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) y[4 * e + k] = __uint_as_float(v[4 * e + k]) * (HALF ? s4[k] * token : s4[k]);
-              }
-              if (p.glu.act == PEQA_ACT_SILU) glu_pack<PEQA_ACT_SILU>(y, o + 4 * side);
-              else glu_pack<PEQA_ACT_GELU_TANH>(y, o + 4 * side);
-              if (p.out) {
-                if (side == 0) {
-                  if (lane == 0) bulk_wait_group_read0();
+            for (int side = 0; side < 2; ++side) {
+              const int at = u + side;
+              if (at < mine) {
+                tmem_ld_32x16(acc + at * 16, v);
+                tmem_ld_wait();
+                if (at + 1 == mine) {
+                  // nothing of this block is left in tensor memory for this warp
+                  tc_fence_before();
                   __syncwarp();
+                  if (lane == 0) mbar_arrive_cluster(drained);
                 }
+                float y[16];
 #pragma unroll
-                for (int q = 0; q < 2; ++q)
-                  *reinterpret_cast<uint4*>(srow + (((side * 2 + q) ^ sw) << 4)) =
-                      make_uint4(bf16_pair(y[8 * q], y[8 * q + 1]), bf16_pair(y[8 * q + 2], y[8 * q + 3]),
-                                 bf16_pair(y[8 * q + 4], y[8 * q + 5]), bf16_pair(y[8 * q + 6], y[8 * q + 7]));
+                for (int e = 0; e < 4; ++e) {
+                  const float4 sc = *reinterpret_cast<const float4*>(sm_scales + first + at * 16 + 4 * e);
+                  const float s4[4] = {sc.x, sc.y, sc.z, sc.w};
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) y[4 * e + k] = __uint_as_float(v[4 * e + k]) * (HALF ? s4[k] * token : s4[k]);
+                }
+                if (p.glu.act == PEQA_ACT_SILU) glu_pack<PEQA_ACT_SILU>(y, o + 4 * side);
+                else glu_pack<PEQA_ACT_GELU_TANH>(y, o + 4 * side);
+                if (p.out) {
+                  if (side == 0) {
+                    if (lane == 0) bulk_wait_group_read0();
+                    __syncwarp();
+                  }
+#pragma unroll
+                  for (int q = 0; q < 2; ++q)
+                    *reinterpret_cast<uint4*>(srow + (((side * 2 + q) ^ sw) << 4)) =
+                        make_uint4(bf16_pair(y[8 * q], y[8 * q + 1]), bf16_pair(y[8 * q + 2], y[8 * q + 3]),
+                                   bf16_pair(y[8 * q + 4], y[8 * q + 5]), bf16_pair(y[8 * q + 6], y[8 * q + 7]));
+                }
+              }
+            }
+            if (p.out) {
+              fence_proxy_async_smem();
+              __syncwarp();
+              if (lane == 0 && rows < p.T) {
+                tma_store_2d(&tmap_y, smem_u32(stage), n0 + first + u * 16, rows);
+                bulk_commit_group();
+              }
+            }
+            if (live) {
+              __nv_bfloat16* to = h_row + u * 8;
+              if (p.glu.wide) {
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(o[0]), "r"(o[1]), "r"(o[2]),
+                             "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
+              } else {
+                *reinterpret_cast<uint4*>(to) = make_uint4(o[0], o[1], o[2], o[3]);
+                if (u + 1 < mine) *reinterpret_cast<uint4*>(to + 8) = make_uint4(o[4], o[5], o[6], o[7]);
               }
             }
           }
-          if (p.out) {
-            fence_proxy_async_smem();
+          if (mine == 0) {
+            tc_fence_before();
             __syncwarp();
-            if (lane == 0 && row0 < p.T) {
-              tma_store_2d(&tmap_y, smem_u32(stage), n0 + u * 16, row0);
-              bulk_commit_group();
-            }
+            if (lane == 0) mbar_arrive_cluster(drained);
           }
-          if (live) {
-            __nv_bfloat16* to = h_row + u * 8;
-            if (p.glu.wide) {
-              asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(o[0]), "r"(o[1]), "r"(o[2]),
-                           "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
-            } else {
-              *reinterpret_cast<uint4*>(to) = make_uint4(o[0], o[1], o[2], o[3]);
-              if (u + 1 < units) *reinterpret_cast<uint4*>(to + 8) = make_uint4(o[4], o[5], o[6], o[7]);
-            }
-          }
-        }
-        if (units <= 0) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(acc_empty_leader);
         }
         continue;
       }
