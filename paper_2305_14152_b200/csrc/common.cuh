@@ -234,6 +234,7 @@ int launch_dx(const peqa_qweight_t* w, const float* zeros_f, int g, const void* 
 // channel_scales: a forward that multiplies by one scale per channel at the end
 long long split_ns(const peqa_qweight_t* w, int T, bool trans);
 bool split_is_faster(const peqa_qweight_t* w, int T, bool trans, bool channel_scales);
+bool split_glu_is_faster(const peqa_qweight_t* w, int T, bool channel_scales);
 int split_ds_slots(const peqa_qweight_t* w, int T);
 int split_part_tokens(const peqa_qweight_t* w, int T_call, bool trans);
 int launch_split(const peqa_qweight_t* w, const float* zeros_f, int g, const void* act, int T, void* out,

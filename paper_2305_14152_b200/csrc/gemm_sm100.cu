@@ -1020,7 +1020,7 @@ int launch_fwd(const peqa_qweight_t* w, const float* zeros_f, int g, const void*
 }
 
 int launch_glu_fwd(const peqa_qweight_t* w, int g, const void* X, int T, void* Y, const GluOut& glu, cudaStream_t st) {
-  if (split_is_faster(w, T, false, g == w->in_features))
+  if (split_glu_is_faster(w, T, g == w->in_features))
     return launch_split(w, nullptr, g, X, T, Y, false, nullptr, nullptr, st, T, 0, kInOrder, &glu);
   return launch_fwd_pair(w, nullptr, g, X, T, Y, nullptr, nullptr, st, kInOrder, &glu);
 }

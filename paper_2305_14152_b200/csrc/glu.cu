@@ -59,11 +59,17 @@ __global__ void __launch_bounds__(kBackThreads) glu_bwd_kernel(const uint4* Y, c
 }
 
 // Operands of a block with groups, in binary16 (see GluOut).  A CTA a token: its largest channel brought to [2^14, 2^15), so that all that is more than
-// 2^-28 of it keeps its bits.  Behind the tokens' CTAs a warp for eight rows: a row's largest scale brought to [1, 2).  (A warp a token and a
-// warp a row took 7.5 us for 77 tokens and 22016 rows of 32 groups, 16 for 4096 tokens.)
-constexpr int kRowsOfWarp = 8;
-constexpr int kRowsOfCta = kRowsOfWarp * kBackThreads / 32;
+// 2^-28 of it keeps its bits.  Behind the tokens' CTAs the rows: a row's largest scale brought to [1, 2), by as many lanes as hold
+// its groups in kRowHeld registers each, so that every scale is asked for before the first is used.  (Against a warp for eight rows, one after the other, the
+// forward of 77 tokens, us: 4096 rows of 172 groups 34.4 / 22.0, 8192 of 128 at 300 tokens 64.1 / 51.8, 22016 of 32 38.4 / 37.5.)
+constexpr int kRowHeld = 8;
 constexpr int kHeld = 4;                          // 16-byte pieces of a token that a thread keeps between the two passes
+// lanes of a row, a power of two
+__host__ __device__ inline int row_lanes(int G) {
+  int lanes = 1;
+  while (lanes < 32 && lanes * kRowHeld < G) lanes *= 2;
+  return lanes;
+}
 
 // 2^e for |e| <= 126, and the exponent that takes the largest of these bits to 2^target; what is not finite stays so.
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
@@ -122,23 +128,45 @@ __global__ void __launch_bounds__(kBackThreads) glu_operands_kernel(const uint4*
     if (threadIdx.x == 0) factors[N + blockIdx.x] = power_of_two(-e);
     return;
   }
-  const int row0 = ((int)blockIdx.x - T) * kRowsOfCta + warp * kRowsOfWarp;
-  float s[kRowsOfWarp];                           // the first 32 groups of each row, all asked for before the first is used
+  const int lanes = row_lanes(G), at = lane & (lanes - 1);
+  const int row = (((int)blockIdx.x - T) * kBackThreads + (int)threadIdx.x) / lanes;
+  const float* from = scales + (size_t)row * G;
+  float* to = scaled + (size_t)row * G;
+  // group of register i; rows of a multiple of four begin on 16 bytes
+  const bool fours = G % 4 == 0;
+  auto group = [&](int i) { return fours ? (at + i / 4 * lanes) * 4 + i % 4 : at + i * lanes; };
+  float s[kRowHeld];
+  if (fours) {
 #pragma unroll
-  for (int r = 0; r < kRowsOfWarp; ++r) s[r] = row0 + r < N && lane < G ? ptx::ld_global(scales + (size_t)(row0 + r) * G + lane) : 0.0f;
+    for (int i = 0; i < kRowHeld; i += 4) {
+      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (row < N && group(i) < G) v = ptx::ld_global(reinterpret_cast<const float4*>(from + group(i)));
+      s[i] = v.x, s[i + 1] = v.y, s[i + 2] = v.z, s[i + 3] = v.w;
+    }
+  } else {
 #pragma unroll
-  for (int r = 0; r < kRowsOfWarp; ++r) {
-    if (row0 + r >= N) break;
-    const float* from = scales + (size_t)(row0 + r) * G;
-    float* to = scaled + (size_t)(row0 + r) * G;
-    uint32_t most = __float_as_uint(s[r]) & 0x7FFFFFFFu;
-    for (int g = lane + 32; g < G; g += 32) most = max(most, __float_as_uint(ptx::ld_global(from + g)) & 0x7FFFFFFFu);
-    const int e = shift_to(__reduce_max_sync(0xffffffffu, most), 0);
-    const float by = power_of_two(e);
-    if (lane < G) to[lane] = s[r] * by;
-    for (int g = lane + 32; g < G; g += 32) to[g] = ptx::ld_global(from + g) * by;
-    if (lane == 0) factors[row0 + r] = power_of_two(-e);
+    for (int i = 0; i < kRowHeld; ++i) s[i] = row < N && group(i) < G ? ptx::ld_global(from + group(i)) : 0.0f;
   }
+  uint32_t most = 0u;
+#pragma unroll
+  for (int i = 0; i < kRowHeld; ++i) most = max(most, __float_as_uint(s[i]) & 0x7FFFFFFFu);
+  if (row < N)                                    // (more than 256 groups: a warp is one row)
+    for (int g = at + kRowHeld * lanes; g < G; g += lanes) most = max(most, __float_as_uint(ptx::ld_global(from + g)) & 0x7FFFFFFFu);
+  for (int o = lanes >> 1; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+  if (row >= N) return;
+  const int e = shift_to(most, 0);
+  const float by = power_of_two(e);
+  if (fours) {
+#pragma unroll
+    for (int i = 0; i < kRowHeld; i += 4)
+      if (group(i) < G) *reinterpret_cast<float4*>(to + group(i)) = make_float4(s[i] * by, s[i + 1] * by, s[i + 2] * by, s[i + 3] * by);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kRowHeld; ++i)
+      if (group(i) < G) to[group(i)] = s[i] * by;
+  }
+  for (int g = at + kRowHeld * lanes; g < G; g += lanes) to[g] = ptx::ld_global(from + g) * by;
+  if (at == 0) factors[row] = power_of_two(-e);
 }
 
 // The workspace of a block with groups.
@@ -181,7 +209,8 @@ extern "C" int peqa_qglu_fwd(const peqa_qweight_t* w, int activation, const void
   if (reinterpret_cast<uintptr_t>(workspace) & 255u) return PEQA_ERR_ALIGNMENT;
   char* ws = static_cast<char*>(workspace);
   float *scaled = reinterpret_cast<float*>(ws + at.scaled), *factors = reinterpret_cast<float*>(ws + at.factors);
-  const long long ctas = (long long)T + (w->out_features + kRowsOfCta - 1) / kRowsOfCta;
+  const int rows_of_cta = kBackThreads / row_lanes(G);
+  const long long ctas = (long long)T + (w->out_features + rows_of_cta - 1) / rows_of_cta;
   if (ctas > INT32_MAX) return PEQA_ERR_TOO_LARGE;
   PEQA_TRY(launch_after(glu_operands_kernel, (int)ctas, kBackThreads, st, static_cast<const uint4*>(X), w->scales, T, (int)w->in_features,
                         (int)w->out_features, G, reinterpret_cast<uint4*>(ws + at.halves), scaled, factors));

@@ -168,7 +168,7 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
   auto r0_of = [&](int it) { return ((first_tile + j0 + (it < split_at ? 0 : 1)) % p.r_tiles) * SM_ROWS; };
   auto t0_of = [&](int it) { return ((first_tile + j0 + (it < split_at ? 0 : 1)) / p.r_tiles - p.t_first) * p.nt; };
 
-  const bool beside = TRANS && p.side == kBeside;     // (a forward is the first of its call)
+  const bool beside = (TRANS || GLU) && p.side == kBeside;     // (a linear's forward is the first of its call)
   begin_beside(beside);
   // Forward: the first codes, scales and zero-points are asked for in L2 at once.  (Nothing is read: the preceding
   // kernel may still be writing them, and L2 is where it writes.)  us before / after: 256 x 256 at 64 tokens 5.8 / 5.4,
@@ -682,6 +682,56 @@ SplitPlan plan_split(int r_tiles, int C, int T, int sms, bool trans) {
   return plans[1].ns >= 0 && plans[1].ns * (plans[1].nt < 64 ? 103 : 100) < plans[0].ns * 100 ? plans[1] : plans[0];
 }
 
+// A gated block's forward may go in two launches side by side (kFollowed, kBeside): whole waves of clusters for the first tiles, and what is
+// left over, in clusters of the shape that suits so few: SMs idled in waves of one shape for all, 172 tiles in clusters of four with three each.  us, one
+// launch / two: 22016 x 4096 at 77 tokens 41.2 / 32.2, in groups of 128 47.7 / 38.4, 44032 x 8192 131 / 119, 22016 x 8192 at 256 109 / 90.
+// (A linear keeps to one: its sums keep their order.)
+struct SplitCut {
+  int at;              // tiles of the first launch, all of them where it is the only one
+  SplitPlan head, rest;
+};
+SplitCut plan_glu(int r_tiles, int C, int T, int sms) {
+  SplitCut best = {};
+  best.head = plan_split(r_tiles, C, T, sms, false);
+  best.at = r_tiles * best.head.t_tiles;
+  const int nt = best.head.nt, tiles = best.at;
+  const long long k_blocks = (C + SM_BK - 1) / SM_BK;
+  const int active[4] = {sms, sms / 2, sms * 33 / 148, sms * 15 / 148};
+  // the best shape for n tiles, whole waves of it alone or not
+  auto shape = [&](int n, bool whole, SplitPlan& best_shape, int& taken) {
+    double rate = 0.0;
+    for (int ci = 0; ci < 4; ++ci) {
+      for (int q = 1; active[ci] > 0 && q <= (1 << ci); ++q) {
+        if (split_tmem_stages(nt, q) < 3) continue;
+        const int wave = q * active[ci], waves = whole ? n / wave : (n + wave - 1) / wave, took = whole ? waves * wave : n;
+        if (took == 0) continue;
+        const long long stages = (q * k_blocks + (1 << ci) - 1) >> ci;
+        const long long ns = split_fwd_ns(waves, stages, nt, q) + 50 * ci;
+        const double r = (double)took / ns;
+        if (r > rate) {
+          rate = r;
+          taken = took;
+          best_shape = best.head;
+          best_shape.q = q;
+          best_shape.cshift = ci;
+          best_shape.waves = waves;
+          best_shape.stages = (int)stages;
+          best_shape.ns = ns;
+        }
+      }
+    }
+    return rate > 0.0;
+  };
+  SplitPlan head, rest;
+  int at = 0, left = 0;
+  if (!shape(tiles, true, head, at) || at == tiles || !shape(tiles - at, false, rest, left)) return best;
+  if ((head.ns + rest.ns) * 100 >= best.head.ns * 97) return best;
+  best.at = at;
+  best.head = head;
+  best.rest = rest;
+  return best;
+}
+
 // The pair kernels on the same call: rounds of 512 x 256 tiles over the pairs of SMs.  dX, fitted to 400
 // random calls, launches back to back (256 to 22016 rows and columns, 17 to 2600 tokens): a stage of 64
 // takes 0.58 us, with two blocks of tokens in the tile 0.67; a round 3.3 us more, with two blocks
@@ -694,6 +744,27 @@ long long pair_ns(int R, int C, int T, bool trans, bool channel_scales, int sms)
   const long long rounds = (tiles + pairs - 1) / pairs, stages = (C + 63) / 64;
   if (trans) return rounds * (T > 256 ? 4300 + stages * 666 : 3300 + stages * 580) + 3200;
   return rounds * (T > 256 ? 3450 + stages * 618 : 1850 + stages * 550) + (channel_scales ? 4950 : 4400);
+}
+
+// The rest of a launch's parameters, which follows from the shape of its clusters; its bytes of shared memory.
+size_t fit_split(SplitParams& p, const SplitPlan& plan, bool trans) {
+  p.q = plan.q;
+  p.cshift = plan.cshift;
+  const int stage_bytes = 2 * ((trans ? SM_A_BYTES : 0) + p.nt * (SM_HALF * 2));
+  p.stages = (SM_SMEM_LIMIT - SM_SMEM_FIXED) / stage_bytes;
+  if (p.stages > SM_MAX_STAGES) p.stages = SM_MAX_STAGES;
+  const int segs = p.q > 1 ? 2 : 1;          // partial sums a CTA may hold
+  if (trans) {
+    p.acc2 = SM_MAX_NT;
+    p.a_col = 0;
+  } else {
+    p.acc2 = (p.nt + 31) & ~31;
+    p.stages = p.stages < split_tmem_stages(p.nt, p.q) ? p.stages : split_tmem_stages(p.nt, p.q);
+    p.a_col = 512 - p.stages * (SM_BK / 2);
+  }
+  const int dump = segs * (p.nt < SM_DUMP_TOK ? p.nt : SM_DUMP_TOK) * SM_ROWS * 4;
+  p.region = p.stages * stage_bytes > dump ? p.stages * stage_bytes : dump;
+  return (size_t)p.region + SM_SMEM_FIXED;
 }
 
 }  // namespace
@@ -719,6 +790,14 @@ long long split_ns(const peqa_qweight_t* w, int T, bool trans) {
 bool split_is_faster(const peqa_qweight_t* w, int T, bool trans, bool channel_scales) {
   const int R = trans ? w->in_features : w->out_features, C = trans ? w->out_features : w->in_features;
   return split_ns(w, T, trans) * 100 < pair_ns(R, C, T, trans, channel_scales, sm_count_or(148)) * 97;
+}
+
+// The same for a gated block's forward, whose plan is another.  us, pair / here: 11008 x 4096 in 3 bits at 320 tokens 50 / 40, 28672 x 8192 at 320
+// 165 / 144.
+bool split_glu_is_faster(const peqa_qweight_t* w, int T, bool channel_scales) {
+  const int sms = sm_count_or(148);
+  const SplitCut cut = plan_glu((w->out_features + SM_ROWS - 1) / SM_ROWS, w->in_features, T, sms);
+  return (cut.head.ns + cut.rest.ns) * 100 < pair_ns(w->out_features, w->in_features, T, false, channel_scales, sms) * 97;
 }
 
 // Partial sums per channel that a forward with dS writes.
@@ -763,29 +842,12 @@ int launch_split(const peqa_qweight_t* w, const float* zeros_f, int g, const voi
   p.r_tiles = (p.R + SM_ROWS - 1) / SM_ROWS;
   const SplitPlan plan = plan_split(p.r_tiles, C, T_call, sm_count_or(148), trans);
   p.nt = plan.nt;
-  p.q = plan.q;
-  p.cshift = plan.cshift;
   p.tiles = p.r_tiles * plan.t_tiles;
   p.tile0 = p.r_tiles * (t0 / plan.nt);
   p.tile1 = p.r_tiles * ((t0 + T + plan.nt - 1) / plan.nt);
-  p.first = p.tile0 / p.q * p.q;
+  p.first = p.tile0 / plan.q * plan.q;
   p.t_first = t0 / plan.nt;
   p.k_blocks = (C + SM_BK - 1) / SM_BK;
-  const int stage_bytes = 2 * ((trans ? SM_A_BYTES : 0) + p.nt * (SM_HALF * 2));
-  p.stages = (SM_SMEM_LIMIT - SM_SMEM_FIXED) / stage_bytes;
-  if (p.stages > SM_MAX_STAGES) p.stages = SM_MAX_STAGES;
-  const int segs = p.q > 1 ? 2 : 1;          // partial sums a CTA may hold
-  if (trans) {
-    p.acc2 = SM_MAX_NT;
-    p.a_col = 0;
-  } else {
-    p.acc2 = (p.nt + 31) & ~31;
-    p.stages = p.stages < split_tmem_stages(p.nt, p.q) ? p.stages : split_tmem_stages(p.nt, p.q);
-    p.a_col = 512 - p.stages * (SM_BK / 2);
-  }
-  const int dump = segs * (p.nt < SM_DUMP_TOK ? p.nt : SM_DUMP_TOK) * SM_ROWS * 4;
-  p.region = p.stages * stage_bytes > dump ? p.stages * stage_bytes : dump;
-  const size_t smem = (size_t)p.region + SM_SMEM_FIXED;
   PEQA_TRY(status_word(st, &p.status));
   EncodeTiledFn enc = nullptr;
   PEQA_TRY(tensor_map_encoder(&enc));
@@ -814,11 +876,24 @@ int launch_split(const peqa_qweight_t* w, const float* zeros_f, int g, const voi
   }
   const bool b4 = w->bits == 4;
   if (glu) {
-    if (p.G > 1) return b4 ? launch_split_t<4, false, true, false, false, true>(ta, tp, p, smem, st)
-                           : launch_split_t<3, false, true, false, false, true>(ta, tp, p, smem, st);
-    return b4 ? launch_split_t<4, false, false, false, false, true>(ta, tp, p, smem, st)
-              : launch_split_t<3, false, false, false, false, true>(ta, tp, p, smem, st);
+    auto kern = p.G > 1 ? (b4 ? launch_split_t<4, false, true, false, false, true> : launch_split_t<3, false, true, false, false, true>)
+                        : (b4 ? launch_split_t<4, false, false, false, false, true> : launch_split_t<3, false, false, false, false, true>);
+    const SplitCut cut = plan_glu(p.r_tiles, C, T_call, sm_count_or(148));
+    const int tiles = p.tiles;
+    if (cut.at < tiles) {
+      p.side = kFollowed;
+      p.tiles = p.tile1 = cut.at;
+    }
+    const size_t first = fit_split(p, cut.head, false);
+    PEQA_TRY(kern(ta, tp, p, first, st));
+    if (cut.at == tiles) return PEQA_OK;
+    p.side = kBeside;
+    p.first = p.tile0 = cut.at;
+    p.tiles = p.tile1 = tiles;
+    const size_t second = fit_split(p, cut.rest, false);
+    return kern(ta, tp, p, second, st);
   }
+  const size_t smem = fit_split(p, plan, trans);
   if (trans) {
     if (zeros_f) return b4 ? launch_split_t<4, true, true, true>(ta, tp, p, smem, st)
                            : launch_split_t<3, true, true, true>(ta, tp, p, smem, st);

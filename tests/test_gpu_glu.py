@@ -35,6 +35,58 @@ def test_forward(T, F, K, group, bits):
     assert_within(H, want, tol, "H")
 
 
+#: row tiles (of 128) that a few clusters are left with behind whole waves of 148
+WIDE = [(33, 10240, 1024), (77, 9480, 1024), (200, 10240, 512)]
+
+
+@pytest.mark.parametrize("bits,group", [(4, 0), (4, 128), (3, 64)])
+@pytest.mark.parametrize("T,F,K", WIDE)
+def test_forward_of_a_wide_block(T, F, K, bits, group):
+    w, W, _ = block(F, K, bits, group, seed=F)
+    X = rows(T, K, T)
+    H, Y = binding.qglu_fwd(w, X)
+    alone, _ = binding.qglu_fwd(w, X, keep=False)
+    assert torch.equal(H, alone)
+    binding.check_status()
+    want, want_Y, tol, tol_Y = forward(X, W, "silu", w.G > 1)
+    assert_within(Y, want_Y, tol_Y, "Y")
+    assert_within(H, want, tol, "H")
+
+
+@pytest.mark.parametrize("group", [0, 128])
+def test_wide_blocks_one_behind_another(group):
+    """Every call reads what the one before has written, eagerly and captured, and no result is left to timing."""
+    T, F, K = 33, 10240, 1024
+    up, _, _ = block(F, K, 4, group, seed=1)
+    down, _, _ = block(K // 2, F, 4, group, seed=2)
+    X = rows(T, K, 3)
+    H = torch.empty((T, F), dtype=torch.bfloat16, device="cuda")
+    Z = torch.empty((T, K), dtype=torch.bfloat16, device="cuda")
+    space = binding.alloc_workspace(binding.OP_GLU_FWD, T, up)
+
+    def chain(pause):
+        Z.copy_(X)
+        for _ in range(6):
+            binding.qglu_fwd(up, Z, keep=False, H=H, workspace=space)
+            pause()
+            binding.qlinear_fwd(down, H, Z)
+            pause()
+
+    chain(torch.cuda.synchronize)
+    want = Z.clone()
+    assert want.isfinite().all()
+    chain(lambda: None)
+    assert torch.equal(Z, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain(lambda: None)
+    for _ in range(5):
+        Z.zero_()
+        graph.replay()
+        assert torch.equal(Z, want)
+    binding.check_status()
+
+
 @pytest.mark.parametrize("T,F,K", [(9, 40, 64), (100, 88, 192), (700, 72, 320)])
 def test_forward_of_odd_multiples_of_64_columns(T, F, K):
     w, W, _ = block(F, K, 4, 64, seed=3)
