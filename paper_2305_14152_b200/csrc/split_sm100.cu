@@ -48,6 +48,7 @@ constexpr int SM_MAX_NT = 256;                // tokens per tile
 constexpr int SM_A_BYTES = SM_ROWS * SM_HALF * 2;   // weights of one half
 constexpr int SM_PK_BYTES = 8192;             // packed codes of one stage
 constexpr int SM_PK_SLOTS = 4;
+constexpr int SM_PK_MORE = 8;                 // of a gated block, see fit_split
 constexpr int SM_MAX_STAGES = 4;
 constexpr int kSplitThreads = 640;
 constexpr int kSplitWorkers = 512;            // threads of the dequant warps
@@ -58,8 +59,8 @@ constexpr int SM_SMEM_FIXED = SM_PK_SLOTS * SM_PK_BYTES + 1024 /*align*/ + 512 /
 struct SplitBarriers {
   uint64_t full[SM_MAX_STAGES];       // weight tile written and activation bytes landed
   uint64_t empty[SM_MAX_STAGES];      // MMAs that read the stage completed
-  uint64_t full_pk[SM_PK_SLOTS];
-  uint64_t empty_pk[SM_PK_SLOTS];
+  uint64_t full_pk[SM_PK_MORE];
+  uint64_t empty_pk[SM_PK_MORE];
   uint64_t acc_full;                  // every MMA of this CTA completed
   uint32_t tmem_base;
   int abort_flag;
@@ -133,8 +134,8 @@ __device__ __forceinline__ UnitZS split_load_zs(const SplitParams& p, int i, int
 // DS (forward with one scale per channel): where the fp32 sums of a tile are complete they are also
 // multiplied by dY and summed over the tile's tokens, dS[i] = sum_t dY[t,i] * u[t,i] (see the
 // pair kernel).
-// GLU (forward): the outputs of a gated block beside or instead of Y, see glu.cuh.
-template <int BITS, bool TRANS, bool FOLD, bool ZF, bool DS, bool GLU>
+// GLU (forward): the outputs of a gated block beside or instead of Y, see glu.cuh, and its slots of codes.
+template <int BITS, bool TRANS, bool FOLD, bool ZF, bool DS, int GLU>
 __global__ void __launch_bounds__(kSplitThreads, 1)
 qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constant__ CUtensorMap tmap_pk,
               const SplitParams p) {
@@ -145,7 +146,8 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
   const int half_bytes = kWBytes + p.nt * (SM_HALF * 2);        // weights, then activations
   const int stage_bytes = 2 * half_bytes;
   uint8_t* sm_pk = base + p.region;
-  SplitBarriers* bars = reinterpret_cast<SplitBarriers*>(sm_pk + SM_PK_SLOTS * SM_PK_BYTES);
+  constexpr int kSlots = GLU ? GLU : SM_PK_SLOTS;
+  SplitBarriers* bars = reinterpret_cast<SplitBarriers*>(sm_pk + kSlots * SM_PK_BYTES);
   const int warp = warp_index(), lane = threadIdx.x & 31;
   volatile int* abort_flag = &bars->abort_flag;
 
@@ -174,7 +176,7 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
   // kernel may still be writing them, and L2 is where it writes.)  us before / after: 256 x 256 at 64 tokens 5.8 / 5.4,
   // 4096 x 4096 at 77 12.55 / 12.3; dX gained nothing (13.0 / 13.2).
   if constexpr (!TRANS) {
-    if (n_it > 0 && warp == 3 && lane < min(n_it, SM_PK_SLOTS)) {
+    if (n_it > 0 && warp == 3 && lane < min(n_it, kSlots)) {
       prefetch_tile_2d(&tmap_pk, kb_of(lane) * (4 * BITS), r0_of(lane));
     } else if (n_it > 0 && warp >= 4 && warp < 8) {
       const int i = r0_of(0) + (int)threadIdx.x - 128, col = kb_of(0) * SM_BK;
@@ -194,7 +196,7 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
       mbar_init(smem_u32(&bars->empty[s]), 1);
     }
 #pragma unroll 1
-    for (int s = 0; s < SM_PK_SLOTS; ++s) {
+    for (int s = 0; s < kSlots; ++s) {
       mbar_init(smem_u32(&bars->full_pk[s]), 1);
       mbar_init(smem_u32(&bars->empty_pk[s]), 8);
     }
@@ -247,8 +249,8 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
       const int ra = r0_of(0), rb = r0_of(split_at);
 #pragma unroll 1
       for (int it = 0; it < n_it; ++it) {
-        const int s = it % SM_PK_SLOTS;
-        if (!mbar_wait(smem_u32(&bars->empty_pk[s]), ((it / SM_PK_SLOTS) & 1u) ^ 1u, abort_flag)) break;
+        const int s = it % kSlots;
+        if (!mbar_wait(smem_u32(&bars->empty_pk[s]), ((it / kSlots) & 1u) ^ 1u, abort_flag)) break;
         const uint32_t bar = smem_u32(&bars->full_pk[s]);
         const int kb = kb_of(it), r0 = it < split_at ? ra : rb;
         mbar_arrive_expect_tx(bar, 128 * 16 * BITS);
@@ -333,8 +335,8 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
     };
     auto turn = [&](int it, const UnitZS (&cur)[2], UnitZS (&next)[2]) -> bool {
       load_zs(it + 2, next);
-      const int pq = it % SM_PK_SLOTS;
-      if (!warp_wait(smem_u32(&bars->full_pk[pq]), (it / SM_PK_SLOTS) & 1u, abort_flag)) return false;
+      const int pq = it % kSlots;
+      if (!warp_wait(smem_u32(&bars->full_pk[pq]), (it / kSlots) & 1u, abort_flag)) return false;
       const uint8_t* src = sm_pk + pq * SM_PK_BYTES;
       uint32_t w[2][BITS];
       if constexpr (!TRANS) {
@@ -474,6 +476,11 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
           if (rl < b0 && j > j_lo) second |= 1u << r;
         }
         float4 ds = make_float4(0.f, 0.f, 0.f, 0.f);   // vec_per divides kSplitWorkers: a thread keeps its rows
+        float4 row_scale = ds;
+        if constexpr (GLU) {
+          const int row = r0 + (wtid & (vec_per - 1)) * 4;
+          if (row < p.R) row_scale = ld_global(reinterpret_cast<const float4*>((FOLD ? p.zeros_f : p.scales) + row));
+        }
         // One vector per thread and turn, the sums of four CTAs requested before the first is used.  (Two vectors a
         // turn were twice the code for a launch to fetch, us, one / two: forward 2672 x 1856 at 142 tokens 11.8 / 12.6, 1096 x
         // 768 at 32 5.7 / 6.0, 2.1 % over 180 forwards; dX 8192 x 8192 at 45 28.2 / 28.9.)
@@ -507,33 +514,24 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
             ds.z = fmaf(a.z, __uint_as_float(y.y << 16), ds.z);
             ds.w = fmaf(a.w, __uint_as_float(y.y & 0xFFFF0000u), ds.w);
           }
-          if constexpr (GLU && FOLD) {
-            const float4 sc = ld_global(reinterpret_cast<const float4*>(p.zeros_f + row));
-            const float token = ld_global(p.zeros_f + p.N + t0 + t);
-            a.x *= sc.x * token; a.y *= sc.y * token; a.z *= sc.z * token; a.w *= sc.w * token;
-          }
-          if (!FOLD) {
+          if constexpr (GLU) {
+            float token = 1.0f;
+            if (FOLD) token = ld_global(p.zeros_f + p.N + t0 + t);
+            a.x *= row_scale.x * token; a.y *= row_scale.y * token; a.z *= row_scale.z * token; a.w *= row_scale.w * token;
+          } else if (!FOLD) {
             const float4 sc = ld_global(reinterpret_cast<const float4*>(p.scales + row));   // one scale per channel
             a.x *= sc.x; a.y *= sc.y; a.z *= sc.z; a.w *= sc.w;
           }
           if constexpr (GLU) {
             // A CTA finishes a multiple of 16 rows, four lanes' vectors: gate, gate, up, up of eight channels of a token.  The four have
-            // come here together.
+            // come here together; a gate's lane takes its first two channels, the up's its last two.
             const uint32_t four = 0xFu << (lane & 28);
-            float4 up;
-            up.x = __shfl_xor_sync(four, a.x, 2);
-            up.y = __shfl_xor_sync(four, a.y, 2);
-            up.z = __shfl_xor_sync(four, a.z, 2);
-            up.w = __shfl_xor_sync(four, a.w, 2);
-            if (!(lane & 2)) {
-              const __nv_bfloat162 b0 = __floats2bfloat162_rn(glu_value(a.x, up.x, p.act), glu_value(a.y, up.y, p.act));
-              const __nv_bfloat162 b1 = __floats2bfloat162_rn(glu_value(a.z, up.z, p.act), glu_value(a.w, up.w, p.act));
-              uint2 o;
-              o.x = *reinterpret_cast<const uint32_t*>(&b0);
-              o.y = *reinterpret_cast<const uint32_t*>(&b1);
-              const int channel = (row >> 4) * kGluRun + (row & 7);
-              *reinterpret_cast<uint2*>(p.H + (size_t)(t0 + t) * (p.R >> 1) + channel) = o;
-            }
+            const bool is_up = lane & 2;
+            const float x = __shfl_xor_sync(four, is_up ? a.x : a.z, 2), y = __shfl_xor_sync(four, is_up ? a.y : a.w, 2);
+            const __nv_bfloat162 h = __floats2bfloat162_rn(glu_value(is_up ? x : a.x, is_up ? a.z : x, p.act),
+                                                           glu_value(is_up ? y : a.y, is_up ? a.w : y, p.act));
+            const int channel = (row >> 4) * kGluRun + (row & 7) + (is_up ? 2 : 0);
+            *reinterpret_cast<uint32_t*>(p.H + (size_t)(t0 + t) * (p.R >> 1) + channel) = *reinterpret_cast<const uint32_t*>(&h);
             if (!p.out) continue;
           }
           __nv_bfloat162 h0 = __floats2bfloat162_rn(a.x, a.y), h1 = __floats2bfloat162_rn(a.z, a.w);
@@ -590,7 +588,7 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
   if (beside && blockIdx.x == 0 && threadIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-template <int BITS, bool TRANS, bool FOLD, bool ZF, bool DS = false, bool GLU = false>
+template <int BITS, bool TRANS, bool FOLD, bool ZF, bool DS = false, int GLU = 0>
 int launch_split_t(const CUtensorMap& ta, const CUtensorMap& tp, const SplitParams& p, size_t smem,
                    cudaStream_t st) {
   auto kern = qsplit_kernel<BITS, TRANS, FOLD, ZF, DS, GLU>;
@@ -876,22 +874,29 @@ int launch_split(const peqa_qweight_t* w, const float* zeros_f, int g, const voi
   }
   const bool b4 = w->bits == 4;
   if (glu) {
-    auto kern = p.G > 1 ? (b4 ? launch_split_t<4, false, true, false, false, true> : launch_split_t<3, false, true, false, false, true>)
-                        : (b4 ? launch_split_t<4, false, false, false, false, true> : launch_split_t<3, false, false, false, false, true>);
+    // Eight slots of codes where they cost no stage.  us, four / eight: 22016 x 4096 at 77 tokens 31.7 / 30.9, in groups of 128 36.9 / 35.9, 4096 x 11008
+    // 16.6 / 16.2, at 20 15.0 / 14.5, 44032 x 8192 in groups of 128 112 / 104.
+    auto launch = [&](const SplitPlan& shape) {
+      const size_t smem = fit_split(p, shape, false), more = smem + (SM_PK_MORE - SM_PK_SLOTS) * SM_PK_BYTES;
+      if (more <= SM_SMEM_LIMIT) {
+        auto kern = p.G > 1 ? (b4 ? launch_split_t<4, false, true, false, false, SM_PK_MORE> : launch_split_t<3, false, true, false, false, SM_PK_MORE>)
+                            : (b4 ? launch_split_t<4, false, false, false, false, SM_PK_MORE> : launch_split_t<3, false, false, false, false, SM_PK_MORE>);
+        return kern(ta, tp, p, more, st);
+      }
+      auto kern = p.G > 1 ? (b4 ? launch_split_t<4, false, true, false, false, SM_PK_SLOTS> : launch_split_t<3, false, true, false, false, SM_PK_SLOTS>)
+                          : (b4 ? launch_split_t<4, false, false, false, false, SM_PK_SLOTS> : launch_split_t<3, false, false, false, false, SM_PK_SLOTS>);
+      return kern(ta, tp, p, smem, st);
+    };
     const SplitCut cut = plan_glu(p.r_tiles, C, T_call, sm_count_or(148));
     const int tiles = p.tiles;
-    if (cut.at < tiles) {
-      p.side = kFollowed;
-      p.tiles = p.tile1 = cut.at;
-    }
-    const size_t first = fit_split(p, cut.head, false);
-    PEQA_TRY(kern(ta, tp, p, first, st));
-    if (cut.at == tiles) return PEQA_OK;
+    if (cut.at == tiles) return launch(cut.head);
+    p.side = kFollowed;
+    p.tiles = p.tile1 = cut.at;
+    PEQA_TRY(launch(cut.head));
     p.side = kBeside;
     p.first = p.tile0 = cut.at;
     p.tiles = p.tile1 = tiles;
-    const size_t second = fit_split(p, cut.rest, false);
-    return kern(ta, tp, p, second, st);
+    return launch(cut.rest);
   }
   const size_t smem = fit_split(p, plan, trans);
   if (trans) {
