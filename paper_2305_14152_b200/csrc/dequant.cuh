@@ -180,23 +180,39 @@ __device__ __forceinline__ void unit32_natural(const uint32_t (&w)[BITS], uint32
 }
 
 // The same in binary16, (q - z) * s with s rounded to it: each rounding is off by 2^-11 at most where bf16's is by 2^-8.  s and z are such that
-// nothing leaves binary16's range.
+// nothing leaves binary16's range.  Four bits: the columns of a block of eight come in the order 0 4 1 5 2 6 3 7 (half_column), which the other operand
+// is written in.  Two pairs of a word and two of the word shifted by eight lie in place, at bits 0 and 4 (biases 2^10 and 2^6), so five
+// integer operations make eight codes where the natural order takes nine (22016 x 4096 in groups of 128, 77 tokens, us, natural / this 35.7 / 34.3).
+__host__ __device__ constexpr int half_column(int bits, int k) { return bits == 4 ? (k & 1) * 4 + (k >> 1) : k; }
+
 template <int BITS>
 __device__ __forceinline__ void unit32_half(const uint32_t (&w)[BITS], uint32_t z, float s, uint32_t (&out)[16]) {
-  constexpr uint32_t step[3] = {BITS == 4 ? 0x00010001u : 0x00080001u, 0x00020004u, 0x00080010u};
-  uint32_t zc[natural_kinds(BITS)], s2;
+  uint32_t zc[natural_kinds(3)], s2, x[4][4];
+  if constexpr (BITS == 4) {
+    zc[0] = z * 0x00010001u + 0x64006400u;
+    zc[1] = z * 0x00100010u + 0x54005400u;
 #pragma unroll
-  for (int k = 0; k < natural_kinds(BITS); ++k) zc[k] = z * step[k] + natural_bias<BITS, true>(k);
+    for (int b = 0; b < 4; ++b) {
+      const uint32_t c = w[b] >> 8;
+      x[b][0] = lop3_and_or(w[b], 0x000F000Fu, 0x64006400u);
+      x[b][1] = lop3_and_or(w[b], 0x00F000F0u, 0x54005400u);
+      x[b][2] = lop3_and_or(c, 0x000F000Fu, 0x64006400u);
+      x[b][3] = lop3_and_or(c, 0x00F000F0u, 0x54005400u);
+    }
+  } else {
+    constexpr uint32_t step[3] = {0x00080001u, 0x00020004u, 0x00080010u};
+#pragma unroll
+    for (int k = 0; k < natural_kinds(BITS); ++k) zc[k] = z * step[k] + natural_bias<BITS, true>(k);
+    block8_raw<BITS, 0, true>(w, x[0]);
+    block8_raw<BITS, 1, true>(w, x[1]);
+    block8_raw<BITS, 2, true>(w, x[2]);
+    block8_raw<BITS, 3, true>(w, x[3]);
+  }
   asm("cvt.rn.f16x2.f32 %0, %1, %1;" : "=r"(s2) : "f"(s));
-  uint32_t x[4][4];
-  block8_raw<BITS, 0, true>(w, x[0]);
-  block8_raw<BITS, 1, true>(w, x[1]);
-  block8_raw<BITS, 2, true>(w, x[2]);
-  block8_raw<BITS, 3, true>(w, x[3]);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     uint32_t d;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(x[i / 4][i % 4]), "r"(zc[natural_kind(BITS, i % 4)]));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(x[i / 4][i % 4]), "r"(zc[BITS == 4 ? i & 1 : natural_kind(BITS, i % 4)]));
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(out[i]) : "r"(d), "r"(s2));
   }
 }

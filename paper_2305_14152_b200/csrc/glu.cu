@@ -7,6 +7,7 @@
 #include <cuda_bf16.h>
 
 #include "common.cuh"
+#include "dequant.cuh"
 #include "glu.cuh"
 #include "sm100_ptx.cuh"
 
@@ -84,14 +85,21 @@ __device__ __forceinline__ uint32_t largest_of(const uint4& v) {
   for (int e = 0; e < 4; ++e) most = max(most, max(w[e] << 16 & 0x7FFF0000u, w[e] & 0x7FFF0000u));
   return most;
 }
+// Eight channels, in the order of the codes' (dq::half_column).
+template <int BITS>
 __device__ __forceinline__ uint4 to_half(const uint4& v, float by) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  float x[8];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) x[2 * q] = low(w[q]) * by, x[2 * q + 1] = high(w[q]) * by;
   uint32_t o[4];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(o[q]) : "f"(high(w[q]) * by), "f"(low(w[q]) * by));
+  for (int q = 0; q < 4; ++q)
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(o[q]) : "f"(x[dq::half_column(BITS, 2 * q + 1)]), "f"(x[dq::half_column(BITS, 2 * q)]));
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
+template <int BITS>
 __global__ void __launch_bounds__(kBackThreads) glu_operands_kernel(const uint4* X, const float* scales, int T, int K, int N, int G,
                                                                     uint4* halves, float* scaled, float* factors) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -122,9 +130,9 @@ __global__ void __launch_bounds__(kBackThreads) glu_operands_kernel(const uint4*
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
       const int c = (int)threadIdx.x + i * kBackThreads;
-      if (c < pieces) out[c] = to_half(held[i], by);
+      if (c < pieces) out[c] = to_half<BITS>(held[i], by);
     }
-    for (int c = (int)threadIdx.x + kHeld * kBackThreads; c < pieces; c += kBackThreads) out[c] = to_half(ptx::ld_global(x + c), by);
+    for (int c = (int)threadIdx.x + kHeld * kBackThreads; c < pieces; c += kBackThreads) out[c] = to_half<BITS>(ptx::ld_global(x + c), by);
     if (threadIdx.x == 0) factors[N + blockIdx.x] = power_of_two(-e);
     return;
   }
@@ -212,7 +220,7 @@ extern "C" int peqa_qglu_fwd(const peqa_qweight_t* w, int activation, const void
   const int rows_of_cta = kBackThreads / row_lanes(G);
   const long long ctas = (long long)T + (w->out_features + rows_of_cta - 1) / rows_of_cta;
   if (ctas > INT32_MAX) return PEQA_ERR_TOO_LARGE;
-  PEQA_TRY(launch_after(glu_operands_kernel, (int)ctas, kBackThreads, st, static_cast<const uint4*>(X), w->scales, T, (int)w->in_features,
+  PEQA_TRY(launch_after(w->bits == 4 ? glu_operands_kernel<4> : glu_operands_kernel<3>, (int)ctas, kBackThreads, st, static_cast<const uint4*>(X), w->scales, T, (int)w->in_features,
                         (int)w->out_features, G, reinterpret_cast<uint4*>(ws + at.halves), scaled, factors));
   peqa_qweight_t half = *w;
   half.scales = scaled;
