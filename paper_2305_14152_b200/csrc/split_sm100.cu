@@ -322,7 +322,17 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
     const int ra = r0_of(0), rb = r0_of(split_at);
     // (forward) the second unit shares the first one's group unless groups are not multiples of 64 columns
     const bool one_group = !TRANS && (p.G == 1 || (p.g & 63) == 0);
+    // (a gated block with one scale per row) the rows' zero-points
+    uint32_t z_first = 0u, z_then = 0u;
+    if constexpr (GLU && !FOLD) {
+      if (ra + rowl < p.N) z_first = ld_global(p.zeros + ra + rowl);
+      if (rb + rowl < p.N) z_then = ld_global(p.zeros + rb + rowl);
+    }
     auto load_zs = [&](int it, UnitZS (&u)[2]) {
+      if constexpr (GLU && !FOLD) {
+        u[0] = UnitZS{it < split_at ? z_first : z_then, 0.f};
+        return;
+      }
       if (it >= n_it) { u[0] = UnitZS{0u, 0.f}; u[1] = u[0]; return; }
       const int c0 = kb_of(it) * SM_BK + half * SM_HALF, r0 = it < split_at ? ra : rb;
       if (TRANS) {
