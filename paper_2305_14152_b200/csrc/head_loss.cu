@@ -25,8 +25,8 @@
 // A tile belongs to a pair of CTAs (cta_group::2), operands come by TMA through a ring of six stages of 64, and two accumulators of
 // 256 columns fill tensor memory, so that one tile's epilogue runs under the next one's contraction.
 //
-// The tensor cores bound it, under the power limit: 4096 tokens at 32000 x 8192 take 3410 us, 1.26 PFLOP/s (losses alone, 2048 tokens at 32000 x 4096,
-// 406; their kernel 1.4 PFLOP/s, what a library's product of the size sustains).  A launch with both kinds of tiles keeps the tensor pipe busy 90 to 93 %
+// The tensor cores bound it, under the power limit: 4096 tokens at 32000 x 8192 take 3350 to 3430 us, 1.25 to 1.28 PFLOP/s (losses alone, 2048 tokens at 32000 x 4096,
+// 406 to 417; their kernel 1.4 PFLOP/s, what a library's product of the size sustains).  A launch with both kinds of tiles keeps the tensor pipe busy 90 to 93 %
 // of the time.  Tiles of the gradient dealt out column by column in groups of token blocks instead of row by row: 3551 -> 3435 us, as a piece's
 // rows of the head (134 MB at 8192 features) were read once for every 74 tiles before.
 #include <cuda.h>

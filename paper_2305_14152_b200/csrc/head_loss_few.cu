@@ -8,7 +8,7 @@
 // An epilogue thread is an entry or a feature.  Sums over the entries go across the lanes: at distance o a lane keeps the tokens that
 // agree with it in bit o and hands the others over, 31 exchanges for 32 tokens.  Every warp of a tile leaves its own.
 //
-// HBM bounds it: one token at 32000 x 4096 takes 49 us (46 for the kernel, 5.7 TB/s, of 40), 150 with gradient 129, of which 108 are the two passes
+// HBM bounds it: one token at 32000 x 4096 takes 49 us (46 for the kernel, 5.7 TB/s, of 40), 150 with gradient 129 to 133, of which 108 are the two passes
 // over the head.  For the second to find in L2 what the first read last, all parts of the gradient's sums go through the vocabulary together, from its end.
 #include "head_loss.cuh"
 #include "kv_cache.cuh"
