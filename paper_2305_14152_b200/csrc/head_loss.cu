@@ -460,6 +460,7 @@ struct GatherParams {
   __nv_bfloat16* rows;     // live tokens' X, side by side
   int* again;              // flags of the chunks
   int chunks;
+  const int* counts;       // of spans of kCountSpan tokens, or nullptr
   float* loss;
   __nv_bfloat16* dX;       // or nullptr
   int* status;
@@ -479,8 +480,22 @@ __device__ __forceinline__ V over_block(V v, V* part, F&& join) {
 }
 __device__ __forceinline__ float add_floats(float a, float b) { return a + b; }
 
+// Tokens that count, span by span, where there are so many that a gathering CTA would not count them all itself.
+constexpr int kCountSpan = 4096;
+constexpr int kCountFrom = 16 * kCountSpan;
+__global__ void __launch_bounds__(kSideThreads) loss_count_kernel(const int32_t* labels, int T, int V, int* counts) {
+  wait_for_kernel_before();
+  let_kernel_behind_in();
+  __shared__ int part[kSideThreads / 32];
+  const int first = blockIdx.x * kCountSpan, behind = min(T, first + kCountSpan);
+  int n = 0;
+  for (int i = first + (int)threadIdx.x; i < behind; i += kSideThreads) n += (unsigned)ld_global(labels + i) < (unsigned)V;
+  n = over_block(n, part, [](int a, int b) { return a + b; });
+  if (threadIdx.x == 0) counts[blockIdx.x] = n;
+}
+
 // ROWS tokens a CTA, 8 / ROWS warps a token: its place among those that count, its row beside theirs, and the logit of its label.
-// A CTA counts the tokens before its own itself (16 KB of labels at 4096 tokens).  One token a CTA where there are few.
+// A CTA counts the tokens before its own itself (16 KB of labels at 4096 tokens), or those of its span.  One token a CTA where there are few.
 template <int ROWS>
 __global__ void __launch_bounds__(kSideThreads) loss_gather_kernel(const GatherParams p) {
   wait_for_kernel_before();
@@ -494,8 +509,13 @@ __global__ void __launch_bounds__(kSideThreads) loss_gather_kernel(const GatherP
   const int t = t0 + mine, label = __shfl_sync(0xffffffffu, near, mine);
   const bool live = alive >> mine & 1u;
   const size_t own = (size_t)t * p.K;
-  int before = 0;
-  for (int i = threadIdx.x; i < t0; i += kSideThreads) before += (unsigned)ld_global(p.labels + i) < (unsigned)p.V;
+  int before = 0, from = 0;
+  if (p.counts) {
+    const int spans = t0 / kCountSpan;
+    for (int i = threadIdx.x; i < spans; i += kSideThreads) before += ld_global(p.counts + i);
+    from = spans * kCountSpan;
+  }
+  for (int i = from + (int)threadIdx.x; i < t0; i += kSideThreads) before += (unsigned)ld_global(p.labels + i) < (unsigned)p.V;
   before = over_block(before, counts, [](int a, int b) { return a + b; });
   if (blockIdx.x == 0)
     for (int c = threadIdx.x; c < p.chunks; c += kSideThreads) p.again[c] = 0;
@@ -641,7 +661,7 @@ struct LossPlan {
   int group, back_group;
   bool few;                  // head_loss_few.cu
   // offsets into the workspace
-  size_t count, again, index, label, ref, above, x, sums, e[2], grads, bytes;
+  size_t count, again, counts, index, label, ref, above, x, sums, e[2], grads, bytes;
   ShareRule rule(int K, int pairs) const {
     return {rows / kTile, pieces, (K + kTile - 1) / kTile, pairs, splits, tiles / pieces * width / kDepth};
   }
@@ -719,6 +739,7 @@ LossPlan plan_loss(int T, int V, int K, bool grad, int sms) {
   const size_t rows_all = (size_t)c.chunks * c.rows;
   c.count = take(4);
   c.again = take((size_t)c.chunks * 4);
+  c.counts = take(T > kCountFrom ? (size_t)(T + kCountSpan - 1) / kCountSpan * 4 : 0);
   c.index = take(rows_all * 4);
   c.label = take(rows_all * 4);
   c.ref = take(rows_all * 4);
@@ -858,6 +879,11 @@ extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* label
   gp.loss = loss;
   gp.dX = static_cast<__nv_bfloat16*>(dX);
   gp.status = status;
+  if (T > kCountFrom) {
+    int* counts = reinterpret_cast<int*>(ws + c.counts);
+    PEQA_TRY(launch_after(loss_count_kernel, (T + kCountSpan - 1) / kCountSpan, kSideThreads, st, labels, T, V, counts));
+    gp.counts = counts;
+  }
   // one token a CTA while that fills no more than two rounds of the SMs
   const bool alone = T <= 2 * 8 * sms;
   PEQA_TRY(alone ? launch_after(loss_gather_kernel<1>, T, kSideThreads, st, gp)

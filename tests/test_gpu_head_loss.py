@@ -53,6 +53,14 @@ def test_mostly_ignored(T, V, K, ignored):
     check(X, W, labels, weight, grad=False)
 
 
+@pytest.mark.parametrize("T", [65536, 65537, 150003])
+def test_long_batches(T):
+    """More tokens than a gathering CTA counts itself."""
+    X, W, labels, weight = inputs(T, 300, 40, seed=T, ignored=0.3)
+    check(X, W, labels, weight)
+    check(X, W, labels, weight, grad=False)
+
+
 @pytest.mark.parametrize("T", [40, 200, 600])
 @pytest.mark.parametrize("grad", [True, False])
 def test_labels_far_below_the_largest_logit(T, grad):
