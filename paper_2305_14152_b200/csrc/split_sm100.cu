@@ -170,7 +170,7 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
   auto r0_of = [&](int it) { return ((first_tile + j0 + (it < split_at ? 0 : 1)) % p.r_tiles) * SM_ROWS; };
   auto t0_of = [&](int it) { return ((first_tile + j0 + (it < split_at ? 0 : 1)) / p.r_tiles - p.t_first) * p.nt; };
 
-  const bool beside = (TRANS || GLU) && p.side == kBeside;     // (a linear's forward is the first of its call)
+  const bool beside = p.side == kBeside;      // (a linear's forward, the first of its call, never is)
   begin_beside(beside);
   // Forward: the first codes, scales and zero-points are asked for in L2 at once.  (Nothing is read: the preceding
   // kernel may still be writing them, and L2 is where it writes.)  us before / after: 256 x 256 at 64 tokens 5.8 / 5.4,
