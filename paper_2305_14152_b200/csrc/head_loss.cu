@@ -425,10 +425,12 @@ head_loss_kernel(const __grid_constant__ LossMaps maps, const LossParams p, cons
             atomicMax(p.live.above + p.row0 + row, __float_as_int(most - ref));
             *p.again = 1;
           }
-          // the halves of the staging memory change hands by turns of c; the next tile may be of the other kind
-          if (lane == 0) bulk_wait_group_read0();
-          __syncwarp();
         }
+      }
+      if (GRAD) {
+        // the halves of the staging memory change hands by turns of c; the next tile may be of the other kind
+        if (lane == 0) bulk_wait_group_read0();
+        __syncwarp();
       }
     }
     if (lane == 0) bulk_wait_group0();

@@ -61,6 +61,17 @@ def test_long_batches(T):
     check(X, W, labels, weight, grad=False)
 
 
+@pytest.mark.parametrize("T,V,K", [(1810, 29303, 552), (1395, 34181, 952), (4096, 32000, 1000)])
+def test_sums_of_any_pitch_over_several_pieces(T, V, K):
+    """Copies of the gradient's sums to rows that do not begin on 128 bytes take longer than others; tiles of logits follow them."""
+    X, W, labels, weight = inputs(T, V, K, seed=K)
+    check(X, W, labels, weight)
+    loss, dX = binding.head_loss(X, W, labels, weight)
+    for _ in range(4):
+        again, dX_again = binding.head_loss(X, W, labels, weight)
+        assert torch.equal(again, loss) and torch.equal(dX_again, dX)
+
+
 @pytest.mark.parametrize("T", [40, 200, 600])
 @pytest.mark.parametrize("grad", [True, False])
 def test_labels_far_below_the_largest_logit(T, grad):
