@@ -300,7 +300,7 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
     const int sw = (lane >> 1) & 3;
     int local = 0;
     bool ok = true;
-    for (int tile = pair; ok && tile < total_tiles; tile += n_pairs, ++local) {
+    for (int tile = pair; (GLU || ok) && tile < total_tiles; tile += n_pairs, ++local) {
       int n_tile, tt0, blocks;
       pair_item(p.items, tile, p.T, n_tile, tt0, blocks);
       const int n0 = n_tile * 256;
@@ -308,12 +308,13 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
       if constexpr (GLU) {
         // Sixteen columns at a time, eight channels' gate and up sums.  (The next sixteen asked for meanwhile took registers that the dequant warps'
         // code went without: 1024 columns, us, so / as it is 175.6 / 169.3.)  Scales come from shared memory, four a read that all lanes share.
-        // (All warps of a CTA come by these barriers as often, whether or not a wait runs out: a tile's accumulators are full for all or for none.)
+        // (All warps of a CTA come by these barriers as often: one whose wait has run out goes on through them alone.)
         const int own = (warp - 4) * 32 + lane;
         named_barrier_sync(2, 256);              // the last tile's have been read
         sm_scales[own] = n0 + own < p.N ? ld_global((HALF ? p.zeros_f : p.scales) + n0 + own) : 0.0f;
         named_barrier_sync(2, 256);
-        if (!warp_wait_cluster(smem_u32(&bars->acc_full), (uint32_t)(local & 1), abort_flag)) { ok = false; break; }
+        ok = ok && warp_wait_cluster(smem_u32(&bars->acc_full), (uint32_t)(local & 1), abort_flag);
+        if (!ok) continue;
         tc_fence_after();
         // All warps take the first block of tokens, then the second, 128 columns each, so that the next tile's products for the first may begin under
         // the second's epilogue.

@@ -41,3 +41,11 @@ def test_gated_block(T, group):
     w, _, _ = block(4096, 1024, 4, group, seed=2)
     X = torch.randn((T, 1024), device="cuda").bfloat16()
     starved(lambda: binding.qglu_fwd(w, X))
+
+
+@pytest.mark.parametrize("group", [0, 64])
+def test_wide_gated_block_of_few_tokens(group):
+    """Two launches side by side."""
+    w, _, _ = block(10240, 1024, 4, group, seed=3)
+    X = torch.randn((33, 1024), device="cuda").bfloat16()
+    starved(lambda: binding.qglu_fwd(w, X))
