@@ -574,7 +574,7 @@ __global__ void __launch_bounds__(kSideThreads) loss_finish_kernel(const FinishP
   // everything that the sums are not needed for is asked for before them
   const int mine = threadIdx.x / kSpan, at_thread = threadIdx.x % kSpan, lane = threadIdx.x & 31, row = min(row_b + mine, live - 1);
   const int token = ld_global(p.live.index + p.row0 + row), label = ld_global(p.live.label + p.row0 + row);
-  const float ref = GRAD ? above_of(p.live, p.row0 + row) : ld_global(p.live.ref + p.row0 + row);
+  const float of_label = ld_global(p.live.ref + p.row0 + row), above = GRAD ? above_of(p.live, p.row0 + row) : 0.0f;
   const float weight = GRAD && p.weight ? ld_global(p.weight + token) : 1.0f;
   const __nv_bfloat16* w = p.W + (size_t)label * p.K;
   const float* g = p.grads + (size_t)row * p.K;
@@ -625,12 +625,12 @@ __global__ void __launch_bounds__(kSideThreads) loss_finish_kernel(const FinishP
   }
   const float sum = v.sum;
   if (!GRAD) {
-    if (at_thread == 0) p.loss[token] = loss_of(v, ref);
+    if (at_thread == 0) p.loss[token] = loss_of(v, of_label);
     return;
   }
-  // the reference above the label's logit, and the label's term
-  const float above = ref, own = expf(-above);
-  if (at_thread == 0) p.loss[token] = above == 0.0f ? log1pf(sum) : above + logf(sum + own);
+  // above: the reference above the label's logit; own: the label's term, 1 if there is no such distance
+  const float own = finite_label(of_label) ? expf(-above) : NAN;
+  if (at_thread == 0) p.loss[token] = above == 0.0f ? log1pf(sum * own) : above + logf(sum + own);
   const float by = weight / (sum + own);
   __nv_bfloat16* out = p.dX + (size_t)token * p.K;
 #pragma unroll 1

@@ -120,8 +120,12 @@ __device__ __forceinline__ LogSum join_sums(LogSum a, LogSum b) {
   const float most = fmaxf(a.most, b.most), by = most == -INFINITY ? 0.0f : most;
   return {most, a.sum * exp2_approx((a.most - by) * kLog2e) + b.sum * exp2_approx((b.most - by) * kLog2e)};
 }
+// Whether a label's logit is a number that others can be held against.  What is not finite among the others shows in their sum, but against +infinity
+// every other entry counts 0, and of a vocabulary of one there are no others.
+__device__ __forceinline__ bool finite_label(float logit) { return fabsf(logit) < INFINITY; }
 // loss = log(sum over all entries of exp(l)) - label's logit, from the sum over the others
 __device__ __forceinline__ float loss_of(LogSum others, float label) {
+  if (!finite_label(label)) return NAN;
   const float above = others.most - label;
   return above <= 0.0f ? log1pf(others.sum * expf(above)) : above + logf(others.sum + expf(-above));
 }
