@@ -598,7 +598,7 @@ size_t peqa_attn_workspace_bytes(const peqa_kv_cache_t* cache, int n_heads);
  * K is a multiple of 8; T and V at most 2^24, K 2^20 (else PEQA_ERR_TOO_LARGE).  The logits exist in tensor memory
  * only; of a piece of the vocabulary at a time their exponentials, rounded to bf16 (off by 2^-8 of themselves at most), are kept for dX, whose sums are binary32.
  * workspace: peqa_head_loss_workspace_bytes(T, V, K, dX != NULL) bytes, 256-byte aligned, in use until the call's work has ended;
- * its contents before do not matter.  The same inputs on the same device give the same bits.  A token whose label's logit is not
+ * its contents before do not matter, and one for T tokens serves every batch of fewer.  The same inputs on the same device give the same bits.  A token whose label's logit is not
  * finite (X or W is not, or the product leaves binary32) has the loss NaN and a row of NaN; one with another logit that is NaN or +infinity a loss and a row
  * that are not finite.  Another logit of -infinity counts nothing in the loss; dX is then NaN in the features in which that row of W is infinite.
  */

@@ -632,7 +632,7 @@ def attn_decode(cache: KVCache, q: torch.Tensor, seq_lens: torch.Tensor, scale: 
 
 
 def alloc_head_loss_workspace(X: torch.Tensor, W: torch.Tensor, need_grad: bool = True) -> torch.Tensor:
-    """Scratch of head_loss for as many tokens as X has."""
+    """Scratch of head_loss for as many tokens as X has, or fewer."""
     n = int(lib().peqa_head_loss_workspace_bytes(X.shape[0], W.shape[0], W.shape[1], 1 if need_grad else 0))
     if n == 0:
         raise PeqaError(-3, "peqa_head_loss_workspace_bytes")

@@ -792,7 +792,16 @@ static bool loss_size_ok(int T, int V, int K) { return T <= (1 << 24) && V <= (1
 
 extern "C" size_t peqa_head_loss_workspace_bytes(int T, int V, int K, int need_grad) {
   if (!loss_shape_ok(T, V, K) || !loss_size_ok(T, V, K)) return 0;
-  return plan_loss(T, V, K, need_grad != 0, sm_count_or(148)).bytes;
+  const int sms = sm_count_or(148);
+  const LossPlan c = plan_loss(T, V, K, need_grad != 0, sms);
+  // A shorter batch may want more: its exponentials are rounded to other pieces, its sums of the gradient come in parts where tiles are few, those of
+  // the vocabulary in eighths of a tile up to 256 tokens.  So that one workspace serves them all: the most of any batch up to T, by blocks of 256 tokens within a chunk.
+  size_t bytes = c.bytes;
+  for (int t = kTile; t <= c.rows && t < T; t += kTile) {
+    const size_t shorter = plan_loss(t, V, K, need_grad != 0, sms).bytes;
+    bytes = shorter > bytes ? shorter : bytes;
+  }
+  return bytes;
 }
 
 extern "C" int peqa_head_loss(const void* X, const void* W, const int32_t* labels, const float* weight, int T, int V, int K,
