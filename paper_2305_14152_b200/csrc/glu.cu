@@ -34,8 +34,9 @@ __device__ __forceinline__ void glu_slopes(float x, float up, float dh, float& d
   const float t = __expf(-fabsf(v)), r = __fdividef(1.0f, 1.0f + t);
   const float p = v < 0.0f ? t * r : r, q = v < 0.0f ? r : t * r;
   d_up = dh * (x * p);
-  // far out q is 0, where dv may have overflowed
-  d_gate = dh * up * (ACT == PEQA_ACT_GELU_TANH && q == 0.0f ? p : fmaf(x * p, q * dv, p));
+  // far out p or q is 0, where dv may have overflowed; the slope is p then
+  const bool flat = ACT == PEQA_ACT_GELU_TANH && (p == 0.0f || q == 0.0f);
+  d_gate = dh * up * (flat ? p : fmaf(x * p, q * dv, p));
 }
 
 template <int ACT>
