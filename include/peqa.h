@@ -466,8 +466,9 @@ int peqa_qlinear_decode_prepared(const peqa_qweight_t* w, const uint32_t* prepar
  *     both apart from X and from each other.
  *     K % 64 == 0, with 3 bits K % 128 == 0; T >= 1.  Needs a workspace of peqa_workspace_bytes(PEQA_OP_GLU_FWD, T, w) bytes, 256-byte aligned,
  *     when that is non-zero: with groups, whose scales go into the operands, these are binary16 (X times a power of two per token, scales times one per row),
- *     so that Y and H are off by little more than their own rounding.  With one scale per row Y agrees with peqa_qlinear_fwd's up to the order of
- *     the sums.
+ *     so that Y and H are off by little more than their own rounding: a scale of 2^-25 of its row's largest or more is off by 2^-11 of itself, and so is its
+ *     product with a code; channels of 2^-28 of their token's largest or more are exact.  What is smaller is off by 2^-36 of that scale for every step
+ *     of a code, or 2^-39 of that channel.  With one scale per row Y agrees with peqa_qlinear_fwd's up to the order of the sums.
  *   peqa_glu_bwd: dY from Y and dH in bf16 [T, F]; dY out bf16 [T, 2F], Y itself or memory apart from it.
  *   peqa_qglu_decode_prepared: H [M, F] of 1 to 16 tokens from the prepared weights; arguments, shapes and the time at which
  *     `prepared` has to be final as with peqa_qlinear_decode_prepared.

@@ -349,7 +349,11 @@ qfwd_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
                   const float4 sc = *reinterpret_cast<const float4*>(sm_scales + first + at * 16 + 4 * e);
                   const float s4[4] = {sc.x, sc.y, sc.z, sc.w};
 #pragma unroll
-                  for (int k = 0; k < 4; ++k) y[4 * e + k] = __uint_as_float(v[4 * e + k]) * (HALF ? s4[k] * token : s4[k]);
+                  for (int k = 0; k < 4; ++k) {
+                    // (HALF) one factor after the other: their product alone may leave binary32's range
+                    y[4 * e + k] = __uint_as_float(v[4 * e + k]) * s4[k];
+                    if (HALF) y[4 * e + k] *= token;
+                  }
                 }
                 if (p.glu.act == PEQA_ACT_SILU) glu_pack<PEQA_ACT_SILU>(y, o + 4 * side);
                 else glu_pack<PEQA_ACT_GELU_TANH>(y, o + 4 * side);

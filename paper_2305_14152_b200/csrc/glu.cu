@@ -61,8 +61,8 @@ __global__ void __launch_bounds__(kBackThreads) glu_bwd_kernel(const uint4* Y, c
 }
 
 // Operands of a block with groups, in binary16 (see GluOut).  A CTA a token: its largest channel brought to [2^14, 2^15), so that all that is more than
-// 2^-28 of it keeps its bits.  Behind the tokens' CTAs the rows: a row's largest scale brought to [1, 2), by as many lanes as hold
-// its groups in kRowHeld registers each, so that every scale is asked for before the first is used.  (Against a warp for eight rows, one after the other, the
+// 2^-28 of it keeps its bits.  Behind the tokens' CTAs the rows: a row's largest scale brought to [2^11, 2^12), which fifteen steps of a code leave within
+// binary16 (65504), so that all that is 2^-25 of it or more keeps its bits; by as many lanes as hold its groups in kRowHeld registers each, so that every scale is asked for before the first is used.  (Against a warp for eight rows, one after the other, the
 // forward of 77 tokens, us: 4096 rows of 172 groups 34.4 / 22.0, 8192 of 128 at 300 tokens 64.1 / 51.8, 22016 of 32 38.4 / 37.5.)
 constexpr int kRowHeld = 8;
 constexpr int kHeld = 4;                          // 16-byte pieces of a token that a thread keeps between the two passes
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(kBackThreads) glu_operands_kernel(const uint4*
     for (int g = at + kRowHeld * lanes; g < G; g += lanes) most = max(most, __float_as_uint(ptx::ld_global(from + g)) & 0x7FFFFFFFu);
   for (int o = lanes >> 1; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
   if (row >= N) return;
-  const int e = shift_to(most, 0);
+  const int e = shift_to(most, 11);
   const float by = power_of_two(e);
   if (fours) {
 #pragma unroll

@@ -527,7 +527,8 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
           if constexpr (GLU) {
             float token = 1.0f;
             if (FOLD) token = ld_global(p.zeros_f + p.N + t0 + t);
-            a.x *= row_scale.x * token; a.y *= row_scale.y * token; a.z *= row_scale.z * token; a.w *= row_scale.w * token;
+            // one factor after the other: their product alone may leave binary32's range
+            a.x = a.x * row_scale.x * token; a.y = a.y * row_scale.y * token; a.z = a.z * row_scale.z * token; a.w = a.w * row_scale.w * token;
           } else if (!FOLD) {
             const float4 sc = ld_global(reinterpret_cast<const float4*>(p.scales + row));   // one scale per channel
             a.x *= sc.x; a.y *= sc.y; a.z *= sc.z; a.w *= sc.w;
