@@ -9,6 +9,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <optional>
 #include <vector>
 
@@ -261,6 +262,17 @@ at::Tensor matrix(PyObject* given, const at::Tensor& like, at::IntArrayRef shape
   return t;
 }
 
+// What a kernel reads or works in beside `like`: contiguous, and on its device.
+void beside(const at::Tensor& t, const at::Tensor& like, const char* name) {
+  if (t.device() == like.device() && t.is_contiguous()) return;
+  PyErr_Format(PyExc_ValueError, "%s: expected a contiguous tensor on the device of X", name);
+  fail();
+}
+Workspace workspace_beside(PyObject* o, const at::Tensor& like) {
+  if (o != Py_None) beside(tensor(o, "workspace"), like, "workspace");
+  return Workspace(o);
+}
+
 int activation(PyObject* o) {
   if (PyUnicode_Check(o)) {
     if (PyUnicode_CompareWithASCIIString(o, "silu") == 0) return PEQA_ACT_SILU;
@@ -270,11 +282,16 @@ int activation(PyObject* o) {
   fail();
 }
 
-// X [tokens, K] of a gated block on the current device, and its tokens.
-int64_t glu_tokens(const at::Tensor& X, const peqa_qweight_t& w) {
+// X [tokens, K] of a gated block on the current device, and its tokens; these of the block's tensors lie beside it.
+int64_t glu_tokens(const at::Tensor& X, const peqa_qweight_t& w, PyObject* block, std::initializer_list<PyObject*> read) {
   if (X.dim() != 2 || X.size(1) != w.in_features || X.get_device() != c10::cuda::current_device()) {
     PyErr_SetString(PyExc_ValueError, "X: expected [tokens, in_features] on the current CUDA device");
     fail();
+  }
+  for (PyObject* name : read) {
+    Ref t(PyObject_GetAttr(block, name));
+    const char* which = PyUnicode_AsUTF8(name);
+    beside(tensor(t.p, which), X, which);
   }
   if (X.size(0) > INT32_MAX) check(PEQA_ERR_TOO_LARGE, "peqa_qglu");
   return X.size(0);
@@ -286,12 +303,12 @@ PyObject* qglu_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   arity(n, 7);
   const peqa_qweight_t w = weight(a[0]);
   const at::Tensor& X = dev(a[1], at::kBFloat16, "X");
-  const int64_t T = glu_tokens(X, w);
+  const int64_t T = glu_tokens(X, w, a[0], {s_qweight, s_zeros, s_scales});
   const int act = activation(a[2]), keep = PyObject_IsTrue(a[3]);
   if (keep < 0) fail();
   at::Tensor H = matrix(a[5], X, {T, w.out_features / 2}, at::kBFloat16, "H"), Y;
   if (keep || a[4] != Py_None) Y = matrix(a[4], X, {T, w.out_features}, at::kBFloat16, "Y");
-  const Workspace given(a[6]);
+  const Workspace given = workspace_beside(a[6], X);
   at::Tensor own;
   void* wp = given.p;
   size_t wb = given.bytes;
@@ -337,7 +354,7 @@ PyObject* qglu_decode_prepared(PyObject*, PyObject* const* a, Py_ssize_t n) {
   arity(n, 7);
   const peqa_qweight_t w = weight(a[0]);
   const at::Tensor &prepared = dev(a[1], at::kInt, "prepared"), &X = dev(a[2], at::kBFloat16, "X");
-  const int64_t M = glu_tokens(X, w);
+  const int64_t M = a[6] == Py_None ? glu_tokens(X, w, a[0], {s_zeros, s_scales}) : glu_tokens(X, w, a[0], {s_zeros});
   const int act = activation(a[3]);
   if ((size_t)prepared.numel() * 4 < peqa_decode_prepared_bytes(&w) || prepared.device() != X.device()) {
     PyErr_SetString(PyExc_ValueError, "prepared: not the prepared copy of this block, or on another device than X");
@@ -398,7 +415,7 @@ PyObject* head_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   at::Tensor loss = matrix(a[5], X, {T}, at::kFloat, "loss"), dX;
   if (grad) dX = matrix(a[6], X, {T, K}, at::kBFloat16, "dX");
-  const Workspace given(a[7]);
+  const Workspace given = workspace_beside(a[7], X);
   at::Tensor own;
   void* wp = given.p;
   size_t wb = given.bytes;
