@@ -170,7 +170,7 @@ qsplit_kernel(const __grid_constant__ CUtensorMap tmap_act, const __grid_constan
   auto r0_of = [&](int it) { return ((first_tile + j0 + (it < split_at ? 0 : 1)) % p.r_tiles) * SM_ROWS; };
   auto t0_of = [&](int it) { return ((first_tile + j0 + (it < split_at ? 0 : 1)) / p.r_tiles - p.t_first) * p.nt; };
 
-  const bool beside = p.side == kBeside;      // (a linear's forward, the first of its call, never is)
+  const bool beside = p.side == kBeside;      // (a linear's forward never is: see launch_split)
   begin_beside(beside);
   // Forward: the first codes, scales and zero-points are asked for in L2 at once.  (Nothing is read: the preceding
   // kernel may still be writing them, and L2 is where it writes.)  us before / after: 256 x 256 at 64 tokens 5.8 / 5.4,
@@ -826,7 +826,8 @@ int split_part_tokens(const peqa_qweight_t* w, int T_call, bool trans) {
 int launch_split(const peqa_qweight_t* w, const float* zeros_f, int g, const void* act, int T, void* out,
                  bool trans, const void* dY, float* ds_part, cudaStream_t st, int T_call, int t0, Side side, const GluOut* glu) {
   SplitParams p;
-  p.side = side;
+  // A linear's forward is the first of its call, whose inputs the kernel before may still be writing: it waits, whatever it is asked for.
+  p.side = !trans && side == kBeside ? kInOrder : side;
   p.zeros = w->zeros;
   p.zeros_f = zeros_f;
   p.scales = w->scales;
