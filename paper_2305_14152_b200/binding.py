@@ -645,7 +645,7 @@ def head_loss(X: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, weight=Non
     respect to X; the logits are not kept.
 
     X bf16 [tokens, features], W bf16 [vocabulary, features] (frozen), labels int32 [tokens]; tokens with a negative label
-    count nothing.  weight fp32 [tokens] is the gradient with respect to each token's loss (1 unless given; it does not multiply the loss).
+    count nothing.  (All lie on 16 bytes: labels shifted by one, labels[1:], have to be copied.)  weight fp32 [tokens] is the gradient with respect to each token's loss (1 unless given; it does not multiply the loss).
     dX may be X itself.  Returns loss fp32 [tokens] and dX bf16 [tokens, features], or None without need_grad."""
     return (_native or _load_native()).head_loss(X, W, labels, weight, need_grad, loss, dX, workspace)
 

@@ -801,7 +801,8 @@ bool split_is_faster(const peqa_qweight_t* w, int T, bool trans, bool channel_sc
   return split_ns(w, T, trans) * 100 < pair_ns(R, C, T, trans, channel_scales, sm_count_or(148)) * 97;
 }
 
-// The same for a gated block's forward, whose plan is another.  us, pair / here: 11008 x 4096 in 3 bits at 320 tokens 50 / 40, 28672 x 8192 at 320
+// The same for a gated block's forward, whose plan is another, by the estimates fitted to the linear's (a stage of the block takes less: 0.38 us at 77 tokens,
+// 0.46 with groups, of 0.67).  us, pair / here: 11008 x 4096 in 3 bits at 320 tokens 50 / 40, 28672 x 8192 at 320
 // 165 / 144.
 bool split_glu_is_faster(const peqa_qweight_t* w, int T, bool channel_scales) {
   const int sms = sm_count_or(148);
